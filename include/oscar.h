@@ -357,6 +357,130 @@ int oscar_decode_step_mixed(const oscar_layout *L, void *pages, void *seg, int32
                             void *stream);
 
 /*
+ * 4-bit cache: the same path with 16 levels per channel, for layers and models that
+ * lose too much at 2 bits, and eviction from it by accumulated attention weight.  The
+ * layout struct, paging, rotations, clipping and metadata formats are those above; only
+ * the codes (0 .. 15) and the page's byte layout differ.
+ *
+ * Page byte layout: page p, kv-head h is the block starting at byte (p*Hkv + h) * B4_ph,
+ * B4_ph = 2*P*d/2 + 2*(d/G)*P*4 (10240 bytes for d = 128, P = 64, G = 32).  Inside a
+ * block, in the order of the decode's matrix-core operands:
+ *   [K codes] 4096 bytes: token slot t = 4 lo + u (u < 4), channel c = 32 kc + 8 hi + e
+ *             (hi < 4, e < 8): little-endian dword (64 u + 16 hi + lo)*4 + kc, nibble
+ *             e/2 + 4*(e%2) (nibble i: bits 4i .. 4i+3)
+ *   [V codes] 4096 bytes: t = 32 kt + 8 hi + 4 f + x (kt, f < 2, hi, x < 4), channel
+ *             c = 32 j + 16 n + lo (n < 2, lo < 16): byte (64 j + 16 hi + lo)*16 + 8 kt
+ *             + 4 f + x/2 + 2*(x%2), nibble n
+ *   [K s,z]   P*(d/G) 4-byte entries, token-major: entry t*(d/G) + c/G, scale then zero
+ *   [V s,z]   same
+ * The stored row is Q(x~)_c = s * (code_c - z).  No byte holds two tokens.
+ */
+
+/* Bytes of one page (all kv-heads) and of the pool; 0 if L is invalid. */
+size_t oscar_kv4_page_bytes(const oscar_layout *L);
+size_t oscar_kv4_pool_bytes(const oscar_layout *L);
+
+/*
+ * oscar_kv4_append -- oscar_kv_append into the 4-bit cache: the same rotation, clipping
+ * threshold and metadata rounding, with
+ *   s = M((b - a)/15), z = M(-a / s), code = clamp(round_half_even(y / s + z), 0, 15)
+ * (stored scale 0: s = 1, z = M(-a), codes 0).  Arguments as there; tokens with a
+ * negative slot are skipped.
+ */
+int oscar_kv4_append(const oscar_layout *L, void *pages, const void *k_new, const void *v_new,
+                     const int64_t *slot_mapping, int32_t n_tok, const float *R_k,
+                     const float *R_v, float clip_k, float clip_v, void *stream);
+
+/*
+ * oscar_kv4_gather -- rows of the cache as values: for token i and kv-head h the K and V
+ * rows Q(k~), Q(v~) of slot slot_mapping[i], in the rotated basis (a caller that needs
+ * the original one multiplies by R^T, or rotates the queries instead: chunked prefill
+ * over a cached prefix).  s * (code - z), each step one fp32 operation; bf16 output is
+ * its nearest-even rounding.
+ *   slot_mapping : int64 [n_tok]; a slot may come more than once; the output rows of
+ *                  negative slots are left as they were
+ *   k_out, v_out : [n_tok, Hkv, d] of out_dtype, 16-byte aligned
+ */
+int oscar_kv4_gather(const oscar_layout *L, const void *pages, const int64_t *slot_mapping,
+                     int32_t n_tok, void *k_out, void *v_out, oscar_dtype out_dtype,
+                     void *stream);
+
+/* Workspace of oscar_kv4_decode_attn / oscar_kv4_decode_step; with_weights != 0: for
+ * calls with weights, which keep every score (4 bytes per query head and token of
+ * max_pages_per_seq pages).  0 if an argument is invalid. */
+size_t oscar_kv4_decode_workspace_bytes(const oscar_layout *L, int32_t B, int32_t Hq,
+                                        int32_t num_splits, int32_t max_pages_per_seq,
+                                        int32_t with_weights);
+
+/*
+ * oscar_kv4_decode_attn -- oscar_decode_attn over the 4-bit cache (same arguments and
+ * evaluation: rotated query, split along the sequences, log-sum-exp merge, back-rotation;
+ * num_splits as there, 0 for the default).  q~, the softmax weights and the codes enter
+ * the matrix cores with all their bits, so the fp32 output is that of fp32 arithmetic.
+ * |q~| log2(e) sm_scale and the scales must stay below 2^56.
+ *   weights, weights_out : both NULL, or fp32 [B, Hkv, max_pages_per_seq * P], 16-byte
+ *       aligned, the same array or disjoint ones: for every cached token
+ *         weights_out[b][h][t] = weights[b][h][t] + sum_i p_{b,i,t},   t < seq_lens[b],
+ *       p the softmax weight of the token in query head i, over the query heads i of
+ *       KV head h.  Entries t >= seq_lens[b] are neither read nor written.
+ *   workspace : >= oscar_kv4_decode_workspace_bytes(L, B, Hq, num_splits,
+ *       max_pages_per_seq, weights != NULL) bytes with num_splits resolved
+ */
+int oscar_kv4_decode_attn(const oscar_layout *L, const void *pages, const void *q, int32_t B,
+                          int32_t Hq, const int32_t *block_table, int32_t max_pages_per_seq,
+                          const int32_t *seq_lens, const float *R_k, const float *R_v,
+                          float sm_scale, int32_t num_splits, const float *weights,
+                          float *weights_out, void *workspace, size_t workspace_bytes,
+                          void *out, oscar_dtype out_dtype, void *stream);
+
+/*
+ * oscar_kv4_decode_step -- oscar_kv4_append of the n_new newest tokens, then
+ * oscar_kv4_decode_attn over the cache including them; the cache update and the query
+ * rotation share one launch.  n_new may be 0 (k_new, v_new, slot_mapping then unused).
+ */
+int oscar_kv4_decode_step(const oscar_layout *L, void *pages, const void *k_new,
+                          const void *v_new, const int64_t *slot_mapping, int32_t n_new,
+                          float clip_k, float clip_v, const void *q, int32_t B, int32_t Hq,
+                          const int32_t *block_table, int32_t max_pages_per_seq,
+                          const int32_t *seq_lens, const float *R_k, const float *R_v,
+                          float sm_scale, int32_t num_splits, const float *weights,
+                          float *weights_out, void *workspace, size_t workspace_bytes,
+                          void *out, oscar_dtype out_dtype, void *stream);
+
+/*
+ * oscar_kv4_evict -- bounds the cache's length: every (sequence b, KV head h) keeps
+ * m = min(seq_lens[b], budget) of its slots, those that received the most attention.
+ * Attention does not depend on the order of cached tokens, so kept tokens below slot m
+ * stay where they are and only the others move, in place.
+ *   position of slot t: pos[b][h][t] if >= 0, else num_seen[b] - (seq_lens[b] - t) (the
+ *       tokens appended since the last eviction; all of them before the first one)
+ *   protected: position < sink or position >= num_seen[b] - recent
+ *   rank: protected tokens first, the others by weights[b][h][t], largest first (a NaN
+ *       last); equal ranks (and protected tokens among themselves) by slot, lowest first
+ *   The m first are kept.  The i-th kept slot >= m (ascending) moves to the i-th slot
+ *   < m that is not kept (ascending): its codes and metadata in the pages, its weight and
+ *   its position.  Afterwards, for t < m weights_out and pos_out hold the slot's weight
+ *   and position; for m <= t < max_pages_per_seq * P they hold 0 and -1.  new_lens[b] = m.
+ * The pages of slots >= m are free for other use; the next token of the sequence goes to
+ * slot m.
+ *   weights, weights_out : fp32 [B, Hkv, max_pages_per_seq * P] (oscar_kv4_decode_attn's)
+ *   pos, pos_out         : int32, same shape; before the first eviction all -1
+ *       each _out the same array as its input or disjoint from it
+ *   num_seen             : int32 [B], tokens of the sequence so far, evicted ones too
+ *   budget >= 1, sink >= 0, recent >= 0
+ *   new_lens             : int32 [B], not seq_lens itself
+ *   workspace            : >= oscar_kv4_evict_workspace_bytes(L, B, max_pages_per_seq)
+ *       bytes, 256-byte aligned, contents need no initialization
+ */
+size_t oscar_kv4_evict_workspace_bytes(const oscar_layout *L, int32_t B,
+                                       int32_t max_pages_per_seq);
+int oscar_kv4_evict(const oscar_layout *L, void *pages, int32_t B, const int32_t *block_table,
+                    int32_t max_pages_per_seq, const int32_t *seq_lens, const float *weights,
+                    float *weights_out, const int32_t *pos, int32_t *pos_out,
+                    const int32_t *num_seen, int32_t budget, int32_t sink, int32_t recent,
+                    int32_t *new_lens, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * bf16 paged-decode baseline (same paging, uncompressed cache), for comparing
  * against the INT2 path on the same GPU.  A bf16 page-head block (page p,
  * kv-head h) starts at element (p*Hkv + h) * 2*P*d and holds K then V in the

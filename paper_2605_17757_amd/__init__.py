@@ -30,6 +30,9 @@ EXPORTS = (
     "oscar_decode_reduce",
     "oscar_seg_bytes", "oscar_mixed_workspace_bytes", "oscar_mixed_append",
     "oscar_decode_attn_mixed", "oscar_decode_step_mixed",
+    "oscar_kv4_page_bytes", "oscar_kv4_pool_bytes", "oscar_kv4_append", "oscar_kv4_gather",
+    "oscar_kv4_decode_workspace_bytes", "oscar_kv4_decode_attn", "oscar_kv4_decode_step",
+    "oscar_kv4_evict_workspace_bytes", "oscar_kv4_evict",
     "oscar_bf16_page_bytes", "oscar_bf16_kv_append", "oscar_bf16_decode_workspace_bytes",
     "oscar_bf16_decode_attn",
     "oscar_calib_workspace_bytes", "oscar_calib_query_cov", "oscar_calib_attn",
@@ -110,6 +113,19 @@ def lib() -> ctypes.CDLL:
             "oscar_decode_step_mixed": (ctypes.c_int, [LP, P, P, i32, i32, P, P, f32, f32, P,
                                                        i32, i32, P, i32, P, P, P, f32, i32, P, sz,
                                                        P, ctypes.c_int, P]),
+            "oscar_kv4_page_bytes": (sz, [LP]),
+            "oscar_kv4_pool_bytes": (sz, [LP]),
+            "oscar_kv4_append": (ctypes.c_int, [LP, P, P, P, P, i32, P, P, f32, f32, P]),
+            "oscar_kv4_gather": (ctypes.c_int, [LP, P, P, i32, P, P, ctypes.c_int, P]),
+            "oscar_kv4_decode_workspace_bytes": (sz, [LP, i32, i32, i32, i32, i32]),
+            "oscar_kv4_decode_attn": (ctypes.c_int, [LP, P, P, i32, i32, P, i32, P, P, P, f32, i32,
+                                                     P, P, P, sz, P, ctypes.c_int, P]),
+            "oscar_kv4_decode_step": (ctypes.c_int, [LP, P, P, P, P, i32, f32, f32, P, i32, i32, P,
+                                                     i32, P, P, P, f32, i32, P, P, P, sz, P,
+                                                     ctypes.c_int, P]),
+            "oscar_kv4_evict_workspace_bytes": (sz, [LP, i32, i32]),
+            "oscar_kv4_evict": (ctypes.c_int, [LP, P, i32, P, i32, P, P, P, P, P, P, i32, i32, i32,
+                                               P, P, sz, P]),
             "oscar_bf16_page_bytes": (sz, [LP]),
             "oscar_bf16_kv_append": (ctypes.c_int, [LP, P, P, P, P, i32, P]),
             "oscar_bf16_decode_workspace_bytes": (sz, [LP, i32, i32, i32]),
@@ -422,6 +438,176 @@ def decode_step_mixed(layout: Layout, pages, seg, S0: int, W: int, k_new, v_new,
         _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
         _ptr(out, out.dtype, "out", B * Hq * d), out_dtype, _stream(stream))
     _check(st, "oscar_decode_step_mixed")
+
+
+# ---------------------------------------------------------------------------
+# 4-bit cache: update, reading back, decode attention, eviction
+# ---------------------------------------------------------------------------
+
+def kv4_page_bytes(layout: Layout) -> int:
+    return int(lib().oscar_kv4_page_bytes(ctypes.byref(layout)))
+
+
+def kv4_pool_bytes(layout: Layout) -> int:
+    return int(lib().oscar_kv4_pool_bytes(ctypes.byref(layout)))
+
+
+def kv4_decode_workspace_bytes(layout: Layout, B: int, Hq: int, num_splits: int,
+                               max_pages_per_seq: int, weights: bool = False) -> int:
+    return int(lib().oscar_kv4_decode_workspace_bytes(ctypes.byref(layout), B, Hq, num_splits,
+                                                      max_pages_per_seq, int(bool(weights))))
+
+
+def kv4_evict_workspace_bytes(layout: Layout, B: int, max_pages_per_seq: int) -> int:
+    return int(lib().oscar_kv4_evict_workspace_bytes(ctypes.byref(layout), B, max_pages_per_seq))
+
+
+def kv4_alloc_pool(layout: Layout, device="cuda") -> torch.Tensor:
+    n = kv4_pool_bytes(layout)
+    if n == 0:
+        raise OscarError(layout_check(layout), "kv4_pool_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def kv4_alloc_workspace(layout: Layout, B: int, Hq: int, num_splits: int, max_pages_per_seq: int,
+                        weights: bool = False, device="cuda") -> torch.Tensor:
+    return _ws(kv4_decode_workspace_bytes(layout, B, Hq, num_splits, max_pages_per_seq, weights),
+               "kv4_decode_workspace_bytes", device)
+
+
+def kv4_alloc_evict_workspace(layout: Layout, B: int, max_pages_per_seq: int, device="cuda"):
+    return _ws(kv4_evict_workspace_bytes(layout, B, max_pages_per_seq), "kv4_evict_workspace_bytes",
+               device)
+
+
+def _on_current_device(*tensors) -> None:
+    """The kernels run on the current device: its tensors only."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError("tensor on %s, but the current device is cuda:%d"
+                             % (t.device, torch.cuda.current_device()))
+
+
+def _out_code(out, name: str) -> int:
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, out.dtype))
+    return OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+
+
+def kv4_append(layout: Layout, pages, k_new, v_new, slot_mapping, R_k, R_v, clip_k: float,
+               clip_v: float, stream=None) -> None:
+    """Rotate, clip, INT4-quantize and pack n_tok new K/V rows into the 4-bit pool
+    ``pages`` (R_k / R_v None: identity)."""
+    n_tok, d, hkv = int(slot_mapping.numel()), layout.head_dim, layout.num_kv_heads
+    _on_current_device(pages, k_new, v_new, slot_mapping, R_k, R_v)
+    st = lib().oscar_kv4_append(
+        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)),
+        _ptr(k_new, torch.bfloat16, "k_new", n_tok * hkv * d),
+        _ptr(v_new, torch.bfloat16, "v_new", n_tok * hkv * d),
+        _ptr(slot_mapping, torch.int64, "slot_mapping"), n_tok, _rptr(R_k, "R_k", d, layout),
+        _rptr(R_v, "R_v", d, layout), float(clip_k), float(clip_v), _stream(stream))
+    _check(st, "oscar_kv4_append")
+
+
+def kv4_gather(layout: Layout, pages, slot_mapping, k_out, v_out, stream=None) -> None:
+    """K and V values of the rows at ``slot_mapping`` (rotated basis) into ``k_out``,
+    ``v_out`` ([n_tok, Hkv, d], both fp32 or both bf16)."""
+    n_tok, d, hkv = int(slot_mapping.numel()), layout.head_dim, layout.num_kv_heads
+    _on_current_device(pages, slot_mapping, k_out, v_out)
+    st = lib().oscar_kv4_gather(
+        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)),
+        _ptr(slot_mapping, torch.int64, "slot_mapping"), n_tok,
+        _ptr(k_out, k_out.dtype, "k_out", n_tok * hkv * d),
+        _ptr(v_out, k_out.dtype, "v_out", n_tok * hkv * d), _out_code(k_out, "k_out"),
+        _stream(stream))
+    _check(st, "oscar_kv4_gather")
+
+
+def _weights_args(layout, B, mp, weights, weights_out):
+    """(weights, weights_out) pointers; weights_out None: in place."""
+    if weights is None:
+        if weights_out is not None:
+            raise ValueError("weights_out without weights")
+        return None, None
+    n = B * layout.num_kv_heads * mp * layout.page_size
+    out = weights if weights_out is None else weights_out
+    return (_ptr(weights, torch.float32, "weights", n), _ptr(out, torch.float32, "weights_out", n))
+
+
+def kv4_decode_attn(layout: Layout, pages, q, block_table, seq_lens, R_k, R_v, sm_scale: float,
+                    num_splits: int, workspace, out, weights=None, weights_out=None,
+                    stream=None) -> None:
+    """One decode step of attention over the 4-bit cache into ``out`` ([B, Hq, d], bf16
+    or fp32).  ``weights`` (fp32 [B, Hkv, max_pages * 64]): every token's attention
+    weight, summed over the KV head's query heads, is added to it into ``weights_out``
+    (None: in place)."""
+    B, Hq, mp = _decode_args(layout, q, block_table, seq_lens)
+    d = layout.head_dim
+    _on_current_device(pages, q, block_table, seq_lens, R_k, R_v, workspace, out, weights, weights_out)
+    w_in, w_out = _weights_args(layout, B, mp, weights, weights_out)
+    st = lib().oscar_kv4_decode_attn(
+        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)),
+        _ptr(q, torch.bfloat16, "q", B * Hq * d), B, Hq,
+        _ptr(block_table, torch.int32, "block_table", B * mp), mp,
+        _ptr(seq_lens, torch.int32, "seq_lens", B), _rptr(R_k, "R_k", d, layout),
+        _rptr(R_v, "R_v", d, layout), float(sm_scale), int(num_splits), w_in, w_out,
+        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _ptr(out, out.dtype, "out", B * Hq * d), _out_code(out, "out"), _stream(stream))
+    _check(st, "oscar_kv4_decode_attn")
+
+
+def kv4_decode_step(layout: Layout, pages, k_new, v_new, slot_mapping, clip_k: float,
+                    clip_v: float, q, block_table, seq_lens, R_k, R_v, sm_scale: float,
+                    num_splits: int, workspace, out, weights=None, weights_out=None,
+                    stream=None) -> None:
+    """One serving decode step over the 4-bit cache: append the new tokens' K/V
+    (``slot_mapping`` may be empty), then kv4_decode_attn."""
+    B, Hq, mp = _decode_args(layout, q, block_table, seq_lens)
+    d, hkv = layout.head_dim, layout.num_kv_heads
+    n_new = int(slot_mapping.numel())
+    _on_current_device(pages, k_new, v_new, slot_mapping, q, block_table, seq_lens, R_k, R_v,
+                       workspace, out, weights, weights_out)
+    w_in, w_out = _weights_args(layout, B, mp, weights, weights_out)
+    kp = _ptr(k_new, torch.bfloat16, "k_new", n_new * hkv * d) if n_new else None
+    vp = _ptr(v_new, torch.bfloat16, "v_new", n_new * hkv * d) if n_new else None
+    sp = _ptr(slot_mapping, torch.int64, "slot_mapping") if n_new else None
+    st = lib().oscar_kv4_decode_step(
+        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)), kp, vp, sp,
+        n_new, float(clip_k), float(clip_v), _ptr(q, torch.bfloat16, "q", B * Hq * d), B, Hq,
+        _ptr(block_table, torch.int32, "block_table", B * mp), mp,
+        _ptr(seq_lens, torch.int32, "seq_lens", B), _rptr(R_k, "R_k", d, layout),
+        _rptr(R_v, "R_v", d, layout), float(sm_scale), int(num_splits), w_in, w_out,
+        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _ptr(out, out.dtype, "out", B * Hq * d), _out_code(out, "out"), _stream(stream))
+    _check(st, "oscar_kv4_decode_step")
+
+
+def kv4_evict(layout: Layout, pages, block_table, seq_lens, weights, pos, num_seen, budget: int,
+              sink: int, recent: int, new_lens, workspace, weights_out=None, pos_out=None,
+              stream=None) -> None:
+    """Keep the ``budget`` tokens of every (sequence, KV head) that received the most
+    attention (``weights``, fp32 [B, Hkv, max_pages * 64]; the first ``sink`` and the last
+    ``recent`` positions go first), moving rows inside ``pages``.  ``pos`` (int32, shape of
+    weights, -1 before the first eviction) holds the kept tokens' positions, ``num_seen``
+    (int32 [B]) the tokens so far.  ``new_lens`` (int32 [B]) receives the lengths;
+    ``weights_out`` and ``pos_out`` None: in place."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages_per_seq]")
+    B, mp = int(block_table.shape[0]), int(block_table.shape[1])
+    n = B * layout.num_kv_heads * mp * layout.page_size
+    w_out = weights if weights_out is None else weights_out
+    p_out = pos if pos_out is None else pos_out
+    _on_current_device(pages, block_table, seq_lens, weights, pos, num_seen, new_lens, workspace,
+                       w_out, p_out)
+    st = lib().oscar_kv4_evict(
+        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)), B,
+        _ptr(block_table, torch.int32, "block_table", B * mp), mp,
+        _ptr(seq_lens, torch.int32, "seq_lens", B), _ptr(weights, torch.float32, "weights", n),
+        _ptr(w_out, torch.float32, "weights_out", n), _ptr(pos, torch.int32, "pos", n),
+        _ptr(p_out, torch.int32, "pos_out", n), _ptr(num_seen, torch.int32, "num_seen", B),
+        int(budget), int(sink), int(recent), _ptr(new_lens, torch.int32, "new_lens", B),
+        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check(st, "oscar_kv4_evict")
 
 
 # ---------------------------------------------------------------------------

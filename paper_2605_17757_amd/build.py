@@ -35,6 +35,8 @@ SOURCES = {
                               "-amdgpu-sched-strategy=max-ilp"],
     # small calls: a team of waves per range
     "decode_mfma_team.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "kv4_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "kv4_cache.hip": ["-ffp-contract=off"],
     "bf16_decode.hip": [],
     "mixed.hip": [],
     "calib.hip": ["-ffp-contract=off"],

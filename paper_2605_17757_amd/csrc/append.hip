@@ -1,4 +1,5 @@
-// Cache update: rotate -> clip -> asymmetric INT2 per 32-channel group -> pack.
+// Cache update: rotate -> clip -> asymmetric INT2 per 32-channel group -> pack, and the
+// same into the 4-bit cache (BITS = 4: 16 levels, the page layout of kv4).
 // (Sec. 4 "KV Cache Update"; App. "Scale Determination and Per-token Clipping
 // Details"; Alg. 1 QuantizeAndWrite.)
 //
@@ -57,9 +58,11 @@ struct QParams {
   float sf, zf;
   bool deg;
 };
+constexpr float top_code(int bits) { return (float)((1 << bits) - 1); }
+template <int BITS = 2>
 __device__ inline QParams quant_params(float a, float b, const QFmt& fmt) {
   QParams p;
-  const float s = __fdiv_rn(__fsub_rn(b, a), 3.0f);
+  const float s = __fdiv_rn(__fsub_rn(b, a), top_code(BITS));
   p.s16 = meta_store(fmt, s);
   p.deg = (p.s16 & 0x7fffu) == 0;
   if (p.deg) {
@@ -73,11 +76,12 @@ __device__ inline QParams quant_params(float a, float b, const QFmt& fmt) {
   }
   return p;
 }
-// Code of one clipped channel value y: clamp(round_half_even(y / s + z), 0, 3).
+// Code of one clipped channel value y: clamp(round_half_even(y / s + z), 0, 2^BITS - 1).
+template <int BITS = 2>
 __device__ inline uint32_t quant_code(float y, const QParams& p) {
   if (p.deg) return 0u;
   const float r = rintf(__fadd_rn(__fdiv_rn(y, p.sf), p.zf));
-  return (uint32_t)fminf(fmaxf(r, 0.0f), 3.0f);
+  return (uint32_t)fminf(fmaxf(r, 0.0f), top_code(BITS));
 }
 
 // Token-wise clip threshold (App. "Scale Determination and Per-token Clipping
@@ -452,11 +456,44 @@ __device__ inline bool fast_scale(float s) { return s >= 0x1p-60f && s <= 0x1p60
 // (A bfloat16 scale is past fast_scale's bounds there.)
 __device__ inline float finite_bound(float tau) { return fminf(tau, FLT_MAX); }
 
+// The 4-bit rows' bytes (lane c of a half wave: codes of channels 4c .. 4c + 3 in the
+// low nibbles of `code`; slot < 0: none).  A K dword holds 8 channels, of two lanes; a V
+// byte holds channel lo (low nibble) and lo + 16 of a block of 32, of lanes 4 apart.
+__device__ inline void store_row4(uint8_t* __restrict__ pages, int Hkv, int h, int64_t slot, int is_v,
+                                  int ng, const uint32_t (&code)[4], const QParams& p, int c) {
+  uint32_t w;  // K: bytes 0 and 2 of the dword (of its bytes 1 and 3 in the odd lane)
+  if (is_v) {
+    w = (code[0] & 15u) | ((code[1] & 15u) << 8) | ((code[2] & 15u) << 16) | ((code[3] & 15u) << 24);
+    w |= (uint32_t)__shfl_xor((int)w, 4, 64) << 4;  // used in the lanes of low nibbles
+  } else {
+    w = (code[0] & 15u) | ((code[2] & 15u) << 4) | ((code[1] & 15u) << 16) | ((code[3] & 15u) << 20);
+    w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0xB1, 0xF, 0xF, false) << 8;  // lane ^ 1
+  }
+  if (slot < 0) return;  // uniform across the half wave
+  const int64_t page = slot / kP;
+  const int t = (int)(slot - page * kP);
+  uint8_t* blk = pages + ((size_t)page * Hkv + h) * kv4_block_bytes(ng);
+  if (is_v) {
+    if ((c & 4) == 0) {
+      uint8_t* b = blk + kv4_v_off(4 * c, t);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[16 * i] = (uint8_t)(w >> (8 * i));
+    }
+  } else if ((c & 1) == 0) {
+    *reinterpret_cast<uint32_t*>(blk + kv4_k_off(4 * c, t)) = w;
+  }
+  const int lanes = 32 / ng;  // per group
+  if ((c & (lanes - 1)) == 0)
+    *reinterpret_cast<uint32_t*>(blk + kv4_sz_off(ng, is_v) + (t * ng + c / lanes) * 4) =
+        (uint32_t)p.s16 | ((uint32_t)p.z16 << 16);
+}
+
 // Clip, quantize, pack and write the wave's two rows (half-wave each, lane c of a
 // half: channels 4c .. 4c + 3 in x) to pool slot `slot` (< 0: the row only takes
 // part in the cross-lane steps).  Clipping is monotone, so the clipped extremes are
 // the clipped values' extremes; a code is rint(clamp(y / s + z, 0, 3)), taken from
 // the low mantissa bits after adding 2^23.
+template <int BITS>
 __device__ inline void store_rows(uint8_t* __restrict__ pages, int Hkv, int h, int64_t slot,
                                   int is_v, float clip, const QFmt& fmt, const float (&x)[4],
                                   int c, int half) {
@@ -468,19 +505,27 @@ __device__ inline void store_rows(uint8_t* __restrict__ pages, int Hkv, int h, i
   mx = lanes_reduce<true>(mx, fmt.ng);
   if (!fmt.quantile) tau = __fmul_rn(clip, fmaxf(fmaxf(-mn, mx), 0.0f));
   auto clamp = [](float v, float lo, float hi) { return __builtin_amdgcn_fmed3f(v, lo, hi); };
-  const QParams p = quant_params(clamp(mn, -tau, tau), clamp(mx, -tau, tau), fmt);
-  uint32_t byte = 0;
+  const QParams p = quant_params<BITS>(clamp(mn, -tau, tau), clamp(mx, -tau, tau), fmt);
+  uint32_t byte = 0, code[4];
   if (fmt.bf16 && __any(!p.deg && !fast_scale(p.sf))) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) byte |= quant_code(clamp(x[e], -tau, tau), p) << (2 * e);
+    for (int e = 0; e < 4; ++e) {
+      code[e] = quant_code<BITS>(clamp(x[e], -tau, tau), p);
+      if (BITS == 2) byte |= code[e] << (2 * e);
+    }
   } else {
     const float s = p.deg ? 1.0f : p.sf, r = p.deg ? 0.0f : __fdiv_rn(1.0f, p.sf);  // deg: y / s = 0
     tau = finite_bound(tau);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float d = div_by_scale(clamp(x[e], -tau, tau), s, r);
-      byte += __float_as_uint(__fadd_rn(clamp(__fadd_rn(d, p.zf), 0.0f, 3.0f), 8388608.0f)) << (2 * e);
+      code[e] = __float_as_uint(__fadd_rn(clamp(__fadd_rn(d, p.zf), 0.0f, top_code(BITS)), 8388608.0f));
+      if (BITS == 2) byte += code[e] << (2 * e);
     }
+  }
+  if constexpr (BITS == 4) {
+    store_row4(pages, Hkv, h, slot, is_v, fmt.ng, code, p, c);
+    return;
   }
   if (slot < 0) return;  // uniform across the half wave
   const int64_t page = slot / kP;
@@ -528,7 +573,7 @@ struct Items {
 // One item per block of 8 waves (a decode step's tokens; more than one in turn past
 // two blocks per CU).
 // bx of gx: the block's items; rph: of head bx % Hkv (gx is a multiple of Hkv).
-template <class Rows>
+template <int BITS = 2, class Rows>
 __device__ inline void append_body(RotSmem& sm, int is_v, int bx, int gx,
                                    uint8_t* __restrict__ pages, const Rows& rows,
                                    const float* __restrict__ Rk, const float* __restrict__ Rv,
@@ -557,7 +602,7 @@ __device__ inline void append_body(RotSmem& sm, int is_v, int bx, int gx,
     } else {
       xt_of(cur.x, x);
     }
-    store_rows(pages, rows.Hkv, it.h, cur.slot, is_v, clip, fmt, x, c, half);
+    store_rows<BITS>(pages, rows.Hkv, it.h, cur.slot, is_v, clip, fmt, x, c, half);
     it.advance();
     if (!it.valid()) break;
     tok = it.g * kItemRows + r;
@@ -659,7 +704,10 @@ __device__ inline float token_quantile_quad(const float (&x)[32], float rmax, fl
 }
 
 // Clip, quantize, pack and write a bulk item's 16 rows (quad-lane layout); same
-// steps as store_rows.
+// steps as store_rows.  BITS = 4: w[2 hi] and w[2 hi + 1] get the even and the odd
+// channels of 8 hi .. 8 hi + 7 (K: the two halves' nibbles), or w[jb] the nibbles of
+// channels 4 jb .. 4 jb + 3 in its bytes (V).
+template <int BITS>
 __device__ inline void store_slice32(uint8_t* __restrict__ pages, int Hkv, int h, int64_t slot,
                                      int is_v, float clip, const QFmt& fmt, const float (&x)[32],
                                      int q) {
@@ -680,7 +728,10 @@ __device__ inline void store_slice32(uint8_t* __restrict__ pages, int Hkv, int h
     tau = __fmul_rn(clip, fmaxf(fmaxf(-mn, mx), 0.0f));
   }
   auto clamp = [](float v, float lo, float hi) { return __builtin_amdgcn_fmed3f(v, lo, hi); };
-  const QParams p = quant_params(clamp(mn, -tau, tau), clamp(mx, -tau, tau), fmt);
+  const QParams p = quant_params<BITS>(clamp(mn, -tau, tau), clamp(mx, -tau, tau), fmt);
+  // 4 bits: channel 4 jb + e of the slice; K: nibble of the half dword, V: byte e
+  const int sh1 = BITS == 2 ? 2 : is_v ? 8 : 16, sh2 = BITS == 2 ? 4 : is_v ? 16 : 4,
+            sh3 = BITS == 2 ? 6 : is_v ? 24 : 20;
   uint32_t w[8];
   if (fmt.bf16 && __any(!p.deg && !fast_scale(p.sf))) {
 #pragma unroll
@@ -691,7 +742,7 @@ __device__ inline void store_slice32(uint8_t* __restrict__ pages, int Hkv, int h
         float v = x[0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) v = i == 4 * jb + e ? x[i] : v;
-        w[jb] |= quant_code(clamp(v, -tau, tau), p) << (2 * e);
+        w[jb] |= quant_code<BITS>(clamp(v, -tau, tau), p) << (e == 0 ? 0 : e == 1 ? sh1 : e == 2 ? sh2 : sh3);
       }
     }
   } else {
@@ -703,14 +754,36 @@ __device__ inline void store_slice32(uint8_t* __restrict__ pages, int Hkv, int h
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float d = div_by_scale(clamp(x[4 * jb + e], -tau, tau), s, r);
-        c[e] = __float_as_uint(__fadd_rn(clamp(__fadd_rn(d, p.zf), 0.0f, 3.0f), 8388608.0f));
+        c[e] = __float_as_uint(__fadd_rn(clamp(__fadd_rn(d, p.zf), 0.0f, top_code(BITS)), 8388608.0f));
+        if (BITS == 4) c[e] &= 15u;
       }
-      w[jb] = c[0] + (c[1] << 2) + (c[2] << 4) + (c[3] << 6);  // the low byte
+      w[jb] = c[0] + (c[1] << sh1) + (c[2] << sh2) + (c[3] << sh3);  // BITS = 2: the low byte
     }
   }
   if (slot < 0) return;
   const int64_t page = slot / kP;
   const int t = (int)(slot - page * kP);
+  if constexpr (BITS == 4) {
+    uint8_t* blk = pages + ((size_t)page * Hkv + h) * kv4_block_bytes(fmt.ng);
+    if (is_v) {
+      uint8_t* b = blk + kv4_v_off(32 * q, t);
+#pragma unroll
+      for (int jb = 0; jb < 4; ++jb) {
+        const uint32_t v = w[jb] | (w[jb + 4] << 4);  // channels 4 jb + e and 16 more
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[16 * (4 * jb + e)] = (uint8_t)(v >> (8 * e));
+      }
+    } else {
+#pragma unroll
+      for (int hi = 0; hi < 4; ++hi)
+        *reinterpret_cast<uint32_t*>(blk + kv4_k_off(32 * q + 8 * hi, t)) = w[2 * hi] | (w[2 * hi + 1] << 8);
+    }
+    const int per = 4 / fmt.ng;  // slices per group
+    if (q % per == 0)
+      *reinterpret_cast<uint32_t*>(blk + kv4_sz_off(fmt.ng, is_v) + (t * fmt.ng + q / per) * 4) =
+          (uint32_t)p.s16 | ((uint32_t)p.z16 << 16);
+    return;
+  }
   uint8_t* blk = pages + ((size_t)page * Hkv + h) * block_bytes(fmt.ng);
   if (is_v) {
 #pragma unroll
@@ -777,7 +850,7 @@ __device__ inline void rotate_wave(const float4 (&Rs)[kD][kD / 4], const uint32_
   }
 }
 
-template <class Rows, bool DEF>
+template <class Rows, bool DEF, int BITS = 2>
 __global__ __launch_bounds__(kBulkWaves * 64) void append_bulk_kernel(
     uint8_t* __restrict__ pages, Rows rows, const float* __restrict__ Rk,
     const float* __restrict__ Rv, float clip_k, float clip_v, QFmt fmt_arg) {
@@ -853,16 +926,16 @@ __global__ __launch_bounds__(kBulkWaves * 64) void append_bulk_kernel(
         x[2 * i + 1] = __uint_as_float(pr & 0xffff0000u);
       }
     }
-    store_slice32(pages, Hkv, h, shfl64(to.slot, rr), is_v, clip, fmt, x, q);
+    store_slice32<BITS>(pages, Hkv, h, shfl64(to.slot, rr), is_v, clip, fmt, x, q);
   }
 }
 
-template <class Rows, bool DEF>
+template <class Rows, bool DEF, int BITS = 2>
 __global__ __launch_bounds__(kRotWaves * 64) __attribute__((amdgpu_waves_per_eu(4, 4))) void append_kernel(
     uint8_t* __restrict__ pages, Rows rows, const float* __restrict__ Rk,
     const float* __restrict__ Rv, float clip_k, float clip_v, QFmt fmt) {
   __shared__ RotSmem sm;
-  append_body(sm, blockIdx.y, blockIdx.x, gridDim.x, pages, rows, Rk, Rv, clip_k, clip_v,
+  append_body<BITS>(sm, blockIdx.y, blockIdx.x, gridDim.x, pages, rows, Rk, Rv, clip_k, clip_v,
               pick(DEF, fmt));
 }
 
@@ -876,7 +949,7 @@ __global__ __launch_bounds__(kRotWaves * 64) void prepare_kernel(const uint16_t*
 // One launch for a decode step's prologue: append_blocks blocks of the K update, as
 // many of the V update, then the query rotation's.  The parts are independent; the
 // split kernel that follows needs them all.
-template <class Rows, bool DEF>
+template <class Rows, bool DEF, int BITS = 2>
 __global__ __launch_bounds__(kRotWaves * 64) __attribute__((amdgpu_waves_per_eu(4, 4))) void prologue_kernel(
     uint8_t* __restrict__ pages, Rows rows, const float* __restrict__ Rk,
     const float* __restrict__ Rv, float clip_k, float clip_v, QFmt fmt_arg, int append_blocks,
@@ -885,7 +958,7 @@ __global__ __launch_bounds__(kRotWaves * 64) __attribute__((amdgpu_waves_per_eu(
   const int bx = blockIdx.x;
   if (bx < 2 * append_blocks) {
     const int is_v = bx >= append_blocks;
-    append_body(sm, is_v, is_v ? bx - append_blocks : bx, append_blocks, pages, rows,
+    append_body<BITS>(sm, is_v, is_v ? bx - append_blocks : bx, append_blocks, pages, rows,
                 Rk, Rv, clip_k, clip_v, pick(DEF, fmt_arg));
   } else {
     prepare_body(bx - 2 * append_blocks, q, q_rows, Rk, qscale, qt, fmt_arg.rph, Hq, rows.Hkv);
@@ -1200,7 +1273,7 @@ int append_blocks(int64_t items, int Hkv, int rph, int64_t most) {
 
 bool is_default(const QFmt& f) { return f.bf16 == 0 && f.quantile == 0 && f.ng == 4 && f.rph == 0; }
 
-template <class Rows>
+template <int BITS = 2, class Rows>
 hipError_t launch_rows(void* pages, const Rows& rows, const float* Rk, const float* Rv,
                        float clip_k, float clip_v, QFmt fmt, hipStream_t st) {
   auto go = [&](auto kernel, int blocks, int waves) {
@@ -1210,17 +1283,17 @@ hipError_t launch_rows(void* pages, const Rows& rows, const float* Rk, const flo
   const bool def = is_default(fmt);
   const int64_t items = append_items(rows.n_tok, rows.Hkv);
   if (items <= device_cus()) {
-    if (def) go(append_kernel<Rows, true>, (int)items, kRotWaves);
-    else go(append_kernel<Rows, false>, (int)items, kRotWaves);
+    if (def) go(append_kernel<Rows, true, BITS>, (int)items, kRotWaves);
+    else go(append_kernel<Rows, false, BITS>, (int)items, kRotWaves);
   } else {
     const int blocks = append_blocks(items, rows.Hkv, fmt.rph, device_cus() / 2);
-    if (def) go(append_bulk_kernel<Rows, true>, blocks, kBulkWaves);
-    else go(append_bulk_kernel<Rows, false>, blocks, kBulkWaves);
+    if (def) go(append_bulk_kernel<Rows, true, BITS>, blocks, kBulkWaves);
+    else go(append_bulk_kernel<Rows, false, BITS>, blocks, kBulkWaves);
   }
   return hipGetLastError();
 }
 
-template <class Rows>
+template <int BITS = 2, class Rows>
 hipError_t launch_prologue(void* pages, const Rows& rows, const float* Rk, const float* Rv,
                            float clip_k, float clip_v, QFmt fmt, const uint16_t* q, int B, int Hq,
                            float qscale, float* qt, hipStream_t st) {
@@ -1232,8 +1305,8 @@ hipError_t launch_prologue(void* pages, const Rows& rows, const float* Rk, const
                        static_cast<uint8_t*>(pages), rows, Rk, Rv, clip_k, clip_v, fmt, ab, q,
                        B1 * Hq, Hq, qscale, qt);
   };
-  if (is_default(fmt)) go(prologue_kernel<Rows, true>);
-  else go(prologue_kernel<Rows, false>);
+  if (is_default(fmt)) go(prologue_kernel<Rows, true, BITS>);
+  else go(prologue_kernel<Rows, false, BITS>);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || B1 == B) return e;
   const size_t o = (size_t)B1 * Hq * kD;  // the other sequences' queries
@@ -1246,6 +1319,13 @@ hipError_t launch_append(void* pages, int64_t Hkv, const uint16_t* k, const uint
                          float clip_k, float clip_v, QuantFmt fmt, hipStream_t st) {
   const PlainRows rows{k, v, slots, n_tok, (int)Hkv};
   return launch_rows(pages, rows, Rk, Rv, clip_k, clip_v, fmt, st);
+}
+
+hipError_t launch_kv4_append(void* pages, int64_t Hkv, const uint16_t* k, const uint16_t* v,
+                             const int64_t* slots, int n_tok, const float* Rk, const float* Rv,
+                             float clip_k, float clip_v, QuantFmt fmt, hipStream_t st) {
+  const PlainRows rows{k, v, slots, n_tok, (int)Hkv};
+  return launch_rows<4>(pages, rows, Rk, Rv, clip_k, clip_v, fmt, st);
 }
 
 hipError_t launch_mixed_append(void* pages, uint16_t* seg, int64_t Hkv, int S0, int W,
@@ -1276,6 +1356,15 @@ hipError_t launch_step_prologue(void* pages, int64_t Hkv, const uint16_t* k, con
                                 hipStream_t st) {
   const PlainRows rows{k, v, slots, n_tok, (int)Hkv};
   return launch_prologue(pages, rows, Rk, Rv, clip_k, clip_v, fmt, q, B, Hq, qscale, qt, st);
+}
+
+hipError_t launch_kv4_step_prologue(void* pages, int64_t Hkv, const uint16_t* k, const uint16_t* v,
+                                    const int64_t* slots, int n_tok, const float* Rk,
+                                    const float* Rv, float clip_k, float clip_v, QuantFmt fmt,
+                                    const uint16_t* q, int B, int Hq, float qscale, float* qt,
+                                    hipStream_t st) {
+  const PlainRows rows{k, v, slots, n_tok, (int)Hkv};
+  return launch_prologue<4>(pages, rows, Rk, Rv, clip_k, clip_v, fmt, q, B, Hq, qscale, qt, st);
 }
 
 hipError_t launch_mixed_step_prologue(void* pages, uint16_t* seg, int64_t Hkv, int S0, int W,

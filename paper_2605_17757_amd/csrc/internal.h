@@ -22,6 +22,27 @@ __host__ __device__ constexpr int off_vsz(int ng) { return kOffKSz + sz_bytes(ng
 __host__ __device__ constexpr int block_bytes(int ng) { return 2 * kCodeBytes + 2 * sz_bytes(ng); }
 constexpr int kMaxGroupHeads = 16;                 // query heads per kv-head
 
+// Page-head block of the 4-bit cache: K codes, V codes, K (scale, zero), V (scale, zero).
+// The code regions are in the order of the decode's matrix-core operands (lane = lo +
+// 16 hi), so that a wave reads one as four contiguous 1 KB loads:
+//   K: load u, lane, dword kc: slot 4 lo + u, channels 32 kc + 8 hi + e, nibble
+//      e / 2 + 4 (e % 2): two 16-bit lanes at a time are channels 2 i, 2 i + 1;
+//   V: load j, lane, byte 8 kt + 4 f + x / 2 + 2 (x % 2): slot 32 kt + 8 hi + 4 f + x,
+//      channels 32 j + lo (low nibble) and 32 j + 16 + lo.
+// A byte holds one slot's channels, so that slots are written independently.
+constexpr int kKv4CodeBytes = kP * kD / 2;  // 4096 per region
+__host__ __device__ constexpr int kv4_block_bytes(int ng) { return 2 * kKv4CodeBytes + 2 * ng * kP * 4; }
+__host__ __device__ constexpr int kv4_sz_off(int ng, int is_v) { return 2 * kKv4CodeBytes + is_v * ng * kP * 4; }
+// The dword of K channels 8 (c / 8) .. + 7 of slot t.
+__host__ __device__ constexpr int kv4_k_off(int c, int t) {
+  return ((64 * (t % 4) + 16 * (c / 8 % 4) + t / 4) * 4 + c / 32) * 4;
+}
+// Byte of V channels c and c + 16 (c % 32 < 16) of slot t.
+__host__ __device__ constexpr int kv4_v_off(int c, int t) {
+  return kKv4CodeBytes + (64 * (c / 32) + 16 * (t / 8 % 4) + c % 16) * 16 + 8 * (t / 32) + 4 * (t / 4 % 2) +
+         t / 2 % 2 + 2 * (t % 2);
+}
+
 // Lanes of one wave hand values to each other through LDS.  The hardware runs a
 // wave's LDS operations in order, so no instruction is needed, but to the compiler
 // each lane is a thread of its own: without a wavefront-scope fence between the
@@ -182,6 +203,47 @@ hipError_t launch_decode_reduce(int B, int Hq, int num_splits, const float* part
                                 const float* part_ml, const float* Rv, void* out, int out_f32,
                                 hipStream_t st, const MixedSpec* mixed = nullptr, int rph = 0,
                                 int Hkv = 1);
+
+// 4-bit cache: the cache update, the decode-step prologue, reading rows back, decode
+// attention's split kernel, the sums of attention weights, eviction.
+hipError_t launch_kv4_append(void* pages, int64_t Hkv, const uint16_t* k, const uint16_t* v,
+                             const int64_t* slots, int n_tok, const float* Rk, const float* Rv,
+                             float clip_k, float clip_v, QuantFmt fmt, hipStream_t st);
+hipError_t launch_kv4_step_prologue(void* pages, int64_t Hkv, const uint16_t* k, const uint16_t* v,
+                                    const int64_t* slots, int n_tok, const float* Rk,
+                                    const float* Rv, float clip_k, float clip_v, QuantFmt fmt,
+                                    const uint16_t* q, int B, int Hq, float qscale, float* qt,
+                                    hipStream_t st);
+hipError_t launch_kv4_gather(const uint8_t* pages, int Hkv, const int64_t* slots, int64_t n_tok,
+                             void* k, void* v, int out_f32, int meta_bf16, int ng, hipStream_t st);
+// scores: null, or [B][Hq][max_pages * 64] in log2 units (entries of cached tokens).
+hipError_t launch_kv4_split(const uint8_t* pages, int Hkv, int B, int Hq, const int32_t* block_table,
+                            int max_pages, const int32_t* seq_lens, int num_splits, const float* qt,
+                            float* part_o, float* part_ml, float* scores, hipStream_t st,
+                            int meta_bf16, int ng);
+// weights_out = weights + every cached token's attention weight, summed over the query
+// heads of its KV head ([B][Hkv][max_pages * 64]).
+hipError_t launch_kv4_weights(int Hkv, int B, int Hq, int max_pages, const int32_t* seq_lens,
+                              int num_splits, const float* part_ml, const float* scores,
+                              const float* weights, float* weights_out, hipStream_t st);
+// Eviction.  ws: kv4_evict_ws_bytes.
+size_t kv4_evict_ws_bytes(int Hkv, int B, int max_pages);
+struct EvictArgs {
+  uint8_t* pages;
+  int Hkv, B, ng;
+  const int32_t* block_table;
+  int max_pages;
+  const int32_t* seq_lens;
+  const float* weights;
+  float* weights_out;
+  const int32_t* pos;
+  int32_t* pos_out;
+  const int32_t* seen;
+  int budget, sink, recent;
+  int32_t* new_lens;
+  void* ws;
+};
+hipError_t launch_kv4_evict(const EvictArgs& a, hipStream_t st);
 
 hipError_t launch_bf16_append(void* pages, int64_t Hkv, const uint16_t* k, const uint16_t* v,
                               const int64_t* slots, int n_tok, hipStream_t st);

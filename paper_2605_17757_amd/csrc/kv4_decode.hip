@@ -1,0 +1,510 @@
+// Decode attention over the 4-bit paged cache: the split kernel and the sums of
+// attention weights (the query rotation and the merge are the 2-bit path's prepare and
+// reduce kernels).
+//
+// For a KV head with g query heads, q~ = q R_k sm_scale log2 e, a page's K as
+// Q(k~)_c = s (n - z) with codes n in 0 .. 15 and one (s, z) per token t and group G of
+// channels:
+//   score_t  = sum_G s (sum_{c in G} q~_c n_c - z sum_{c in G} q~_c)
+//   o~_c     = sum_t w_t n_c - sum_t w_t z_t,    w_t = 2^(score_t - m) s_t (of c's group)
+// Both inner sums run on the bf16 matrix cores and are exact products summed in fp32:
+//   * a code enters as the 16-bit pattern n, the bf16 subnormal n 2^-133, which a mask
+//     and a shift make of the packed nibbles (7 instructions per 8 codes; a conversion
+//     would take 2 per code);
+//   * q~ 2^64 and w 2^64 enter as three bf16 pieces, 8 bits of the significand each,
+//     together the whole fp32 value.  The pieces of one head are three rows of the
+//     16-row operand and 4 heads fill it, so that up to 4 heads per KV head cost no more
+//     matrix products than unsplit operands would; products are about
+//     2^-69 x q~ n, far from the fp32 range's ends for |q~| and scales below 2^56.
+// The fourth row of a head is zero.
+#define OSCAR_SPLIT_DIV32
+#include <hip/hip_fp16.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "internal.h"
+#include "split_ranges.h"
+
+namespace oscar {
+namespace {
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;         // waves of a block: a team on one range of pages
+constexpr int kPw = 40;           // dwords per row of the weights operand in LDS
+constexpr float kSlack = 10.0f;   // how far (log2) a score may exceed the reference maximum
+constexpr float kIn = 0x1p64f;    // scale of the operands, and of the products with codes
+constexpr float kOut = 0x1p69f;   // back: 2^133 / kIn
+
+__device__ inline f4v mfma(const u4v& a, const u4v& b, const f4v& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c,
+                                                 0, 0, 0);
+}
+// Piece i (0: the leading 8 bits, 1, 2: the next; 3: zero) of x, as fp32.
+__device__ inline float top16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ inline uint32_t pack_hi(float lo, float hi) {  // the upper halves of two floats
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+__device__ inline u4v unpack(uint32_t d) {  // nibbles 0, 4, 1, 5, 2, 6, 3, 7 as 16-bit lanes
+  constexpr uint32_t m = 0x000f000fu;
+  return u4v{d & m, (d >> 4) & m, (d >> 8) & m, (d >> 12) & m};
+}
+__device__ inline float row_sum(float x) {  // over the 16 lanes of a row
+#pragma unroll
+  for (int k = 8; k >= 1; k >>= 1) x += __shfl_xor(x, k, 64);
+  return x;
+}
+__device__ inline float row_max(float x) {
+#pragma unroll
+  for (int k = 8; k >= 1; k >>= 1) x = fmaxf(x, __shfl_xor(x, k, 64));
+  return x;
+}
+template <bool BF>
+__device__ inline float meta_lo(uint32_t e) {
+  return BF ? __uint_as_float(e << 16) : __half2float(__ushort_as_half((unsigned short)(e & 0xffffu)));
+}
+template <bool BF>
+__device__ inline float meta_hi(uint32_t e) {
+  return BF ? __uint_as_float(e & 0xffff0000u) : __half2float(__ushort_as_half((unsigned short)(e >> 16)));
+}
+
+template <int NCH>
+struct SplitSmem {
+  u4v qa[NCH][4][64];                     // query operands: chunk, 32-channel block, lane
+  uint32_t pw[kWaves][NCH][16 * kPw];     // weights operand of a group; a wave's o~ [4][128] at the end
+  float ml[kWaves][NCH * 4][2];           // the waves' (m, l)
+};
+
+template <int NCH>
+struct SplitOcc {
+  static constexpr int per_simd = NCH == 1 ? 3 : 2;
+};
+
+template <bool BF, int NG, int NCH>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((
+    amdgpu_waves_per_eu(SplitOcc<NCH>::per_simd, SplitOcc<NCH>::per_simd))) void kv4_split_kernel(
+    const uint8_t* __restrict__ pages, int Hkv, int Hq, const int32_t* __restrict__ block_table,
+    int max_pages, const int32_t* __restrict__ seq_lens, int num_splits, int n_ranges, int B,
+    const float* __restrict__ qt, float* __restrict__ part_o, float* __restrict__ part_ml,
+    float* __restrict__ scores) {
+  __shared__ SplitSmem<NCH> sm;
+  constexpr int KPG = 4 / NG;  // 32-channel blocks per group
+  const int r = (int)(blockIdx.x / (uint32_t)Hkv), kvh = (int)(blockIdx.x % (uint32_t)Hkv);
+  const int g = Hq / Hkv;
+  const int t = threadIdx.x, w = t >> 6, l = t & 63, lo = l & 15, hi = l >> 4;
+  auto len_of = [&](int b) { return min(max(seq_lens[b], 0), max_pages * kP); };
+  auto pages_of = [&](int b) { return (len_of(b) + kP - 1) / kP; };
+
+  // The block's waves take pages p0 + w, p0 + w + 4, .. of pages [p0, p1) of sequence b.
+  auto run_piece = [&](int b, int p0, int p1, int piece, bool last) {
+    const int len = len_of(b);
+    // ---- query operands: rows 4 h + piece of chunk ch, and group sums ----
+    for (int i = w; i < NCH * 4; i += kWaves) {
+      const int ch = i >> 2, kc = i & 3, head = 4 * ch + (lo >> 2), pc = lo & 3;
+      u4v a = u4v{0, 0, 0, 0};
+      if (head < g && pc < 3) {
+        const float* src = qt + ((size_t)b * Hq + kvh * g + head) * kD + 32 * kc + 8 * hi;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = src[e] * kIn;
+          if (pc > 0) x[e] -= top16(x[e]);
+          if (pc > 1) x[e] -= top16(x[e]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = pack_hi(x[2 * k], x[2 * k + 1]);
+      }
+      sm.qa[ch][kc][l] = a;
+    }
+    float qs[NCH][NG];  // sums of q~ over the groups, head 4 ch + hi
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      const int head = 4 * ch + hi;
+      float s = 0.0f;
+      if (head < g) {
+        const float4* src = reinterpret_cast<const float4*>(qt + ((size_t)b * Hq + kvh * g + head) * kD + 8 * lo);
+        const float4 x = src[0], y = src[1];
+        s = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+      }
+#pragma unroll
+      for (int k = 1; k < 16 / NG; k <<= 1) s += __shfl_xor(s, k, 64);
+#pragma unroll
+      for (int q = 0; q < NG; ++q) qs[ch][q] = __shfl(s, (l & 48) + q * (16 / NG), 64);
+    }
+    __syncthreads();
+
+    float m[NCH], lsum[NCH], wz[NCH][NG];
+    f4v o[NCH][8];
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      m[ch] = -INFINITY;
+      lsum[ch] = 0.0f;
+#pragma unroll
+      for (int q = 0; q < NG; ++q) wz[ch][q] = 0.0f;
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) o[ch][ct] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int32_t* __restrict__ bt = block_table + (size_t)b * max_pages;
+    const int n_mine = (p1 - p0 - w + kWaves - 1) / kWaves;  // <= 0: none
+    auto page_ids = [&](int i0) {  // lane i: page i0 + i of the wave's
+      const int p = p0 + w + kWaves * (i0 + l);
+      return i0 + l < n_mine ? bt[p] : 0;
+    };
+    int ids = page_ids(0);
+    auto block_of = [&](int i) {
+      return pages + ((size_t)__builtin_amdgcn_readlane(ids, i & 63) * Hkv + kvh) * kv4_block_bytes(NG);
+    };
+    u4v kr[4], ks[NG];
+    auto load_k = [&](const uint8_t* blk) {
+      const u4v* p = reinterpret_cast<const u4v*>(blk) + l;
+      const u4v* z = reinterpret_cast<const u4v*>(blk + kv4_sz_off(NG, 0)) + lo * NG;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) kr[u] = __builtin_nontemporal_load(p + 64 * u);
+#pragma unroll
+      for (int u = 0; u < NG; ++u) ks[u] = z[u];  // entries (slot 4 lo + u, group)
+    };
+    const uint8_t* blk = pages;
+    if (n_mine > 0) {
+      blk = block_of(0);
+      load_k(blk);
+    }
+    for (int i = 0; i < n_mine; ++i) {
+      const int pg = p0 + w + kWaves * i, ntok = min(kP, len - pg * kP);
+      u4v vr[4], vs[NG];
+      {
+        const u4v* p = reinterpret_cast<const u4v*>(blk + kKv4CodeBytes) + l;
+        const u4v* z = reinterpret_cast<const u4v*>(blk + kv4_sz_off(NG, 1)) + lo * NG;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vr[j] = __builtin_nontemporal_load(p + 64 * j);
+#pragma unroll
+        for (int u = 0; u < NG; ++u) vs[u] = z[u];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // ---- scores of heads 4 ch + hi, slots 4 lo + u ----
+      float sc[NCH][4];
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sc[ch][u] = 0.0f;
+#pragma unroll
+      for (int q = 0; q < NG; ++q) {
+        f4v d[NCH][4];
+#pragma unroll
+        for (int k = 0; k < KPG; ++k) {
+          const int kc = q * KPG + k;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const u4v bop = unpack(kr[u][kc]);
+#pragma unroll
+            for (int ch = 0; ch < NCH; ++ch)
+              d[ch][u] = mfma(sm.qa[ch][kc][l], bop, k == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[ch][u]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t e = ks[(u * NG + q) >> 2][(u * NG + q) & 3];
+          const float s = meta_lo<BF>(e), z = meta_hi<BF>(e);
+          const float so = s * kOut, sz = s * z;
+#pragma unroll
+          for (int ch = 0; ch < NCH; ++ch) {
+            const float dot = (d[ch][u][0] + d[ch][u][1]) + d[ch][u][2];
+            sc[ch][u] = fmaf(so, dot, fmaf(-sz, qs[ch][q], sc[ch][u]));
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < n_mine) {  // the next page's K, while this page's V is used
+        if (((i + 1) & 63) == 0) ids = page_ids(i + 1);
+        blk = block_of(i + 1);
+        load_k(blk);
+      }
+      if (ntok < kP) {  // the partial last page: other slots hold anything
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (4 * lo + u >= ntok) {
+#pragma unroll
+            for (int ch = 0; ch < NCH; ++ch) sc[ch][u] = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < NG; ++q) vs[(u * NG + q) >> 2][(u * NG + q) & 3] = 0u;
+          }
+      }
+      if (scores) {
+#pragma unroll
+        for (int ch = 0; ch < NCH; ++ch)
+          if (4 * ch + hi < g)
+            *reinterpret_cast<float4*>(
+                scores + (((size_t)b * Hq + kvh * g + 4 * ch + hi) * max_pages + pg) * kP + 4 * lo) =
+                make_float4(sc[ch][0], sc[ch][1], sc[ch][2], sc[ch][3]);
+      }
+      // ---- softmax weights; the reference maximum moves only when a score exceeds it
+      // by more than kSlack ----
+      bool need = false;
+      float mx[NCH];
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) {
+        mx[ch] = fmaxf(fmaxf(sc[ch][0], sc[ch][1]), fmaxf(sc[ch][2], sc[ch][3]));
+        need = need || mx[ch] > m[ch] + kSlack;
+      }
+      if (__any(need)) {
+#pragma unroll
+        for (int ch = 0; ch < NCH; ++ch) {
+          const float mn = fmaxf(m[ch], row_max(mx[ch]));
+          const float alpha = __builtin_amdgcn_exp2f(m[ch] - mn);  // m = -inf on the first page -> 0
+          m[ch] = mn;
+          lsum[ch] *= alpha;
+#pragma unroll
+          for (int q = 0; q < NG; ++q) wz[ch][q] *= alpha;
+#pragma unroll
+          for (int ct = 0; ct < 8; ++ct) o[ch][ct] *= alpha;
+        }
+      }
+      float p[NCH][4];
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          p[ch][u] = __builtin_amdgcn_exp2f(sc[ch][u] - m[ch]);
+          lsum[ch] += p[ch][u];
+        }
+      // ---- o~ += w V, group by group: the weights' pieces to LDS as the operand's rows ----
+#pragma unroll
+      for (int q = 0; q < NG; ++q) {
+        float s[4], z[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t e = vs[(u * NG + q) >> 2][(u * NG + q) & 3];
+          s[u] = meta_lo<BF>(e) * kIn;
+          z[u] = meta_hi<BF>(e);
+        }
+        lane_exchange();  // the reads of the previous group's operand come first
+#pragma unroll
+        for (int ch = 0; ch < NCH; ++ch) {
+          float x[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            x[u] = p[ch][u] * s[u];
+            wz[ch][q] = fmaf(x[u], z[u], wz[ch][q]);
+          }
+          uint32_t* row = sm.pw[w][ch] + 4 * hi * kPw + 2 * lo;
+#pragma unroll
+          for (int pc = 0; pc < 3; ++pc) {
+            *reinterpret_cast<uint2*>(row + pc * kPw) = make_uint2(pack_hi(x[0], x[1]), pack_hi(x[2], x[3]));
+            if (pc < 2)
+#pragma unroll
+              for (int u = 0; u < 4; ++u) x[u] -= top16(x[u]);
+          }
+        }
+        lane_exchange();
+        u4v a[NCH][2];
+#pragma unroll
+        for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+            a[ch][kt] = *reinterpret_cast<const u4v*>(sm.pw[w][ch] + lo * kPw + 16 * kt + 4 * hi);
+#pragma unroll
+        for (int k = 0; k < KPG; ++k) {
+          const int j = q * KPG + k;
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt) {
+            // bytes of 8 slots; the low nibbles are channel 32 j + lo, the high ones + 16
+            const u4v x = unpack(vr[j][2 * kt]), y = unpack(vr[j][2 * kt + 1]);
+            const u4v b0 = u4v{x[0], x[2], y[0], y[2]}, b1 = u4v{x[1], x[3], y[1], y[3]};
+#pragma unroll
+            for (int ch = 0; ch < NCH; ++ch) {
+              o[ch][2 * j] = mfma(a[ch][kt], b0, o[ch][2 * j]);
+              o[ch][2 * j + 1] = mfma(a[ch][kt], b1, o[ch][2 * j + 1]);
+            }
+          }
+        }
+      }
+    }
+
+    // ---- the waves' states, merged into the piece's ----
+    lane_exchange();
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      const float lt = row_sum(lsum[ch]);
+      float z[NG];
+#pragma unroll
+      for (int q = 0; q < NG; ++q) z[q] = row_sum(wz[ch][q]) * (1.0f / kIn);
+      float* om = reinterpret_cast<float*>(sm.pw[w][ch]) + hi * kD;
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct)
+        om[16 * ct + lo] = fmaf((o[ch][ct][0] + o[ch][ct][1]) + o[ch][ct][2], kOut, -z[ct / 2 / KPG]);
+      if (lo == 0) {
+        sm.ml[w][4 * ch + hi][0] = m[ch];
+        sm.ml[w][4 * ch + hi][1] = lt;
+      }
+    }
+    __syncthreads();
+    for (int i = t; i < g * kD; i += kWaves * 64) {
+      const int head = i / kD, c = i % kD;
+      float M = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sm.ml[k][head][0]);
+      float v = 0.0f, L = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        const float e = __builtin_amdgcn_exp2f(sm.ml[k][head][0] - M);  // a wave without pages: 0
+        v = fmaf(e, reinterpret_cast<const float*>(sm.pw[k][head >> 2])[(head & 3) * kD + c], v);
+        L = fmaf(e, sm.ml[k][head][1], L);
+      }
+      const size_t slot = ((size_t)b * Hq + kvh * g + head) * num_splits + piece;
+      part_o[slot * kD + c] = v;
+      if (c == 0) {
+        part_ml[2 * slot] = M;
+        part_ml[2 * slot + 1] = L;
+      }
+    }
+    if (last)  // the row's other slots are empty
+      for (int i = t; i < g * (num_splits - 1 - piece); i += kWaves * 64) {
+        const int n = num_splits - 1 - piece;
+        const size_t slot = ((size_t)b * Hq + kvh * g + i / n) * num_splits + piece + 1 + i % n;
+        part_ml[2 * slot] = -INFINITY;
+        part_ml[2 * slot + 1] = 0.0f;
+      }
+    __syncthreads();
+  };
+
+  if (num_splits == 1) {  // whole sequences
+    for (int b = r; b < B; b += n_ranges) {
+      const int n = pages_of(b);
+      if (n) run_piece(b, 0, n, 0, true);
+    }
+    if (kvh == 0 && w == 0) mark_empty(r, n_ranges, B, Hq, 1, 1, part_ml, pages_of);
+    return;
+  }
+  const RangeStart s = range_start(r, n_ranges, B, max_pages, num_splits, pages_of);
+  if (kvh == 0 && w == 0) mark_empty(r, n_ranges, B, Hq, num_splits, num_splits, part_ml, pages_of);
+  if (s.npg == 0) return;
+  int b = s.b, npg_b = s.npg;
+  int64_t x = s.x, before = s.before;
+  while (true) {
+    const int64_t end = min(s.xe, before + npg_b);
+    const int piece = (int)(r - div64(before, s.pw));
+    run_piece(b, (int)(x - before), (int)(end - before), piece, end == before + npg_b);
+    x = end;
+    if (x >= s.xe) break;
+    before += npg_b;
+    do {  // next sequence with pages
+      if (++b >= B) return;  // not reached: pages remain before xe <= T
+      npg_b = pages_of(b);
+    } while (npg_b == 0);
+  }
+}
+
+// weights_out[b][kvh][t] = weights[b][kvh][t] + sum over the g query heads of
+// 2^(score - M) / L, with a head's M and L from the partial states of its pieces.
+// Four tokens per thread, kWeightTokens per block.
+constexpr int kWeightTokens = 1024;
+
+__global__ __launch_bounds__(256) void kv4_weights_kernel(
+    int Hkv, int Hq, int max_pages, const int32_t* __restrict__ seq_lens, int num_splits, int b0,
+    const float* __restrict__ part_ml, const float* __restrict__ scores, const float* weights,
+    float* weights_out) {
+  __shared__ float ms[kMaxGroupHeads], il[kMaxGroupHeads];
+  const int b = b0 + blockIdx.z, kvh = blockIdx.y, g = Hq / Hkv, t = threadIdx.x, w = t >> 6, l = t & 63;
+  const int len = min(max(seq_lens[b], 0), max_pages * kP);
+  if ((int64_t)blockIdx.x * kWeightTokens >= len) return;
+  const size_t row0 = (size_t)b * Hq + kvh * g;
+  for (int h = w; h < g; h += 4) {
+    const float2* ml = reinterpret_cast<const float2*>(part_ml) + (row0 + h) * num_splits;
+    float M = -INFINITY;
+    for (int s = l; s < num_splits; s += 64) M = fmaxf(M, ml[s].x);
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
+    float L = 0.0f;
+    for (int s = l; s < num_splits; s += 64)
+      if (ml[s].x != -INFINITY) L = fmaf(exp2f(ml[s].x - M), ml[s].y, L);
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) L += __shfl_xor(L, k, 64);
+    if (l == 0) {
+      ms[h] = M;
+      il[h] = 1.0f / L;
+    }
+  }
+  __syncthreads();
+  const int t0 = blockIdx.x * kWeightTokens + 4 * t;
+  if (t0 >= len) return;
+  const size_t S = (size_t)max_pages * kP, at = ((size_t)b * Hkv + kvh) * S + t0;
+  float4 a = *reinterpret_cast<const float4*>(weights + at);
+  for (int h = 0; h < g; ++h) {
+    const float4 x = *reinterpret_cast<const float4*>(scores + (row0 + h) * S + t0);
+    a.x = fmaf(__builtin_amdgcn_exp2f(x.x - ms[h]), il[h], a.x);
+    a.y = fmaf(__builtin_amdgcn_exp2f(x.y - ms[h]), il[h], a.y);
+    a.z = fmaf(__builtin_amdgcn_exp2f(x.z - ms[h]), il[h], a.z);
+    a.w = fmaf(__builtin_amdgcn_exp2f(x.w - ms[h]), il[h], a.w);
+  }
+  float* out = weights_out + at;
+  if (t0 + 4 <= len) {
+    *reinterpret_cast<float4*>(out) = a;
+  } else {  // slots past the length stay as they were
+    const float v[4] = {a.x, a.y, a.z, a.w};
+    for (int i = 0; t0 + i < len; ++i) out[i] = v[i];
+  }
+}
+
+template <bool BF, int NG>
+void launch_nch(int nch, const dim3& grid, hipStream_t st, const uint8_t* pages, int Hkv, int Hq,
+                const int32_t* block_table, int max_pages, const int32_t* seq_lens, int num_splits,
+                int ranges, int B, const float* qt, float* part_o, float* part_ml, float* scores) {
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), 0, st, pages, Hkv, Hq, block_table, max_pages,
+                       seq_lens, num_splits, ranges, B, qt, part_o, part_ml, scores);
+  };
+  if (nch == 1) go(kv4_split_kernel<BF, NG, 1>);
+  else if (nch == 2) go(kv4_split_kernel<BF, NG, 2>);
+  else if (nch == 3) go(kv4_split_kernel<BF, NG, 3>);
+  else go(kv4_split_kernel<BF, NG, 4>);
+}
+
+}  // namespace
+
+hipError_t launch_kv4_split(const uint8_t* pages, int Hkv, int B, int Hq, const int32_t* block_table,
+                            int max_pages, const int32_t* seq_lens, int num_splits, const float* qt,
+                            float* part_o, float* part_ml, float* scores, hipStream_t st,
+                            int meta_bf16, int ng) {
+  const int nch = split_chunks(Hq / Hkv);
+  // As many ranges as blocks are resident at once (of the Hkv heads' each), and no more
+  // than the block table can fill at the least pages of a range.
+  const int64_t resident = (int64_t)(nch == 1 ? SplitOcc<1>::per_simd : SplitOcc<2>::per_simd) * device_cus();
+  int64_t ranges = std::max<int64_t>(1, resident / Hkv);
+  if (num_splits > 1) {
+    const int64_t least = std::max<int64_t>(kMinRange, (max_pages + (int64_t)num_splits - 2) / (num_splits - 1));
+    ranges = std::min(ranges, ((int64_t)B * max_pages + least - 1) / least);
+  } else {
+    ranges = std::min<int64_t>(ranges, B);
+  }
+  const dim3 grid((unsigned)(ranges * Hkv));
+  auto by_ng = [&](auto bf) {
+    constexpr bool BF = decltype(bf)::value;
+    auto go = [&](auto n) {
+      launch_nch<BF, decltype(n)::value>(nch, grid, st, pages, Hkv, Hq, block_table, max_pages, seq_lens,
+                                         num_splits, (int)ranges, B, qt, part_o, part_ml, scores);
+    };
+    if (ng == 4) go(std::integral_constant<int, 4>{});
+    else if (ng == 2) go(std::integral_constant<int, 2>{});
+    else go(std::integral_constant<int, 1>{});
+  };
+  if (meta_bf16) by_ng(std::true_type{});
+  else by_ng(std::false_type{});
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_weights(int Hkv, int B, int Hq, int max_pages, const int32_t* seq_lens,
+                              int num_splits, const float* part_ml, const float* scores,
+                              const float* weights, float* weights_out, hipStream_t st) {
+  const unsigned chunks = (unsigned)(((int64_t)max_pages * kP + kWeightTokens - 1) / kWeightTokens);
+  // a launch holds fewer than 2^32 threads
+  const int most = (int)std::max<int64_t>(1, (1 << 23) / ((int64_t)chunks * Hkv));
+  return by_seqs(B, most, [&](int b0, int nb) {
+    hipLaunchKernelGGL(kv4_weights_kernel, dim3(chunks, Hkv, nb), dim3(256), 0, st, Hkv, Hq, max_pages,
+                       seq_lens, num_splits, b0, part_ml, scores, weights, weights_out);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace oscar

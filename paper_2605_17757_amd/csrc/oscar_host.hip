@@ -565,6 +565,240 @@ int oscar_decode_step_mixed(const oscar_layout* L, void* pages, void* seg, int32
 }
 
 // ---------------------------------------------------------------------------
+// 4-bit cache
+// ---------------------------------------------------------------------------
+
+size_t oscar_kv4_page_bytes(const oscar_layout* L) {
+  if (check_layout(L) != OSCAR_OK) return 0;
+  return (size_t)L->num_kv_heads * kv4_block_bytes(groups(L));
+}
+
+size_t oscar_kv4_pool_bytes(const oscar_layout* L) {
+  return oscar_kv4_page_bytes(L) * (L ? (size_t)L->num_pages : 0);
+}
+
+}  // extern "C"
+
+namespace {
+
+// The new rows of a 4-bit cache update (n > 0) and what quantizes them.
+int check_kv4_rows(const oscar_layout* L, const void* k_new, const void* v_new,
+                   const int64_t* slot_mapping, int32_t n) {
+  if (!k_new || !v_new || !slot_mapping) return OSCAR_ERR_INVALID_ARG;
+  if (!aligned(k_new, 4) || !aligned(v_new, 4) || !aligned(slot_mapping, 8)) return OSCAR_ERR_INVALID_ARG;
+  if ((int64_t)n * L->num_kv_heads > 0x7fffffffLL) return OSCAR_ERR_UNSUPPORTED;
+  return OSCAR_OK;
+}
+
+// Token slots per sequence, and the [B][Hkv][slots] arrays: within the kernels' indices.
+int check_kv4_slots(const oscar_layout* L, int32_t max_pages_per_seq) {
+  if (max_pages_per_seq < 1) return OSCAR_ERR_INVALID_ARG;
+  if ((int64_t)max_pages_per_seq * L->page_size > 0x7fffffffLL ||
+      (int64_t)max_pages_per_seq * L->num_kv_heads > (1LL << 27))
+    return OSCAR_ERR_UNSUPPORTED;
+  return OSCAR_OK;
+}
+
+struct Kv4Ws {
+  DecodeWs d;
+  size_t scores_off, total;
+};
+Kv4Ws kv4_ws(const oscar_layout* L, int32_t B, int32_t Hq, int32_t num_splits, int32_t max_pages,
+             bool weights) {
+  Kv4Ws w;
+  w.d = decode_ws(B, Hq, num_splits);
+  w.scores_off = w.d.total;
+  w.total = weights ? align256(w.scores_off + (size_t)B * Hq * max_pages * (size_t)L->page_size * sizeof(float))
+                    : w.d.total;
+  return w;
+}
+
+// Checks of a 4-bit decode call; resolves num_splits.
+int check_kv4_decode(const oscar_layout* L, const void* pages, const void* q, int32_t B, int32_t Hq,
+                     const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                     const float* R_k, const float* R_v, float sm_scale, int32_t* num_splits,
+                     const float* weights, float* weights_out, void* workspace,
+                     size_t workspace_bytes, const void* out, oscar_dtype out_dtype) {
+  int st = check_decode_attn(L, pages, q, B, Hq, block_table, max_pages_per_seq, seq_lens, sm_scale,
+                             num_splits, out, out_dtype);
+  if (st) return st;
+  if ((st = check_kv4_slots(L, max_pages_per_seq))) return st;
+  if ((weights == nullptr) != (weights_out == nullptr)) return OSCAR_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256) || !aligned(R_k, 16) || !aligned(R_v, 16) ||
+      !aligned(weights, 16) || !aligned(weights_out, 16))
+    return OSCAR_ERR_INVALID_ARG;
+  if (workspace_bytes < kv4_ws(L, B, Hq, *num_splits, max_pages_per_seq, weights != nullptr).total)
+    return OSCAR_ERR_WORKSPACE_TOO_SMALL;
+  return OSCAR_OK;
+}
+
+// Split, merge and weights; q~ is in the workspace.
+int launch_kv4_rest(const oscar_layout* L, const void* pages, int32_t B, int32_t Hq,
+                    const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                    const float* R_v, int32_t num_splits, const float* weights, float* weights_out,
+                    void* workspace, void* out, oscar_dtype out_dtype, hipStream_t hs) {
+  const Kv4Ws ws = kv4_ws(L, B, Hq, num_splits, max_pages_per_seq, weights != nullptr);
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  float* po = reinterpret_cast<float*>(base + ws.d.po_off);
+  float* pml = reinterpret_cast<float*>(base + ws.d.pml_off);
+  float* scores = weights ? reinterpret_cast<float*>(base + ws.scores_off) : nullptr;
+  int st = hip_status(launch_kv4_split(static_cast<const uint8_t*>(pages), L->num_kv_heads, B, Hq,
+                                       block_table, max_pages_per_seq, seq_lens, num_splits,
+                                       reinterpret_cast<const float*>(base + ws.d.qt_off), po, pml,
+                                       scores, hs, meta_bf16(L), groups(L)));
+  if (st) return st;
+  st = hip_status(launch_decode_reduce(B, Hq, num_splits, po, pml, R_v, out,
+                                       out_dtype == OSCAR_OUT_F32 ? 1 : 0, hs, nullptr, L->rot_per_head,
+                                       L->num_kv_heads));
+  if (st || !weights) return st;
+  return hip_status(launch_kv4_weights(L->num_kv_heads, B, Hq, max_pages_per_seq, seq_lens, num_splits,
+                                       pml, scores, weights, weights_out, hs));
+}
+
+}  // namespace
+
+extern "C" {
+
+int oscar_kv4_append(const oscar_layout* L, void* pages, const void* k_new, const void* v_new,
+                     const int64_t* slot_mapping, int32_t n_tok, const float* R_k,
+                     const float* R_v, float clip_k, float clip_v, void* stream) {
+  int st = check_layout(L);
+  if (st) return st;
+  if (n_tok < 0 || !clip_ok(clip_k) || !clip_ok(clip_v)) return OSCAR_ERR_INVALID_ARG;
+  if (n_tok == 0) return OSCAR_OK;
+  if (!pages || !aligned(pages, 16) || !aligned(R_k, 16) || !aligned(R_v, 16)) return OSCAR_ERR_INVALID_ARG;
+  if ((st = check_kv4_rows(L, k_new, v_new, slot_mapping, n_tok))) return st;
+  st = debug_check(L, stream, 0, nullptr, 0, nullptr, slot_mapping, n_tok, nullptr, 0);
+  if (st) return st;
+  return hip_status(launch_kv4_append(pages, L->num_kv_heads, static_cast<const uint16_t*>(k_new),
+                                      static_cast<const uint16_t*>(v_new), slot_mapping, n_tok, R_k, R_v,
+                                      clip_k, clip_v, quant_fmt(L), static_cast<hipStream_t>(stream)));
+}
+
+int oscar_kv4_gather(const oscar_layout* L, const void* pages, const int64_t* slot_mapping,
+                     int32_t n_tok, void* k_out, void* v_out, oscar_dtype out_dtype,
+                     void* stream) {
+  int st = check_layout(L);
+  if (st) return st;
+  if (n_tok < 0 || (out_dtype != OSCAR_OUT_BF16 && out_dtype != OSCAR_OUT_F32)) return OSCAR_ERR_INVALID_ARG;
+  if (n_tok == 0) return OSCAR_OK;
+  if (!pages || !slot_mapping || !k_out || !v_out) return OSCAR_ERR_INVALID_ARG;
+  if (!aligned(pages, 16) || !aligned(slot_mapping, 8) || !aligned(k_out, 16) || !aligned(v_out, 16))
+    return OSCAR_ERR_INVALID_ARG;
+  st = debug_check(L, stream, 0, nullptr, 0, nullptr, slot_mapping, n_tok, nullptr, 0);
+  if (st) return st;
+  return hip_status(launch_kv4_gather(static_cast<const uint8_t*>(pages), L->num_kv_heads, slot_mapping,
+                                      n_tok, k_out, v_out, out_dtype == OSCAR_OUT_F32 ? 1 : 0, meta_bf16(L),
+                                      groups(L), static_cast<hipStream_t>(stream)));
+}
+
+size_t oscar_kv4_decode_workspace_bytes(const oscar_layout* L, int32_t B, int32_t Hq,
+                                        int32_t num_splits, int32_t max_pages_per_seq,
+                                        int32_t with_weights) {
+  if (check_decode_common(L, B, Hq, num_splits) != OSCAR_OK || check_kv4_slots(L, max_pages_per_seq) != OSCAR_OK)
+    return 0;
+  return kv4_ws(L, B, Hq, num_splits, max_pages_per_seq, with_weights != 0).total;
+}
+
+int oscar_kv4_decode_attn(const oscar_layout* L, const void* pages, const void* q, int32_t B,
+                          int32_t Hq, const int32_t* block_table, int32_t max_pages_per_seq,
+                          const int32_t* seq_lens, const float* R_k, const float* R_v,
+                          float sm_scale, int32_t num_splits, const float* weights,
+                          float* weights_out, void* workspace, size_t workspace_bytes,
+                          void* out, oscar_dtype out_dtype, void* stream) {
+  int st = check_kv4_decode(L, pages, q, B, Hq, block_table, max_pages_per_seq, seq_lens, R_k, R_v,
+                            sm_scale, &num_splits, weights, weights_out, workspace, workspace_bytes,
+                            out, out_dtype);
+  if (st) return st;
+  st = debug_check(L, stream, B, block_table, max_pages_per_seq, seq_lens, nullptr, 0, nullptr, 0);
+  if (st) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  st = hip_status(launch_decode_prepare(static_cast<const uint16_t*>(q), B, Hq, R_k, sm_scale * kLog2e,
+                                        static_cast<float*>(workspace), hs, L->rot_per_head,
+                                        L->num_kv_heads));
+  if (st) return st;
+  return launch_kv4_rest(L, pages, B, Hq, block_table, max_pages_per_seq, seq_lens, R_v, num_splits,
+                         weights, weights_out, workspace, out, out_dtype, hs);
+}
+
+int oscar_kv4_decode_step(const oscar_layout* L, void* pages, const void* k_new,
+                          const void* v_new, const int64_t* slot_mapping, int32_t n_new,
+                          float clip_k, float clip_v, const void* q, int32_t B, int32_t Hq,
+                          const int32_t* block_table, int32_t max_pages_per_seq,
+                          const int32_t* seq_lens, const float* R_k, const float* R_v,
+                          float sm_scale, int32_t num_splits, const float* weights,
+                          float* weights_out, void* workspace, size_t workspace_bytes,
+                          void* out, oscar_dtype out_dtype, void* stream) {
+  int st = check_layout(L);
+  if (st) return st;
+  if (n_new < 0 || !clip_ok(clip_k) || !clip_ok(clip_v)) return OSCAR_ERR_INVALID_ARG;
+  if (n_new > 0 && (st = check_kv4_rows(L, k_new, v_new, slot_mapping, n_new))) return st;
+  st = check_kv4_decode(L, pages, q, B, Hq, block_table, max_pages_per_seq, seq_lens, R_k, R_v,
+                        sm_scale, &num_splits, weights, weights_out, workspace, workspace_bytes, out,
+                        out_dtype);
+  if (st) return st;
+  st = debug_check(L, stream, B, block_table, max_pages_per_seq, seq_lens,
+                   n_new > 0 ? slot_mapping : nullptr, n_new, nullptr, 0);
+  if (st) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  st = hip_status(launch_kv4_step_prologue(pages, L->num_kv_heads, static_cast<const uint16_t*>(k_new),
+                                           static_cast<const uint16_t*>(v_new), slot_mapping, n_new, R_k,
+                                           R_v, clip_k, clip_v, quant_fmt(L),
+                                           static_cast<const uint16_t*>(q), B, Hq, sm_scale * kLog2e,
+                                           static_cast<float*>(workspace), hs));
+  if (st) return st;
+  return launch_kv4_rest(L, pages, B, Hq, block_table, max_pages_per_seq, seq_lens, R_v, num_splits,
+                         weights, weights_out, workspace, out, out_dtype, hs);
+}
+
+size_t oscar_kv4_evict_workspace_bytes(const oscar_layout* L, int32_t B, int32_t max_pages_per_seq) {
+  if (check_layout(L) != OSCAR_OK || B < 1 || B > 65535 || check_kv4_slots(L, max_pages_per_seq) != OSCAR_OK)
+    return 0;
+  return kv4_evict_ws_bytes(L->num_kv_heads, B, max_pages_per_seq);
+}
+
+int oscar_kv4_evict(const oscar_layout* L, void* pages, int32_t B, const int32_t* block_table,
+                    int32_t max_pages_per_seq, const int32_t* seq_lens, const float* weights,
+                    float* weights_out, const int32_t* pos, int32_t* pos_out,
+                    const int32_t* num_seen, int32_t budget, int32_t sink, int32_t recent,
+                    int32_t* new_lens, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_layout(L);
+  if (st) return st;
+  if (B < 1 || budget < 1 || sink < 0 || recent < 0) return OSCAR_ERR_INVALID_ARG;
+  if (B > 65535) return OSCAR_ERR_UNSUPPORTED;
+  if ((st = check_kv4_slots(L, max_pages_per_seq))) return st;
+  if (!pages || !block_table || !seq_lens || !weights || !weights_out || !pos || !pos_out || !num_seen ||
+      !new_lens || !workspace || new_lens == seq_lens)
+    return OSCAR_ERR_INVALID_ARG;
+  if (!aligned(pages, 16) || !aligned(weights, 16) || !aligned(weights_out, 16) || !aligned(pos, 16) ||
+      !aligned(pos_out, 16) || !aligned(workspace, 256))
+    return OSCAR_ERR_INVALID_ARG;
+  if (workspace_bytes < kv4_evict_ws_bytes(L->num_kv_heads, B, max_pages_per_seq))
+    return OSCAR_ERR_WORKSPACE_TOO_SMALL;
+  st = debug_check(L, stream, B, block_table, max_pages_per_seq, seq_lens, nullptr, 0, nullptr, 0);
+  if (st) return st;
+  EvictArgs a;
+  a.pages = static_cast<uint8_t*>(pages);
+  a.Hkv = L->num_kv_heads;
+  a.B = B;
+  a.ng = groups(L);
+  a.block_table = block_table;
+  a.max_pages = max_pages_per_seq;
+  a.seq_lens = seq_lens;
+  a.weights = weights;
+  a.weights_out = weights_out;
+  a.pos = pos;
+  a.pos_out = pos_out;
+  a.seen = num_seen;
+  a.budget = budget;
+  a.sink = sink;
+  a.recent = recent;
+  a.new_lens = new_lens;
+  a.ws = workspace;
+  return hip_status(launch_kv4_evict(a, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
 // bf16 baseline
 // ---------------------------------------------------------------------------
 
