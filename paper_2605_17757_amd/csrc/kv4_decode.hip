@@ -7,16 +7,20 @@
 // channels:
 //   score_t  = sum_G s (sum_{c in G} q~_c n_c - z sum_{c in G} q~_c)
 //   o~_c     = sum_t w_t n_c - sum_t w_t z_t,    w_t = 2^(score_t - m) s_t (of c's group)
-// Both inner sums run on the bf16 matrix cores and are exact products summed in fp32:
-//   * a code enters as the 16-bit pattern n, the bf16 subnormal n 2^-133, which a mask
-//     and a shift make of the packed nibbles (7 instructions per 8 codes; a conversion
-//     would take 2 per code);
-//   * q~ 2^64 and w 2^64 enter as three bf16 pieces, 8 bits of the significand each,
-//     together the whole fp32 value.  The pieces of one head are three rows of the
-//     16-row operand and 4 heads fill it, so that up to 4 heads per KV head cost no more
-//     matrix products than unsplit operands would; products are about
-//     2^-69 x q~ n, far from the fp32 range's ends for |q~| and scales below 2^56.
-// The fourth row of a head is zero.
+// Both inner sums run on the matrix cores, as exact products summed in fp32.
+//   Scores, bf16: a code enters as the 16-bit pattern n, the bf16 subnormal n 2^-133
+//     (for the odd nibbles of a byte 16 n, in place), which masks and one shift make of
+//     the packed nibbles: 5 instructions per 8 codes.  q~ 2^64 enters as three bf16
+//     pieces, 8 bits of the significand each, together the whole fp32 value.
+//   Values, fp16: a code enters as n - 8 (1024 + n by a mask, then a packed addition).
+//     With the codes centred the two sums over tokens are as small as o~ itself; the
+//     matrix cores drop product bits below the accumulator's last ones, and against
+//     sums of uncentred codes that left errors of 1e-5 of the output.  w is scaled by a
+//     power of two per page and group and enters as two fp16 pieces, the second one of
+//     the rest times 2^12: 22 bits, over 2^25 between the page's weights.
+// The pieces of one head are rows of the 16-row operand and 4 heads fill it, so that up
+// to 4 heads per KV head cost no more matrix products than unsplit operands would.
+// |q~| must stay below 2^56 (scores: 2^-69 n q~ 2^133 2^-64).
 #define OSCAR_SPLIT_DIV32
 #include <hip/hip_fp16.h>
 
@@ -30,51 +34,82 @@ namespace oscar {
 namespace {
 
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef __fp16 fp16x2 __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;         // waves of a block: a team on one range of pages
 constexpr int kPw = 40;           // dwords per row of the weights operand in LDS
-constexpr float kSlack = 10.0f;   // how far (log2) a score may exceed the reference maximum
-constexpr float kIn = 0x1p64f;    // scale of the operands, and of the products with codes
+constexpr float kSlack = 4.0f;    // how far (log2) a score may exceed the reference maximum
+constexpr float kIn = 0x1p64f;    // scale of q~ in the scores' products with codes
 constexpr float kOut = 0x1p69f;   // back: 2^133 / kIn
+constexpr int kTop = 10;          // scales of a page enter below 2^kTop: w < 2^(kTop + kSlack)
+constexpr float kRest = 4096.0f;  // scale of w's second piece
 
 __device__ inline f4v mfma(const u4v& a, const u4v& b, const f4v& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c,
                                                  0, 0, 0);
 }
-// Piece i (0: the leading 8 bits, 1, 2: the next; 3: zero) of x, as fp32.
+__device__ inline f4v mfma_h(const u4v& a, const u4v& b, const f4v& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0,
+                                                0, 0);
+}
 __device__ inline float top16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 __device__ inline uint32_t pack_hi(float lo, float hi) {  // the upper halves of two floats
   return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
-__device__ inline u4v unpack(uint32_t d) {  // nibbles 0, 4, 1, 5, 2, 6, 3, 7 as 16-bit lanes
+// Nibbles of d as 16-bit lanes: (0, 4), (1, 5) x 16, (2, 6), (3, 7) x 16.
+__device__ inline u4v unpack(uint32_t d) {
   constexpr uint32_t m = 0x000f000fu;
-  return u4v{d & m, (d >> 4) & m, (d >> 8) & m, (d >> 12) & m};
+  return u4v{d & m, d & (m << 4), (d >> 8) & m, (d >> 8) & (m << 4)};
 }
-__device__ inline float row_sum(float x) {  // over the 16 lanes of a row
-#pragma unroll
-  for (int k = 8; k >= 1; k >>= 1) x += __shfl_xor(x, k, 64);
-  return x;
+// Over the 16 lanes of a row, the same in each of them (rotations by 8, 4, 2, 1).
+template <class Op>
+__device__ inline float row_reduce(float x, Op op) {
+  auto ror = [](float v, auto ctrl) {
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  x = op(x, ror(x, std::integral_constant<int, 0x128>{}));
+  x = op(x, ror(x, std::integral_constant<int, 0x124>{}));
+  x = op(x, ror(x, std::integral_constant<int, 0x122>{}));
+  return op(x, ror(x, std::integral_constant<int, 0x121>{}));
+}
+__device__ inline float row_sum(float x) {
+  return row_reduce(x, [](float a, float b) { return a + b; });
 }
 __device__ inline float row_max(float x) {
-#pragma unroll
-  for (int k = 8; k >= 1; k >>= 1) x = fmaxf(x, __shfl_xor(x, k, 64));
-  return x;
+  return row_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+}
+// Bytes of 8 slots as fp16 n - 8 of their low nibbles (lo) and 16 (n - 8) of the high ones.
+__device__ inline uint32_t centred(uint32_t v, float mid) {
+  const h2 x = __builtin_bit_cast(h2, v | 0x64006400u) - (_Float16)mid;
+  return __builtin_bit_cast(uint32_t, x);
+}
+__device__ inline void unpack_v(uint32_t d0, uint32_t d1, u4v& lo, u4v& hi) {
+  constexpr uint32_t m = 0x000f000fu;
+  lo = u4v{centred(d0 & m, 1032.0f), centred((d0 >> 8) & m, 1032.0f), centred(d1 & m, 1032.0f),
+           centred((d1 >> 8) & m, 1032.0f)};
+  hi = u4v{centred(d0 & (m << 4), 1152.0f), centred((d0 >> 8) & (m << 4), 1152.0f),
+           centred(d1 & (m << 4), 1152.0f), centred((d1 >> 8) & (m << 4), 1152.0f)};
+}
+// Scale and zero of an entry.  (A binary16 that feeds one fused multiply-add is converted
+// by it: no instruction of its own.)
+template <bool BF>
+__device__ inline float meta_s(uint32_t e) {
+  return BF ? __uint_as_float(e << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)e);
 }
 template <bool BF>
-__device__ inline float meta_lo(uint32_t e) {
-  return BF ? __uint_as_float(e << 16) : __half2float(__ushort_as_half((unsigned short)(e & 0xffffu)));
-}
-template <bool BF>
-__device__ inline float meta_hi(uint32_t e) {
-  return BF ? __uint_as_float(e & 0xffff0000u) : __half2float(__ushort_as_half((unsigned short)(e >> 16)));
+__device__ inline float meta_z(uint32_t e) {
+  return BF ? __uint_as_float(e & 0xffff0000u) : (float)__builtin_bit_cast(_Float16, (uint16_t)(e >> 16));
 }
 
 template <int NCH>
 struct SplitSmem {
   u4v qa[NCH][4][64];                     // query operands: chunk, 32-channel block, lane
-  uint32_t pw[kWaves][NCH][16 * kPw];     // weights operand of a group; a wave's o~ [4][128] at the end
+  uint32_t pw[kWaves][NCH][4 * kD];       // weights operand of a group (8 rows: head, piece); o~ at the end
   float ml[kWaves][NCH * 4][2];           // the waves' (m, l)
 };
 
@@ -110,7 +145,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[e] = src[e] * kIn;
+          x[e] = src[e] * (e & 2 ? kIn / 16.0f : kIn);
           if (pc > 0) x[e] -= top16(x[e]);
           if (pc > 1) x[e] -= top16(x[e]);
         }
@@ -132,12 +167,13 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
 #pragma unroll
       for (int k = 1; k < 16 / NG; k <<= 1) s += __shfl_xor(s, k, 64);
 #pragma unroll
-      for (int q = 0; q < NG; ++q) qs[ch][q] = __shfl(s, (l & 48) + q * (16 / NG), 64);
+      for (int q = 0; q < NG; ++q) qs[ch][q] = __shfl(s, (l & 48) + q * (16 / NG), 64) * (1.0f / kOut);
     }
     __syncthreads();
 
-    float m[NCH], lsum[NCH], wz[NCH][NG];
-    f4v o[NCH][8];
+    // State: o (before the zero points' part: channel 16 ct + lo of head 4 ch + hi), and
+    // per lane, over its own slots, the sums of weights and of weights times (z - 8).
+    float m[NCH], lsum[NCH], wz[NCH][NG], o[NCH][8];
 #pragma unroll
     for (int ch = 0; ch < NCH; ++ch) {
       m[ch] = -INFINITY;
@@ -145,7 +181,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
 #pragma unroll
       for (int q = 0; q < NG; ++q) wz[ch][q] = 0.0f;
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) o[ch][ct] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int ct = 0; ct < 8; ++ct) o[ch][ct] = 0.0f;
     }
     const int32_t* __restrict__ bt = block_table + (size_t)b * max_pages;
     const int n_mine = (p1 - p0 - w + kWaves - 1) / kWaves;  // <= 0: none
@@ -173,6 +209,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
     }
     for (int i = 0; i < n_mine; ++i) {
       const int pg = p0 + w + kWaves * i, ntok = min(kP, len - pg * kP);
+      if (((i + 1) & 63) == 0 && i + 1 < n_mine) ids = page_ids(i + 1);
       u4v vr[4], vs[NG];
       {
         const u4v* p = reinterpret_cast<const u4v*>(blk + kKv4CodeBytes) + l;
@@ -189,38 +226,42 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       for (int ch = 0; ch < NCH; ++ch)
 #pragma unroll
         for (int u = 0; u < 4; ++u) sc[ch][u] = 0.0f;
+      // a slot's sums are used while the next slot's products run
+      f4v d[2][NCH];
 #pragma unroll
-      for (int q = 0; q < NG; ++q) {
-        f4v d[NCH][4];
+      for (int qu = 0; qu <= 4 * NG; ++qu) {
+        const int q = qu / 4, u = qu % 4;
+        if (qu < 4 * NG) {
 #pragma unroll
-        for (int k = 0; k < KPG; ++k) {
-          const int kc = q * KPG + k;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const u4v bop = unpack(kr[u][kc]);
+          for (int k = 0; k < KPG; ++k) {
+            const u4v bop = unpack(kr[u][q * KPG + k]);
 #pragma unroll
             for (int ch = 0; ch < NCH; ++ch)
-              d[ch][u] = mfma(sm.qa[ch][kc][l], bop, k == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[ch][u]);
+              d[qu & 1][ch] = mfma(sm.qa[ch][q * KPG + k][l], bop,
+                                   k == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[qu & 1][ch]);
           }
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t e = ks[(u * NG + q) >> 2][(u * NG + q) & 3];
-          const float s = meta_lo<BF>(e), z = meta_hi<BF>(e);
-          const float so = s * kOut, sz = s * z;
+        if (qu > 0) {
+          const int qp = (qu - 1) / 4, up = (qu - 1) % 4;
+          const uint32_t e = ks[(up * NG + qp) >> 2][(up * NG + qp) & 3];
 #pragma unroll
           for (int ch = 0; ch < NCH; ++ch) {
-            const float dot = (d[ch][u][0] + d[ch][u][1]) + d[ch][u][2];
-            sc[ch][u] = fmaf(so, dot, fmaf(-sz, qs[ch][q], sc[ch][u]));
+            const f4v& x = d[(qu - 1) & 1][ch];
+            sc[ch][up] = fmaf(meta_s<BF>(e), fmaf(meta_z<BF>(e), -qs[ch][qp], (x[0] + x[1]) + x[2]), sc[ch][up]);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sc[ch][u] *= kOut;
       __builtin_amdgcn_sched_barrier(0);
-      if (i + 1 < n_mine) {  // the next page's K, while this page's V is used
-        if (((i + 1) & 63) == 0) ids = page_ids(i + 1);
-        blk = block_of(i + 1);
-        load_k(blk);
-      }
+      // The next page's K, while this page's V is used (after the last page its own again:
+      // with a branch around the loads the compiler moves the sums above behind it, and
+      // keeps the products of all slots in registers).
+      blk = block_of(min(i + 1, n_mine - 1));
+      load_k(blk);
       if (ntok < kP) {  // the partial last page: other slots hold anything
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -272,51 +313,67 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       // ---- o~ += w V, group by group: the weights' pieces to LDS as the operand's rows ----
 #pragma unroll
       for (int q = 0; q < NG; ++q) {
+        __builtin_amdgcn_sched_barrier(0);
         float s[4], z[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const uint32_t e = vs[(u * NG + q) >> 2][(u * NG + q) & 3];
-          s[u] = meta_lo<BF>(e) * kIn;
-          z[u] = meta_hi<BF>(e);
+          s[u] = meta_s<BF>(e);
+          z[u] = fmaf(meta_z<BF>(e), 1.0f, -8.0f);
         }
+        const int ex = __builtin_amdgcn_frexp_expf(row_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])))) - kTop;
+        const float back = __builtin_ldexpf(1.0f, ex);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] = __builtin_ldexpf(s[u], -ex);
         lane_exchange();  // the reads of the previous group's operand come first
 #pragma unroll
         for (int ch = 0; ch < NCH; ++ch) {
-          float x[4];
+          float x[4], y[4], wsum = 0.0f;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             x[u] = p[ch][u] * s[u];
-            wz[ch][q] = fmaf(x[u], z[u], wz[ch][q]);
+            y[u] = (p[ch][u] * kRest) * s[u];
+            wsum = fmaf(x[u], z[u], wsum);
           }
-          uint32_t* row = sm.pw[w][ch] + 4 * hi * kPw + 2 * lo;
-#pragma unroll
-          for (int pc = 0; pc < 3; ++pc) {
-            *reinterpret_cast<uint2*>(row + pc * kPw) = make_uint2(pack_hi(x[0], x[1]), pack_hi(x[2], x[3]));
-            if (pc < 2)
-#pragma unroll
-              for (int u = 0; u < 4; ++u) x[u] -= top16(x[u]);
-          }
+          wz[ch][q] = fmaf(wsum, back, wz[ch][q]);
+          const fp16x2 h0 = __builtin_amdgcn_cvt_pkrtz(x[0], x[1]), h1 = __builtin_amdgcn_cvt_pkrtz(x[2], x[3]);
+          const fp16x2 r0 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h0[0], -kRest, y[0]),
+                                                       fmaf((float)h0[1], -kRest, y[1]));
+          const fp16x2 r1 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h1[0], -kRest, y[2]),
+                                                       fmaf((float)h1[1], -kRest, y[3]));
+          uint32_t* row = sm.pw[w][ch] + 2 * hi * kPw + 2 * lo;
+          *reinterpret_cast<uint2*>(row) =
+              make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
+          *reinterpret_cast<uint2*>(row + kPw) =
+              make_uint2(__builtin_bit_cast(uint32_t, r0), __builtin_bit_cast(uint32_t, r1));
         }
         lane_exchange();
-        u4v a[NCH][2];
+        u4v a[NCH][2];  // rows 4 h + 2, 4 h + 3 of the operand repeat 4 h, 4 h + 1
 #pragma unroll
         for (int ch = 0; ch < NCH; ++ch)
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
-            a[ch][kt] = *reinterpret_cast<const u4v*>(sm.pw[w][ch] + lo * kPw + 16 * kt + 4 * hi);
+            a[ch][kt] = *reinterpret_cast<const u4v*>(sm.pw[w][ch] + ((lo >> 2) * 2 + (lo & 1)) * kPw + 16 * kt +
+                                                      4 * hi);
 #pragma unroll
         for (int k = 0; k < KPG; ++k) {
           const int j = q * KPG + k;
+          __builtin_amdgcn_sched_barrier(0);
+          f4v d[NCH][2];
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt) {
-            // bytes of 8 slots; the low nibbles are channel 32 j + lo, the high ones + 16
-            const u4v x = unpack(vr[j][2 * kt]), y = unpack(vr[j][2 * kt + 1]);
-            const u4v b0 = u4v{x[0], x[2], y[0], y[2]}, b1 = u4v{x[1], x[3], y[1], y[3]};
+            u4v b0, b1;  // channels 32 j + lo and 32 j + 16 + lo
+            unpack_v(vr[j][2 * kt], vr[j][2 * kt + 1], b0, b1);
 #pragma unroll
             for (int ch = 0; ch < NCH; ++ch) {
-              o[ch][2 * j] = mfma(a[ch][kt], b0, o[ch][2 * j]);
-              o[ch][2 * j + 1] = mfma(a[ch][kt], b1, o[ch][2 * j + 1]);
+              d[ch][0] = mfma_h(a[ch][kt], b0, kt == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[ch][0]);
+              d[ch][1] = mfma_h(a[ch][kt], b1, kt == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[ch][1]);
             }
+          }
+#pragma unroll
+          for (int ch = 0; ch < NCH; ++ch) {
+            o[ch][2 * j] = fmaf(fmaf(d[ch][0][1], 1.0f / kRest, d[ch][0][0]), back, o[ch][2 * j]);
+            o[ch][2 * j + 1] = fmaf(fmaf(d[ch][1][1], 1.0f / kRest, d[ch][1][0]), back, o[ch][2 * j + 1]);
           }
         }
       }
@@ -329,11 +386,11 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       const float lt = row_sum(lsum[ch]);
       float z[NG];
 #pragma unroll
-      for (int q = 0; q < NG; ++q) z[q] = row_sum(wz[ch][q]) * (1.0f / kIn);
+      for (int q = 0; q < NG; ++q) z[q] = row_sum(wz[ch][q]);
       float* om = reinterpret_cast<float*>(sm.pw[w][ch]) + hi * kD;
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
-        om[16 * ct + lo] = fmaf((o[ch][ct][0] + o[ch][ct][1]) + o[ch][ct][2], kOut, -z[ct / 2 / KPG]);
+        om[16 * ct + lo] = fmaf(o[ch][ct], ct & 1 ? 1.0f / 16.0f : 1.0f, -z[ct / 2 / KPG]);
       if (lo == 0) {
         sm.ml[w][4 * ch + hi][0] = m[ch];
         sm.ml[w][4 * ch + hi][1] = lt;
@@ -369,30 +426,31 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
     __syncthreads();
   };
 
-  if (num_splits == 1) {  // whole sequences
-    for (int b = r; b < B; b += n_ranges) {
-      const int n = pages_of(b);
-      if (n) run_piece(b, 0, n, 0, true);
-    }
-    if (kvh == 0 && w == 0) mark_empty(r, n_ranges, B, Hq, 1, 1, part_ml, pages_of);
-    return;
+  // One piece at a time: of the block's range of pages, or (num_splits 1) whole sequences.
+  const bool whole = num_splits == 1;
+  RangeStart s;
+  if (whole) {
+    s.b = r;
+    s.npg = r < B ? pages_of(r) : 0;
+    s.x = s.before = 0;
+    s.xe = s.pw = (int64_t)1 << 40;
+  } else {
+    s = range_start(r, n_ranges, B, max_pages, num_splits, pages_of);
   }
-  const RangeStart s = range_start(r, n_ranges, B, max_pages, num_splits, pages_of);
   if (kvh == 0 && w == 0) mark_empty(r, n_ranges, B, Hq, num_splits, num_splits, part_ml, pages_of);
-  if (s.npg == 0) return;
+  if (!whole && s.npg == 0) return;
   int b = s.b, npg_b = s.npg;
   int64_t x = s.x, before = s.before;
-  while (true) {
+  while (b < B) {
     const int64_t end = min(s.xe, before + npg_b);
-    const int piece = (int)(r - div64(before, s.pw));
-    run_piece(b, (int)(x - before), (int)(end - before), piece, end == before + npg_b);
+    if (end > x)
+      run_piece(b, (int)(x - before), (int)(end - before), whole ? 0 : (int)(r - div64(before, s.pw)),
+                end == before + npg_b);
     x = end;
     if (x >= s.xe) break;
     before += npg_b;
-    do {  // next sequence with pages
-      if (++b >= B) return;  // not reached: pages remain before xe <= T
-      npg_b = pages_of(b);
-    } while (npg_b == 0);
+    b += whole ? n_ranges : 1;  // the next sequence; those without pages are passed over
+    npg_b = b < B ? pages_of(b) : 0;
   }
 }
 
