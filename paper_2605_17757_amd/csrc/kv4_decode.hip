@@ -12,7 +12,10 @@
 //     (for the odd nibbles of a byte 16 n, in place), which masks and one shift make of
 //     the packed nibbles: 5 instructions per 8 codes.  q~ 2^64 enters as three bf16
 //     pieces, 8 bits of the significand each, together the whole fp32 value.
-//   Values, fp16: a code enters as n - 8 (1024 + n by a mask, then a packed addition).
+//   Values, fp16: a code enters as (n - 8) 2^-9, a packed multiply-add of the 16-bit
+//     pattern (the fp16 subnormal n 2^-24).  (Subnormal operands lose bits in the matrix
+//     cores, which align products by the operands' exponents: with (n - 8) 2^-24 the
+//     output's error was 1e-5, where it is 5e-7 now.)
 //     With the codes centred the two sums over tokens are as small as o~ itself; the
 //     matrix cores drop product bits below the accumulator's last ones, and against
 //     sums of uncentred codes that left errors of 1e-5 of the output.  w is scaled by a
@@ -36,6 +39,7 @@ namespace {
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef uint16_t us2 __attribute__((ext_vector_type(2)));
 typedef __fp16 fp16x2 __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
@@ -83,18 +87,32 @@ __device__ inline float row_sum(float x) {
 __device__ inline float row_max(float x) {
   return row_reduce(x, [](float a, float b) { return fmaxf(a, b); });
 }
-// Bytes of 8 slots as fp16 n - 8 of their low nibbles (lo) and 16 (n - 8) of the high ones.
-__device__ inline uint32_t centred(uint32_t v, float mid) {
-  const h2 x = __builtin_bit_cast(h2, v | 0x64006400u) - (_Float16)mid;
-  return __builtin_bit_cast(uint32_t, x);
+// Bytes of 8 slots as fp16 (n - 8) 2^-9, of their low (lo) and of their high nibbles (hi).
+__device__ inline uint32_t centred(uint32_t v, float mul) {
+  const _Float16 m = (_Float16)mul, c = (_Float16)-0x1p-6f;
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2, v), h2{m, m}, h2{c, c}));
 }
 __device__ inline void unpack_v(uint32_t d0, uint32_t d1, u4v& lo, u4v& hi) {
   constexpr uint32_t m = 0x000f000fu;
-  lo = u4v{centred(d0 & m, 1032.0f), centred((d0 >> 8) & m, 1032.0f), centred(d1 & m, 1032.0f),
-           centred((d1 >> 8) & m, 1032.0f)};
-  hi = u4v{centred(d0 & (m << 4), 1152.0f), centred((d0 >> 8) & (m << 4), 1152.0f),
-           centred(d1 & (m << 4), 1152.0f), centred((d1 >> 8) & (m << 4), 1152.0f)};
+  lo = u4v{centred(d0 & m, 0x1p15f), centred((d0 >> 8) & m, 0x1p15f), centred(d1 & m, 0x1p15f),
+           centred((d1 >> 8) & m, 0x1p15f)};
+  hi = u4v{centred(d0 & (m << 4), 0x1p11f), centred((d0 >> 8) & (m << 4), 0x1p11f),
+           centred(d1 & (m << 4), 0x1p11f), centred((d1 >> 8) & (m << 4), 0x1p11f)};
 }
+__device__ inline uint32_t pk_max(uint32_t a, uint32_t b) {  // of unsigned 16-bit lanes
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+}
+// Largest of a non-negative float's bits over the 16 lanes of a row.
+__device__ inline uint32_t row_max_u(uint32_t x) {
+  auto ror = [](uint32_t v, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, true);
+  };
+  x = max(x, ror(x, std::integral_constant<int, 0x128>{}));
+  x = max(x, ror(x, std::integral_constant<int, 0x124>{}));
+  x = max(x, ror(x, std::integral_constant<int, 0x122>{}));
+  return max(x, ror(x, std::integral_constant<int, 0x121>{}));
+}
+
 // Scale and zero of an entry.  (A binary16 that feeds one fused multiply-add is converted
 // by it: no instruction of its own.)
 template <bool BF>
@@ -109,13 +127,13 @@ __device__ inline float meta_z(uint32_t e) {
 template <int NCH>
 struct SplitSmem {
   u4v qa[NCH][4][64];                     // query operands: chunk, 32-channel block, lane
-  uint32_t pw[kWaves][NCH][4 * kD];       // weights operand of a group (8 rows: head, piece); o~ at the end
+  uint32_t pw[kWaves][NCH][16 * kPw];     // weights operands of two groups (8 rows: head, piece); o~ at the end
   float ml[kWaves][NCH * 4][2];           // the waves' (m, l)
 };
 
 template <int NCH>
 struct SplitOcc {
-  static constexpr int per_simd = NCH == 1 ? 3 : 2;
+  static constexpr int per_simd = NCH == 1 ? 2 : 2;
 };
 
 template <bool BF, int NG, int NCH>
@@ -226,28 +244,31 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       for (int ch = 0; ch < NCH; ++ch)
 #pragma unroll
         for (int u = 0; u < 4; ++u) sc[ch][u] = 0.0f;
-      // a slot's sums are used while the next slot's products run
-      f4v d[2][NCH];
+      // a slot's sums are used while the next slot's products run; query operands one
+      // 32-channel block ahead
+      u4v qa[2][NCH];
+      f4v d[4][NCH];
 #pragma unroll
-      for (int qu = 0; qu <= 4 * NG; ++qu) {
-        const int q = qu / 4, u = qu % 4;
-        if (qu < 4 * NG) {
+      for (int ch = 0; ch < NCH; ++ch) qa[0][ch] = sm.qa[ch][0][l];
 #pragma unroll
-          for (int k = 0; k < KPG; ++k) {
-            const u4v bop = unpack(kr[u][q * KPG + k]);
+      for (int i = 0; i <= 16; ++i) {
+        const int kc = i / 4, u = i % 4;
+        if (i < 16) {
+          const u4v bop = unpack(kr[u][kc]);
 #pragma unroll
-            for (int ch = 0; ch < NCH; ++ch)
-              d[qu & 1][ch] = mfma(sm.qa[ch][q * KPG + k][l], bop,
-                                   k == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[qu & 1][ch]);
-          }
+          for (int ch = 0; ch < NCH; ++ch)
+            d[u][ch] = mfma(qa[kc & 1][ch], bop, kc % KPG == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[u][ch]);
+          if (u == 0 && kc < 3)
+#pragma unroll
+            for (int ch = 0; ch < NCH; ++ch) qa[(kc + 1) & 1][ch] = sm.qa[ch][kc + 1][l];
         }
-        if (qu > 0) {
-          const int qp = (qu - 1) / 4, up = (qu - 1) % 4;
-          const uint32_t e = ks[(up * NG + qp) >> 2][(up * NG + qp) & 3];
+        if (i > 0 && (i - 1) / 4 % KPG == KPG - 1) {
+          const int q = (i - 1) / 4 / KPG, up = (i - 1) % 4;
+          const uint32_t e = ks[(up * NG + q) >> 2][(up * NG + q) & 3];
 #pragma unroll
           for (int ch = 0; ch < NCH; ++ch) {
-            const f4v& x = d[(qu - 1) & 1][ch];
-            sc[ch][up] = fmaf(meta_s<BF>(e), fmaf(meta_z<BF>(e), -qs[ch][qp], (x[0] + x[1]) + x[2]), sc[ch][up]);
+            const f4v& x = d[up][ch];
+            sc[ch][up] = fmaf(meta_s<BF>(e), fmaf(meta_z<BF>(e), -qs[ch][q], (x[0] + x[1]) + x[2]), sc[ch][up]);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -311,21 +332,23 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
           lsum[ch] += p[ch][u];
         }
       // ---- o~ += w V, group by group: the weights' pieces to LDS as the operand's rows ----
-#pragma unroll
-      for (int q = 0; q < NG; ++q) {
-        __builtin_amdgcn_sched_barrier(0);
+      float back[NG];
+      auto stage = [&](int q) {
+        // scales 2^-ex s, below 2^kTop, and 2 (z - 8)  (single fused operations on the
+        // stored halves; the scales are not negative, so that their bits order them)
         float s[4], z[4];
+        uint32_t e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) e[u] = vs[(u * NG + q) >> 2][(u * NG + q) & 3];
+        const uint32_t big = row_max_u(pk_max(pk_max(e[0], e[1]), pk_max(e[2], e[3])) & 0xffffu);
+        const int ex = __builtin_amdgcn_frexp_expf(meta_s<BF>(big)) - kTop;
+        const float scale = __builtin_ldexpf(1.0f, -ex);
+        back[q] = __builtin_ldexpf(1.0f, ex);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const uint32_t e = vs[(u * NG + q) >> 2][(u * NG + q) & 3];
-          s[u] = meta_s<BF>(e);
-          z[u] = fmaf(meta_z<BF>(e), 1.0f, -8.0f);
+          s[u] = fmaf(meta_s<BF>(e[u]), scale, 0.0f);
+          z[u] = fmaf(meta_z<BF>(e[u]), 2.0f, -16.0f);
         }
-        const int ex = __builtin_amdgcn_frexp_expf(row_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])))) - kTop;
-        const float back = __builtin_ldexpf(1.0f, ex);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) s[u] = __builtin_ldexpf(s[u], -ex);
-        lane_exchange();  // the reads of the previous group's operand come first
 #pragma unroll
         for (int ch = 0; ch < NCH; ++ch) {
           float x[4], y[4], wsum = 0.0f;
@@ -335,17 +358,25 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
             y[u] = (p[ch][u] * kRest) * s[u];
             wsum = fmaf(x[u], z[u], wsum);
           }
-          wz[ch][q] = fmaf(wsum, back, wz[ch][q]);
+          wz[ch][q] = fmaf(wsum, 0.5f * back[q], wz[ch][q]);
           const fp16x2 h0 = __builtin_amdgcn_cvt_pkrtz(x[0], x[1]), h1 = __builtin_amdgcn_cvt_pkrtz(x[2], x[3]);
           const fp16x2 r0 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h0[0], -kRest, y[0]),
                                                        fmaf((float)h0[1], -kRest, y[1]));
           const fp16x2 r1 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h1[0], -kRest, y[2]),
                                                        fmaf((float)h1[1], -kRest, y[3]));
-          uint32_t* row = sm.pw[w][ch] + 2 * hi * kPw + 2 * lo;
+          uint32_t* row = sm.pw[w][ch] + (q & 1) * 8 * kPw + 2 * hi * kPw + 2 * lo;
           *reinterpret_cast<uint2*>(row) =
               make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
           *reinterpret_cast<uint2*>(row + kPw) =
               make_uint2(__builtin_bit_cast(uint32_t, r0), __builtin_bit_cast(uint32_t, r1));
+        }
+      };
+      if (NCH == 1) stage(0);
+#pragma unroll
+      for (int q = 0; q < NG; ++q) {
+        if (NCH > 1) {  // (a group ahead the wide instances would spill)
+          __builtin_amdgcn_sched_barrier(0);
+          stage(q);
         }
         lane_exchange();
         u4v a[NCH][2];  // rows 4 h + 2, 4 h + 3 of the operand repeat 4 h, 4 h + 1
@@ -353,8 +384,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
         for (int ch = 0; ch < NCH; ++ch)
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
-            a[ch][kt] = *reinterpret_cast<const u4v*>(sm.pw[w][ch] + ((lo >> 2) * 2 + (lo & 1)) * kPw + 16 * kt +
-                                                      4 * hi);
+            a[ch][kt] = *reinterpret_cast<const u4v*>(sm.pw[w][ch] + (q & 1) * 8 * kPw +
+                                                      ((lo >> 2) * 2 + (lo & 1)) * kPw + 16 * kt + 4 * hi);
+        __builtin_amdgcn_sched_barrier(0);
+        if (NCH == 1 && q + 1 < NG) stage(q + 1);  // into the other half of the buffer, while the reads are under way
 #pragma unroll
         for (int k = 0; k < KPG; ++k) {
           const int j = q * KPG + k;
@@ -372,11 +405,13 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
           }
 #pragma unroll
           for (int ch = 0; ch < NCH; ++ch) {
-            o[ch][2 * j] = fmaf(fmaf(d[ch][0][1], 1.0f / kRest, d[ch][0][0]), back, o[ch][2 * j]);
-            o[ch][2 * j + 1] = fmaf(fmaf(d[ch][1][1], 1.0f / kRest, d[ch][1][0]), back, o[ch][2 * j + 1]);
+            o[ch][2 * j] = fmaf(fmaf(d[ch][0][1], 1.0f / kRest, d[ch][0][0]), 0x1p9f * back[q], o[ch][2 * j]);
+            o[ch][2 * j + 1] =
+                fmaf(fmaf(d[ch][1][1], 1.0f / kRest, d[ch][1][0]), 0x1p9f * back[q], o[ch][2 * j + 1]);
           }
         }
       }
+      lane_exchange();  // the reads come before the next page's weights
     }
 
     // ---- the waves' states, merged into the piece's ----
@@ -390,7 +425,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       float* om = reinterpret_cast<float*>(sm.pw[w][ch]) + hi * kD;
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
-        om[16 * ct + lo] = fmaf(o[ch][ct], ct & 1 ? 1.0f / 16.0f : 1.0f, -z[ct / 2 / KPG]);
+        om[16 * ct + lo] = o[ch][ct] - z[ct / 2 / KPG];
       if (lo == 0) {
         sm.ml[w][4 * ch + hi][0] = m[ch];
         sm.ml[w][4 * ch + hi][1] = lt;
