@@ -13,47 +13,157 @@ __device__ inline uint16_t bf16_rne(float f) {  // finite values
   return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
 }
 
+// Scale and zero of a metadata entry.
+__device__ inline float2 meta_of(uint32_t e, int bf16) {
+  return bf16 ? make_float2(__uint_as_float(e << 16), __uint_as_float(e & 0xffff0000u))
+              : make_float2(__half2float(__ushort_as_half((unsigned short)e)),
+                            __half2float(__ushort_as_half((unsigned short)(e >> 16))));
+}
+// Value of code (x >> sh) & 15.
+__device__ inline float value_of(uint32_t x, int sh, float2 m) { return m.x * ((float)((x >> sh) & 15u) - m.y); }
+
 // ---------------------------------------------------------------------------
 // gather: value s (n - z) of every channel of the rows at `slots`, in fp32 steps (the
-// bf16 output rounds the product once).  32 threads per (token, head, tensor), 4
-// channels each.  Bound: HBM writes.
+// bf16 output rounds the product once).  Bound: HBM writes (fp32: 1024 bytes per token
+// and head against 128 + 8 ng read).
+//
+// Row by row (half a wave per tensor, 4 channels a lane) a V row is 64 single bytes of 32
+// cache lines.  Calls of 64 tokens or more take tiles of 64 tokens, one block per (tile,
+// head): the tile's slots are grouped by page, and of a page with kPageRows members or
+// more the block reads the whole page-head block in its 16-byte units, a quarter per
+// wave, and stores the members' rows from registers; rows of other pages go one by one.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void kv4_gather_kernel(const uint8_t* __restrict__ pages, int Hkv,
-                                                         const int64_t* __restrict__ slots, int64_t n_rows,
-                                                         void* __restrict__ k, void* __restrict__ v,
-                                                         int out_f32, int meta_bf16, int ng) {
-  const int c = threadIdx.x & 31, is_v = (threadIdx.x >> 5) & 1;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < n_rows; row += (int64_t)gridDim.x * 4) {
-    const int64_t tok = row / Hkv;
-    const int h = (int)(row - tok * Hkv);
-    const int64_t slot = slots[tok];
-    if (slot < 0) continue;
-    const int64_t page = slot / kP;
-    const int t = (int)(slot - page * kP);
-    const uint8_t* blk = pages + ((size_t)page * Hkv + h) * kv4_block_bytes(ng);
-    const uint32_t e = *reinterpret_cast<const uint32_t*>(blk + kv4_sz_off(ng, is_v) + (t * ng + c * ng / 32) * 4);
-    const float s = meta_bf16 ? __uint_as_float(e << 16) : __half2float(__ushort_as_half((unsigned short)e));
-    const float z = meta_bf16 ? __uint_as_float(e & 0xffff0000u)
-                              : __half2float(__ushort_as_half((unsigned short)(e >> 16)));
-    float x[4];
-    if (is_v) {
-      const uint8_t* b = blk + kv4_v_off(4 * c - 16 * (c >> 2 & 1), t);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = s * ((float)((b[16 * i] >> (c & 4)) & 15) - z);
-    } else {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + kv4_k_off(4 * c, t)) >> (8 * (c & 1));
-      x[0] = s * ((float)(w & 15) - z);
-      x[1] = s * ((float)((w >> 16) & 15) - z);
-      x[2] = s * ((float)((w >> 4) & 15) - z);
-      x[3] = s * ((float)((w >> 20) & 15) - z);
+struct GatherArgs {
+  const uint8_t* pages;
+  int Hkv;
+  const int64_t* slots;
+  int64_t n_tok;
+  void* k;
+  void* v;
+  int meta_bf16, ng;
+};
+
+template <bool F32>
+__device__ inline void put4(void* out, size_t at, float a, float b, float c, float d) {  // at: element, % 4 == 0
+  if (F32) *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(a, b, c, d);
+  else
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
+        make_uint2(bf16_rne(a) | ((uint32_t)bf16_rne(b) << 16), bf16_rne(c) | ((uint32_t)bf16_rne(d) << 16));
+}
+template <bool F32>
+__device__ inline void put1(void* out, size_t at, float x) {
+  if (F32) static_cast<float*>(out)[at] = x;
+  else static_cast<uint16_t*>(out)[at] = bf16_rne(x);
+}
+
+// One row by one wave: lanes 0 .. 31 K, 32 .. 63 V.
+template <bool F32>
+__device__ inline void gather_row(const GatherArgs& a, int64_t tok, int h, int64_t slot, int l) {
+  const int c = l & 31, is_v = l >> 5;
+  const int64_t page = slot / kP;
+  const int t = (int)(slot - page * kP);
+  const uint8_t* blk = a.pages + ((size_t)page * a.Hkv + h) * kv4_block_bytes(a.ng);
+  const float2 m = meta_of(*reinterpret_cast<const uint32_t*>(blk + kv4_sz_off(a.ng, is_v) +
+                                                              (t * a.ng + c * a.ng / 32) * 4), a.meta_bf16);
+  const size_t at = ((size_t)tok * a.Hkv + h) * kD + 4 * c;
+  if (is_v) {
+    const uint8_t* b = blk + kv4_v_off(4 * c - 16 * (c >> 2 & 1), t);
+    const int sh = c & 4;
+    put4<F32>(a.v, at, value_of(b[0], sh, m), value_of(b[16], sh, m), value_of(b[32], sh, m),
+              value_of(b[48], sh, m));
+  } else {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + kv4_k_off(4 * c, t)) >> (8 * (c & 1));
+    put4<F32>(a.k, at, value_of(w, 0, m), value_of(w, 16, m), value_of(w, 4, m), value_of(w, 20, m));
+  }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void kv4_gather_rows_kernel(GatherArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.n_tok * a.Hkv) return;
+  const int64_t tok = row / a.Hkv, slot = a.slots[tok];
+  if (slot >= 0) gather_row<F32>(a, tok, (int)(row - tok * a.Hkv), slot, threadIdx.x & 63);
+}
+
+constexpr int kPageRows = 8;  // members of a page from which on it is read whole
+
+template <bool F32>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void kv4_gather_kernel(GatherArgs a) {
+  __shared__ int idx_all[4][kP];  // per wave, of a page's slots: the tile's token, or -1
+  __shared__ uint32_t vsz_all[4][kP];
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lo = l & 15, hi = l >> 4, ng = a.ng;
+  // Blocks go to the 8 XCDs in turn: the heads of a tile, whose output rows are
+  // neighbours, to the same one.
+  const unsigned turn = blockIdx.x / 8;
+  const int64_t tok0 = ((int64_t)(turn / (unsigned)a.Hkv) * 8 + blockIdx.x % 8) * 64;
+  const int h = (int)(turn % (unsigned)a.Hkv);
+  if (tok0 >= a.n_tok) return;
+  int* idx = idx_all[w];
+  uint32_t* vsz = vsz_all[w];
+  const int64_t slot = tok0 + l < a.n_tok ? a.slots[tok0 + l] : -1;
+  const int64_t page = slot >= 0 ? slot / kP : -1;
+  const int t = (int)(slot - page * kP);
+  uint64_t open = __ballot(slot >= 0);
+  while (open) {  // one page per turn, the same in the four waves
+    const int first = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)open) - 1);
+    const int64_t p = ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(page >> 32), first) << 32) |
+                      (uint32_t)__builtin_amdgcn_readlane((int)page, first);
+    const bool member = (open >> l & 1) && page == p;
+    const uint64_t members = __ballot(member);
+    if (__popcll(members) < kPageRows) {
+      int n = 0;
+      for (uint64_t left = members; left; left &= left - 1, ++n) {
+        const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)left) - 1);
+        if ((n & 3) == w) gather_row<F32>(a, tok0 + i, h, p * kP + __builtin_amdgcn_readlane(t, i), l);
+      }
+      open &= ~members;
+      continue;
     }
-    void* out = is_v ? v : k;
-    if (out_f32)
-      reinterpret_cast<float4*>(out)[row * 32 + c] = make_float4(x[0], x[1], x[2], x[3]);
-    else
-      reinterpret_cast<uint2*>(out)[row * 32 + c] =
-          make_uint2(bf16_rne(x[0]) | ((uint32_t)bf16_rne(x[1]) << 16),
-                     bf16_rne(x[2]) | ((uint32_t)bf16_rne(x[3]) << 16));
+    // the wave's quarter, whole rows: K of slots 16 w .. + 15 (lane: slot 16 w + l / 4,
+    // channels 32 kc + 8 (l % 4) ..), V of slots 8 w .. + 7 and 32 more (lane: channels
+    // 32 hi + lo, + 16)
+    const uint8_t* blk = a.pages + ((size_t)p * a.Hkv + h) * kv4_block_bytes(ng);
+    const int tk = 16 * w + (l >> 2), c8 = l & 3;
+    const uint4 kr = reinterpret_cast<const uint4*>(blk)[64 * (tk & 3) + 16 * c8 + (tk >> 2)];
+    const uint4 vr = reinterpret_cast<const uint4*>(blk + kKv4CodeBytes)[64 * hi + 16 * w + lo];
+    uint32_t zk[4];
+#pragma unroll
+    for (int kc = 0; kc < 4; ++kc)
+      zk[kc] = reinterpret_cast<const uint32_t*>(blk + kv4_sz_off(ng, 0))[tk * ng + kc * ng / 4];
+    // V entries of the wave's slots: lane (slot 32 (l / 32) + 8 w + l / 4 % 8, block l % 4)
+    const uint32_t zv = reinterpret_cast<const uint32_t*>(
+        blk + kv4_sz_off(ng, 1))[(32 * (l >> 5) + 8 * w + (l >> 2 & 7)) * ng + (l & 3) * ng / 4];
+    lane_exchange();  // the last turn's reads come first
+    idx[l] = -1;
+    vsz[l] = zv;
+    lane_exchange();
+    if (member) idx[t] = l;
+    lane_exchange();
+    open &= ~__ballot(member && idx[t] == l);  // of a slot that comes twice the other token waits
+    if (const int i = idx[tk]; i >= 0) {
+      const size_t at = ((size_t)(tok0 + i) * a.Hkv + h) * kD + 8 * c8;
+      const uint32_t d[4] = {kr.x, kr.y, kr.z, kr.w};
+#pragma unroll
+      for (int kc = 0; kc < 4; ++kc) {
+        const float2 m = meta_of(zk[kc], a.meta_bf16);
+        put4<F32>(a.k, at + 32 * kc, value_of(d[kc], 0, m), value_of(d[kc], 16, m), value_of(d[kc], 4, m),
+                  value_of(d[kc], 20, m));
+        put4<F32>(a.k, at + 32 * kc + 4, value_of(d[kc], 8, m), value_of(d[kc], 24, m), value_of(d[kc], 12, m),
+                  value_of(d[kc], 28, m));
+      }
+    }
+    const uint32_t d[4] = {vr.x, vr.y, vr.z, vr.w};
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {  // slot 32 kt + 8 w + 4 f + x
+      const int kt = k >> 3, f = k >> 2 & 1, x = k & 3;
+      const int i = __builtin_amdgcn_readfirstlane(idx[32 * kt + 8 * w + 4 * f + x]);
+      if (i < 0) continue;
+      const float2 m = meta_of(vsz[4 * k + hi], a.meta_bf16);
+      const uint32_t b = d[2 * kt + f] >> (8 * (x / 2 + 2 * (x % 2)));
+      const size_t at = ((size_t)(tok0 + i) * a.Hkv + h) * kD + 32 * hi + lo;
+      put1<F32>(a.v, at, value_of(b, 0, m));
+      put1<F32>(a.v, at + 16, value_of(b, 4, m));
+    }
   }
 }
 
@@ -64,12 +174,18 @@ __global__ __launch_bounds__(256) void kv4_gather_kernel(const uint8_t* __restri
 // below m, so that only rows that must move do, sources and destinations are disjoint,
 // and the moves can run in any order, in place.
 //
-//   select: one block per row.  The m-th largest rank by radix selection on ordered
-//           32-bit keys (4 histograms of 8 bits), then one pass in slot order that marks
-//           what is kept, with block-wide counts for ties, holes and movers.
-//   move:   the moved rows' bytes (codes, scales, zeros) from page to page.
+//   select: one block of 16 waves per row, each wave a contiguous part of the slots.  The
+//           m-th largest rank by radix selection on ordered 32-bit keys (3 histograms of
+//           11, 11 and 10 bits), kept in registers up to 32 slots a thread; then every
+//           wave counts what it keeps, one block-wide sum gives it its places in the
+//           lists of holes and movers, and a last pass fills them and pairs them off.
+//   move:   the moved rows' bytes (codes, scales, zeros) from page to page, one block per
+//           page that receives any.
+// Bounds: select the latency of its passes (one block per row), move the cache lines of
+// the sources' V codes (a row's 64 bytes lie in 32 lines).
 // ---------------------------------------------------------------------------
 constexpr int kSel = 1024;  // threads of a select block
+constexpr int kBatch = 4;   // slots per thread whose loads are issued together
 
 // Larger key, larger rank: finite weights in order (-0 as 0), NaN below all, protected
 // tokens above all.
@@ -80,39 +196,22 @@ __device__ inline uint32_t rank_key(float w, bool safe) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Exclusive prefix sum over the block's threads in order, and the total.
-__device__ inline int block_scan(int v, int* part, int& total) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const int y = __shfl_up(x, k, 64);
-    if (l >= k) x += y;
-  }
-  __syncthreads();  // earlier reads of part
-  if (l == 63) part[w] = x;
-  __syncthreads();
-  int before = 0;
-  total = 0;
-#pragma unroll
-  for (int k = 0; k < kSel / 64; ++k) {
-    before += k < w ? part[k] : 0;
-    total += part[k];
-  }
-  return before + x - v;
-}
-
+// ITEMS: slots per thread whose keys are kept in registers; 0: any number, formed anew
+// in every pass.
+template <int ITEMS>
 __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
     int Hkv, int64_t S, int max_pages, const int32_t* __restrict__ seq_lens, const float* weights,
     float* weights_out, const int32_t* pos, int32_t* pos_out, const int32_t* __restrict__ seen_all,
     int budget, int sink, int recent, int32_t* __restrict__ new_lens, int32_t* __restrict__ counts,
-    int2* __restrict__ moves, int64_t row0) {
-  __shared__ int hist[256];
-  __shared__ int part[kSel / 64];
+    int2* __restrict__ moves, int32_t* __restrict__ source, int64_t row0) {
+  constexpr int kW = kSel / 64;
+  __shared__ int hist[2 * kSel];
+  __shared__ int3 part[kW];  // per wave: keys equal to the last kept one, holes, movers
+  __shared__ int above_all[kW];
   __shared__ uint32_t found;
-  __shared__ int left;
+  __shared__ int left, same_all;
   const int64_t row = row0 + blockIdx.x;
-  const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv), t = threadIdx.x;
+  const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv), t = threadIdx.x, w = t >> 6, l = t & 63;
   const int n = min(max(seq_lens[b], 0), max_pages * kP), m = min(n, budget), seen = seen_all[b];
   const float* w_in = weights + row * S;
   const int32_t* p_in = pos + row * S;
@@ -123,10 +222,6 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
     const int p = p_in[i];
     return p >= 0 ? p : seen - (n - i);
   };
-  auto key_of = [&](int i) {
-    const int p = pos_of(i);
-    return rank_key(w_in[i], p < sink || p >= seen - recent);
-  };
   int n_moves = 0;
   if (n <= budget) {
     for (int i = t; i < n; i += kSel) {
@@ -134,75 +229,151 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
       p_out[i] = pos_of(i);
     }
   } else {
+    // the wave's slots: [s0, s1), s0 + 64 i + lane for i < reps
+    const int reps = (n + kSel - 1) / kSel, s0 = w * 64 * reps, s1 = min(n, s0 + 64 * reps);
+    // kBatch keys from item i0 on, all loads first (keys past s1 are not used)
+    auto load_keys = [&](int i0, uint32_t* key) {
+      int p[kBatch];
+      float x[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int at = min(s0 + 64 * (i0 + i) + l, n - 1);
+        p[i] = p_in[at];
+        x[i] = w_in[at];
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int at = min(s0 + 64 * (i0 + i) + l, n - 1), q = p[i] >= 0 ? p[i] : seen - (n - at);
+        key[i] = rank_key(x[i], q < sink || q >= seen - recent);
+      }
+    };
+    uint32_t keys[ITEMS ? ITEMS : 1];
+    if (ITEMS) {
+#pragma unroll
+      for (int i0 = 0; i0 < ITEMS; i0 += kBatch)
+        if (i0 < reps) load_keys(i0, keys + i0);
+    }
+    // f(i, key, valid) of the wave's slots in order
+    auto each = [&](auto&& f) {
+      if (ITEMS) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+          if (i < reps) f(i, keys[i], s0 + 64 * i + l < s1);
+      } else {
+        for (int i0 = 0; i0 < reps; i0 += kBatch) {
+          uint32_t k[kBatch];
+          load_keys(i0, k);
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i)
+            if (i0 + i < reps) f(i0 + i, k[i], s0 + 64 * (i0 + i) + l < s1);
+        }
+      }
+    };
     uint32_t prefix = 0;
     int need = m;  // slots still to be kept among the keys that share the prefix
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (t < 256) hist[t] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+      hist[2 * t] = hist[2 * t + 1] = 0;
       __syncthreads();
-      for (int i = t; i < n; i += kSel) {
-        const uint32_t k = key_of(i);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+      each([&](int, uint32_t k, bool valid) {
+        if (valid && (pass == 0 || (k >> (shift + bits)) == (prefix >> (shift + bits))))
+          atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1);
+      });
+      __syncthreads();
+      const int c0 = hist[2 * t], c1 = hist[2 * t + 1];  // digits 2 t, 2 t + 1
+      int above = c0 + c1;  // inclusive sum over the wave's lanes from l up
+#pragma unroll
+      for (int k = 1; k < 64; k <<= 1) {
+        const int y = __shfl_down(above, k, 64);
+        if (l + k < 64) above += y;
       }
+      if (l == 0) above_all[w] = above;
       __syncthreads();
-      if (t < 64) {  // digits 4 t .. 4 t + 3, counted from the top
-        int c[4], sum = 0;
-#pragma unroll
-        for (int i = 3; i >= 0; --i) sum += c[i] = hist[4 * t + i];
-        int above = sum;  // inclusive sum over the lanes from t up
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) {
-          const int y = __shfl_down(above, k, 64);
-          if (t + k < 64) above += y;
-        }
-        above -= sum;
-#pragma unroll
-        for (int i = 3; i >= 0; --i) {
-          if (above < need && above + c[i] >= need) {
-            found = (uint32_t)(4 * t + i);
-            left = need - above;
-          }
-          above += c[i];
-        }
+      above -= c0 + c1;  // digits above 2 t + 1: of the wave, then of the waves after it
+      for (int i = w + 1; i < kW; ++i) above += above_all[i];
+      if (above < need && above + c1 >= need) {
+        found = 2 * t + 1;
+        left = need - above;
+        same_all = c1;
+      } else if (above + c1 < need && above + c1 + c0 >= need) {
+        found = 2 * t;
+        left = need - above - c1;
+        same_all = c0;
       }
       __syncthreads();
       prefix |= found << shift;
       need = left;
+    }
+    // kept: keys above the prefix, and the first `need` slots of equal key (all of them
+    // if no more are equal: no tie to break)
+    const bool ties = same_all > need;
+    const uint64_t below = (1ull << l) - 1;
+    int eq0 = 0;  // equal keys of the waves before
+    if (ties) {
+      int eq = 0;
+      each([&](int, uint32_t k, bool valid) { eq += __popcll(__ballot(valid && k == prefix)); });
+      if (l == 0) part[w].x = eq;
       __syncthreads();
+      for (int i = 0; i < w; ++i) eq0 += part[i].x;
     }
-    // kept: keys above the prefix, and the first `need` slots of equal key
+    auto kept_of = [&](uint32_t k, bool valid, int& e) {
+      if (!ties) return valid && k >= prefix;
+      const uint64_t same = __ballot(valid && k == prefix);
+      const bool kept = valid && (k > prefix || (k == prefix && e + __popcll(same & below) < need));
+      e += __popcll(same);
+      return kept;
+    };
+    int e = eq0, holes = 0, movers = 0;
+    each([&](int i, uint32_t k, bool valid) {
+      const int at = s0 + 64 * i + l;
+      const bool kept = kept_of(k, valid, e);
+      holes += valid && at < m && !kept;
+      movers += kept && at >= m;
+    });
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) {
+      holes += __shfl_xor(holes, k, 64);
+      movers += __shfl_xor(movers, k, 64);
+    }
+    if (l == 0) {
+      part[w].y = holes;
+      part[w].z = movers;
+    }
+    __syncthreads();
+    holes = movers = 0;
+    for (int i = 0; i < kW; ++i) {
+      if (i < w) {
+        holes += part[i].y;
+        movers += part[i].z;
+      }
+      n_moves += part[i].z;
+    }
     int2* mv = moves + row * (S / 2);
-    int n_equal = 0, holes = 0, movers = 0;
-    for (int base = 0; base < n; base += kSel) {
-      const int i = base + t;
-      uint32_t k = 0;
-      bool equal = false;
-      if (i < n) {
-        k = key_of(i);
-        equal = k == prefix;
-      }
-      int total;
-      const int before = n_equal + block_scan(equal, part, total);
-      n_equal += total;
-      const bool kept = i < n && (k > prefix || (equal && before < need));
-      const bool hole = i < m && !kept, mover = kept && i >= m;
-      const int at = block_scan(hole ? 1 : mover ? 1 << 16 : 0, part, total);
-      if (hole) mv[holes + (at & 0xffff)].y = i;
-      if (mover) mv[movers + (at >> 16)].x = i;
-      holes += total & 0xffff;
-      movers += total >> 16;
+    e = eq0;
+    each([&](int i, uint32_t k, bool valid) {
+      const int at = s0 + 64 * i + l;
+      const bool kept = kept_of(k, valid, e);
+      const bool hole = valid && at < m && !kept, mover = kept && at >= m;
+      const uint64_t hs = __ballot(hole), ms = __ballot(mover);
+      if (hole) mv[holes + __popcll(hs & below)].y = at;
+      if (mover) mv[movers + __popcll(ms & below)].x = at;
+      holes += __popcll(hs);
+      movers += __popcll(ms);
       if (kept && !mover) {
-        w_out[i] = w_in[i];
-        p_out[i] = pos_of(i);
+        w_out[at] = w_in[at];
+        p_out[at] = pos_of(at);
+        source[row * S + at] = -1;
       }
-    }
-    n_moves = movers;
+    });
     __syncthreads();
     for (int i = t; i < n_moves; i += kSel) {
       const int2 x = mv[i];
       w_out[x.y] = w_in[x.x];
       p_out[x.y] = pos_of(x.x);
+      source[row * S + x.y] = x.x;
     }
-    __syncthreads();
+    __syncthreads();  // in place, the sources lie in what is cleared now
   }
   for (int64_t i = m + t; i < S; i += kSel) {
     w_out[i] = 0.0f;
@@ -211,32 +382,87 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
   if (t == 0) counts[row] = n_moves;
 }
 
-// One wave per moved row: 16 dwords of K codes, 64 bytes of V codes, 2 ng metadata entries.
+// Rows that move into destination page blockIdx.x of row blockIdx.y, by source slot.
+// Fewer than kPageRows of them go one at a time, a wave each: 16 dwords of K codes, 64
+// bytes of V codes, 2 ng metadata entries.  More are put together in the page's own units: wave
+// w takes the K units of slots 4 lo + w (16 bytes of one slot per lane) and the V units
+// of channels 32 w .. (16 slots of a channel pair per lane: 16 byte loads, of which 16
+// lanes share a cache line or two, and one store; a wave per row took 64 lines and 64
+// single bytes each way: 32 x 8 rows of 16k to 1024 slots, 116 us).
 __global__ __launch_bounds__(256) void kv4_evict_move_kernel(uint8_t* __restrict__ pages, int Hkv, int64_t S,
                                                              int ng, const int32_t* __restrict__ block_table,
                                                              int max_pages, const int32_t* __restrict__ counts,
-                                                             const int2* __restrict__ moves, int64_t row0) {
+                                                             const int32_t* __restrict__ source, int budget,
+                                                             int64_t row0) {
+  __shared__ const uint8_t* from_all[4][kP];  // per wave, of a page's slots: the source's block
+  __shared__ int src_all[4][kP];              // and its slot in it, or -1
   const int64_t row = row0 + blockIdx.y;
-  const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv), l = threadIdx.x & 63;
-  const int n = counts[row];
-  const int2* mv = moves + row * (S / 2);
+  if (counts[row] == 0) return;  // then source is not written
+  const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv);
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lo = l & 15, hi = l >> 4;
   const int32_t* bt = block_table + (size_t)b * max_pages;
-  for (int i = blockIdx.x * 4 + (threadIdx.x >> 6); i < n; i += gridDim.x * 4) {
-    const int2 x = mv[i];
-    const int ts = x.x % kP, td = x.y % kP;
-    const uint8_t* from = pages + ((size_t)bt[x.x / kP] * Hkv + h) * kv4_block_bytes(ng);
-    uint8_t* to = pages + ((size_t)bt[x.y / kP] * Hkv + h) * kv4_block_bytes(ng);
-    const int cv = 32 * (l >> 4) + (l & 15);
-    const uint8_t v = from[kv4_v_off(cv, ts)];
-    uint32_t d = 0;
-    const int sz = l - 16;  // lanes 16 ..: metadata entries of K, then of V
-    if (l < 16) d = *reinterpret_cast<const uint32_t*>(from + kv4_k_off(8 * l, ts));
-    else if (sz < 2 * ng)
-      d = *reinterpret_cast<const uint32_t*>(from + kv4_sz_off(ng, sz >= ng) + (ts * ng + sz % ng) * 4);
-    to[kv4_v_off(cv, td)] = v;
-    if (l < 16) *reinterpret_cast<uint32_t*>(to + kv4_k_off(8 * l, td)) = d;
-    else if (sz < 2 * ng)
-      *reinterpret_cast<uint32_t*>(to + kv4_sz_off(ng, sz >= ng) + (td * ng + sz % ng) * 4) = d;
+  const int slot = blockIdx.x * kP + l;
+  const int from = slot < budget ? source[row * S + slot] : -1;  // (moves: the row has more than budget slots)
+  const uint64_t moved = __ballot(from >= 0);
+  if (!moved) return;
+  const uint8_t* src = nullptr;
+  if (from >= 0) src = pages + ((size_t)bt[from / kP] * Hkv + h) * kv4_block_bytes(ng);
+  uint8_t* to = pages + ((size_t)bt[blockIdx.x] * Hkv + h) * kv4_block_bytes(ng);
+  const uint8_t** from_of = from_all[w];
+  int* src_of = src_all[w];
+  from_of[l] = src;
+  src_of[l] = from >= 0 ? from % kP : -1;
+  lane_exchange();
+  if (__popcll(moved) < kPageRows) {
+    const int cv = 32 * (l >> 4) + (l & 15), sz = l - 16;  // lanes 16 ..: metadata entries of K, then of V
+    int n = 0;
+    for (uint64_t todo = moved; todo; todo &= todo - 1, ++n) {
+      if ((n & 3) != w) continue;
+      const int td = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)todo) - 1), ts = src_of[td];
+      const uint8_t* f = from_of[td];
+      const uint8_t v = f[kv4_v_off(cv, ts)];
+      uint32_t d = 0;
+      if (l < 16) d = *reinterpret_cast<const uint32_t*>(f + kv4_k_off(8 * l, ts));
+      else if (sz < 2 * ng)
+        d = *reinterpret_cast<const uint32_t*>(f + kv4_sz_off(ng, sz >= ng) + (ts * ng + sz % ng) * 4);
+      to[kv4_v_off(cv, td)] = v;
+      if (l < 16) *reinterpret_cast<uint32_t*>(to + kv4_k_off(8 * l, td)) = d;
+      else if (sz < 2 * ng)
+        *reinterpret_cast<uint32_t*>(to + kv4_sz_off(ng, sz >= ng) + (td * ng + sz % ng) * 4) = d;
+    }
+    return;
+  }
+  // V units: the bytes of slots that do not move come from the page itself
+  uint4* vu = reinterpret_cast<uint4*>(to + kKv4CodeBytes) + 64 * w + l;
+  const uint4 old = *vu;
+  uint32_t got[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {  // slot 32 kt + 8 hi + 4 f + x
+    const int kt = k >> 3, f = k >> 2 & 1, x = k & 3, ts = 32 * kt + 8 * hi + 4 * f + x;
+    const int s = src_of[ts];
+    got[k] = s < 0 ? 256u : from_of[ts][kv4_v_off(32 * w + lo, s)];
+  }
+  const int tk = 4 * lo + w, sk = src_of[tk];
+  uint4 kd = make_uint4(0, 0, 0, 0);
+  if (sk >= 0) kd = reinterpret_cast<const uint4*>(from_of[tk])[64 * (sk % 4) + 16 * hi + sk / 4];
+  uint32_t zd[2] = {0, 0};  // metadata entries of slot l: group w of K and of V
+  const int sl = src_of[l];
+  if (sl >= 0 && w < ng) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      zd[i] = *reinterpret_cast<const uint32_t*>(from_of[l] + kv4_sz_off(ng, i) + (sl * ng + w) * 4);
+  }
+  uint32_t d[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int x = k & 3, sh = 8 * (x / 2 + 2 * (x % 2));
+    d[k >> 2] = got[k] > 255u ? d[k >> 2] : (d[k >> 2] & ~(255u << sh)) | (got[k] << sh);
+  }
+  *vu = make_uint4(d[0], d[1], d[2], d[3]);
+  if (sk >= 0) reinterpret_cast<uint4*>(to)[64 * (tk % 4) + 16 * hi + tk / 4] = kd;
+  if (sl >= 0 && w < ng) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<uint32_t*>(to + kv4_sz_off(ng, i) + (l * ng + w) * 4) = zd[i];
   }
 }
 
@@ -244,22 +470,38 @@ __global__ __launch_bounds__(256) void kv4_evict_move_kernel(uint8_t* __restrict
 
 hipError_t launch_kv4_gather(const uint8_t* pages, int Hkv, const int64_t* slots, int64_t n_tok,
                              void* k, void* v, int out_f32, int meta_bf16, int ng, hipStream_t st) {
-  const int64_t rows = n_tok * Hkv;
-  const unsigned blocks = (unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 20);
-  hipLaunchKernelGGL(kv4_gather_kernel, dim3(blocks), dim3(256), 0, st, pages, Hkv, slots, rows, k, v,
-                     out_f32, meta_bf16, ng);
-  return hipGetLastError();
+  // a launch holds fewer than 2^32 threads: 2^24 (token, head) rows at a time
+  const int64_t most = std::max<int64_t>(64, (1 << 24) / Hkv / 64 * 64);  // (at most 2^18 blocks)
+  for (int64_t t0 = 0; t0 < n_tok; t0 += most) {
+    const int64_t n = std::min(most, n_tok - t0), at = t0 * Hkv * kD * (out_f32 ? 4 : 2);
+    const GatherArgs a{pages, Hkv, slots + t0, n, static_cast<char*>(k) + at, static_cast<char*>(v) + at,
+                       meta_bf16, ng};
+    const int64_t blocks = n < 64 ? (n * Hkv + 3) / 4 : (n + 511) / 512 * 8 * Hkv;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
+    if (n < 64) {
+      if (out_f32) go(kv4_gather_rows_kernel<true>);
+      else go(kv4_gather_rows_kernel<false>);
+    } else {
+      if (out_f32) go(kv4_gather_kernel<true>);
+      else go(kv4_gather_kernel<false>);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 namespace {
+// Moves per row, their lists (hole, mover), and the source of every slot that receives one.
 struct EvictWs {
-  size_t moves_off, total;
+  size_t moves_off, source_off, total;
 };
 EvictWs evict_ws(int Hkv, int B, int max_pages) {
-  const size_t rows = (size_t)B * Hkv;
+  const size_t rows = (size_t)B * Hkv, S = (size_t)max_pages * kP;
   EvictWs w;
   w.moves_off = align256(rows * sizeof(int32_t));
-  w.total = align256(w.moves_off + rows * ((size_t)max_pages * kP / 2) * sizeof(int2));
+  w.source_off = align256(w.moves_off + rows * (S / 2) * sizeof(int2));
+  w.total = align256(w.source_off + rows * S * sizeof(int32_t));
   return w;
 }
 }  // namespace
@@ -268,23 +510,30 @@ size_t kv4_evict_ws_bytes(int Hkv, int B, int max_pages) { return evict_ws(Hkv, 
 
 hipError_t launch_kv4_evict(const EvictArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.B * a.Hkv, S = (int64_t)a.max_pages * kP;
-  int32_t* counts = static_cast<int32_t*>(a.ws);
-  int2* moves = reinterpret_cast<int2*>(static_cast<uint8_t*>(a.ws) +
-                                        evict_ws(a.Hkv, a.B, a.max_pages).moves_off);
+  const EvictWs ws = evict_ws(a.Hkv, a.B, a.max_pages);
+  uint8_t* base = static_cast<uint8_t*>(a.ws);
+  int32_t* counts = reinterpret_cast<int32_t*>(base);
+  int2* moves = reinterpret_cast<int2*>(base + ws.moves_off);
+  int32_t* source = reinterpret_cast<int32_t*>(base + ws.source_off);
   for (int64_t r0 = 0; r0 < rows; r0 += 1 << 20) {  // a launch holds fewer than 2^32 threads
-    hipLaunchKernelGGL(kv4_evict_select_kernel, dim3((unsigned)std::min<int64_t>(rows - r0, 1 << 20)),
-                       dim3(kSel), 0, st, a.Hkv, S, a.max_pages, a.seq_lens, a.weights, a.weights_out, a.pos,
-                       a.pos_out, a.seen, a.budget, a.sink, a.recent, a.new_lens, counts, moves, r0);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(rows - r0, 1 << 20)), dim3(kSel), 0, st,
+                         a.Hkv, S, a.max_pages, a.seq_lens, a.weights, a.weights_out, a.pos, a.pos_out, a.seen,
+                         a.budget, a.sink, a.recent, a.new_lens, counts, moves, source, r0);
+    };
+    if (S <= 4 * kSel) go(kv4_evict_select_kernel<4>);
+    else if (S <= 12 * kSel) go(kv4_evict_select_kernel<12>);
+    else if (S <= 32 * kSel) go(kv4_evict_select_kernel<32>);
+    else go(kv4_evict_select_kernel<0>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const int64_t most = std::min<int64_t>(a.budget, S / 2);  // moves of a row
-  const unsigned gx = (unsigned)std::max<int64_t>(
-      1, std::min((most + 3) / 4, (16 * (int64_t)device_cus() + rows - 1) / rows));
-  for (int64_t r0 = 0; r0 < rows; r0 += 65535) {
-    hipLaunchKernelGGL(kv4_evict_move_kernel, dim3(gx, (unsigned)std::min<int64_t>(rows - r0, 65535)),
-                       dim3(256), 0, st, a.pages, a.Hkv, S, a.ng, a.block_table, a.max_pages, counts, moves,
-                       r0);
+  const int64_t pages = std::min<int64_t>(a.max_pages, ((int64_t)a.budget + kP - 1) / kP);  // that keep rows
+  const int64_t most = std::min<int64_t>(65535, std::max<int64_t>(1, (1 << 23) / pages));
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    hipLaunchKernelGGL(kv4_evict_move_kernel, dim3((unsigned)pages, (unsigned)std::min(rows - r0, most)),
+                       dim3(256), 0, st, a.pages, a.Hkv, S, a.ng, a.block_table, a.max_pages, counts, source,
+                       a.budget, r0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
