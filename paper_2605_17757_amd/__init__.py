@@ -480,58 +480,100 @@ def kv4_alloc_evict_workspace(layout: Layout, B: int, max_pages_per_seq: int, de
                device)
 
 
-def _on_current_device(*tensors) -> None:
-    """The kernels run on the current device: its tensors only."""
-    for t in tensors:
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
-            raise ValueError("tensor on %s, but the current device is cuda:%d"
-                             % (t.device, torch.cuda.current_device()))
+# A serving step's tensors are checked on every call: the checks below are the ones of
+# _ptr, and that a tensor lies on the current device, at a third of their time.
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _dev_stream(stream):
+    """(index of the current device, stream handle)."""
+    dev = torch.cuda.current_device()
+    if stream is None and _raw_stream is not None:
+        return dev, _raw_stream(dev)
+    return dev, _stream(stream)
+
+
+def _arg(t, dtype, name: str, numel, dev: int) -> int:
+    """Address of a contiguous tensor of the current device (numel None: any size)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and \
+            t.is_contiguous() and (numel is None or t.numel() == numel):
+        return t.data_ptr()
+    _ptr(t, dtype, name, numel)  # raises
+    raise ValueError("%s is on %s, but the current device is cuda:%d" % (name, t.device, dev))
+
+
+def _rarg(R, name: str, layout: Layout, dev: int):
+    if R is None:
+        return None
+    n = HEAD_DIM * HEAD_DIM
+    return _arg(R, torch.float32, name, n * layout.num_kv_heads if layout.rot_per_head else n, dev)
+
+
+def _kv4_pool(layout: Layout, pages, dev: int) -> int:
+    return _arg(pages, torch.uint8, "pages", kv4_pool_bytes(layout), dev)
 
 
 def _out_code(out, name: str) -> int:
-    if out.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, out.dtype))
-    return OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+    if not isinstance(out, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if out.dtype is torch.float32:
+        return OUT_F32
+    if out.dtype is torch.bfloat16:
+        return OUT_BF16
+    raise TypeError("%s must be float32 or bfloat16, got %s" % (name, out.dtype))
 
 
 def kv4_append(layout: Layout, pages, k_new, v_new, slot_mapping, R_k, R_v, clip_k: float,
                clip_v: float, stream=None) -> None:
     """Rotate, clip, INT4-quantize and pack n_tok new K/V rows into the 4-bit pool
     ``pages`` (R_k / R_v None: identity)."""
-    n_tok, d, hkv = int(slot_mapping.numel()), layout.head_dim, layout.num_kv_heads
-    _on_current_device(pages, k_new, v_new, slot_mapping, R_k, R_v)
-    st = lib().oscar_kv4_append(
-        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)),
-        _ptr(k_new, torch.bfloat16, "k_new", n_tok * hkv * d),
-        _ptr(v_new, torch.bfloat16, "v_new", n_tok * hkv * d),
-        _ptr(slot_mapping, torch.int64, "slot_mapping"), n_tok, _rptr(R_k, "R_k", d, layout),
-        _rptr(R_v, "R_v", d, layout), float(clip_k), float(clip_v), _stream(stream))
-    _check(st, "oscar_kv4_append")
+    dev, st = _dev_stream(stream)
+    n_tok = int(slot_mapping.numel())
+    n = n_tok * layout.num_kv_heads * layout.head_dim
+    _check(lib().oscar_kv4_append(
+        ctypes.byref(layout), _kv4_pool(layout, pages, dev),
+        _arg(k_new, torch.bfloat16, "k_new", n, dev), _arg(v_new, torch.bfloat16, "v_new", n, dev),
+        _arg(slot_mapping, torch.int64, "slot_mapping", None, dev), n_tok,
+        _rarg(R_k, "R_k", layout, dev), _rarg(R_v, "R_v", layout, dev), float(clip_k), float(clip_v),
+        st),
+        "oscar_kv4_append")
 
 
 def kv4_gather(layout: Layout, pages, slot_mapping, k_out, v_out, stream=None) -> None:
     """K and V values of the rows at ``slot_mapping`` (rotated basis) into ``k_out``,
     ``v_out`` ([n_tok, Hkv, d], both fp32 or both bf16)."""
-    n_tok, d, hkv = int(slot_mapping.numel()), layout.head_dim, layout.num_kv_heads
-    _on_current_device(pages, slot_mapping, k_out, v_out)
-    st = lib().oscar_kv4_gather(
-        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)),
-        _ptr(slot_mapping, torch.int64, "slot_mapping"), n_tok,
-        _ptr(k_out, k_out.dtype, "k_out", n_tok * hkv * d),
-        _ptr(v_out, k_out.dtype, "v_out", n_tok * hkv * d), _out_code(k_out, "k_out"),
-        _stream(stream))
-    _check(st, "oscar_kv4_gather")
+    dev, st = _dev_stream(stream)
+    n_tok = int(slot_mapping.numel())
+    n = n_tok * layout.num_kv_heads * layout.head_dim
+    code = _out_code(k_out, "k_out")
+    _check(lib().oscar_kv4_gather(
+        ctypes.byref(layout), _kv4_pool(layout, pages, dev),
+        _arg(slot_mapping, torch.int64, "slot_mapping", None, dev), n_tok,
+        _arg(k_out, k_out.dtype, "k_out", n, dev), _arg(v_out, k_out.dtype, "v_out", n, dev), code, st),
+        "oscar_kv4_gather")
 
 
-def _weights_args(layout, B, mp, weights, weights_out):
-    """(weights, weights_out) pointers; weights_out None: in place."""
-    if weights is None:
-        if weights_out is not None:
-            raise ValueError("weights_out without weights")
-        return None, None
-    n = B * layout.num_kv_heads * mp * layout.page_size
-    out = weights if weights_out is None else weights_out
-    return (_ptr(weights, torch.float32, "weights", n), _ptr(out, torch.float32, "weights_out", n))
+def _kv4_decode_args(layout, pages, q, block_table, seq_lens, R_k, R_v, sm_scale, num_splits,
+                     workspace, out, weights, weights_out, dev):
+    """The arguments that kv4_decode_attn and kv4_decode_step share: (pages, those from q on)."""
+    B, Hq, mp = _decode_args(layout, q, block_table, seq_lens)
+    n = B * Hq * layout.head_dim
+    w_in = w_out = None
+    if weights is not None:
+        n_w = B * layout.num_kv_heads * mp * layout.page_size
+        w_in = _arg(weights, torch.float32, "weights", n_w, dev)
+        w_out = w_in if weights_out is None else _arg(weights_out, torch.float32, "weights_out", n_w, dev)
+    elif weights_out is not None:
+        raise ValueError("weights_out without weights")
+    code = _out_code(out, "out")
+    return _kv4_pool(layout, pages, dev), (
+        _arg(q, torch.bfloat16, "q", n, dev), B, Hq,
+        _arg(block_table, torch.int32, "block_table", B * mp, dev), mp,
+        _arg(seq_lens, torch.int32, "seq_lens", B, dev), _rarg(R_k, "R_k", layout, dev),
+        _rarg(R_v, "R_v", layout, dev), float(sm_scale), int(num_splits), w_in, w_out,
+        _arg(workspace, torch.uint8, "workspace", None, dev), workspace.numel(),
+        _arg(out, out.dtype, "out", n, dev), code)
 
 
 def kv4_decode_attn(layout: Layout, pages, q, block_table, seq_lens, R_k, R_v, sm_scale: float,
@@ -541,19 +583,10 @@ def kv4_decode_attn(layout: Layout, pages, q, block_table, seq_lens, R_k, R_v, s
     or fp32).  ``weights`` (fp32 [B, Hkv, max_pages * 64]): every token's attention
     weight, summed over the KV head's query heads, is added to it into ``weights_out``
     (None: in place)."""
-    B, Hq, mp = _decode_args(layout, q, block_table, seq_lens)
-    d = layout.head_dim
-    _on_current_device(pages, q, block_table, seq_lens, R_k, R_v, workspace, out, weights, weights_out)
-    w_in, w_out = _weights_args(layout, B, mp, weights, weights_out)
-    st = lib().oscar_kv4_decode_attn(
-        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)),
-        _ptr(q, torch.bfloat16, "q", B * Hq * d), B, Hq,
-        _ptr(block_table, torch.int32, "block_table", B * mp), mp,
-        _ptr(seq_lens, torch.int32, "seq_lens", B), _rptr(R_k, "R_k", d, layout),
-        _rptr(R_v, "R_v", d, layout), float(sm_scale), int(num_splits), w_in, w_out,
-        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
-        _ptr(out, out.dtype, "out", B * Hq * d), _out_code(out, "out"), _stream(stream))
-    _check(st, "oscar_kv4_decode_attn")
+    dev, st = _dev_stream(stream)
+    pool, rest = _kv4_decode_args(layout, pages, q, block_table, seq_lens, R_k, R_v, sm_scale,
+                                  num_splits, workspace, out, weights, weights_out, dev)
+    _check(lib().oscar_kv4_decode_attn(ctypes.byref(layout), pool, *rest, st), "oscar_kv4_decode_attn")
 
 
 def kv4_decode_step(layout: Layout, pages, k_new, v_new, slot_mapping, clip_k: float,
@@ -562,24 +595,18 @@ def kv4_decode_step(layout: Layout, pages, k_new, v_new, slot_mapping, clip_k: f
                     stream=None) -> None:
     """One serving decode step over the 4-bit cache: append the new tokens' K/V
     (``slot_mapping`` may be empty), then kv4_decode_attn."""
-    B, Hq, mp = _decode_args(layout, q, block_table, seq_lens)
-    d, hkv = layout.head_dim, layout.num_kv_heads
+    dev, st = _dev_stream(stream)
     n_new = int(slot_mapping.numel())
-    _on_current_device(pages, k_new, v_new, slot_mapping, q, block_table, seq_lens, R_k, R_v,
-                       workspace, out, weights, weights_out)
-    w_in, w_out = _weights_args(layout, B, mp, weights, weights_out)
-    kp = _ptr(k_new, torch.bfloat16, "k_new", n_new * hkv * d) if n_new else None
-    vp = _ptr(v_new, torch.bfloat16, "v_new", n_new * hkv * d) if n_new else None
-    sp = _ptr(slot_mapping, torch.int64, "slot_mapping") if n_new else None
-    st = lib().oscar_kv4_decode_step(
-        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)), kp, vp, sp,
-        n_new, float(clip_k), float(clip_v), _ptr(q, torch.bfloat16, "q", B * Hq * d), B, Hq,
-        _ptr(block_table, torch.int32, "block_table", B * mp), mp,
-        _ptr(seq_lens, torch.int32, "seq_lens", B), _rptr(R_k, "R_k", d, layout),
-        _rptr(R_v, "R_v", d, layout), float(sm_scale), int(num_splits), w_in, w_out,
-        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
-        _ptr(out, out.dtype, "out", B * Hq * d), _out_code(out, "out"), _stream(stream))
-    _check(st, "oscar_kv4_decode_step")
+    kp = vp = sp = None
+    if n_new:
+        n = n_new * layout.num_kv_heads * layout.head_dim
+        kp = _arg(k_new, torch.bfloat16, "k_new", n, dev)
+        vp = _arg(v_new, torch.bfloat16, "v_new", n, dev)
+        sp = _arg(slot_mapping, torch.int64, "slot_mapping", None, dev)
+    pool, rest = _kv4_decode_args(layout, pages, q, block_table, seq_lens, R_k, R_v, sm_scale,
+                                  num_splits, workspace, out, weights, weights_out, dev)
+    _check(lib().oscar_kv4_decode_step(ctypes.byref(layout), pool, kp, vp, sp, n_new,
+                                       float(clip_k), float(clip_v), *rest, st), "oscar_kv4_decode_step")
 
 
 def kv4_evict(layout: Layout, pages, block_table, seq_lens, weights, pos, num_seen, budget: int,
@@ -593,21 +620,21 @@ def kv4_evict(layout: Layout, pages, block_table, seq_lens, weights, pos, num_se
     ``weights_out`` and ``pos_out`` None: in place."""
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages_per_seq]")
-    B, mp = int(block_table.shape[0]), int(block_table.shape[1])
+    dev, st = _dev_stream(stream)
+    B, mp = block_table.shape
     n = B * layout.num_kv_heads * mp * layout.page_size
-    w_out = weights if weights_out is None else weights_out
-    p_out = pos if pos_out is None else pos_out
-    _on_current_device(pages, block_table, seq_lens, weights, pos, num_seen, new_lens, workspace,
-                       w_out, p_out)
-    st = lib().oscar_kv4_evict(
-        ctypes.byref(layout), _ptr(pages, torch.uint8, "pages", kv4_pool_bytes(layout)), B,
-        _ptr(block_table, torch.int32, "block_table", B * mp), mp,
-        _ptr(seq_lens, torch.int32, "seq_lens", B), _ptr(weights, torch.float32, "weights", n),
-        _ptr(w_out, torch.float32, "weights_out", n), _ptr(pos, torch.int32, "pos", n),
-        _ptr(p_out, torch.int32, "pos_out", n), _ptr(num_seen, torch.int32, "num_seen", B),
-        int(budget), int(sink), int(recent), _ptr(new_lens, torch.int32, "new_lens", B),
-        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
-    _check(st, "oscar_kv4_evict")
+    w_in = _arg(weights, torch.float32, "weights", n, dev)
+    p_in = _arg(pos, torch.int32, "pos", n, dev)
+    w_out = w_in if weights_out is None else _arg(weights_out, torch.float32, "weights_out", n, dev)
+    p_out = p_in if pos_out is None else _arg(pos_out, torch.int32, "pos_out", n, dev)
+    _check(lib().oscar_kv4_evict(
+        ctypes.byref(layout), _kv4_pool(layout, pages, dev), B,
+        _arg(block_table, torch.int32, "block_table", B * mp, dev), mp,
+        _arg(seq_lens, torch.int32, "seq_lens", B, dev), w_in, w_out, p_in, p_out,
+        _arg(num_seen, torch.int32, "num_seen", B, dev), int(budget), int(sink), int(recent),
+        _arg(new_lens, torch.int32, "new_lens", B, dev),
+        _arg(workspace, torch.uint8, "workspace", None, dev), workspace.numel(), st),
+        "oscar_kv4_evict")
 
 
 # ---------------------------------------------------------------------------

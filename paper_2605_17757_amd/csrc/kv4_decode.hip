@@ -19,8 +19,8 @@
 //     With the codes centred the two sums over tokens are as small as o~ itself; the
 //     matrix cores drop product bits below the accumulator's last ones, and against
 //     sums of uncentred codes that left errors of 1e-5 of the output.  w is scaled by a
-//     power of two per page and group and enters as two fp16 pieces, the second one of
-//     the rest times 2^12: 22 bits, over 2^25 between the page's weights.
+//     power of two per page and group, its largest values near 2^14, and enters as two
+//     fp16 pieces: 22 bits, down to 2^-16 of the row's largest weight, then fewer.
 // The pieces of one head are rows of the 16-row operand and 4 heads fill it, so that up
 // to 4 heads per KV head cost no more matrix products than unsplit operands would.
 // |q~| must stay below 2^56 (scores: 2^-69 n q~ 2^133 2^-64).
@@ -49,8 +49,7 @@ constexpr int kPw = 40;           // dwords per row of the weights operand in LD
 constexpr float kSlack = 4.0f;    // how far (log2) a score may exceed the reference maximum
 constexpr float kIn = 0x1p64f;    // scale of q~ in the scores' products with codes
 constexpr float kOut = 0x1p69f;   // back: 2^133 / kIn
-constexpr int kTop = 10;          // scales of a page enter below 2^kTop: w < 2^(kTop + kSlack)
-constexpr float kRest = 4096.0f;  // scale of w's second piece
+constexpr int kTop = 11;          // scales of a page enter below 2^kTop: w < 2^(kTop + kSlack)
 
 __device__ inline f4v mfma(const u4v& a, const u4v& b, const f4v& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c,
@@ -131,14 +130,11 @@ struct SplitSmem {
   float ml[kWaves][NCH * 4][2];           // the waves' (m, l)
 };
 
-template <int NCH>
-struct SplitOcc {
-  static constexpr int per_simd = NCH == 1 ? 2 : 2;
-};
+constexpr int kPerSimd = 2;  // waves per SIMD
 
 template <bool BF, int NG, int NCH>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((
-    amdgpu_waves_per_eu(SplitOcc<NCH>::per_simd, SplitOcc<NCH>::per_simd))) void kv4_split_kernel(
+    amdgpu_waves_per_eu(kPerSimd, kPerSimd))) void kv4_split_kernel(
     const uint8_t* __restrict__ pages, int Hkv, int Hq, const int32_t* __restrict__ block_table,
     int max_pages, const int32_t* __restrict__ seq_lens, int num_splits, int n_ranges, int B,
     const float* __restrict__ qt, float* __restrict__ part_o, float* __restrict__ part_ml,
@@ -154,34 +150,70 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
   // The block's waves take pages p0 + w, p0 + w + 4, .. of pages [p0, p1) of sequence b.
   auto run_piece = [&](int b, int p0, int p1, int piece, bool last) {
     const int len = len_of(b);
-    // ---- query operands: rows 4 h + piece of chunk ch, and group sums ----
-    for (int i = w; i < NCH * 4; i += kWaves) {
-      const int ch = i >> 2, kc = i & 3, head = 4 * ch + (lo >> 2), pc = lo & 3;
-      u4v a = u4v{0, 0, 0, 0};
-      if (head < g && pc < 3) {
-        const float* src = qt + ((size_t)b * Hq + kvh * g + head) * kD + 32 * kc + 8 * hi;
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = src[e] * (e & 2 ? kIn / 16.0f : kIn);
-          if (pc > 0) x[e] -= top16(x[e]);
-          if (pc > 1) x[e] -= top16(x[e]);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] = pack_hi(x[2 * k], x[2 * k + 1]);
-      }
-      sm.qa[ch][kc][l] = a;
-    }
-    float qs[NCH][NG];  // sums of q~ over the groups, head 4 ch + hi
+    // ---- loads in the order of their use: page ids, the query, the first page's K ----
+    const int32_t* __restrict__ bt = block_table + (size_t)b * max_pages;
+    const int n_mine = (p1 - p0 - w + kWaves - 1) / kWaves;  // <= 0: none
+    auto page_ids = [&](int i0) {  // lane i: page i0 + i of the wave's
+      const int p = p0 + w + kWaves * (i0 + l);
+      return i0 + l < n_mine ? bt[p] : 0;
+    };
+    int ids = page_ids(0);
+    // wave w makes operands (chunk, 32-channel block) w, w + 4, ..: rows 4 h + piece
+    float4 xr[NCH][2], xs[NCH][2];
 #pragma unroll
     for (int ch = 0; ch < NCH; ++ch) {
-      const int head = 4 * ch + hi;
-      float s = 0.0f;
+      const int head = 4 * ch + (lo >> 2), hs = 4 * ch + hi;
+      const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      xr[ch][0] = xr[ch][1] = xs[ch][0] = xs[ch][1] = none;
+      const float* row = qt + ((size_t)b * Hq + kvh * g) * kD;
       if (head < g) {
-        const float4* src = reinterpret_cast<const float4*>(qt + ((size_t)b * Hq + kvh * g + head) * kD + 8 * lo);
-        const float4 x = src[0], y = src[1];
-        s = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+        const float4* src = reinterpret_cast<const float4*>(row + head * kD + 32 * w + 8 * hi);
+        xr[ch][0] = src[0];
+        xr[ch][1] = src[1];
       }
+      if (hs < g) {
+        const float4* src = reinterpret_cast<const float4*>(row + hs * kD + 8 * lo);
+        xs[ch][0] = src[0];
+        xs[ch][1] = src[1];
+      }
+    }
+    auto block_of = [&](int i) {
+      return pages + ((size_t)__builtin_amdgcn_readlane(ids, i & 63) * Hkv + kvh) * kv4_block_bytes(NG);
+    };
+    u4v kr[4], ks[NG];
+    auto load_k = [&](const uint8_t* blk) {
+      const u4v* p = reinterpret_cast<const u4v*>(blk) + l;
+      const u4v* z = reinterpret_cast<const u4v*>(blk + kv4_sz_off(NG, 0)) + lo * NG;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) kr[u] = __builtin_nontemporal_load(p + 64 * u);
+#pragma unroll
+      for (int u = 0; u < NG; ++u) ks[u] = z[u];  // entries (slot 4 lo + u, group)
+    };
+    const uint8_t* blk = pages;
+    if (n_mine > 0) {
+      blk = block_of(0);
+      load_k(blk);
+    }
+    // ---- query operands and group sums ----
+    float qs[NCH][NG];  // sums of q~ over the groups, head 4 ch + hi, in the products' scale
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      const int pc = lo & 3;
+      float x[8] = {xr[ch][0].x, xr[ch][0].y, xr[ch][0].z, xr[ch][0].w,
+                    xr[ch][1].x, xr[ch][1].y, xr[ch][1].z, xr[ch][1].w};
+      u4v a;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] *= e & 2 ? kIn / 16.0f : kIn;
+        if (pc > 0) x[e] -= top16(x[e]);
+        if (pc > 1) x[e] -= top16(x[e]);
+        if (pc > 2) x[e] = 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = pack_hi(x[2 * k], x[2 * k + 1]);
+      sm.qa[ch][w][l] = a;
+      float s = ((xs[ch][0].x + xs[ch][0].y) + (xs[ch][0].z + xs[ch][0].w)) +
+                ((xs[ch][1].x + xs[ch][1].y) + (xs[ch][1].z + xs[ch][1].w));
 #pragma unroll
       for (int k = 1; k < 16 / NG; k <<= 1) s += __shfl_xor(s, k, 64);
 #pragma unroll
@@ -200,30 +232,6 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       for (int q = 0; q < NG; ++q) wz[ch][q] = 0.0f;
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) o[ch][ct] = 0.0f;
-    }
-    const int32_t* __restrict__ bt = block_table + (size_t)b * max_pages;
-    const int n_mine = (p1 - p0 - w + kWaves - 1) / kWaves;  // <= 0: none
-    auto page_ids = [&](int i0) {  // lane i: page i0 + i of the wave's
-      const int p = p0 + w + kWaves * (i0 + l);
-      return i0 + l < n_mine ? bt[p] : 0;
-    };
-    int ids = page_ids(0);
-    auto block_of = [&](int i) {
-      return pages + ((size_t)__builtin_amdgcn_readlane(ids, i & 63) * Hkv + kvh) * kv4_block_bytes(NG);
-    };
-    u4v kr[4], ks[NG];
-    auto load_k = [&](const uint8_t* blk) {
-      const u4v* p = reinterpret_cast<const u4v*>(blk) + l;
-      const u4v* z = reinterpret_cast<const u4v*>(blk + kv4_sz_off(NG, 0)) + lo * NG;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) kr[u] = __builtin_nontemporal_load(p + 64 * u);
-#pragma unroll
-      for (int u = 0; u < NG; ++u) ks[u] = z[u];  // entries (slot 4 lo + u, group)
-    };
-    const uint8_t* blk = pages;
-    if (n_mine > 0) {
-      blk = block_of(0);
-      load_k(blk);
     }
     for (int i = 0; i < n_mine; ++i) {
       const int pg = p0 + w + kWaves * i, ntok = min(kP, len - pg * kP);
@@ -351,19 +359,16 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
         }
 #pragma unroll
         for (int ch = 0; ch < NCH; ++ch) {
-          float x[4], y[4], wsum = 0.0f;
+          float x[4], wsum = 0.0f;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             x[u] = p[ch][u] * s[u];
-            y[u] = (p[ch][u] * kRest) * s[u];
             wsum = fmaf(x[u], z[u], wsum);
           }
           wz[ch][q] = fmaf(wsum, 0.5f * back[q], wz[ch][q]);
           const fp16x2 h0 = __builtin_amdgcn_cvt_pkrtz(x[0], x[1]), h1 = __builtin_amdgcn_cvt_pkrtz(x[2], x[3]);
-          const fp16x2 r0 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h0[0], -kRest, y[0]),
-                                                       fmaf((float)h0[1], -kRest, y[1]));
-          const fp16x2 r1 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h1[0], -kRest, y[2]),
-                                                       fmaf((float)h1[1], -kRest, y[3]));
+          const fp16x2 r0 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h0[0], -1.0f, x[0]), fmaf((float)h0[1], -1.0f, x[1]));
+          const fp16x2 r1 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h1[0], -1.0f, x[2]), fmaf((float)h1[1], -1.0f, x[3]));
           uint32_t* row = sm.pw[w][ch] + (q & 1) * 8 * kPw + 2 * hi * kPw + 2 * lo;
           *reinterpret_cast<uint2*>(row) =
               make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
@@ -405,9 +410,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
           }
 #pragma unroll
           for (int ch = 0; ch < NCH; ++ch) {
-            o[ch][2 * j] = fmaf(fmaf(d[ch][0][1], 1.0f / kRest, d[ch][0][0]), 0x1p9f * back[q], o[ch][2 * j]);
-            o[ch][2 * j + 1] =
-                fmaf(fmaf(d[ch][1][1], 1.0f / kRest, d[ch][1][0]), 0x1p9f * back[q], o[ch][2 * j + 1]);
+            o[ch][2 * j] = fmaf(d[ch][0][0] + d[ch][0][1], 0x1p9f * back[q], o[ch][2 * j]);
+            o[ch][2 * j + 1] = fmaf(d[ch][1][0] + d[ch][1][1], 0x1p9f * back[q], o[ch][2 * j + 1]);
           }
         }
       }
@@ -563,7 +567,7 @@ hipError_t launch_kv4_split(const uint8_t* pages, int Hkv, int B, int Hq, const 
   const int nch = split_chunks(Hq / Hkv);
   // As many ranges as blocks are resident at once (of the Hkv heads' each), and no more
   // than the block table can fill at the least pages of a range.
-  const int64_t resident = (int64_t)(nch == 1 ? SplitOcc<1>::per_simd : SplitOcc<2>::per_simd) * device_cus();
+  const int64_t resident = (int64_t)kPerSimd * device_cus();
   int64_t ranges = std::max<int64_t>(1, resident / Hkv);
   if (num_splits > 1) {
     const int64_t least = std::max<int64_t>(kMinRange, (max_pages + (int64_t)num_splits - 2) / (num_splits - 1));
