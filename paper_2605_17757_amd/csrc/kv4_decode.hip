@@ -527,7 +527,8 @@ __global__ __launch_bounds__(256) void kv4_weights_kernel(
   const int t0 = blockIdx.x * kWeightTokens + 4 * t;
   if (t0 >= len) return;
   const size_t S = (size_t)max_pages * kP, at = ((size_t)b * Hkv + kvh) * S + t0;
-  float4 a = *reinterpret_cast<const float4*>(weights + at);
+  const float4 w_in = *reinterpret_cast<const float4*>(weights + at);
+  float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // the step's part, added to the sum with one rounding
   for (int h = 0; h < g; ++h) {
     const float4 x = *reinterpret_cast<const float4*>(scores + (row0 + h) * S + t0);
     a.x = fmaf(__builtin_amdgcn_exp2f(x.x - ms[h]), il[h], a.x);
@@ -535,6 +536,7 @@ __global__ __launch_bounds__(256) void kv4_weights_kernel(
     a.z = fmaf(__builtin_amdgcn_exp2f(x.z - ms[h]), il[h], a.z);
     a.w = fmaf(__builtin_amdgcn_exp2f(x.w - ms[h]), il[h], a.w);
   }
+  a = make_float4(w_in.x + a.x, w_in.y + a.y, w_in.z + a.z, w_in.w + a.w);
   float* out = weights_out + at;
   if (t0 + 4 <= len) {
     *reinterpret_cast<float4*>(out) = a;
