@@ -221,11 +221,12 @@ hipError_t launch_kv4_split(const uint8_t* pages, int Hkv, int B, int Hq, const 
                             int max_pages, const int32_t* seq_lens, int num_splits, const float* qt,
                             float* part_o, float* part_ml, float* scores, hipStream_t st,
                             int meta_bf16, int ng);
-// weights_out = weights + every cached token's attention weight, summed over the query
-// heads of its KV head ([B][Hkv][max_pages * 64]).
-hipError_t launch_kv4_weights(int Hkv, int B, int Hq, int max_pages, const int32_t* seq_lens,
-                              int num_splits, const float* part_ml, const float* scores,
-                              const float* weights, float* weights_out, hipStream_t st);
+// launch_decode_reduce, and weights_out = weights + every cached token's attention weight,
+// summed over the query heads of its KV head ([B][Hkv][max_pages * 64]).
+hipError_t launch_kv4_finish(int Hkv, int B, int Hq, int max_pages, const int32_t* seq_lens,
+                             int num_splits, const float* part_o, const float* part_ml, const float* Rv,
+                             void* out, int out_f32, int rph, const float* scores, const float* weights,
+                             float* weights_out, hipStream_t st);
 // Eviction.  ws: kv4_evict_ws_bytes.
 size_t kv4_evict_ws_bytes(int Hkv, int B, int max_pages);
 struct EvictArgs {

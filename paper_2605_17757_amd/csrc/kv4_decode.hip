@@ -1,6 +1,6 @@
-// Decode attention over the 4-bit paged cache: the split kernel and the sums of
-// attention weights (the query rotation and the merge are the 2-bit path's prepare and
-// reduce kernels).
+// Decode attention over the 4-bit paged cache: the split kernel, and the merge with the
+// sums of attention weights (the query rotation, and the merge without them, are the
+// 2-bit path's prepare and reduce kernels).
 //
 // For a KV head with g query heads, q~ = q R_k sm_scale log2 e, a page's K as
 // Q(k~)_c = s (n - z) with codes n in 0 .. 15 and one (s, z) per token t and group G of
@@ -30,7 +30,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "internal.h"
+#include "reduce_body.h"
 #include "split_ranges.h"
 
 namespace oscar {
@@ -493,28 +493,41 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
   }
 }
 
-// weights_out[b][kvh][t] = weights[b][kvh][t] + sum over the g query heads of
-// 2^(score - M) / L, with a head's M and L from the partial states of its pieces.
-// Four tokens per thread, kWeightTokens per block.
-constexpr int kWeightTokens = 1024;
+// Merge and weights in one launch: the reduce kernel's blocks, then those of the weights,
+// which need no more than the pieces' (m, l) either.  In a launch of their own the weights
+// took 4 us of a small call (2 sequences of 31001 tokens, 32/8 heads: 35.0 us, 31 now).
+//
+//   weights_out[b][kvh][t] = weights[b][kvh][t] + sum over the g query heads of
+//                            2^(score - M) / L,  M and L from the partial states of the pieces
+// Four tokens per thread, kWeightTokens per block.  Bound: HBM reads, 4 (g + 1) bytes per
+// token and KV head, and the writes.
+constexpr int kWeightTokens = 4 * kRedThreads;
 
-__global__ __launch_bounds__(256) void kv4_weights_kernel(
-    int Hkv, int Hq, int max_pages, const int32_t* __restrict__ seq_lens, int num_splits, int b0,
-    const float* __restrict__ part_ml, const float* __restrict__ scores, const float* weights,
-    float* weights_out) {
+struct WeightArgs {
+  int Hkv, Hq, max_pages, chunks;  // blocks per (sequence, KV head)
+  const int32_t* seq_lens;
+  int num_splits;
+  const float* part_ml;
+  const float* scores;
+  const float* weights;
+  float* weights_out;  // may be weights itself
+};
+
+__device__ inline void weights_body(int bx, const WeightArgs& a) {
   __shared__ float ms[kMaxGroupHeads], il[kMaxGroupHeads];
-  const int b = b0 + blockIdx.z, kvh = blockIdx.y, g = Hq / Hkv, t = threadIdx.x, w = t >> 6, l = t & 63;
-  const int len = min(max(seq_lens[b], 0), max_pages * kP);
-  if ((int64_t)blockIdx.x * kWeightTokens >= len) return;
-  const size_t row0 = (size_t)b * Hq + kvh * g;
-  for (int h = w; h < g; h += 4) {
-    const float2* ml = reinterpret_cast<const float2*>(part_ml) + (row0 + h) * num_splits;
+  const int chunk = bx % a.chunks, kvh = bx / a.chunks % a.Hkv, b = bx / a.chunks / a.Hkv, g = a.Hq / a.Hkv;
+  const int t = threadIdx.x, w = t >> 6, l = t & 63;
+  const int len = min(max(a.seq_lens[b], 0), a.max_pages * kP);
+  if ((int64_t)chunk * kWeightTokens >= len) return;
+  const size_t row0 = (size_t)b * a.Hq + kvh * g;
+  for (int h = w; h < g; h += kRedThreads / 64) {
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + (row0 + h) * a.num_splits;
     float M = -INFINITY;
-    for (int s = l; s < num_splits; s += 64) M = fmaxf(M, ml[s].x);
+    for (int s = l; s < a.num_splits; s += 64) M = fmaxf(M, ml[s].x);
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
     float L = 0.0f;
-    for (int s = l; s < num_splits; s += 64)
+    for (int s = l; s < a.num_splits; s += 64)
       if (ml[s].x != -INFINITY) L = fmaf(exp2f(ml[s].x - M), ml[s].y, L);
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) L += __shfl_xor(L, k, 64);
@@ -524,26 +537,40 @@ __global__ __launch_bounds__(256) void kv4_weights_kernel(
     }
   }
   __syncthreads();
-  const int t0 = blockIdx.x * kWeightTokens + 4 * t;
+  const int t0 = chunk * kWeightTokens + 4 * t;
   if (t0 >= len) return;
-  const size_t S = (size_t)max_pages * kP, at = ((size_t)b * Hkv + kvh) * S + t0;
-  const float4 w_in = *reinterpret_cast<const float4*>(weights + at);
-  float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // the step's part, added to the sum with one rounding
+  const size_t S = (size_t)a.max_pages * kP, at = ((size_t)b * a.Hkv + kvh) * S + t0;
+  const float4 w_in = *reinterpret_cast<const float4*>(a.weights + at);
+  float4 p = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // the step's part, added to the sum with one rounding
   for (int h = 0; h < g; ++h) {
-    const float4 x = *reinterpret_cast<const float4*>(scores + (row0 + h) * S + t0);
-    a.x = fmaf(__builtin_amdgcn_exp2f(x.x - ms[h]), il[h], a.x);
-    a.y = fmaf(__builtin_amdgcn_exp2f(x.y - ms[h]), il[h], a.y);
-    a.z = fmaf(__builtin_amdgcn_exp2f(x.z - ms[h]), il[h], a.z);
-    a.w = fmaf(__builtin_amdgcn_exp2f(x.w - ms[h]), il[h], a.w);
+    const float4 x = *reinterpret_cast<const float4*>(a.scores + (row0 + h) * S + t0);
+    p.x = fmaf(__builtin_amdgcn_exp2f(x.x - ms[h]), il[h], p.x);
+    p.y = fmaf(__builtin_amdgcn_exp2f(x.y - ms[h]), il[h], p.y);
+    p.z = fmaf(__builtin_amdgcn_exp2f(x.z - ms[h]), il[h], p.z);
+    p.w = fmaf(__builtin_amdgcn_exp2f(x.w - ms[h]), il[h], p.w);
   }
-  a = make_float4(w_in.x + a.x, w_in.y + a.y, w_in.z + a.z, w_in.w + a.w);
-  float* out = weights_out + at;
+  p = make_float4(w_in.x + p.x, w_in.y + p.y, w_in.z + p.z, w_in.w + p.w);
+  float* out = a.weights_out + at;
   if (t0 + 4 <= len) {
-    *reinterpret_cast<float4*>(out) = a;
+    *reinterpret_cast<float4*>(out) = p;
   } else {  // slots past the length stay as they were
-    const float v[4] = {a.x, a.y, a.z, a.w};
+    const float v[4] = {p.x, p.y, p.z, p.w};
     for (int i = 0; t0 + i < len; ++i) out[i] = v[i];
   }
+}
+
+template <int RB>
+__global__ __launch_bounds__(kRedThreads) void kv4_finish_kernel(int reduce_blocks, int rows,
+                                                                 const float* __restrict__ part_o,
+                                                                 const float* __restrict__ Rv,
+                                                                 void* __restrict__ out, int out_f32, int rph,
+                                                                 WeightArgs a) {
+  const int bx = blockIdx.x;
+  if (bx >= reduce_blocks) {
+    weights_body(bx - reduce_blocks, a);
+    return;
+  }
+  reduce_body<false, RB>(bx, rows, a.num_splits, part_o, a.part_ml, Rv, out, out_f32, rph, a.Hq, a.Hkv);
 }
 
 template <bool BF, int NG>
@@ -593,15 +620,30 @@ hipError_t launch_kv4_split(const uint8_t* pages, int Hkv, int B, int Hq, const 
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_weights(int Hkv, int B, int Hq, int max_pages, const int32_t* seq_lens,
-                              int num_splits, const float* part_ml, const float* scores,
-                              const float* weights, float* weights_out, hipStream_t st) {
-  const unsigned chunks = (unsigned)(((int64_t)max_pages * kP + kWeightTokens - 1) / kWeightTokens);
-  // a launch holds fewer than 2^32 threads
-  const int most = (int)std::max<int64_t>(1, (1 << 23) / ((int64_t)chunks * Hkv));
+hipError_t launch_kv4_finish(int Hkv, int B, int Hq, int max_pages, const int32_t* seq_lens,
+                             int num_splits, const float* part_o, const float* part_ml, const float* Rv,
+                             void* out, int out_f32, int rph, const float* scores, const float* weights,
+                             float* weights_out, hipStream_t st) {
+  const size_t S = (size_t)max_pages * kP;
+  const int chunks = (int)((S + kWeightTokens - 1) / kWeightTokens);
+  // a launch holds fewer than 2^32 threads: at most 2^20 blocks of the merge and 2^22 of the weights
+  const int most = (int)std::min<int64_t>(launch_seqs(Hq),
+                                          std::max<int64_t>(1, (1 << 22) / ((int64_t)chunks * Hkv)));
   return by_seqs(B, most, [&](int b0, int nb) {
-    hipLaunchKernelGGL(kv4_weights_kernel, dim3(chunks, Hkv, nb), dim3(256), 0, st, Hkv, Hq, max_pages,
-                       seq_lens, num_splits, b0, part_ml, scores, weights, weights_out);
+    const size_t row = (size_t)b0 * Hq, part = row * num_splits, kv = (size_t)b0 * Hkv;
+    const WeightArgs a{Hkv, Hq, max_pages, chunks, seq_lens + b0, num_splits, part_ml + part * 2,
+                       scores + row * S, weights + kv * S, weights_out + kv * S};
+    const int rows = nb * Hq, rb = reduce_rows(rows), rblocks = query_blocks(nb, Hq, Hkv, rph, rb);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(rblocks + (int64_t)nb * Hkv * chunks)), dim3(kRedThreads), 0, st,
+                         rblocks, rows, part_o + part * kD, Rv,
+                         static_cast<void*>(static_cast<char*>(out) + row * kD * (out_f32 ? 4 : 2)), out_f32,
+                         rph, a);
+    };
+    if (rb == 16) go(kv4_finish_kernel<16>);
+    else if (rb == 8) go(kv4_finish_kernel<8>);
+    else if (rb == 4) go(kv4_finish_kernel<4>);
+    else go(kv4_finish_kernel<2>);
     return hipGetLastError();
   });
 }

@@ -647,12 +647,13 @@ int launch_kv4_rest(const oscar_layout* L, const void* pages, int32_t B, int32_t
                                        reinterpret_cast<const float*>(base + ws.d.qt_off), po, pml,
                                        scores, hs, meta_bf16(L), groups(L)));
   if (st) return st;
-  st = hip_status(launch_decode_reduce(B, Hq, num_splits, po, pml, R_v, out,
-                                       out_dtype == OSCAR_OUT_F32 ? 1 : 0, hs, nullptr, L->rot_per_head,
-                                       L->num_kv_heads));
-  if (st || !weights) return st;
-  return hip_status(launch_kv4_weights(L->num_kv_heads, B, Hq, max_pages_per_seq, seq_lens, num_splits,
-                                       pml, scores, weights, weights_out, hs));
+  const int out_f32 = out_dtype == OSCAR_OUT_F32 ? 1 : 0;
+  if (!weights)
+    return hip_status(launch_decode_reduce(B, Hq, num_splits, po, pml, R_v, out, out_f32, hs, nullptr,
+                                           L->rot_per_head, L->num_kv_heads));
+  return hip_status(launch_kv4_finish(L->num_kv_heads, B, Hq, max_pages_per_seq, seq_lens, num_splits, po,
+                                      pml, R_v, out, out_f32, L->rot_per_head, scores, weights, weights_out,
+                                      hs));
 }
 
 }  // namespace
