@@ -462,11 +462,14 @@ int oscar_kv4_decode_step(const oscar_layout *L, void *pages, const void *k_new,
  *   its position.  Afterwards, for t < m weights_out and pos_out hold the slot's weight
  *   and position; for m <= t < max_pages_per_seq * P they hold 0 and -1.  new_lens[b] = m.
  * The pages of slots >= m are free for other use; the next token of the sequence goes to
- * slot m.
+ * slot m.  Rows move inside the sequence's own pages: none of them may belong to another
+ * sequence too (a shared prefix), in this call or outside it.  max_pages_per_seq * P is
+ * at most 2^30, and max_pages_per_seq * Hkv at most 2^27, here and with weights.
  *   weights, weights_out : fp32 [B, Hkv, max_pages_per_seq * P] (oscar_kv4_decode_attn's)
  *   pos, pos_out         : int32, same shape; before the first eviction all -1
  *       each _out the same array as its input or disjoint from it
  *   num_seen             : int32 [B], tokens of the sequence so far, evicted ones too
+ *       (>= seq_lens[b])
  *   budget >= 1, sink >= 0, recent >= 0
  *   new_lens             : int32 [B], not seq_lens itself
  *   workspace            : >= oscar_kv4_evict_workspace_bytes(L, B, max_pages_per_seq)

@@ -24,7 +24,6 @@
 // The pieces of one head are rows of the 16-row operand and 4 heads fill it, so that up
 // to 4 heads per KV head cost no more matrix products than unsplit operands would.
 // |q~| must stay below 2^56 (scores: 2^-69 n q~ 2^133 2^-64).
-#define OSCAR_SPLIT_DIV32
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
@@ -46,7 +45,7 @@ typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;         // waves of a block: a team on one range of pages
 constexpr int kPw = 40;           // dwords per row of the weights operand in LDS
-constexpr float kSlack = 4.0f;    // how far (log2) a score may exceed the reference maximum
+constexpr float kSlack = 4.0f;    // how far (log2) a score may exceed the reference maximum before it moves
 constexpr float kIn = 0x1p64f;    // scale of q~ in the scores' products with codes
 constexpr float kOut = 0x1p69f;   // back: 2^133 / kIn
 constexpr int kTop = 11;          // scales of a page enter below 2^kTop: w < 2^(kTop + kSlack)
@@ -130,6 +129,30 @@ struct SplitSmem {
   float ml[kWaves][NCH * 4][2];           // the waves' (m, l)
 };
 
+// ---------------------------------------------------------------------------
+// split: the pages of all sequences end to end, cut into equal ranges (split_ranges.h),
+// as many as blocks are resident; one block per (range, KV head), so that a page-head
+// block is read once.  A block's 4 waves take every fourth page of the range's part of a
+// sequence and merge their states in LDS: one partial state per part, and a short
+// sequence's pages at once.  Per page a wave has
+//   K in 4 loads of 1 KB (lane: slot 4 lo + u, channels 8 hi .. of four blocks of 32):
+//     16 products per chunk of 4 heads, lane (head hi, slot) holds a score's pieces;
+//   V in 4 loads (lane: 16 slots of channels 32 j + lo, + 16): the weights of a group go
+//     through LDS into the operand's rows, 16 products per chunk, added to o~ (lane:
+//     head hi, 8 channels) after the page.
+// The next page's K is loaded once this page's is used up, so that 5 KB per wave are
+// always on their way at 8 waves per CU.
+//
+// Bound: up to 4 heads per KV head HBM (64 sequences of 16k to 32k tokens, 32/8 heads:
+// 2.0 GB in 314 us, 6.4 TB/s; 555 vector instructions per page, VALU busy 61 %).  Beyond,
+// the VALU: per chunk and page about 200 instructions (scores 68, weights and their pieces
+// 100, sums 16, softmax 16) beside 310 that all chunks share (unpacking 224, metadata 84).
+// 12 heads (16 x 128k tokens): 968 a page, busy 76 %, matrix cores 30 %, 640 us, 4.2 TB/s.
+// Two waves per SIMD: at three, which the 4-head instances allow, 342 us for 340.  With
+// the products' sums kept in the accumulators across pages (32 registers per chunk
+// instead of 8) more than 8 heads went to scratch: 16 heads 555 us, 310 now.  Rotating
+// the query in these blocks instead of a launch before: 21.6 us for 18.4 at batch 1.
+// ---------------------------------------------------------------------------
 constexpr int kPerSimd = 2;  // waves per SIMD
 
 template <bool BF, int NG, int NCH>

@@ -593,7 +593,7 @@ int check_kv4_rows(const oscar_layout* L, const void* k_new, const void* v_new,
 // Token slots per sequence, and the [B][Hkv][slots] arrays: within the kernels' indices.
 int check_kv4_slots(const oscar_layout* L, int32_t max_pages_per_seq) {
   if (max_pages_per_seq < 1) return OSCAR_ERR_INVALID_ARG;
-  if ((int64_t)max_pages_per_seq * L->page_size > 0x7fffffffLL ||
+  if ((int64_t)max_pages_per_seq * L->page_size > (1LL << 30) ||
       (int64_t)max_pages_per_seq * L->num_kv_heads > (1LL << 27))
     return OSCAR_ERR_UNSUPPORTED;
   return OSCAR_OK;

@@ -1,5 +1,6 @@
-// The balanced split's page ranges: the pages of all sequences laid end to end and cut
-// into equal ranges, as each wave works them out from the sequences' page counts.
+// The 4-bit split's page ranges, cut as the 2-bit split cuts its own (decode_mfma.hip): the
+// pages of all sequences laid end to end, in equal ranges, as each wave works them out from
+// the sequences' page counts.
 #pragma once
 
 #include "internal.h"
@@ -15,13 +16,10 @@ __device__ inline int wave_sum_i(int x) {
   return x;
 }
 
-// a / b for a >= 0, b > 0; for small calls in 32 bits where both fit (a 64-bit division
-// is some 150 dependent instructions; elsewhere the second path sends 8 bytes of the
-// mixed cache's one-chunk instance to scratch).
+// a / b for a >= 0, b > 0, in 32 bits where both fit (a 64-bit division is some 150
+// dependent instructions).
 __device__ inline int64_t div64(int64_t a, int64_t b) {
-#if defined(OSCAR_SPLIT_TEAM_UNIT) || defined(OSCAR_SPLIT_DIV32)
   if (((a | b) >> 32) == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
-#endif
   return a / b;
 }
 
