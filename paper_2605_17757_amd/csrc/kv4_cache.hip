@@ -27,7 +27,7 @@ __device__ inline float value_of(uint32_t x, int sh, float2 m) { return m.x * ((
 // bf16 output rounds the product once).  Bound: HBM writes (fp32: 1024 bytes per token
 // and head against 128 + 8 ng read).
 //
-// Row by row (half a wave per tensor, 4 channels a lane) a V row is 64 single bytes of 32
+// Row by row (half a wave per tensor, 4 channels a lane) a V row is 64 single bytes of 8
 // cache lines.  Calls of 64 tokens or more take tiles of 64 tokens, one block per (tile,
 // head): the tile's slots are grouped by page, and of a page with kPageRows members or
 // more the block reads the whole page-head block in its 16-byte units, a quarter per
@@ -184,14 +184,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
 //           lists of holes and movers, and a last pass fills them and pairs them off.
 //   move:   the moved rows' bytes (codes, scales, zeros) from page to page, one block per
 //           page that receives any.
-// Bounds: select the latency of its passes (one block per row; 32 x 8 rows of 8k to 16k
-// slots: 40 us, of which 13 load the keys, 8 find the threshold, 11 place, 8 clear the
-// tail; 73 with keys formed anew in every pass, two block-wide sums per 1024 slots).  Move
-// the cache lines of the sources' V codes, of which a row's 64 bytes touch 32: the same rows
-// to 1024 slots, 240000 moves, 80 us for about 350 MB of lines (116 a wave per row).
+// Bounds: select the latency of its passes, one block per row: 32 x 8 rows of 8k to 16k
+// slots 32 us, 13 of them the two streams' bytes at the copy rate; 8 rows of 2k slots 9 us
+// (40 and 11.4 with the lists in the workspace and every wave copying its own kept slots;
+// 73 with keys formed anew in every pass, two block-wide sums per 1024 slots).  Move the
+// cache lines of the sources' V codes, 64 bytes of a row in 8 lines: the same rows to 1024
+// slots, 240000 moves, 80 us for about 250 MB of lines (116 a wave per row).
 // ---------------------------------------------------------------------------
-constexpr int kSel = 1024;  // threads of a select block
-constexpr int kBatch = 4;   // slots per thread whose loads are issued together
+constexpr int kSel = 1024;            // threads of a select block
+constexpr int kSelLds = 32 * kSel;    // slots up to which they fit into its registers and LDS
 
 // Larger key, larger rank: finite weights in order (-0 as 0), NaN below all, protected
 // tokens above all.
@@ -202,20 +203,35 @@ __device__ inline uint32_t rank_key(float w, bool safe) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// ITEMS: slots per thread whose keys are kept in registers; 0: any number, formed anew
-// in every pass.
+// Inclusive prefix sum over the wave's lanes (DPP: shifts inside rows of 16 lanes, then the
+// rows' last lanes broadcast).
+__device__ inline int wave_prefix(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
+// ITEMS: slots per thread whose keys are kept in registers and whose lists of holes and
+// movers (at most S / 2 of each) in LDS; 0: any number, keys formed anew in every pass,
+// lists in the workspace.
 template <int ITEMS>
 __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
     int Hkv, int64_t S, int max_pages, const int32_t* __restrict__ seq_lens, const float* weights,
     float* weights_out, const int32_t* pos, int32_t* pos_out, const int32_t* __restrict__ seen_all,
     int budget, int sink, int recent, int32_t* __restrict__ new_lens, int32_t* __restrict__ counts,
     int2* __restrict__ moves, int32_t* __restrict__ source, int64_t row0) {
-  constexpr int kW = kSel / 64;
-  __shared__ int hist[2 * kSel];
-  __shared__ int3 part[kW];  // per wave: keys equal to the last kept one, holes, movers
+  constexpr int kW = kSel / 64, kB = ITEMS == 12 ? 6 : 4;  // kB: slots per thread whose loads are issued together
+  __shared__ int2 hist[kSel];  // entry i of the ints: keys whose digit is 2047 - i
+  __shared__ int3 part[kW];    // per wave: keys equal to the last kept one, holes, movers
   __shared__ int above_all[kW];
   __shared__ uint32_t found;
   __shared__ int left, same_all;
+  __shared__ uint16_t list[2][ITEMS ? ITEMS * kSel / 2 : 1];  // holes, movers, ascending
+  __shared__ uint64_t stays[ITEMS ? ITEMS * kSel / 64 : 1];   // bit per slot: kept, and below m
   const int64_t row = row0 + blockIdx.x;
   const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv), t = threadIdx.x, w = t >> 6, l = t & 63;
   const int n = min(max(seq_lens[b], 0), max_pages * kP), m = min(n, budget), seen = seen_all[b];
@@ -223,6 +239,7 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
   const int32_t* p_in = pos + row * S;
   float* w_out = weights_out + row * S;
   int32_t* p_out = pos_out + row * S;
+  int32_t* src = source + row * S;
   if (h == 0 && t == 0) new_lens[b] = m;
   auto pos_of = [&](int i) {
     const int p = p_in[i];
@@ -237,26 +254,27 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
   } else {
     // the wave's slots: [s0, s1), s0 + 64 i + lane for i < reps
     const int reps = (n + kSel - 1) / kSel, s0 = w * 64 * reps, s1 = min(n, s0 + 64 * reps);
-    // kBatch keys from item i0 on, all loads first (keys past s1 are not used)
+    // kB keys from item i0 on, all loads first (keys past s1 are not used)
     auto load_keys = [&](int i0, uint32_t* key) {
-      int p[kBatch];
-      float x[kBatch];
+      int p[kB];
+      float x[kB];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
+      for (int i = 0; i < kB; ++i) {
         const int at = min(s0 + 64 * (i0 + i) + l, n - 1);
         p[i] = p_in[at];
         x[i] = w_in[at];
       }
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
+      for (int i = 0; i < kB; ++i) {
         const int at = min(s0 + 64 * (i0 + i) + l, n - 1), q = p[i] >= 0 ? p[i] : seen - (n - at);
         key[i] = rank_key(x[i], q < sink || q >= seen - recent);
       }
     };
+    hist[t] = make_int2(0, 0);
     uint32_t keys[ITEMS ? ITEMS : 1];
     if (ITEMS) {
 #pragma unroll
-      for (int i0 = 0; i0 < ITEMS; i0 += kBatch)
+      for (int i0 = 0; i0 < ITEMS; i0 += kB)
         if (i0 < reps) load_keys(i0, keys + i0);
     }
     // f(i, key, valid) of the wave's slots in order
@@ -266,46 +284,42 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
         for (int i = 0; i < ITEMS; ++i)
           if (i < reps) f(i, keys[i], s0 + 64 * i + l < s1);
       } else {
-        for (int i0 = 0; i0 < reps; i0 += kBatch) {
-          uint32_t k[kBatch];
+        for (int i0 = 0; i0 < reps; i0 += kB) {
+          uint32_t k[kB];
           load_keys(i0, k);
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i)
+          for (int i = 0; i < kB; ++i)
             if (i0 + i < reps) f(i0 + i, k[i], s0 + 64 * (i0 + i) + l < s1);
         }
       }
     };
     uint32_t prefix = 0;
     int need = m;  // slots still to be kept among the keys that share the prefix
+    __syncthreads();
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-      hist[2 * t] = hist[2 * t + 1] = 0;
-      __syncthreads();
       each([&](int, uint32_t k, bool valid) {
         if (valid && (pass == 0 || (k >> (shift + bits)) == (prefix >> (shift + bits))))
-          atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1);
+          atomicAdd(&reinterpret_cast<int*>(hist)[2047 - ((k >> shift) & ((1u << bits) - 1))], 1);
       });
       __syncthreads();
-      const int c0 = hist[2 * t], c1 = hist[2 * t + 1];  // digits 2 t, 2 t + 1
-      int above = c0 + c1;  // inclusive sum over the wave's lanes from l up
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) {
-        const int y = __shfl_down(above, k, 64);
-        if (l + k < 64) above += y;
-      }
-      if (l == 0) above_all[w] = above;
+      const int2 c = hist[t];  // digits 2047 - 2 t, 2046 - 2 t
+      hist[t] = make_int2(0, 0);
+      int above = wave_prefix(c.x + c.y);  // of the wave's keys, those of digits from 2046 - 2 t up
+      if (l == 63) above_all[w] = above;
       __syncthreads();
-      above -= c0 + c1;  // digits above 2 t + 1: of the wave, then of the waves after it
-      for (int i = w + 1; i < kW; ++i) above += above_all[i];
-      if (above < need && above + c1 >= need) {
-        found = 2 * t + 1;
+      above -= c.x + c.y;
+#pragma unroll
+      for (int i = 0; i < kW; ++i) above += i < w ? above_all[i] : 0;
+      if (above < need && above + c.x >= need) {
+        found = 2047 - 2 * t;
         left = need - above;
-        same_all = c1;
-      } else if (above + c1 < need && above + c1 + c0 >= need) {
-        found = 2 * t;
-        left = need - above - c1;
-        same_all = c0;
+        same_all = c.x;
+      } else if (above + c.x < need && above + c.x + c.y >= need) {
+        found = 2046 - 2 * t;
+        left = need - above - c.x;
+        same_all = c.y;
       }
       __syncthreads();
       prefix |= found << shift;
@@ -322,7 +336,8 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
       each([&](int, uint32_t k, bool valid) { eq += __popcll(__ballot(valid && k == prefix)); });
       if (l == 0) part[w].x = eq;
       __syncthreads();
-      for (int i = 0; i < w; ++i) eq0 += part[i].x;
+#pragma unroll
+      for (int i = 0; i < kW; ++i) eq0 += i < w ? part[i].x : 0;
     }
     auto kept_of = [&](uint32_t k, bool valid, int& e) {
       if (!ties) return valid && k >= prefix;
@@ -335,50 +350,57 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
     each([&](int i, uint32_t k, bool valid) {
       const int at = s0 + 64 * i + l;
       const bool kept = kept_of(k, valid, e);
-      holes += valid && at < m && !kept;
-      movers += kept && at >= m;
+      holes += __popcll(__ballot(valid && at < m && !kept));
+      movers += __popcll(__ballot(kept && at >= m));
     });
-#pragma unroll
-    for (int k = 32; k >= 1; k >>= 1) {
-      holes += __shfl_xor(holes, k, 64);
-      movers += __shfl_xor(movers, k, 64);
-    }
     if (l == 0) {
       part[w].y = holes;
       part[w].z = movers;
     }
     __syncthreads();
     holes = movers = 0;
+#pragma unroll
     for (int i = 0; i < kW; ++i) {
-      if (i < w) {
-        holes += part[i].y;
-        movers += part[i].z;
-      }
+      holes += i < w ? part[i].y : 0;
+      movers += i < w ? part[i].z : 0;
       n_moves += part[i].z;
     }
     int2* mv = moves + row * (S / 2);
+    auto stay = [&](int at) {
+      w_out[at] = w_in[at];
+      p_out[at] = pos_of(at);
+      src[at] = -1;
+    };
     e = eq0;
     each([&](int i, uint32_t k, bool valid) {
       const int at = s0 + 64 * i + l;
       const bool kept = kept_of(k, valid, e);
       const bool hole = valid && at < m && !kept, mover = kept && at >= m;
       const uint64_t hs = __ballot(hole), ms = __ballot(mover);
-      if (hole) mv[holes + __popcll(hs & below)].y = at;
-      if (mover) mv[movers + __popcll(ms & below)].x = at;
+      const int ih = holes + __popcll(hs & below), im = movers + __popcll(ms & below);
+      if (ITEMS) {
+        if (hole) list[0][ih] = (uint16_t)at;
+        if (mover) list[1][im] = (uint16_t)at;
+        const uint64_t st = __ballot(kept && at < m);
+        if (l == 0) stays[s0 / 64 + i] = st;
+      } else {
+        if (hole) mv[ih].y = at;
+        if (mover) mv[im].x = at;
+        if (kept && !mover) stay(at);
+      }
       holes += __popcll(hs);
       movers += __popcll(ms);
-      if (kept && !mover) {
-        w_out[at] = w_in[at];
-        p_out[at] = pos_of(at);
-        source[row * S + at] = -1;
-      }
     });
     __syncthreads();
+    if (ITEMS) {  // the slots below m, over all threads
+      for (int i = t; i < m; i += kSel)
+        if (stays[i / 64] >> (i & 63) & 1) stay(i);
+    }
     for (int i = t; i < n_moves; i += kSel) {
-      const int2 x = mv[i];
-      w_out[x.y] = w_in[x.x];
-      p_out[x.y] = pos_of(x.x);
-      source[row * S + x.y] = x.x;
+      const int x = ITEMS ? list[1][i] : mv[i].x, y = ITEMS ? list[0][i] : mv[i].y;
+      w_out[y] = w_in[x];
+      p_out[y] = pos_of(x);
+      src[y] = x;
     }
     __syncthreads();  // in place, the sources lie in what is cleared now
   }
@@ -394,8 +416,8 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
 // bytes of V codes, 2 ng metadata entries.  More are put together in the page's own units: wave
 // w takes the K units of slots 4 lo + w (16 bytes of one slot per lane) and the V units
 // of channels 32 w .. (16 slots of a channel pair per lane: 16 byte loads, of which 16
-// lanes share a cache line or two, and one store; a wave per row took 64 lines and 64
-// single bytes each way: 32 x 8 rows of 16k to 1024 slots, 116 us).
+// lanes share two cache lines, and one store; a wave per row moved 64 single bytes both
+// ways: 32 x 8 rows of 16k to 1024 slots, 116 us).
 __global__ __launch_bounds__(256) void kv4_evict_move_kernel(uint8_t* __restrict__ pages, int Hkv, int64_t S,
                                                              int ng, const int32_t* __restrict__ block_table,
                                                              int max_pages, const int32_t* __restrict__ counts,
@@ -499,7 +521,8 @@ hipError_t launch_kv4_gather(const uint8_t* pages, int Hkv, const int64_t* slots
 }
 
 namespace {
-// Moves per row, their lists (hole, mover), and the source of every slot that receives one.
+// Moves per row, their lists (hole, mover) where they do not fit into the select block's LDS,
+// and the source of every slot below the budget.
 struct EvictWs {
   size_t moves_off, source_off, total;
 };
@@ -507,7 +530,7 @@ EvictWs evict_ws(int Hkv, int B, int max_pages) {
   const size_t rows = (size_t)B * Hkv, S = (size_t)max_pages * kP;
   EvictWs w;
   w.moves_off = align256(rows * sizeof(int32_t));
-  w.source_off = align256(w.moves_off + rows * (S / 2) * sizeof(int2));
+  w.source_off = align256(w.moves_off + (S <= kSelLds ? 0 : rows * (S / 2) * sizeof(int2)));
   w.total = align256(w.source_off + rows * S * sizeof(int32_t));
   return w;
 }
@@ -530,7 +553,7 @@ hipError_t launch_kv4_evict(const EvictArgs& a, hipStream_t st) {
     };
     if (S <= 4 * kSel) go(kv4_evict_select_kernel<4>);
     else if (S <= 12 * kSel) go(kv4_evict_select_kernel<12>);
-    else if (S <= 32 * kSel) go(kv4_evict_select_kernel<32>);
+    else if (S <= kSelLds) go(kv4_evict_select_kernel<32>);
     else go(kv4_evict_select_kernel<0>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -57,7 +57,7 @@ def test_sizes(L):
     assert ok.kv4_decode_workspace_bytes(lay, 4, 30, 3, 20) == 0
     assert ok.kv4_decode_workspace_bytes(lay, 4, 32, 3, 0) == 0
     assert ok.kv4_decode_workspace_bytes(lay, 4, 32, 3, 1 << 25) == 0   # slots pass 32 bits
-    assert ok.kv4_evict_workspace_bytes(lay, 4, 20) >= 4 * 8 * 20 * 64 * 8
+    assert ok.kv4_evict_workspace_bytes(lay, 4, 20) >= 4 * 8 * 20 * 64 * 4
     for args in ((0, 20), (65536, 20), (4, 0), (4, 1 << 25)):
         assert ok.kv4_evict_workspace_bytes(lay, *args) == 0
 
