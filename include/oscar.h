@@ -422,7 +422,7 @@ size_t oscar_kv4_decode_workspace_bytes(const oscar_layout *L, int32_t B, int32_
  *       aligned, the same array or disjoint ones: for every cached token
  *         weights_out[b][h][t] = weights[b][h][t] + sum_i p_{b,i,t},   t < seq_lens[b],
  *       p the softmax weight of the token in query head i, over the query heads i of
- *       KV head h.  Entries t >= seq_lens[b] are neither read nor written.
+ *       KV head h.  Entries t >= seq_lens[b] may hold anything and stay as they are.
  *   workspace : >= oscar_kv4_decode_workspace_bytes(L, B, Hq, num_splits,
  *       max_pages_per_seq, weights != NULL) bytes with num_splits resolved
  */
@@ -471,7 +471,7 @@ int oscar_kv4_decode_step(const oscar_layout *L, void *pages, const void *k_new,
  *   num_seen             : int32 [B], tokens of the sequence so far, evicted ones too
  *       (>= seq_lens[b])
  *   budget >= 1, sink >= 0, recent >= 0
- *   new_lens             : int32 [B], not seq_lens itself
+ *   new_lens             : int32 [B], disjoint from seq_lens
  *   workspace            : >= oscar_kv4_evict_workspace_bytes(L, B, max_pages_per_seq)
  *       bytes, 256-byte aligned, contents need no initialization
  */

@@ -599,6 +599,15 @@ int check_kv4_slots(const oscar_layout* L, int32_t max_pages_per_seq) {
   return OSCAR_OK;
 }
 
+// Arrays of `bytes` bytes that share some of them without being the same array.
+bool partly_shared(const void* a, const void* b, size_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x != y && (x < y ? y - x : x - y) < bytes;
+}
+size_t kv4_slots_bytes(const oscar_layout* L, int32_t B, int32_t max_pages) {
+  return (size_t)B * L->num_kv_heads * max_pages * (size_t)L->page_size * sizeof(float);
+}
+
 struct Kv4Ws {
   DecodeWs d;
   size_t scores_off, total;
@@ -625,7 +634,8 @@ int check_kv4_decode(const oscar_layout* L, const void* pages, const void* q, in
   if ((st = check_kv4_slots(L, max_pages_per_seq))) return st;
   if ((weights == nullptr) != (weights_out == nullptr)) return OSCAR_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, 256) || !aligned(R_k, 16) || !aligned(R_v, 16) ||
-      !aligned(weights, 16) || !aligned(weights_out, 16))
+      !aligned(weights, 16) || !aligned(weights_out, 16) ||
+      partly_shared(weights, weights_out, kv4_slots_bytes(L, B, max_pages_per_seq)))
     return OSCAR_ERR_INVALID_ARG;
   if (workspace_bytes < kv4_ws(L, B, Hq, *num_splits, max_pages_per_seq, weights != nullptr).total)
     return OSCAR_ERR_WORKSPACE_TOO_SMALL;
@@ -770,6 +780,10 @@ int oscar_kv4_evict(const oscar_layout* L, void* pages, int32_t B, const int32_t
   if ((st = check_kv4_slots(L, max_pages_per_seq))) return st;
   if (!pages || !block_table || !seq_lens || !weights || !weights_out || !pos || !pos_out || !num_seen ||
       !new_lens || !workspace || new_lens == seq_lens)
+    return OSCAR_ERR_INVALID_ARG;
+  const size_t slots = kv4_slots_bytes(L, B, max_pages_per_seq);
+  if (partly_shared(weights, weights_out, slots) || partly_shared(pos, pos_out, slots) ||
+      partly_shared(new_lens, seq_lens, (size_t)B * sizeof(int32_t)))
     return OSCAR_ERR_INVALID_ARG;
   if (!aligned(pages, 16) || !aligned(weights, 16) || !aligned(weights_out, 16) || !aligned(pos, 16) ||
       !aligned(pos_out, 16) || !aligned(workspace, 256))

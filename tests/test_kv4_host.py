@@ -104,6 +104,9 @@ def test_decode_refusals(L, step):
     assert call(ws=ctypes.c_void_p(0x10010)) == INV and call(Rv=ctypes.c_void_p(0x10004)) == INV
     assert call(w=FAKE) == INV and call(wo=FAKE) == INV                      # one without the other
     assert call(w=ctypes.c_void_p(0x10004), wo=FAKE) == INV
+    n = 2 * 8 * 4 * 64 * 4                                                   # weights: [2][8][4 * 64] fp32
+    for d in (16, n - 16, 16 - n):                                           # partly the same bytes
+        assert call(w=FAKE, wo=ctypes.c_void_p(FAKE.value + d)) == INV
     lay = ok.Layout(8, 10)
     assert call(size=ok.kv4_decode_workspace_bytes(lay, 2, 32, 2, 4) - 1) == SMALL
     assert call(w=FAKE, wo=FAKE, size=ok.kv4_decode_workspace_bytes(lay, 2, 32, 2, 4, True) - 1) == SMALL
@@ -122,6 +125,10 @@ def test_evict_refusals(L):
     for name in ("pages", "bt", "lens", "w", "wo", "p", "po", "seen", "new", "ws"):
         assert call(**{name: None}) == INV, name
     assert call(new=FAKE) == INV                                             # seq_lens itself
+    assert call(new=ctypes.c_void_p(FAKE.value + 4)) == INV                  # part of it
+    n = 2 * 8 * 4 * 64 * 4
+    for d in (16, n - 16, 16 - n):
+        assert call(wo=ctypes.c_void_p(FAKE.value + d)) == INV and call(po=ctypes.c_void_p(FAKE.value + d)) == INV
     for name in ("pages", "w", "wo", "p", "po"):
         assert call(**{name: ctypes.c_void_p(0x10008)}) == INV, name
     assert call(size=ok.kv4_evict_workspace_bytes(ok.Layout(8, 10), 2, 4) - 1) == SMALL
