@@ -372,7 +372,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
 #pragma unroll
         for (int u = 0; u < 4; ++u) e[u] = vs[(u * NG + q) >> 2][(u * NG + q) & 3];
         const uint32_t big = row_max_u(pk_max(pk_max(e[0], e[1]), pk_max(e[2], e[3])) & 0xffffu);
-        const int ex = __builtin_amdgcn_frexp_expf(meta_s<BF>(big)) - kTop;
+        int ex = __builtin_amdgcn_frexp_expf(meta_s<BF>(big)) - kTop;
+        if (BF) ex = max(ex, -120);  // 2^-ex is finite for every scale
         const float scale = __builtin_ldexpf(1.0f, -ex);
         back[q] = __builtin_ldexpf(1.0f, ex);
 #pragma unroll

@@ -119,6 +119,12 @@ def test_magnitudes(scale, q_scale, meta):
     c.check((0, 1))
 
 
+@pytest.mark.parametrize("g", (4, 9))
+def test_smallest_bf16_scales(g):
+    """Scales near the least normal bf16, whose reciprocals have no power of two in fp32."""
+    Case(9, (90, 700), 2 * g, 2, 32, 1, rot="identity", scale=1e-37).check((0, 1))
+
+
 def test_one_heavy_token_among_many():
     """A token with nearly all the weight, and 5000 others 2^-17 of it each: the small
     weights keep their bits."""
