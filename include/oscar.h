@@ -10,7 +10,8 @@
  * computes softmax(q K^T / sqrt(d)) V against the reconstructed rows
  * K^ = Q(K R_k) R_k^T, V^ = Q(V R_v) R_v^T (Sec. 2 quantization notation;
  * Alg. 1 DecodeStep) as a split-K flash-decoding pass with a log-sum-exp merge
- * (Sec. 4 "Decoding Attention Kernel").
+ * (Sec. 4 "Decoding Attention Kernel").  The 4-bit cache (below) is the same path with
+ * 16 levels per channel, and eviction from it by accumulated attention weight.
  *
  * Plain C, no HIP include: load it with any FFI.
  *

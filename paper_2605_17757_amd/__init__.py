@@ -1,5 +1,5 @@
-"""Python binding of liboscar (INT2 KV-cache append + paged decode attention for
-OSCAR, arXiv 2605.17757, on MI355X / gfx950).
+"""Python binding of liboscar (INT2 and 4-bit KV-cache append + paged decode attention
+for OSCAR, arXiv 2605.17757, on MI355X / gfx950).
 
 Argument marshalling only: every function checks tensor dtypes, devices and
 shapes, then calls the C ABI of ``liboscar.so`` (declared in include/oscar.h)
