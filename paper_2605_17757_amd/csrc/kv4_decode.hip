@@ -21,8 +21,12 @@
 //     sums of uncentred codes that left errors of 1e-5 of the output.  w is scaled by a
 //     power of two per page and group, its largest values near 2^14, and enters as two
 //     fp16 pieces: 22 bits, down to 2^-16 of the row's largest weight, then fewer.
-// The pieces of one head are rows of the 16-row operand and 4 heads fill it, so that up
-// to 4 heads per KV head cost no more matrix products than unsplit operands would.
+// Where the pieces go (NCH chunks of 4 heads per KV head).  As rows of one 16-row operand:
+// 4 heads fill it, one product per chunk does, and a lane adds the pieces of a sum.  As
+// operands of their own, a row per head: 3 products (values: 2) serve 16 heads, the matrix
+// cores add the pieces, smallest first.  Scores as rows up to 8 heads, values up to 4, where
+// they take fewer products; past that as operands (12 heads, 16 x 128k tokens: 682 us as
+// rows, 620; 16 heads, 16 x 65k: 403 and 332; 8 heads either way within 2 %).
 // |q~| must stay below 2^56 (scores: 2^-69 n q~ 2^133 2^-64).
 #include <hip/hip_fp16.h>
 
@@ -44,7 +48,8 @@ typedef float f4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;         // waves of a block: a team on one range of pages
-constexpr int kPw = 40;           // dwords per row of the weights operand in LDS
+constexpr int kPw = 40;           // dwords per row of the weights operand in LDS, NCH 1
+constexpr int kPwWide = 36;       // wider: 16 rows read at once, 4 dwords each, take all banks
 constexpr float kSlack = 4.0f;    // how far (log2) a score may exceed the reference maximum before it moves
 constexpr float kIn = 0x1p64f;    // scale of q~ in the scores' products with codes
 constexpr float kOut = 0x1p69f;   // back: 2^133 / kIn
@@ -122,11 +127,18 @@ __device__ inline float meta_z(uint32_t e) {
   return BF ? __uint_as_float(e & 0xffff0000u) : (float)__builtin_bit_cast(_Float16, (uint16_t)(e >> 16));
 }
 
+// Weights operands in LDS, rows of kPw dwords (64 slots), per wave.  NCH 1: of two groups, 8
+// rows (head, piece) each.  Wider: of one, 16 rows for each of the two pieces.
+template <int NCH>
+constexpr int weight_dwords() {
+  return NCH == 1 ? 16 * kPw : std::max(32 * kPwWide, NCH * 4 * kD);
+}
+
 template <int NCH>
 struct SplitSmem {
-  u4v qa[NCH][4][64];                     // query operands: chunk, 32-channel block, lane
-  uint32_t pw[kWaves][NCH][16 * kPw];     // weights operands of two groups (8 rows: head, piece); o~ at the end
-  float ml[kWaves][NCH * 4][2];           // the waves' (m, l)
+  u4v qa[NCH <= 2 ? NCH : 3][4][64];          // query operands: chunk or piece, 32-channel block, lane
+  uint32_t pw[kWaves][weight_dwords<NCH>()];  // weights operands; o~ at the end
+  float ml[kWaves][NCH * 4][2];               // the waves' (m, l)
 };
 
 // ---------------------------------------------------------------------------
@@ -136,18 +148,19 @@ struct SplitSmem {
 // sequence and merge their states in LDS: one partial state per part, and a short
 // sequence's pages at once.  Per page a wave has
 //   K in 4 loads of 1 KB (lane: slot 4 lo + u, channels 8 hi .. of four blocks of 32):
-//     16 products per chunk of 4 heads, lane (head hi, slot) holds a score's pieces;
+//     16 products per chunk (48 in all past 8 heads), lane (hi, slot) gets the sums of
+//     heads NCH hi ..;
 //   V in 4 loads (lane: 16 slots of channels 32 j + lo, + 16): the weights of a group go
-//     through LDS into the operand's rows, 16 products per chunk, added to o~ (lane:
-//     head hi, 8 channels) after the page.
+//     through LDS into the operand's rows, 16 products (32 past 4 heads), added to o~
+//     (lane: heads NCH hi .., 8 channels) after the page.
 // The next page's K is loaded once this page's is used up, so that 5 KB per wave are
 // always on their way at 8 waves per CU.
 //
 // Bound: up to 4 heads per KV head HBM (64 sequences of 16k to 32k tokens, 32/8 heads:
 // 2.0 GB in 314 us, 6.4 TB/s; 555 vector instructions per page, VALU busy 61 %).  Beyond,
-// the VALU: per chunk and page about 200 instructions (scores 68, weights and their pieces
-// 100, sums 16, softmax 16) beside 310 that all chunks share (unpacking 224, metadata 84).
-// 12 heads (16 x 128k tokens): 968 a page, busy 76 %, matrix cores 30 %, 640 us, 4.2 TB/s.
+// the VALU: per page about 310 instructions that all chunks share (unpacking 224, metadata
+// 84) and about 170 per chunk (scores 36, weights and their pieces 70, softmax 20, sums 8).
+// 12 heads (16 x 128k tokens): 828 a page, busy 74 %, matrix cores 28 %, 570 us, 4.7 TB/s.
 // Two waves per SIMD: at three, which the 4-head instances allow, 342 us for 340.  With
 // the products' sums kept in the accumulators across pages (32 registers per chunk
 // instead of 8) more than 8 heads went to scratch: 16 heads 555 us, 310 now.  Rotating
@@ -163,7 +176,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
     const float* __restrict__ qt, float* __restrict__ part_o, float* __restrict__ part_ml,
     float* __restrict__ scores) {
   __shared__ SplitSmem<NCH> sm;
-  constexpr int KPG = 4 / NG;  // 32-channel blocks per group
+  constexpr int KPG = 4 / NG;                  // 32-channel blocks per group
+  constexpr int kPieces = 3;                   // of q~
   const int r = (int)(blockIdx.x / (uint32_t)Hkv), kvh = (int)(blockIdx.x % (uint32_t)Hkv);
   const int g = Hq / Hkv;
   const int t = threadIdx.x, w = t >> 6, l = t & 63, lo = l & 15, hi = l >> 4;
@@ -181,23 +195,32 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       return i0 + l < n_mine ? bt[p] : 0;
     };
     int ids = page_ids(0);
-    // wave w makes operands (chunk, 32-channel block) w, w + 4, ..: rows 4 h + piece
-    float4 xr[NCH][2], xs[NCH][2];
-#pragma unroll
-    for (int ch = 0; ch < NCH; ++ch) {
-      const int head = 4 * ch + (lo >> 2), hs = 4 * ch + hi;
+    // The lane's heads are NCH hi + ch.  Wave w makes the operands of 32-channel block w: of
+    // chunk ch, row 4 h + piece of head NCH h + ch; or of a piece, row 4 h + ch of that head.
+    constexpr int kXr = NCH <= 2 ? NCH : 1;
+    float4 xr[kXr][2], xs[NCH][2];
+    {
       const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      xr[ch][0] = xr[ch][1] = xs[ch][0] = xs[ch][1] = none;
       const float* row = qt + ((size_t)b * Hq + kvh * g) * kD;
-      if (head < g) {
-        const float4* src = reinterpret_cast<const float4*>(row + head * kD + 32 * w + 8 * hi);
-        xr[ch][0] = src[0];
-        xr[ch][1] = src[1];
+#pragma unroll
+      for (int k = 0; k < kXr; ++k) {
+        const int head = NCH <= 2 ? NCH * (lo >> 2) + k : (lo & 3) < NCH ? NCH * (lo >> 2) + (lo & 3) : g;
+        xr[k][0] = xr[k][1] = none;
+        if (head < g) {
+          const float4* src = reinterpret_cast<const float4*>(row + head * kD + 32 * w + 8 * hi);
+          xr[k][0] = src[0];
+          xr[k][1] = src[1];
+        }
       }
-      if (hs < g) {
-        const float4* src = reinterpret_cast<const float4*>(row + hs * kD + 8 * lo);
-        xs[ch][0] = src[0];
-        xs[ch][1] = src[1];
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) {
+        const int hs = NCH * hi + ch;
+        xs[ch][0] = xs[ch][1] = none;
+        if (hs < g) {
+          const float4* src = reinterpret_cast<const float4*>(row + hs * kD + 8 * lo);
+          xs[ch][0] = src[0];
+          xs[ch][1] = src[1];
+        }
       }
     }
     auto block_of = [&](int i) {
@@ -218,23 +241,35 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       load_k(blk);
     }
     // ---- query operands and group sums ----
-    float qs[NCH][NG];  // sums of q~ over the groups, head 4 ch + hi, in the products' scale
+#pragma unroll
+    for (int k = 0; k < kXr; ++k) {
+      float x[8] = {xr[k][0].x, xr[k][0].y, xr[k][0].z, xr[k][0].w, xr[k][1].x, xr[k][1].y, xr[k][1].z, xr[k][1].w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= e & 2 ? kIn / 16.0f : kIn;
+      auto operand = [&]() {
+        return u4v{pack_hi(x[0], x[1]), pack_hi(x[2], x[3]), pack_hi(x[4], x[5]), pack_hi(x[6], x[7])};
+      };
+      if (NCH <= 2) {
+        const int pc = lo & 3;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (pc > 0) x[e] -= top16(x[e]);
+          if (pc > 1) x[e] -= top16(x[e]);
+          if (pc > 2) x[e] = 0.0f;
+        }
+        sm.qa[k][w][l] = operand();
+      } else {
+#pragma unroll
+        for (int pc = 0; pc < 3; ++pc) {
+          sm.qa[pc][w][l] = operand();
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] -= top16(x[e]);
+        }
+      }
+    }
+    float qs[NCH][NG];  // sums of q~ over the groups, head NCH hi + ch, in the products' scale
 #pragma unroll
     for (int ch = 0; ch < NCH; ++ch) {
-      const int pc = lo & 3;
-      float x[8] = {xr[ch][0].x, xr[ch][0].y, xr[ch][0].z, xr[ch][0].w,
-                    xr[ch][1].x, xr[ch][1].y, xr[ch][1].z, xr[ch][1].w};
-      u4v a;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] *= e & 2 ? kIn / 16.0f : kIn;
-        if (pc > 0) x[e] -= top16(x[e]);
-        if (pc > 1) x[e] -= top16(x[e]);
-        if (pc > 2) x[e] = 0.0f;
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) a[k] = pack_hi(x[2 * k], x[2 * k + 1]);
-      sm.qa[ch][w][l] = a;
       float s = ((xs[ch][0].x + xs[ch][0].y) + (xs[ch][0].z + xs[ch][0].w)) +
                 ((xs[ch][1].x + xs[ch][1].y) + (xs[ch][1].z + xs[ch][1].w));
 #pragma unroll
@@ -244,7 +279,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
     }
     __syncthreads();
 
-    // State: o (before the zero points' part: channel 16 ct + lo of head 4 ch + hi), and
+    // State: o (before the zero points' part: channel 16 ct + lo of head NCH hi + ch), and
     // per lane, over its own slots, the sums of weights and of weights times (z - 8).
     float m[NCH], lsum[NCH], wz[NCH][NG], o[NCH][8];
 #pragma unroll
@@ -269,40 +304,67 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
         for (int u = 0; u < NG; ++u) vs[u] = z[u];
       }
       __builtin_amdgcn_sched_barrier(0);
-      // ---- scores of heads 4 ch + hi, slots 4 lo + u ----
+      // ---- scores of heads NCH hi + ch, slots 4 lo + u ----
       float sc[NCH][4];
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch)
 #pragma unroll
         for (int u = 0; u < 4; ++u) sc[ch][u] = 0.0f;
-      // a slot's sums are used while the next slot's products run; query operands one
-      // 32-channel block ahead
-      u4v qa[2][NCH];
-      f4v d[4][NCH];
+      auto add = [&](int q, int u, int ch, float x) {  // x: products of group q
+        const uint32_t e = ks[(u * NG + q) >> 2][(u * NG + q) & 3];
+        sc[ch][u] = fmaf(meta_s<BF>(e), fmaf(meta_z<BF>(e), -qs[ch][q], x), sc[ch][u]);
+      };
+      if (NCH <= 2) {  // a slot's sums are used while the next slot's products run
+        u4v qa[2][NCH];  // query operands one 32-channel block ahead
+        f4v d[4][NCH];
 #pragma unroll
-      for (int ch = 0; ch < NCH; ++ch) qa[0][ch] = sm.qa[ch][0][l];
+        for (int ch = 0; ch < NCH; ++ch) qa[0][ch] = sm.qa[ch][0][l];
 #pragma unroll
-      for (int i = 0; i <= 16; ++i) {
-        const int kc = i / 4, u = i % 4;
-        if (i < 16) {
-          const u4v bop = unpack(kr[u][kc]);
+        for (int i = 0; i <= 16; ++i) {
+          const int kc = i / 4, u = i % 4;
+          if (i < 16) {
+            const u4v bop = unpack(kr[u][kc]);
 #pragma unroll
-          for (int ch = 0; ch < NCH; ++ch)
-            d[u][ch] = mfma(qa[kc & 1][ch], bop, kc % KPG == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[u][ch]);
-          if (u == 0 && kc < 3)
+            for (int ch = 0; ch < NCH; ++ch)
+              d[u][ch] = mfma(qa[kc & 1][ch], bop, kc % KPG == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[u][ch]);
+            if (u == 0 && kc < 3)
 #pragma unroll
-            for (int ch = 0; ch < NCH; ++ch) qa[(kc + 1) & 1][ch] = sm.qa[ch][kc + 1][l];
-        }
-        if (i > 0 && (i - 1) / 4 % KPG == KPG - 1) {
-          const int q = (i - 1) / 4 / KPG, up = (i - 1) % 4;
-          const uint32_t e = ks[(up * NG + q) >> 2][(up * NG + q) & 3];
-#pragma unroll
-          for (int ch = 0; ch < NCH; ++ch) {
-            const f4v& x = d[up][ch];
-            sc[ch][up] = fmaf(meta_s<BF>(e), fmaf(meta_z<BF>(e), -qs[ch][q], (x[0] + x[1]) + x[2]), sc[ch][up]);
+              for (int ch = 0; ch < NCH; ++ch) qa[(kc + 1) & 1][ch] = sm.qa[ch][kc + 1][l];
           }
+          if (i > 0 && (i - 1) / 4 % KPG == KPG - 1)
+#pragma unroll
+            for (int ch = 0; ch < NCH; ++ch) {
+              const f4v& x = d[(i - 1) % 4][ch];
+              add((i - 1) / 4 / KPG, (i - 1) % 4, ch, (x[0] + x[1]) + x[2]);
+            }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+      } else {  // a block's sums while the next block's products run, small pieces first
+        f4v d[2][4];
+#pragma unroll
+        for (int kc = 0; kc <= 4; ++kc) {
+          if (kc < 4) {
+            u4v qa[kPieces], bop[4];
+#pragma unroll
+            for (int pc = kPieces - 1; pc >= 0; --pc) qa[pc] = sm.qa[pc][kc][l];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) bop[u] = unpack(kr[u][kc]);
+#pragma unroll
+            for (int pc = kPieces - 1; pc >= 0; --pc)
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                d[kc & 1][u] = mfma(qa[pc], bop[u],
+                                    pc < kPieces - 1 ? d[kc & 1][u]
+                                    : kc % KPG == 0  ? f4v{0.0f, 0.0f, 0.0f, 0.0f}
+                                                     : d[(kc - 1) & 1][u]);
+          }
+          if (kc > 0 && (kc - 1) % KPG == KPG - 1)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+              for (int ch = 0; ch < NCH; ++ch) add((kc - 1) / KPG, u, ch, d[(kc - 1) & 1][u][ch]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch)
@@ -327,9 +389,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       if (scores) {
 #pragma unroll
         for (int ch = 0; ch < NCH; ++ch)
-          if (4 * ch + hi < g)
+          if (NCH * hi + ch < g)
             *reinterpret_cast<float4*>(
-                scores + (((size_t)b * Hq + kvh * g + 4 * ch + hi) * max_pages + pg) * kP + 4 * lo) =
+                scores + (((size_t)b * Hq + kvh * g + NCH * hi + ch) * max_pages + pg) * kP + 4 * lo) =
                 make_float4(sc[ch][0], sc[ch][1], sc[ch][2], sc[ch][3]);
       }
       // ---- softmax weights; the reference maximum moves only when a score exceeds it
@@ -393,10 +455,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
           const fp16x2 h0 = __builtin_amdgcn_cvt_pkrtz(x[0], x[1]), h1 = __builtin_amdgcn_cvt_pkrtz(x[2], x[3]);
           const fp16x2 r0 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h0[0], -1.0f, x[0]), fmaf((float)h0[1], -1.0f, x[1]));
           const fp16x2 r1 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h1[0], -1.0f, x[2]), fmaf((float)h1[1], -1.0f, x[3]));
-          uint32_t* row = sm.pw[w][ch] + (q & 1) * 8 * kPw + 2 * hi * kPw + 2 * lo;
+          uint32_t* row = sm.pw[w] + 2 * lo + (NCH == 1 ? ((q & 1) * 8 + 2 * hi) * kPw : (4 * hi + ch) * kPwWide);
           *reinterpret_cast<uint2*>(row) =
               make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
-          *reinterpret_cast<uint2*>(row + kPw) =
+          *reinterpret_cast<uint2*>(row + (NCH == 1 ? kPw : 16 * kPwWide)) =
               make_uint2(__builtin_bit_cast(uint32_t, r0), __builtin_bit_cast(uint32_t, r1));
         }
       };
@@ -408,35 +470,35 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
           stage(q);
         }
         lane_exchange();
-        u4v a[NCH][2];  // rows 4 h + 2, 4 h + 3 of the operand repeat 4 h, 4 h + 1
+        u4v a[2][2];  // (wider: piece,) half of the slots; NCH 1: rows 4 h + 2, 4 h + 3 repeat 4 h, 4 h + 1
 #pragma unroll
-        for (int ch = 0; ch < NCH; ++ch)
+        for (int pc = 0; pc < (NCH == 1 ? 1 : 2); ++pc)
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
-            a[ch][kt] = *reinterpret_cast<const u4v*>(sm.pw[w][ch] + (q & 1) * 8 * kPw +
-                                                      ((lo >> 2) * 2 + (lo & 1)) * kPw + 16 * kt + 4 * hi);
+            a[pc][kt] = *reinterpret_cast<const u4v*>(
+                sm.pw[w] + 16 * kt + 4 * hi +
+                (NCH == 1 ? ((q & 1) * 8 + (lo >> 2) * 2 + (lo & 1)) * kPw : (16 * pc + lo) * kPwWide));
         __builtin_amdgcn_sched_barrier(0);
         if (NCH == 1 && q + 1 < NG) stage(q + 1);  // into the other half of the buffer, while the reads are under way
 #pragma unroll
         for (int k = 0; k < KPG; ++k) {
           const int j = q * KPG + k;
           __builtin_amdgcn_sched_barrier(0);
-          f4v d[NCH][2];
+          f4v d[2] = {f4v{0.0f, 0.0f, 0.0f, 0.0f}, f4v{0.0f, 0.0f, 0.0f, 0.0f}};
+          u4v b[2][2];  // channels 32 j + lo and 32 j + 16 + lo
 #pragma unroll
-          for (int kt = 0; kt < 2; ++kt) {
-            u4v b0, b1;  // channels 32 j + lo and 32 j + 16 + lo
-            unpack_v(vr[j][2 * kt], vr[j][2 * kt + 1], b0, b1);
+          for (int kt = 0; kt < 2; ++kt) unpack_v(vr[j][2 * kt], vr[j][2 * kt + 1], b[kt][0], b[kt][1]);
 #pragma unroll
-            for (int ch = 0; ch < NCH; ++ch) {
-              d[ch][0] = mfma_h(a[ch][kt], b0, kt == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[ch][0]);
-              d[ch][1] = mfma_h(a[ch][kt], b1, kt == 0 ? f4v{0.0f, 0.0f, 0.0f, 0.0f} : d[ch][1]);
-            }
-          }
+          for (int pc = (NCH == 1 ? 0 : 1); pc >= 0; --pc)
 #pragma unroll
-          for (int ch = 0; ch < NCH; ++ch) {
-            o[ch][2 * j] = fmaf(d[ch][0][0] + d[ch][0][1], 0x1p9f * back[q], o[ch][2 * j]);
-            o[ch][2 * j + 1] = fmaf(d[ch][1][0] + d[ch][1][1], 0x1p9f * back[q], o[ch][2 * j + 1]);
-          }
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+              for (int n = 0; n < 2; ++n) d[n] = mfma_h(a[pc][kt], b[kt][n], d[n]);
+#pragma unroll
+          for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              o[ch][2 * j + n] = fmaf(NCH == 1 ? d[n][0] + d[n][1] : d[n][ch], 0x1p9f * back[q], o[ch][2 * j + n]);
         }
       }
       lane_exchange();  // the reads come before the next page's weights
@@ -450,13 +512,13 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       float z[NG];
 #pragma unroll
       for (int q = 0; q < NG; ++q) z[q] = row_sum(wz[ch][q]);
-      float* om = reinterpret_cast<float*>(sm.pw[w][ch]) + hi * kD;
+      float* om = reinterpret_cast<float*>(sm.pw[w]) + (NCH * hi + ch) * kD;
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
         om[16 * ct + lo] = o[ch][ct] - z[ct / 2 / KPG];
       if (lo == 0) {
-        sm.ml[w][4 * ch + hi][0] = m[ch];
-        sm.ml[w][4 * ch + hi][1] = lt;
+        sm.ml[w][NCH * hi + ch][0] = m[ch];
+        sm.ml[w][NCH * hi + ch][1] = lt;
       }
     }
     __syncthreads();
@@ -469,7 +531,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
         const float e = __builtin_amdgcn_exp2f(sm.ml[k][head][0] - M);  // a wave without pages: 0
-        v = fmaf(e, reinterpret_cast<const float*>(sm.pw[k][head >> 2])[(head & 3) * kD + c], v);
+        v = fmaf(e, reinterpret_cast<const float*>(sm.pw[k])[head * kD + c], v);
         L = fmaf(e, sm.ml[k][head][1], L);
       }
       const size_t slot = ((size_t)b * Hq + kvh * g + head) * num_splits + piece;
