@@ -181,7 +181,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
 //           m-th largest rank by radix selection on ordered 32-bit keys (3 histograms of
 //           11, 11 and 10 bits), kept in registers up to 32 slots a thread; then every
 //           wave counts what it keeps, one block-wide sum gives it its places in the
-//           lists of holes and movers, and a last pass fills them and pairs them off.
+//           lists of holes and movers, and a last pass fills them and pairs them off.  Rows
+//           of more than 32768 slots take several blocks each (kv4_evict_part_kernel).
 //   move:   the moved rows' bytes (codes, scales, zeros) from page to page, one block per
 //           page that receives any.
 // Bounds: select the latency of its passes, one block per row: 32 x 8 rows of 8k to 16k
@@ -215,23 +216,22 @@ __device__ inline int wave_prefix(int v) {
   return v;
 }
 
-// ITEMS: slots per thread whose keys are kept in registers and whose lists of holes and
-// movers (at most S / 2 of each) in LDS; 0: any number, keys formed anew in every pass,
-// lists in the workspace.
+// The select in one block per row.  ITEMS: slots per thread at most; their keys are kept in
+// registers, the lists of holes and movers (at most S / 2 of each) in LDS.
 template <int ITEMS>
 __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
     int Hkv, int64_t S, int max_pages, const int32_t* __restrict__ seq_lens, const float* weights,
     float* weights_out, const int32_t* pos, int32_t* pos_out, const int32_t* __restrict__ seen_all,
     int budget, int sink, int recent, int32_t* __restrict__ new_lens, int32_t* __restrict__ counts,
-    int2* __restrict__ moves, int32_t* __restrict__ source, int64_t row0) {
-  constexpr int kW = kSel / 64, kB = ITEMS == 12 ? 6 : 4;  // kB: slots per thread whose loads are issued together
+    int32_t* __restrict__ source, int64_t row0) {
+  constexpr int kW = kSel / 64, kB = ITEMS % 6 == 0 ? 6 : 4;  // kB: slots per thread whose loads are issued together
   __shared__ int2 hist[kSel];  // entry i of the ints: keys whose digit is 2047 - i
   __shared__ int3 part[kW];    // per wave: keys equal to the last kept one, holes, movers
   __shared__ int above_all[kW];
   __shared__ uint32_t found;
   __shared__ int left, same_all;
-  __shared__ uint16_t list[2][ITEMS ? ITEMS * kSel / 2 : 1];  // holes, movers, ascending
-  __shared__ uint64_t stays[ITEMS ? ITEMS * kSel / 64 : 1];   // bit per slot: kept, and below m
+  __shared__ uint16_t list[2][ITEMS * kSel / 2];  // holes, movers, ascending
+  __shared__ uint64_t stays[ITEMS * kSel / 64];   // bit per slot: kept, and below m
   const int64_t row = row0 + blockIdx.x;
   const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv), t = threadIdx.x, w = t >> 6, l = t & 63;
   const int n = min(max(seq_lens[b], 0), max_pages * kP), m = min(n, budget), seen = seen_all[b];
@@ -271,27 +271,15 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
       }
     };
     hist[t] = make_int2(0, 0);
-    uint32_t keys[ITEMS ? ITEMS : 1];
-    if (ITEMS) {
+    uint32_t keys[ITEMS];
 #pragma unroll
-      for (int i0 = 0; i0 < ITEMS; i0 += kB)
-        if (i0 < reps) load_keys(i0, keys + i0);
-    }
+    for (int i0 = 0; i0 < ITEMS; i0 += kB)
+      if (i0 < reps) load_keys(i0, keys + i0);
     // f(i, key, valid) of the wave's slots in order
     auto each = [&](auto&& f) {
-      if (ITEMS) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-          if (i < reps) f(i, keys[i], s0 + 64 * i + l < s1);
-      } else {
-        for (int i0 = 0; i0 < reps; i0 += kB) {
-          uint32_t k[kB];
-          load_keys(i0, k);
-#pragma unroll
-          for (int i = 0; i < kB; ++i)
-            if (i0 + i < reps) f(i0 + i, k[i], s0 + 64 * (i0 + i) + l < s1);
-        }
-      }
+      for (int i = 0; i < ITEMS; ++i)
+        if (i < reps) f(i, keys[i], s0 + 64 * i + l < s1);
     };
     uint32_t prefix = 0;
     int need = m;  // slots still to be kept among the keys that share the prefix
@@ -365,12 +353,6 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
       movers += i < w ? part[i].z : 0;
       n_moves += part[i].z;
     }
-    int2* mv = moves + row * (S / 2);
-    auto stay = [&](int at) {
-      w_out[at] = w_in[at];
-      p_out[at] = pos_of(at);
-      src[at] = -1;
-    };
     e = eq0;
     each([&](int i, uint32_t k, bool valid) {
       const int at = s0 + 64 * i + l;
@@ -378,26 +360,22 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
       const bool hole = valid && at < m && !kept, mover = kept && at >= m;
       const uint64_t hs = __ballot(hole), ms = __ballot(mover);
       const int ih = holes + __popcll(hs & below), im = movers + __popcll(ms & below);
-      if (ITEMS) {
-        if (hole) list[0][ih] = (uint16_t)at;
-        if (mover) list[1][im] = (uint16_t)at;
-        const uint64_t st = __ballot(kept && at < m);
-        if (l == 0) stays[s0 / 64 + i] = st;
-      } else {
-        if (hole) mv[ih].y = at;
-        if (mover) mv[im].x = at;
-        if (kept && !mover) stay(at);
-      }
+      if (hole) list[0][ih] = (uint16_t)at;
+      if (mover) list[1][im] = (uint16_t)at;
+      const uint64_t st = __ballot(kept && at < m);
+      if (l == 0) stays[s0 / 64 + i] = st;
       holes += __popcll(hs);
       movers += __popcll(ms);
     });
     __syncthreads();
-    if (ITEMS) {  // the slots below m, over all threads
-      for (int i = t; i < m; i += kSel)
-        if (stays[i / 64] >> (i & 63) & 1) stay(i);
-    }
+    for (int i = t; i < m; i += kSel)  // over all threads, whichever wave the slots are
+      if (stays[i / 64] >> (i & 63) & 1) {
+        w_out[i] = w_in[i];
+        p_out[i] = pos_of(i);
+        src[i] = -1;
+      }
     for (int i = t; i < n_moves; i += kSel) {
-      const int x = ITEMS ? list[1][i] : mv[i].x, y = ITEMS ? list[0][i] : mv[i].y;
+      const int x = list[1][i], y = list[0][i];
       w_out[y] = w_in[x];
       p_out[y] = pos_of(x);
       src[y] = x;
@@ -411,6 +389,203 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
   if (t == 0) counts[row] = n_moves;
 }
 
+// ---------------------------------------------------------------------------
+// The select over several blocks per row, part `c` of `parts` each, for rows that do not fit
+// into one block or are too few to fill the device with one: a launch per histogram, every
+// block writing its own and, in the next launch, adding up the row's; then one that places.
+// With the counts of the parts before its own a block knows, slot by slot, how many kept
+// slots come before: a hole at slot s is the (s - before)-th, a mover the (before - kept
+// slots below m)-th.  (A pass whose digit settles the selection ends the histograms.)  Bound:
+// two to four reads of the row's weights and positions, 8 bytes a slot, and five launches: 256
+// rows of 100000 slots 402 us with the moved rows' reading back, 8 rows of 70000 44 us.  Holes
+// leave their number in `source`, movers their slot, position and
+// weight in a list, counted from its end (m - 1 - before), and the move kernel pairs them.
+// ---------------------------------------------------------------------------
+struct Found {        // after a pass
+  uint32_t prefix;    // of the key of the last kept slot
+  int need;           // slots still to be kept among those that share it; 0: all above it are kept, and no more
+  int same;           // how many share it
+  int before;         // kept slots of the row's parts before, by the digits so far
+};
+struct Mover {
+  int slot, pos;
+  float w;
+};
+struct Parts {
+  int Hkv;
+  int64_t S;
+  int max_pages;
+  const int32_t* __restrict__ seq_lens;
+  const float* weights;
+  float* weights_out;
+  const int32_t* pos;
+  int32_t* pos_out;
+  const int32_t* __restrict__ seen;
+  int budget, sink, recent;
+  int32_t* __restrict__ new_lens;
+  int32_t* __restrict__ counts;
+  Mover* __restrict__ movers;    // [row][S / 2]
+  int32_t* __restrict__ source;  // [row][S]
+  int2* __restrict__ hist;       // [row][part][3][kSel]
+  Found* __restrict__ found;     // [row][part][2]
+  int parts;
+};
+constexpr int kMaxParts = 16;
+
+// PASS 0 .. 2: histogram of that digit of the keys; 3: place.
+template <int PASS>
+__global__ __launch_bounds__(kSel) void kv4_evict_part_kernel(Parts a, int64_t row0) {
+  constexpr int kW = kSel / 64, kB = 4;
+  __shared__ int2 hist[kSel];
+  __shared__ int2 sums[kW];
+  __shared__ Found got;
+  __shared__ int got_same_before;
+  const int64_t row = row0 + blockIdx.x / a.parts;
+  const int c = (int)(blockIdx.x % a.parts), t = threadIdx.x, w = t >> 6, l = t & 63;
+  const int b = (int)(row / a.Hkv), h = (int)(row - (int64_t)b * a.Hkv);
+  const int n = min(max(a.seq_lens[b], 0), a.max_pages * kP), m = min(n, a.budget), seen = a.seen[b];
+  const float* w_in = a.weights + row * a.S;
+  const int32_t* p_in = a.pos + row * a.S;
+  float* w_out = a.weights_out + row * a.S;
+  int32_t* p_out = a.pos_out + row * a.S;
+  if (PASS < 3 && n <= a.budget) return;
+  // the wave's slots: [s0, s1), s0 + 64 i + lane for i < reps
+  const int reps = (int)(((int64_t)n + a.parts * kSel - 1) / (a.parts * kSel));
+  const int64_t first = ((int64_t)c * kW + w) * 64 * reps;
+  const int s0 = (int)min((int64_t)n, first), s1 = (int)min((int64_t)n, first + 64 * reps);
+  // f(slot, key, weight, position, valid) of the wave's slots in order
+  auto each = [&](auto&& f) {
+    for (int i0 = 0; i0 < reps && s0 + 64 * i0 < s1; i0 += kB) {
+      int p[kB];
+      float x[kB];
+#pragma unroll
+      for (int i = 0; i < kB; ++i) {
+        const int at = min(s0 + 64 * (i0 + i) + l, n - 1);
+        p[i] = p_in[at];
+        x[i] = w_in[at];
+      }
+#pragma unroll
+      for (int i = 0; i < kB; ++i) {
+        const int at = s0 + 64 * (i0 + i) + l, q = p[i] >= 0 ? p[i] : seen - (n - at);
+        f(at, rank_key(x[i], q < a.sink || q >= seen - a.recent), x[i], q, at < s1);
+      }
+    }
+  };
+  const int64_t part = row * a.parts + c;
+  if (PASS == 3) {
+    if (h == 0 && c == 0 && t == 0) a.new_lens[b] = m;
+    for (int64_t i = n + (int64_t)c * kSel + t; i < a.S; i += (int64_t)a.parts * kSel) {
+      w_out[i] = 0.0f;
+      p_out[i] = -1;
+    }
+    if (n <= a.budget) {
+      if (c == 0 && t == 0) a.counts[row] = 0;
+      each([&](int at, uint32_t, float x, int q, bool valid) {
+        if (!valid) return;
+        w_out[at] = x;
+        p_out[at] = q;
+      });
+      return;
+    }
+  }
+  Found f{0u, m, 0, 0};
+  int same_before = 0;
+  if (PASS > 1) f = a.found[part * 2 + PASS - 2];
+  if (PASS > 0 && f.need > 0) {  // the digit of the pass before
+    constexpr int kShift = PASS == 1 ? 21 : PASS == 2 ? 10 : 0;
+    int2 all = make_int2(0, 0), bef = make_int2(0, 0);  // digits 2047 - 2 t, 2046 - 2 t: of the row, of the parts before
+#pragma unroll 4
+    for (int k = 0; k < a.parts; ++k) {
+      const int2 x = a.hist[((row * a.parts + k) * 3 + PASS - 1) * kSel + t];
+      all.x += x.x;
+      all.y += x.y;
+      bef.x += k < c ? x.x : 0;
+      bef.y += k < c ? x.y : 0;
+    }
+    int above = wave_prefix(all.x + all.y), above_bef = wave_prefix(bef.x + bef.y);
+    if (l == 63) sums[w] = make_int2(above, above_bef);
+    __syncthreads();
+    above -= all.x + all.y;
+    above_bef -= bef.x + bef.y;
+#pragma unroll
+    for (int i = 0; i < kW; ++i) {
+      above += i < w ? sums[i].x : 0;
+      above_bef += i < w ? sums[i].y : 0;
+    }
+    auto set = [&](int digit, int ab, int ab_bef, int same, int same_bef) {
+      if (ab < f.need && ab + same >= f.need) {
+        got = Found{f.prefix | (uint32_t)digit << kShift, f.need - ab, same, f.before + ab_bef};
+        got_same_before = same_bef;
+      }
+    };
+    set(2047 - 2 * t, above, above_bef, all.x, bef.x);
+    set(2046 - 2 * t, above + all.x, above_bef + bef.x, all.y, bef.y);
+    __syncthreads();
+    f = got;
+    same_before = got_same_before;
+    if (f.same == f.need) {  // all of them are kept: those above prefix - 1, and the lower digits do not matter
+      f.prefix -= 1;
+      f.before += same_before;
+      f.need = same_before = 0;
+    }
+  }
+  if (PASS > 0 && PASS < 3) {
+    if (t == 0) a.found[part * 2 + PASS - 1] = f;
+    if (f.need == 0) return;
+  }
+  if (PASS < 3) {
+    constexpr int kShift = PASS == 0 ? 21 : PASS == 1 ? 10 : 0, kBits = PASS == 2 ? 10 : 11;
+    hist[t] = make_int2(0, 0);
+    __syncthreads();
+    each([&](int, uint32_t k, float, int, bool valid) {
+      if (valid && (PASS == 0 || (k >> ((kShift + kBits) & 31)) == (f.prefix >> ((kShift + kBits) & 31))))
+        atomicAdd(&reinterpret_cast<int*>(hist)[2047 - ((k >> kShift) & ((1u << kBits) - 1))], 1);
+    });
+    __syncthreads();
+    a.hist[(part * 3 + PASS) * kSel + t] = hist[t];
+    return;
+  }
+  // place: kept are the keys above the prefix and the first f.need slots of equal key
+  int more = 0, same = 0;
+  each([&](int, uint32_t k, float, int, bool valid) {
+    more += __popcll(__ballot(valid && k > f.prefix));
+    same += __popcll(__ballot(valid && k == f.prefix));
+  });
+  if (l == 0) sums[w] = make_int2(more, same);
+  __syncthreads();
+  more = f.before;
+  same = same_before;
+#pragma unroll
+  for (int i = 0; i < kW; ++i) {
+    more += i < w ? sums[i].x : 0;
+    same += i < w ? sums[i].y : 0;
+  }
+  Mover* movers = a.movers + row * (a.S / 2);
+  int32_t* src = a.source + row * a.S;
+  const uint64_t below = (1ull << l) - 1;
+  each([&](int at, uint32_t k, float x, int q, bool valid) {
+    const uint64_t gt = __ballot(valid && k > f.prefix), eq = __ballot(valid && k == f.prefix);
+    const int same_at = same + __popcll(eq & below);
+    const int before = more + __popcll(gt & below) + min(same_at, f.need);  // kept slots below this one
+    const bool kept = valid && (k > f.prefix || (k == f.prefix && same_at < f.need));
+    more += __popcll(gt);
+    same += __popcll(eq);
+    if (!valid) return;
+    if (at == m) a.counts[row] = m - before;
+    if (at < m) {
+      src[at] = kept ? -1 : -2 - (at - before);
+      if (kept) {
+        w_out[at] = x;
+        p_out[at] = q;
+      }
+    } else {
+      if (kept) movers[m - 1 - before] = Mover{at, q, x};
+      w_out[at] = 0.0f;
+      p_out[at] = -1;
+    }
+  });
+}
+
 // Rows that move into destination page blockIdx.x of row blockIdx.y, by source slot.
 // Fewer than kPageRows of them go one at a time, a wave each: 16 dwords of K codes, 64
 // bytes of V codes, 2 ng metadata entries.  More are put together in the page's own units: wave
@@ -421,17 +596,29 @@ __global__ __launch_bounds__(kSel) void kv4_evict_select_kernel(
 __global__ __launch_bounds__(256) void kv4_evict_move_kernel(uint8_t* __restrict__ pages, int Hkv, int64_t S,
                                                              int ng, const int32_t* __restrict__ block_table,
                                                              int max_pages, const int32_t* __restrict__ counts,
-                                                             const int32_t* __restrict__ source, int budget,
+                                                             const int32_t* __restrict__ source,
+                                                             const Mover* __restrict__ movers,
+                                                             float* __restrict__ weights_out,
+                                                             int32_t* __restrict__ pos_out, int budget,
                                                              int64_t row0) {
   __shared__ const uint8_t* from_all[4][kP];  // per wave, of a page's slots: the source's block
   __shared__ int src_all[4][kP];              // and its slot in it, or -1
   const int64_t row = row0 + blockIdx.y;
-  if (counts[row] == 0) return;  // then source is not written
+  const int n_moves = counts[row];
+  if (n_moves == 0) return;  // then source is not written
   const int b = (int)(row / Hkv), h = (int)(row - (int64_t)b * Hkv);
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lo = l & 15, hi = l >> 4;
   const int32_t* bt = block_table + (size_t)b * max_pages;
   const int slot = blockIdx.x * kP + l;
-  const int from = slot < budget ? source[row * S + slot] : -1;  // (moves: the row has more than budget slots)
+  int from = slot < budget ? source[row * S + slot] : -1;  // (moves: the row has more than budget slots)
+  if (from < -1) {  // hole -2 - from, of the select in parts
+    const Mover e = movers[row * (S / 2) + n_moves + 1 + from];
+    from = e.slot;
+    if (w == 0) {
+      weights_out[row * S + slot] = e.w;
+      pos_out[row * S + slot] = e.pos;
+    }
+  }
   const uint64_t moved = __ballot(from >= 0);
   if (!moved) return;
   const uint8_t* src = nullptr;
@@ -521,17 +708,29 @@ hipError_t launch_kv4_gather(const uint8_t* pages, int Hkv, const int64_t* slots
 }
 
 namespace {
-// Moves per row, their lists (hole, mover) where they do not fit into the select block's LDS,
-// and the source of every slot below the budget.
+// Parts of a row's select, or 0: in one block per row, which takes up to 32768 slots.  (Of
+// full tables in parts would be the faster way from 24000 slots on where rows are few, 8 rows
+// of 32000 slots 37 us for 46, of short sequences in such tables one block is.)  About one
+// part for each of 256 CUs: at two 64 rows of 49000 slots take 107 us for 93, since every block adds up
+// its row's histograms.  In one block each, keys formed anew in every pass, they took 140; 8
+// rows of 70000 slots 114 for 43.
+int evict_parts(int64_t rows, int64_t S) {
+  return S <= kSelLds ? 0 : (int)std::max<int64_t>(2, std::min<int64_t>(kMaxParts, 256 / rows));
+}
+// Moves per row, the source of every slot below the budget, and for a select in parts the
+// lists of movers, the histograms and what was found in them.
 struct EvictWs {
-  size_t moves_off, source_off, total;
+  size_t source_off, movers_off, hist_off, found_off, total;
 };
 EvictWs evict_ws(int Hkv, int B, int max_pages) {
   const size_t rows = (size_t)B * Hkv, S = (size_t)max_pages * kP;
+  const size_t parts = evict_parts(rows, S), many = parts ? rows : 0;
   EvictWs w;
-  w.moves_off = align256(rows * sizeof(int32_t));
-  w.source_off = align256(w.moves_off + (S <= kSelLds ? 0 : rows * (S / 2) * sizeof(int2)));
-  w.total = align256(w.source_off + rows * S * sizeof(int32_t));
+  w.source_off = align256(rows * sizeof(int32_t));
+  w.movers_off = align256(w.source_off + rows * S * sizeof(int32_t));
+  w.hist_off = align256(w.movers_off + many * (S / 2) * sizeof(Mover));
+  w.found_off = align256(w.hist_off + many * parts * 3 * kSel * sizeof(int2));
+  w.total = align256(w.found_off + many * parts * 2 * sizeof(Found));
   return w;
 }
 }  // namespace
@@ -543,18 +742,32 @@ hipError_t launch_kv4_evict(const EvictArgs& a, hipStream_t st) {
   const EvictWs ws = evict_ws(a.Hkv, a.B, a.max_pages);
   uint8_t* base = static_cast<uint8_t*>(a.ws);
   int32_t* counts = reinterpret_cast<int32_t*>(base);
-  int2* moves = reinterpret_cast<int2*>(base + ws.moves_off);
   int32_t* source = reinterpret_cast<int32_t*>(base + ws.source_off);
-  for (int64_t r0 = 0; r0 < rows; r0 += 1 << 20) {  // a launch holds fewer than 2^32 threads
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(rows - r0, 1 << 20)), dim3(kSel), 0, st,
-                         a.Hkv, S, a.max_pages, a.seq_lens, a.weights, a.weights_out, a.pos, a.pos_out, a.seen,
-                         a.budget, a.sink, a.recent, a.new_lens, counts, moves, source, r0);
-    };
-    if (S <= 4 * kSel) go(kv4_evict_select_kernel<4>);
-    else if (S <= 12 * kSel) go(kv4_evict_select_kernel<12>);
-    else if (S <= kSelLds) go(kv4_evict_select_kernel<32>);
-    else go(kv4_evict_select_kernel<0>);
+  Mover* movers = reinterpret_cast<Mover*>(base + ws.movers_off);
+  const int parts = evict_parts(rows, S);
+  const int64_t step = (1 << 20) / std::max(parts, 1);  // rows per launch, which holds fewer than 2^32 threads
+  for (int64_t r0 = 0; r0 < rows; r0 += step) {
+    const unsigned nr = (unsigned)std::min<int64_t>(rows - r0, step);
+    if (parts) {
+      const Parts p{a.Hkv, S, a.max_pages, a.seq_lens, a.weights, a.weights_out, a.pos, a.pos_out, a.seen,
+                    a.budget, a.sink, a.recent, a.new_lens, counts, movers, source,
+                    reinterpret_cast<int2*>(base + ws.hist_off), reinterpret_cast<Found*>(base + ws.found_off),
+                    parts};
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nr * parts), dim3(kSel), 0, st, p, r0); };
+      go(kv4_evict_part_kernel<0>);
+      go(kv4_evict_part_kernel<1>);
+      go(kv4_evict_part_kernel<2>);
+      go(kv4_evict_part_kernel<3>);
+    } else {
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(nr), dim3(kSel), 0, st, a.Hkv, S, a.max_pages, a.seq_lens, a.weights,
+                           a.weights_out, a.pos, a.pos_out, a.seen, a.budget, a.sink, a.recent, a.new_lens,
+                           counts, source, r0);
+      };
+      if (S <= 4 * kSel) go(kv4_evict_select_kernel<4>);
+      else if (S <= 12 * kSel) go(kv4_evict_select_kernel<12>);
+      else go(kv4_evict_select_kernel<32>);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -563,7 +776,7 @@ hipError_t launch_kv4_evict(const EvictArgs& a, hipStream_t st) {
   for (int64_t r0 = 0; r0 < rows; r0 += most) {
     hipLaunchKernelGGL(kv4_evict_move_kernel, dim3((unsigned)pages, (unsigned)std::min(rows - r0, most)),
                        dim3(256), 0, st, a.pages, a.Hkv, S, a.ng, a.block_table, a.max_pages, counts, source,
-                       a.budget, r0);
+                       movers, a.weights_out, a.pos_out, a.budget, r0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -287,3 +287,25 @@ def test_debug_checks(monkeypatch):
         with pytest.raises(ok.OscarError) as e:
             attend(lay, dev(pool), torch.zeros(2, 4, 128, dtype=torch.bfloat16, device="cuda"), dev(t), dev(n))
         assert e.value.status == ok.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("budget,sink,recent", ((1, 0, 0), (700, 4, 16), (9000, 0, 1), (19999, 30000, 5), (33000, 1, 1)))
+@pytest.mark.parametrize("kind", ("plain", "equal", "nan"))
+def test_select_in_parts(budget, sink, recent, kind):
+    """Tables of more slots than one block takes, with rows of any length in them."""
+    rng, lens, table, pool, weights, pos, lay = setup(budget, (33270, 0, 700, 20000, 1), 2, 128, mp=520)
+    if kind == "equal":
+        weights[:, :, : 15000] = np.float32(0.7)
+        weights[:, 1] = 3.0
+    elif kind == "nan":
+        weights[:, :, ::3] = np.nan
+        weights[:, :, 1::5] = -np.inf
+    pos[3, :, :9000] = rng.permutation(19000)[:9000]   # evicted before
+    seen = lens + np.int32(12000) * (np.arange(5) == 3).astype(np.int32)
+    check(lay, lens, table, pool, weights, pos, seen, budget, sink, recent, 128, in_place=(kind == "plain",))
+
+
+def test_many_rows_in_parts():
+    """So many rows that a row's select is of two parts only."""
+    rng, lens, table, pool, weights, pos, lay = setup(11, [66 + i % 70 for i in range(300)], 2, 128, mp=520)
+    check(lay, lens, table, pool, weights, pos, lens, 66, 1, 8, 128, in_place=(True,))
