@@ -28,13 +28,16 @@ __device__ inline float value_of(uint32_t x, int sh, float2 m) { return m.x * ((
 // and head against 128 + 8 ng read).
 //
 // Row by row (half a wave per tensor, 4 channels a lane) a V row is 64 single bytes of 8
-// cache lines.  Calls of 64 tokens or more take tiles of 64 tokens, one block per (tile,
-// head): the tile's slots are grouped by page, and of a page with kPageRows members or
-// more the block reads the whole page-head block in its 16-byte units, a quarter per
+// cache lines.  Calls of more than kRowsMost rows take tiles of 64 tokens, one block per
+// (tile, head): the tile's slots are grouped by page, and of a page with kPageRows members
+// or more the block reads the whole page-head block in its 16-byte units, a quarter per
 // wave, and stores the members' rows from registers; rows of other pages go one by one.
+// Row by row against tiles, 8 heads: 1000 tokens in order 6.1 us against 6.9, 2048 8.0
+// against 7.2, 4200 13.2 against 10.2; of as many pages (a step's new tokens) 97 tokens 6.2
+// against 20, 4200 15 against 25, 131072 513 against 705.
 // 131072 tokens x 8 heads, fp32 (1.24 GB): 539 us row by row, 217 us (5.7 TB/s) by tiles
 // at three waves per SIMD; at eight, whose half-written output lines do not fit the L2,
-// 307, at two 245, with non-temporal stores 450.  2103 tokens: 8.8 us, row by row 9.0.
+// 307, at two 245, with non-temporal stores 450.
 // ---------------------------------------------------------------------------
 struct GatherArgs {
   const uint8_t* pages;
@@ -59,25 +62,32 @@ __device__ inline void put1(void* out, size_t at, float x) {
   else static_cast<uint16_t*>(out)[at] = bf16_rne(x);
 }
 
-// One row by one wave: lanes 0 .. 31 K, 32 .. 63 V.
-template <bool F32>
-__device__ inline void gather_row(const GatherArgs& a, int64_t tok, int h, int64_t slot, int l) {
+// One row by one wave: lanes 0 .. 31 K, 32 .. 63 V, channels 4 (l % 32) ..
+struct RowPart {
+  uint32_t codes, meta;  // codes: value i in nibble i of the lane's order
+};
+__device__ inline RowPart load_row(const GatherArgs& a, int h, int64_t slot, int l) {
   const int c = l & 31, is_v = l >> 5;
   const int64_t page = slot / kP;
   const int t = (int)(slot - page * kP);
   const uint8_t* blk = a.pages + ((size_t)page * a.Hkv + h) * kv4_block_bytes(a.ng);
-  const float2 m = meta_of(*reinterpret_cast<const uint32_t*>(blk + kv4_sz_off(a.ng, is_v) +
-                                                              (t * a.ng + c * a.ng / 32) * 4), a.meta_bf16);
-  const size_t at = ((size_t)tok * a.Hkv + h) * kD + 4 * c;
+  RowPart r;
+  r.meta = *reinterpret_cast<const uint32_t*>(blk + kv4_sz_off(a.ng, is_v) + (t * a.ng + c * a.ng / 32) * 4);
   if (is_v) {
     const uint8_t* b = blk + kv4_v_off(4 * c - 16 * (c >> 2 & 1), t);
-    const int sh = c & 4;
-    put4<F32>(a.v, at, value_of(b[0], sh, m), value_of(b[16], sh, m), value_of(b[32], sh, m),
-              value_of(b[48], sh, m));
+    r.codes = (b[0] | (uint32_t)b[16] << 8 | (uint32_t)b[32] << 16 | (uint32_t)b[48] << 24) >> (c & 4);
   } else {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + kv4_k_off(4 * c, t)) >> (8 * (c & 1));
-    put4<F32>(a.k, at, value_of(w, 0, m), value_of(w, 16, m), value_of(w, 4, m), value_of(w, 20, m));
+    r.codes = *reinterpret_cast<const uint32_t*>(blk + kv4_k_off(4 * c, t)) >> (8 * (c & 1));
   }
+  return r;
+}
+template <bool F32>
+__device__ inline void store_row(const GatherArgs& a, int64_t tok, int h, int l, const RowPart& r) {
+  const size_t at = ((size_t)tok * a.Hkv + h) * kD + 4 * (l & 31);
+  const float2 m = meta_of(r.meta, a.meta_bf16);
+  const uint32_t x = r.codes;
+  if (l >> 5) put4<F32>(a.v, at, value_of(x, 0, m), value_of(x, 8, m), value_of(x, 16, m), value_of(x, 24, m));
+  else put4<F32>(a.k, at, value_of(x, 0, m), value_of(x, 16, m), value_of(x, 4, m), value_of(x, 20, m));
 }
 
 template <bool F32>
@@ -85,10 +95,13 @@ __global__ __launch_bounds__(256) void kv4_gather_rows_kernel(GatherArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= a.n_tok * a.Hkv) return;
   const int64_t tok = row / a.Hkv, slot = a.slots[tok];
-  if (slot >= 0) gather_row<F32>(a, tok, (int)(row - tok * a.Hkv), slot, threadIdx.x & 63);
+  const int h = (int)(row - tok * a.Hkv), l = threadIdx.x & 63;
+  if (slot >= 0) store_row<F32>(a, tok, h, l, load_row(a, h, slot, l));
 }
 
-constexpr int kPageRows = 8;  // members of a page from which on it is read whole
+constexpr int kRowsMost = 12 << 10;  // (token, head) rows up to which they are read one by one
+constexpr int kPageRows = 8;        // members of a page from which on it is read whole
+constexpr int kSmallPages = 8;      // pages with fewer after which the rest of a tile is read row by row
 
 template <bool F32>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void kv4_gather_kernel(GatherArgs a) {
@@ -106,7 +119,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
   const int64_t slot = tok0 + l < a.n_tok ? a.slots[tok0 + l] : -1;
   const int64_t page = slot >= 0 ? slot / kP : -1;
   const int t = (int)(slot - page * kP);
-  uint64_t open = __ballot(slot >= 0);
+  uint64_t open = __ballot(slot >= 0), loose = 0;
+  int small = 0;  // pages of fewer members
   while (open) {  // one page per turn, the same in the four waves
     const int first = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)open) - 1);
     const int64_t p = ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(page >> 32), first) << 32) |
@@ -114,12 +128,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
     const bool member = (open >> l & 1) && page == p;
     const uint64_t members = __ballot(member);
     if (__popcll(members) < kPageRows) {
-      int n = 0;
-      for (uint64_t left = members; left; left &= left - 1, ++n) {
-        const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)left) - 1);
-        if ((n & 3) == w) gather_row<F32>(a, tok0 + i, h, p * kP + __builtin_amdgcn_readlane(t, i), l);
-      }
-      open &= ~members;
+      const uint64_t rest = ++small < kSmallPages ? members : open;  // (then the others hardly have more)
+      loose |= rest;
+      open &= ~rest;
       continue;
     }
     // the wave's quarter, whole rows: K of slots 16 w .. + 15 (lane: slot 16 w + l / 4,
@@ -167,6 +178,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       put1<F32>(a.v, at, value_of(b, 0, m));
       put1<F32>(a.v, at + 16, value_of(b, 4, m));
     }
+  }
+  // rows of the other pages: every fourth token of the tile, four at a time
+  for (uint64_t mine = loose & (0x1111111111111111ull << w); mine;) {
+    int tok[4];
+    RowPart r[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k, mine &= mine - 1) {
+      tok[k] = __builtin_amdgcn_readfirstlane(mine ? __ffsll((unsigned long long)mine) - 1 : -1);
+      if (tok[k] < 0) continue;
+      const int64_t at = ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(slot >> 32), tok[k]) << 32) |
+                         (uint32_t)__builtin_amdgcn_readlane((int)slot, tok[k]);
+      r[k] = load_row(a, h, at, l);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (tok[k] >= 0) store_row<F32>(a, tok0 + tok[k], h, l, r[k]);
   }
 }
 
@@ -692,9 +719,10 @@ hipError_t launch_kv4_gather(const uint8_t* pages, int Hkv, const int64_t* slots
     const int64_t n = std::min(most, n_tok - t0), at = t0 * Hkv * kD * (out_f32 ? 4 : 2);
     const GatherArgs a{pages, Hkv, slots + t0, n, static_cast<char*>(k) + at, static_cast<char*>(v) + at,
                        meta_bf16, ng};
-    const int64_t blocks = n < 64 ? (n * Hkv + 3) / 4 : (n + 511) / 512 * 8 * Hkv;
+    const bool by_row = n * Hkv <= kRowsMost;
+    const int64_t blocks = by_row ? (n * Hkv + 3) / 4 : (n + 511) / 512 * 8 * Hkv;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
-    if (n < 64) {
+    if (by_row) {
       if (out_f32) go(kv4_gather_rows_kernel<true>);
       else go(kv4_gather_rows_kernel<false>);
     } else {

@@ -168,3 +168,46 @@ def test_debug_checks(monkeypatch):
         with pytest.raises(ok.OscarError) as e:
             call()
         assert e.value.status == ok.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("name", FORMATS)
+@pytest.mark.parametrize("kind", ("pages", "scattered", "short runs", "twice"))
+def test_gather_by_tiles(name, kind):
+    """Calls of more than 12288 rows, which read whole pages where a tile of tokens has
+    several of one."""
+    fmt = FORMATS[name]
+    rng = np.random.default_rng(13)
+    Hkv, pages = 40, 60
+    lay = layout(Hkv, pages, fmt)
+    pool = R.random_pool(rng, pages, Hkv, fmt[0], fmt[1])
+    every = np.arange(pages * 64)
+    slots = {"pages": np.concatenate([p * 64 + np.arange(64) for p in rng.permutation(pages)])[: 64 * 13 + 5],
+             "scattered": rng.permutation(every)[:777],
+             "short runs": np.concatenate([p * 64 + 11 + np.arange(3 + p % 11) for p in range(pages)] * 2),
+             "twice": np.concatenate([np.arange(64, 100), np.arange(80, 120), [64] * 12, [-1] * 3, every[::5]])}[kind]
+    assert len(slots) * Hkv > 12288
+    for dtype in (torch.float32, torch.bfloat16):
+        k, v = gathered(lay, dev(pool), slots, dtype)
+        blocks = pool.reshape(pages, Hkv, -1)
+        for out, is_v in ((k, 0), (v, 1)):
+            vals = torch.from_numpy(R.block_values(blocks, fmt[0], fmt[1], is_v))
+            want = vals.permute(0, 2, 1, 3).reshape(pages * 64, Hkv, 128)[np.maximum(slots, 0)].to(dtype)
+            want[slots < 0] = 7.0
+            assert torch.equal(out.cpu(), want)
+
+
+def test_gather_by_tiles_past_4_gib():
+    rng = np.random.default_rng(14)
+    Hkv = 8
+    lay = ok.Layout(Hkv, 54000)
+    pool = torch.empty(ok.kv4_pool_bytes(lay), dtype=torch.uint8, device="cuda")
+    ends = R.random_pool(rng, 2, Hkv, 32, 0)
+    for i, p in enumerate((30000, 53999)):
+        pool[p * ok.kv4_page_bytes(lay):(p + 1) * ok.kv4_page_bytes(lay)] = dev(ends[i * ok.kv4_page_bytes(lay):(i + 1) * ok.kv4_page_bytes(lay)])
+    runs = np.concatenate([53999 * 64 + np.arange(64), 30000 * 64 + np.arange(3), [53999 * 64 + 5], 30000 * 64 + np.arange(60)])
+    slots = np.concatenate([runs] * 32)
+    got = gathered(lay, pool, slots, torch.float32)
+    page = np.where(slots // 64 == 53999, 1, 0)
+    for out, is_v in zip(got, (0, 1)):
+        vals = R.block_values(ends.reshape(2, Hkv, -1), 32, 0, is_v)
+        assert np.array_equal(out.cpu().numpy(), vals[page, :, slots % 64])
