@@ -467,6 +467,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       for (int q = 0; q < NG; ++q) {
         if (NCH > 1) {  // (a group ahead the wide instances would spill)
           __builtin_amdgcn_sched_barrier(0);
+          lane_exchange();  // the last group's reads come before this one's weights
           stage(q);
         }
         lane_exchange();
