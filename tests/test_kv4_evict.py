@@ -309,3 +309,41 @@ def test_many_rows_in_parts():
     """So many rows that a row's select is of two parts only."""
     rng, lens, table, pool, weights, pos, lay = setup(11, [66 + i % 70 for i in range(300)], 2, 128, mp=520)
     check(lay, lens, table, pool, weights, pos, lens, 66, 1, 8, 128, in_place=(True,))
+
+
+def test_parts_captured_and_two_at_once():
+    """The select in parts from a captured graph, replayed, and in two calls on two streams."""
+    rng, lens, table, pool, weights, pos, lay = setup(15, (20000, 700, 33000), 2, 128, mp=520)
+    t, ln, ps = dev(table), dev(lens), dev(pos)
+
+    def buffers():
+        return dict(p=dev(pool), w=dev(weights), w2=torch.zeros_like(ps, dtype=torch.float32), p2=torch.zeros_like(ps),
+                    new=torch.zeros(3, dtype=torch.int32, device="cuda"), ws=ok.kv4_alloc_evict_workspace(lay, 3, 520))
+
+    def call(b):
+        ok.kv4_evict(lay, b["p"], t, ln, b["w"], ps, ln, 3000, 4, 100, b["new"], b["ws"], weights_out=b["w2"],
+                     pos_out=b["p2"])
+    x, y = buffers(), buffers()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(x)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(x)
+    for i in range(4):
+        w = np.exp(2 * rng.standard_normal(weights.shape)).astype(np.float32)
+        for b in (x, y):
+            b["w"].copy_(dev(w))
+            b["p"].copy_(dev(pool))
+        side.wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        with torch.cuda.stream(side):
+            call(y)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        want = R.evict(pool, 2, 128, table, lens, w, pos, lens, 3000, 4, 100) if i == 0 else None
+        for name, j in (("p", 0), ("w2", 1), ("p2", 2), ("new", 3)):
+            assert torch.equal(x[name], y[name]), (i, name)
+            assert want is None or np.array_equal(x[name].cpu().numpy(), want[j]), name
