@@ -34,7 +34,7 @@ __device__ inline float value_of(uint32_t x, int sh, float2 m) { return m.x * ((
 // wave, and stores the members' rows from registers; rows of other pages go one by one.
 // Row by row against tiles, 8 heads: 1000 tokens in order 6.1 us against 6.9, 2048 8.0
 // against 7.2, 4200 13.2 against 10.2; of as many pages (a step's new tokens) 97 tokens 6.2
-// against 20, 4200 15 against 25, 131072 513 against 705.
+// against 20, 4200 15 against 25, 131072 513 against 646.
 // 131072 tokens x 8 heads, fp32 (1.24 GB): 539 us row by row, 217 us (5.7 TB/s) by tiles
 // at three waves per SIMD; at eight, whose half-written output lines do not fit the L2,
 // 307, at two 245, with non-temporal stores 450.
@@ -179,21 +179,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       put1<F32>(a.v, at + 16, value_of(b, 4, m));
     }
   }
-  // rows of the other pages: every fourth token of the tile, four at a time
-  for (uint64_t mine = loose & (0x1111111111111111ull << w); mine;) {
-    int tok[4];
-    RowPart r[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k, mine &= mine - 1) {
-      tok[k] = __builtin_amdgcn_readfirstlane(mine ? __ffsll((unsigned long long)mine) - 1 : -1);
-      if (tok[k] < 0) continue;
-      const int64_t at = ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(slot >> 32), tok[k]) << 32) |
-                         (uint32_t)__builtin_amdgcn_readlane((int)slot, tok[k]);
-      r[k] = load_row(a, h, at, l);
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (tok[k] >= 0) store_row<F32>(a, tok0 + tok[k], h, l, r[k]);
+  // rows of the other pages: every fourth token of the tile (four at a time, whose
+  // half-written lines leave the L2: 131072 tokens of as many pages 712 us for 646)
+  for (uint64_t mine = loose & (0x1111111111111111ull << w); mine; mine &= mine - 1) {
+    const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)mine) - 1);
+    const int64_t at = ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(slot >> 32), i) << 32) |
+                       (uint32_t)__builtin_amdgcn_readlane((int)slot, i);
+    store_row<F32>(a, tok0 + i, h, l, load_row(a, h, at, l));
   }
 }
 
