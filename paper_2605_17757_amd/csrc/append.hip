@@ -853,27 +853,27 @@ __device__ inline void rotate_wave(const float4 (&Rs)[kD][kD / 4], const uint32_
 template <class Rows, bool DEF, int BITS = 2>
 __global__ __launch_bounds__(kBulkWaves * 64) void append_bulk_kernel(
     uint8_t* __restrict__ pages, Rows rows, const float* __restrict__ Rk,
-    const float* __restrict__ Rv, float clip_k, float clip_v, QFmt fmt_arg) {
+    const float* __restrict__ Rv, float clip_k, float clip_v, QFmt fmt_arg, int k_blocks) {
   __shared__ float4 Rs[kD][kD / 4];                                  // 64 KB
   __shared__ uint32_t area_all[kBulkWaves][kItemRows * kHalfPitch];  // 68 KB
   __shared__ int taken;
   const QFmt fmt = pick(DEF, fmt_arg);
-  const int is_v = blockIdx.y, bx = blockIdx.x, gx = gridDim.x, Hkv = rows.Hkv;
+  const int is_v = blockIdx.x >= k_blocks, bx = is_v ? blockIdx.x - k_blocks : blockIdx.x;
+  const int gx = is_v ? gridDim.x - k_blocks : k_blocks, Hkv = rows.Hkv;
   const float* __restrict__ R = is_v ? Rv : Rk;  // nullptr: identity
   const float clip = is_v ? clip_v : clip_k;
   const int t = threadIdx.x, w = t >> 6, l = t & 63, kq = l >> 4, j = l & 15;
   if (R) stage_rot<kBulkWaves>(Rs, R + (fmt.rph ? (size_t)(bx % Hkv) * kD * kD : 0), t);  // gx: a multiple of Hkv
-  if (t == 0) taken = 0;
+  if (t == 0) taken = kBulkWaves;
   __syncthreads();
   uint32_t* area = area_all[w];
   float* xt = reinterpret_cast<float*>(area);
   const int groups = (rows.n_tok + kItemRows - 1) / kItemRows;
   const int n_items = groups * Hkv, n_mine = (n_items - bx + gx - 1) / gx;
-  for (;;) {
-    int n = 0;
-    if (l == 0) n = atomicAdd(&taken, 1);
-    n = __builtin_amdgcn_readfirstlane(n);
-    if (n >= n_mine) break;
+  // A wave's first item is the w-th, so that few items go to all four SIMDs (waves 0, 1, ..
+  // run on one after the other; with the first items taken in the order of arrival 700
+  // tokens x 8 heads, 3 items per block, took up to 31 us for 15), the next ones whoever is done.
+  for (int n = __builtin_amdgcn_readfirstlane(w); n < n_mine;) {
     const int item = bx + n * gx, tok0 = item / Hkv * kItemRows, h = item % Hkv;
     // rows of the item: lane l their channels 2 l, 2 l + 1; destination of row l % 16
     uint32_t row[kItemRows];
@@ -927,6 +927,8 @@ __global__ __launch_bounds__(kBulkWaves * 64) void append_bulk_kernel(
       }
     }
     store_slice32<BITS>(pages, Hkv, h, shfl64(to.slot, rr), is_v, clip, fmt, x, q);
+    if (l == 0) n = atomicAdd(&taken, 1);
+    n = __builtin_amdgcn_readfirstlane(n);
   }
 }
 
@@ -1276,19 +1278,31 @@ bool is_default(const QFmt& f) { return f.bf16 == 0 && f.quantile == 0 && f.ng =
 template <int BITS = 2, class Rows>
 hipError_t launch_rows(void* pages, const Rows& rows, const float* Rk, const float* Rv,
                        float clip_k, float clip_v, QFmt fmt, hipStream_t st) {
-  auto go = [&](auto kernel, int blocks, int waves) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, 2), dim3(waves * 64), 0, st,
-                       static_cast<uint8_t*>(pages), rows, Rk, Rv, clip_k, clip_v, fmt);
-  };
   const bool def = is_default(fmt);
   const int64_t items = append_items(rows.n_tok, rows.Hkv);
   if (items <= device_cus()) {
-    if (def) go(append_kernel<Rows, true, BITS>, (int)items, kRotWaves);
-    else go(append_kernel<Rows, false, BITS>, (int)items, kRotWaves);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)items, 2), dim3(kRotWaves * 64), 0, st,
+                         static_cast<uint8_t*>(pages), rows, Rk, Rv, clip_k, clip_v, fmt);
+    };
+    if (def) go(append_kernel<Rows, true, BITS>);
+    else go(append_kernel<Rows, false, BITS>);
   } else {
-    const int blocks = append_blocks(items, rows.Hkv, fmt.rph, device_cus() / 2);
-    if (def) go(append_bulk_kernel<Rows, true, BITS>, blocks, kBulkWaves);
-    else go(append_bulk_kernel<Rows, false, BITS>, blocks, kBulkWaves);
+    // One block per CU, halved between K and V.  Of a rotated and an unrotated tensor the
+    // first gets three quarters, as its items take about three times as long (131072 tokens
+    // x 8 heads, R_v NULL: 1137 us in halves, 770; with 13 of 16 parts 716, but by the
+    // quantile rule, which costs the unrotated rows as much, 1287 for 972 and 1432 in halves).
+    auto blocks_of = [&](bool rotated, bool other) {
+      const int64_t cus = device_cus();
+      return append_blocks(items, rows.Hkv, fmt.rph, rotated == other ? cus / 2 : rotated ? cus * 3 / 4 : cus / 4);
+    };
+    const int kb = blocks_of(Rk, Rv), vb = blocks_of(Rv, Rk);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(kb + vb)), dim3(kBulkWaves * 64), 0, st,
+                         static_cast<uint8_t*>(pages), rows, Rk, Rv, clip_k, clip_v, fmt, kb);
+    };
+    if (def) go(append_bulk_kernel<Rows, true, BITS>);
+    else go(append_bulk_kernel<Rows, false, BITS>);
   }
   return hipGetLastError();
 }
