@@ -624,14 +624,14 @@ __device__ inline void append_body(RotSmem& sm, int is_v, int bx, int gx,
 // Bound: the fp64 matrix core, 16,384 of a SIMD's cycles per item: 74 % busy over a
 // prompt of 131072 tokens, 37 % where a wave has 1.6 items in the token-quantile format.
 // With four waves per SIMD at different points of their items, the rest of an item (980
-// vector instructions beside its 256 products, 2,570 with the token quantile, and the
+// vector instructions beside its 256 products, 2,200 with the token quantile, and the
 // dependent loads that route its rows) runs while other waves' products do.  At the 128
 // registers of 16 waves the instances keep 12 to 44 bytes per lane in scratch.  The quantizer has the most
 // work per lane here (32 channels), which costs the fewest instructions; 32 lanes a
 // row, as in store_rows, took 1,700 and 7,000.  131072 tokens x 8 heads: 1474 us with
 // two waves per SIMD, IEEE divisions per code and the routing loads in front of each
 // item's products, 1156 us now (1092 without the stores); 6408 tokens x 8 heads in the
-// token-quantile format: 288 -> 89 us.
+// token-quantile format: 288 -> 89 us, then, on another card, 96 -> 91.
 // ---------------------------------------------------------------------------
 constexpr int kBulkWaves = 16;
 constexpr int kStagePitch = 66;  // dwords per staged bf16 row (8-byte reads of 16 rows: all banks)
@@ -664,8 +664,10 @@ __device__ inline int quad_sum(int v) {
 // Token quantile of 16 rows at once in the quad-lane layout; rmax: the row's
 // largest |x~|.  Bisection over the bit patterns of |x~| (positive floats order
 // like their bits) for a threshold t with exactly k + 1 values at or below it,
-// which ends as soon as t separates a_k from a_{k+1} (about 17 of the 31 halvings
-// on Gaussian rows); equal values run it down to the smallest t with at least k + 1.
+// which ends as soon as t separates a_k from a_{k+1}; equal values run it down to the
+// smallest t with at least k + 1.  The first t is rmax / 4, which a clipping quantile is
+// nearly always above (131072 tokens x 8 heads, 4 bits: 1452 us starting in the middle of
+// all bit patterns, 1374 now).
 __device__ inline float token_quantile_quad(const float (&x)[32], float rmax, float rho) {
   int k;
   float f;
@@ -679,16 +681,16 @@ __device__ inline float token_quantile_quad(const float (&x)[32], float rmax, fl
     return quad_sum(c);
   };
   // smallest t with count >= k + 1 in [lo, hi]; n = count at hi
-  uint32_t lo = 0, hi = __float_as_uint(rmax);
+  uint32_t lo = 0, hi = __float_as_uint(rmax), mid = hi - min(hi, 2u << 23);
   int n = kD;
   while (__any(lo < hi && n != k + 1)) {
-    const uint32_t mid = lo + ((hi - lo) >> 1);
     const int c = count_le(mid);
     const bool open = lo < hi && n != k + 1;
     const bool up = open && c < k + 1, down = open && c >= k + 1;
     lo = up ? mid + 1 : lo;
     hi = down ? mid : hi;
     n = down ? c : n;
+    mid = lo + ((hi - lo) >> 1);
   }
   const float t = __uint_as_float(hi);
   float ak = 0.0f, ak1 = INFINITY;  // largest value at or below t, smallest above
