@@ -612,10 +612,11 @@ __device__ inline void append_body(RotSmem& sm, int is_v, int bx, int gx,
 
 // ---------------------------------------------------------------------------
 // Bulk cache update (more items than teams of 8 waves fit on the GPU): one
-// persistent block of 16 independent waves per CU, half of the blocks per tensor.  A
-// wave takes an item at a time from the block's list (a counter in LDS: the oldest
-// wave of a SIMD issues first and would be done early with a fixed share), stages
-// its rows as bf16, rotates them over all eight column tiles and quantizes them in
+// persistent block of 16 independent waves per CU, half of the blocks per tensor where
+// both or none are rotated.  A wave takes the w-th item, then one at a time from the rest
+// of the block's list (a counter in LDS: the oldest wave of a SIMD issues first and would
+// be done early with a fixed share), stages its rows as bf16, rotates them over all eight
+// column tiles and quantizes them in
 // the quad-lane layout.  The products are as in rotate16; tile t holds channels
 // 64 (t / 4) + 4 j + t % 4 (j = column), so that a lane's B values are two 16-byte
 // reads of the fp32 R in LDS, and x~ goes through the wave's 4 KB area one channel

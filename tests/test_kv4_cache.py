@@ -211,3 +211,18 @@ def test_gather_by_tiles_past_4_gib():
     for out, is_v in zip(got, (0, 1)):
         vals = R.block_values(ends.reshape(2, Hkv, -1), 32, 0, is_v)
         assert np.array_equal(out.cpu().numpy(), vals[page, :, slots % 64])
+
+
+@pytest.mark.parametrize("n,Hkv", ((530, 8), (1700, 3)))   # just past the small kernel's calls, and several items a wave
+@pytest.mark.parametrize("rot", ("identity_k", "per_head_k", "per_head_v"))
+def test_append_one_rotated_tensor(n, Hkv, rot):
+    """Longer calls of which one tensor is rotated: the blocks are shared out unevenly."""
+    rng = np.random.default_rng(n)
+    pages = -(-n // 64) + 2
+    slots = rng.permutation(pages * 64)[:n]
+    slots[::11] = -1
+    per = np.stack([R.rotation(rng) for _ in range(Hkv)])
+    Rk, Rv = {"identity_k": (None, per[0]), "per_head_k": (per, None), "per_head_v": (None, per)}[rot]
+    for name in FORMATS:
+        check_append(FORMATS[name], Hkv, rows(rng, n, Hkv), rows(rng, n, Hkv), slots, pages, Rk, Rv, 0.97, 0.97,
+                     int(rot != "identity_k"))
