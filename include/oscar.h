@@ -19,6 +19,8 @@
  *   - Pointers named in the argument lists are DEVICE pointers unless marked
  *     "host".  The caller owns and allocates every buffer: pages, inputs,
  *     rotation matrices, workspace and output.  The library never allocates.
+ *   - An array that a call writes shares no bytes with its other arguments, unless an
+ *     entry point says so.
  *   - Calls are asynchronous on `stream` (a hipStream_t passed as void*; NULL
  *     is the default stream).  OSCAR_OK means "validated and launched".
  *     OSCAR_ERR_HIP reports a launch error (hipGetLastError right after the
@@ -468,11 +470,12 @@ int oscar_kv4_decode_step(const oscar_layout *L, void *pages, const void *k_new,
  * at most 2^30, and max_pages_per_seq * Hkv at most 2^27, here and with weights.
  *   weights, weights_out : fp32 [B, Hkv, max_pages_per_seq * P] (oscar_kv4_decode_attn's)
  *   pos, pos_out         : int32, same shape; before the first eviction all -1
- *       each _out the same array as its input or disjoint from it
+ *       each _out may be its input itself; apart from that no array that the call writes
+ *       (pages, weights_out, pos_out, new_lens, workspace) shares bytes with another
  *   num_seen             : int32 [B], tokens of the sequence so far, evicted ones too
  *       (>= seq_lens[b])
  *   budget >= 1, sink >= 0, recent >= 0
- *   new_lens             : int32 [B], disjoint from seq_lens
+ *   new_lens             : int32 [B]
  *   workspace            : >= oscar_kv4_evict_workspace_bytes(L, B, max_pages_per_seq)
  *       bytes, 256-byte aligned, contents need no initialization
  */

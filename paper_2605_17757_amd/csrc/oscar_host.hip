@@ -604,6 +604,15 @@ bool partly_shared(const void* a, const void* b, size_t bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x != y && (x < y ? y - x : x - y) < bytes;
 }
+// One array of a call.
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+bool share_bytes(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return x < y ? y - x < a.bytes : x - y < b.bytes;
+}
 size_t kv4_slots_bytes(const oscar_layout* L, int32_t B, int32_t max_pages) {
   return (size_t)B * L->num_kv_heads * max_pages * (size_t)L->page_size * sizeof(float);
 }
@@ -781,15 +790,33 @@ int oscar_kv4_evict(const oscar_layout* L, void* pages, int32_t B, const int32_t
   if (!pages || !block_table || !seq_lens || !weights || !weights_out || !pos || !pos_out || !num_seen ||
       !new_lens || !workspace || new_lens == seq_lens)
     return OSCAR_ERR_INVALID_ARG;
-  const size_t slots = kv4_slots_bytes(L, B, max_pages_per_seq);
+  const size_t slots = kv4_slots_bytes(L, B, max_pages_per_seq), per_seq = (size_t)B * sizeof(int32_t);
   if (partly_shared(weights, weights_out, slots) || partly_shared(pos, pos_out, slots) ||
-      partly_shared(new_lens, seq_lens, (size_t)B * sizeof(int32_t)))
+      partly_shared(new_lens, seq_lens, per_seq))
     return OSCAR_ERR_INVALID_ARG;
   if (!aligned(pages, 16) || !aligned(weights, 16) || !aligned(weights_out, 16) || !aligned(pos, 16) ||
       !aligned(pos_out, 16) || !aligned(workspace, 256))
     return OSCAR_ERR_INVALID_ARG;
-  if (workspace_bytes < kv4_evict_ws_bytes(L->num_kv_heads, B, max_pages_per_seq))
-    return OSCAR_ERR_WORKSPACE_TOO_SMALL;
+  const size_t ws_bytes = kv4_evict_ws_bytes(L->num_kv_heads, B, max_pages_per_seq);
+  if (workspace_bytes < ws_bytes) return OSCAR_ERR_WORKSPACE_TOO_SMALL;
+  // The blocks of a launch write while others read: no array that is written may share
+  // bytes with another, but for weights_out and pos_out in place.  (The first five are
+  // written.)
+  const Span spans[] = {{pages, oscar_kv4_pool_bytes(L)},
+                        {weights_out, slots},
+                        {pos_out, slots},
+                        {new_lens, per_seq},
+                        {workspace, ws_bytes},
+                        {block_table, per_seq * (size_t)max_pages_per_seq},
+                        {seq_lens, per_seq},
+                        {num_seen, per_seq},
+                        {weights, slots},
+                        {pos, slots}};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < 10; ++j) {
+      const bool in_place = ((i == 1 && j == 8) || (i == 2 && j == 9)) && spans[i].at == spans[j].at;
+      if (i != j && !in_place && share_bytes(spans[i], spans[j])) return OSCAR_ERR_INVALID_ARG;
+    }
   st = debug_check(L, stream, B, block_table, max_pages_per_seq, seq_lens, nullptr, 0, nullptr, 0);
   if (st) return st;
   EvictArgs a;
