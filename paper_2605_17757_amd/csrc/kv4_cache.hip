@@ -151,9 +151,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
     idx[l] = -1;
     vsz[l] = zv;
     lane_exchange();
-    if (member) idx[t] = l;
+    // Of tokens of the same slot the last one goes first and the others wait.  (The waves
+    // must take the same one, as each stores its part of the row, and which of several
+    // stores to one LDS word remains is not defined: a maximum is.)
+    if (member) atomicMax(&idx[t], l);
     lane_exchange();
-    open &= ~__ballot(member && idx[t] == l);  // of a slot that comes twice the other token waits
+    open &= ~__ballot(member && idx[t] == l);
     if (const int i = idx[tk]; i >= 0) {
       const size_t at = ((size_t)(tok0 + i) * a.Hkv + h) * kD + 8 * c8;
       const uint32_t d[4] = {kr.x, kr.y, kr.z, kr.w};
