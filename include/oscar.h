@@ -421,6 +421,8 @@ size_t oscar_kv4_decode_workspace_bytes(const oscar_layout *L, int32_t B, int32_
  * num_splits as there, 0 for the default).  q~, the softmax weights and the codes enter
  * the matrix cores with all their bits, so the fp32 output is that of fp32 arithmetic.
  * |q~| log2(e) sm_scale and the scales must stay below 2^56.
+ * A query row with a NaN or an infinity gives NaN: in its own output row, and in the sums
+ * of weights of its KV head's cached tokens.
  *   weights, weights_out : both NULL, or fp32 [B, Hkv, max_pages_per_seq * P], 16-byte
  *       aligned, the same array or disjoint ones: for every cached token
  *         weights_out[b][h][t] = weights[b][h][t] + sum_i p_{b,i,t},   t < seq_lens[b],

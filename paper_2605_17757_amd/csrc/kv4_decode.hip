@@ -538,7 +538,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       const size_t slot = ((size_t)b * Hq + kvh * g + head) * num_splits + piece;
       part_o[slot * kD + c] = v;
       if (c == 0) {
-        part_ml[2 * slot] = M;
+        // A query that is not finite has NaN for every score, which leaves no maximum: its
+        // piece must not pass for an empty one (M = -inf), so that the NaN reaches the output.
+        part_ml[2 * slot] = L == L ? M : 0.0f;
         part_ml[2 * slot + 1] = L;
       }
     }
