@@ -418,8 +418,12 @@ size_t oscar_kv4_decode_workspace_bytes(const oscar_layout *L, int32_t B, int32_
 /*
  * oscar_kv4_decode_attn -- oscar_decode_attn over the 4-bit cache (same arguments and
  * evaluation: rotated query, split along the sequences, log-sum-exp merge, back-rotation;
- * num_splits as there, 0 for the default).  q~, the softmax weights and the codes enter
- * the matrix cores with all their bits, so the fp32 output is that of fp32 arithmetic.
+ * num_splits as there, 0 for the default).  Products and sums are of fp32's precision with
+ * two exceptions.  In the sums of values a softmax weight times its scale is rounded to two
+ * fp16 pieces: off by 2^-22 of itself at most, or, for weights below about 2^-13 of their
+ * row's largest, by 2^-35 of that largest weight times the largest scale of the token's
+ * page and group.  In the scores' products the matrix cores may drop low bits of a K code
+ * times a channel of q~, as much as 2^-20 of the sum over channels of |q~| s (15 + |z|).
  * |q~| log2(e) sm_scale and the scales must stay below 2^56.
  * A query row with a NaN or an infinity gives NaN: in its own output row, and in the sums
  * of weights of its KV head's cached tokens.

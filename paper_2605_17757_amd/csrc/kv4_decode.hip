@@ -19,8 +19,10 @@
 //     With the codes centred the two sums over tokens are as small as o~ itself; the
 //     matrix cores drop product bits below the accumulator's last ones, and against
 //     sums of uncentred codes that left errors of 1e-5 of the output.  w is scaled by a
-//     power of two per page and group, its largest values near 2^14, and enters as two
-//     fp16 pieces: 22 bits, down to 2^-16 of the row's largest weight, then fewer.
+//     power of two per page and group (s: 2^10 .. 2^11 at the page's largest) and enters as
+//     two fp16 pieces, both rounded to nearest (truncated, the errors of many small weights
+//     had one sign and added up): off by 2^-22 of itself at most, or by 2^-35 of the row's
+//     largest weight at the page's largest scale where that is more.
 // Where the pieces go (NCH chunks of 4 heads per KV head).  As rows of one 16-row operand:
 // 4 heads fill it, one product per chunk does, and a lane adds the pieces of a sum.  As
 // operands of their own, a row per head: 3 products (values: 2) serve 16 heads, the matrix
@@ -43,7 +45,7 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef uint16_t us2 __attribute__((ext_vector_type(2)));
-typedef __fp16 fp16x2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
@@ -102,6 +104,7 @@ __device__ inline void unpack_v(uint32_t d0, uint32_t d1, u4v& lo, u4v& hi) {
   hi = u4v{centred(d0 & (m << 4), 0x1p11f), centred((d0 >> 8) & (m << 4), 0x1p11f),
            centred(d1 & (m << 4), 0x1p11f), centred((d1 >> 8) & (m << 4), 0x1p11f)};
 }
+__device__ inline h2 half2_of(float a, float b) { return __builtin_convertvector((f2{a, b}), h2); }  // nearest even
 __device__ inline uint32_t pk_max(uint32_t a, uint32_t b) {  // of unsigned 16-bit lanes
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
 }
@@ -452,9 +455,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
             wsum = fmaf(x[u], z[u], wsum);
           }
           wz[ch][q] = fmaf(wsum, 0.5f * back[q], wz[ch][q]);
-          const fp16x2 h0 = __builtin_amdgcn_cvt_pkrtz(x[0], x[1]), h1 = __builtin_amdgcn_cvt_pkrtz(x[2], x[3]);
-          const fp16x2 r0 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h0[0], -1.0f, x[0]), fmaf((float)h0[1], -1.0f, x[1]));
-          const fp16x2 r1 = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h1[0], -1.0f, x[2]), fmaf((float)h1[1], -1.0f, x[3]));
+          const h2 h0 = half2_of(x[0], x[1]), h1 = half2_of(x[2], x[3]);
+          const h2 r0 = half2_of(fmaf((float)h0[0], -1.0f, x[0]), fmaf((float)h0[1], -1.0f, x[1]));
+          const h2 r1 = half2_of(fmaf((float)h1[0], -1.0f, x[2]), fmaf((float)h1[1], -1.0f, x[3]));
           uint32_t* row = sm.pw[w] + 2 * lo + (NCH == 1 ? ((q & 1) * 8 + 2 * hi) * kPw : (4 * hi + ch) * kPwWide);
           *reinterpret_cast<uint2*>(row) =
               make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
