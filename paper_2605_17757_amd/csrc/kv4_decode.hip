@@ -421,12 +421,13 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
       }
       float p[NCH][4];
 #pragma unroll
-      for (int ch = 0; ch < NCH; ++ch)
+      for (int ch = 0; ch < NCH; ++ch) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          p[ch][u] = __builtin_amdgcn_exp2f(sc[ch][u] - m[ch]);
-          lsum[ch] += p[ch][u];
-        }
+        for (int u = 0; u < 4; ++u) p[ch][u] = __builtin_amdgcn_exp2f(sc[ch][u] - m[ch]);
+        // (one rounding of the running sum per page: beside a heavy token's 1 the roundings
+        // of many equal small weights add up)
+        lsum[ch] += (p[ch][0] + p[ch][1]) + (p[ch][2] + p[ch][3]);
+      }
       // ---- o~ += w V, group by group: the weights' pieces to LDS as the operand's rows ----
       float back[NG];
       auto stage = [&](int q) {
