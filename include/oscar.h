@@ -473,7 +473,8 @@ int oscar_kv4_decode_step(const oscar_layout *L, void *pages, const void *k_new,
  * The pages of slots >= m are free for other use; the next token of the sequence goes to
  * slot m.  Rows move inside the sequence's own pages: none of them may belong to another
  * sequence too (a shared prefix), in this call or outside it.  max_pages_per_seq * P is
- * at most 2^30, and max_pages_per_seq * Hkv at most 2^27, here and with weights.
+ * below 2^30 (at most 2^30 in attention), and max_pages_per_seq * Hkv at most 2^27, here
+ * and in attention.
  *   weights, weights_out : fp32 [B, Hkv, max_pages_per_seq * P] (oscar_kv4_decode_attn's)
  *   pos, pos_out         : int32, same shape; before the first eviction all -1
  *       each _out may be its input itself; apart from that no array that the call writes

@@ -599,6 +599,13 @@ int check_kv4_slots(const oscar_layout* L, int32_t max_pages_per_seq) {
   return OSCAR_OK;
 }
 
+// Eviction: a launch holds a block of 256 threads for every page that keeps rows, and fewer
+// than 2^32 threads.
+int check_evict_slots(const oscar_layout* L, int32_t max_pages_per_seq) {
+  const int st = check_kv4_slots(L, max_pages_per_seq);
+  return st == OSCAR_OK && max_pages_per_seq >= 1 << 24 ? OSCAR_ERR_UNSUPPORTED : st;
+}
+
 // Arrays of `bytes` bytes that share some of them without being the same array.
 bool partly_shared(const void* a, const void* b, size_t bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -772,7 +779,7 @@ int oscar_kv4_decode_step(const oscar_layout* L, void* pages, const void* k_new,
 }
 
 size_t oscar_kv4_evict_workspace_bytes(const oscar_layout* L, int32_t B, int32_t max_pages_per_seq) {
-  if (check_layout(L) != OSCAR_OK || B < 1 || B > 65535 || check_kv4_slots(L, max_pages_per_seq) != OSCAR_OK)
+  if (check_layout(L) != OSCAR_OK || B < 1 || B > 65535 || check_evict_slots(L, max_pages_per_seq) != OSCAR_OK)
     return 0;
   return kv4_evict_ws_bytes(L->num_kv_heads, B, max_pages_per_seq);
 }
@@ -786,7 +793,7 @@ int oscar_kv4_evict(const oscar_layout* L, void* pages, int32_t B, const int32_t
   if (st) return st;
   if (B < 1 || budget < 1 || sink < 0 || recent < 0) return OSCAR_ERR_INVALID_ARG;
   if (B > 65535) return OSCAR_ERR_UNSUPPORTED;
-  if ((st = check_kv4_slots(L, max_pages_per_seq))) return st;
+  if ((st = check_evict_slots(L, max_pages_per_seq))) return st;
   if (!pages || !block_table || !seq_lens || !weights || !weights_out || !pos || !pos_out || !num_seen ||
       !new_lens || !workspace || new_lens == seq_lens)
     return OSCAR_ERR_INVALID_ARG;
