@@ -52,6 +52,7 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "split_ranges.h"
 
 namespace oscar {
 namespace {
@@ -1402,18 +1403,11 @@ using SplitLds = typename std::conditional<NCH == 1, WaveLds<1>, WideLds<NCH>>::
 // Hkv, kv-head u % Hkv).  Waves per SIMD: 4 for one chunk (128 VGPRs), 2 for the
 // wide instances (their query operands, chunk states and prefetched page; at 3
 // waves the prefetched page spills to scratch).
-constexpr int kMinRange = 4;
 constexpr int kTeam = 4;
 template <int NCH>
 struct SplitWaves {
   static constexpr int per_simd = NCH == 1 ? 4 : 2;
 };
-
-__device__ inline int wave_sum_i(int x) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
-  return x;
-}
 
 // The INT2 tokens of sequence b: all of them, or with MIXED the history [lo, hi),
 // lo = min(S0, n), hi = max(lo, n - W) (the bf16 sink and recent window are handled
@@ -1427,86 +1421,13 @@ __device__ inline TokRange int2_range(const int32_t* __restrict__ seq_lens, int 
   return tok_range(lo, max(lo, len - W));
 }
 
-// a / b for a >= 0, b > 0; for small calls in 32 bits where both fit (a 64-bit division
-// is some 150 dependent instructions; elsewhere the second path sends 8 bytes of the
-// mixed cache's one-chunk instance to scratch).
-__device__ inline int64_t div64(int64_t a, int64_t b) {
+// Divisions of the page ranges: in 32 bits where both sides fit for small calls; elsewhere
+// the second path sends 8 bytes of the mixed cache's one-chunk instance to scratch.
 #ifdef OSCAR_SPLIT_TEAM_UNIT
-  if (((a | b) >> 32) == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
+constexpr bool kShortDiv = true;
+#else
+constexpr bool kShortDiv = false;
 #endif
-  return a / b;
-}
-
-// Pages of a range: [x, xe) of all sequences' pages end to end, the first of them in
-// sequence b, which has npg pages, `before` of the pages lie in earlier sequences
-// (npg == 0: the range is empty).  pw: pages per range.
-struct RangeStart {
-  int64_t x, xe, before, pw;
-  int b, npg;
-};
-template <class Pages>  // pages_of(b): pages of sequence b; called by whole waves
-__device__ inline RangeStart range_start(int r, int n_ranges, int B, int max_pages, int num_splits,
-                                         Pages&& pages_of) {
-  const int l = threadIdx.x & 63;
-  RangeStart s;
-  // pages of 64 sequences, and their inclusive prefix sum over the lanes (DPP: shifts
-  // inside rows of 16 lanes, then the rows' last lanes broadcast)
-  auto scan = [&](int b0, int& np) {
-    const int bb = b0 + l;
-    np = bb < B ? pages_of(bb) : 0;
-    int v = np;
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-    return v;
-  };
-  int np, incl = scan(0, np);
-  int64_t T = __builtin_amdgcn_readlane(incl, 63);
-  for (int b0 = 64; b0 < B; b0 += 64) {
-    const int bb = b0 + l;
-    T += __builtin_amdgcn_readfirstlane(wave_sum_i(bb < B ? pages_of(bb) : 0));
-  }
-  s.pw = max(max(div64(T + n_ranges - 1, n_ranges),
-                 (int64_t)((max_pages + num_splits - 2) / (num_splits - 1))),
-             (int64_t)kMinRange);
-  s.x = (int64_t)r * s.pw;
-  s.xe = min(T, s.x + s.pw);
-  s.b = s.npg = 0;
-  s.before = 0;
-  if (s.x >= s.xe) return s;
-  for (int b0 = 0;;) {
-    const uint64_t hit = __ballot(b0 + l < B && np > 0 && s.before + (incl - np) <= s.x &&
-                                  s.x < s.before + incl);
-    if (hit) {
-      const int lane = __ffsll((unsigned long long)hit) - 1;
-      s.b = b0 + lane;
-      s.npg = __builtin_amdgcn_readlane(np, lane);
-      s.before += __builtin_amdgcn_readlane(incl - np, lane);
-      return s;
-    }
-    s.before += __builtin_amdgcn_readlane(incl, 63);
-    b0 += 64;
-    if (b0 >= B) return s;  // not reached: page x < T lies in some sequence
-    incl = scan(b0, np);
-  }
-}
-
-// A sequence with no pages gets empty slots from the wave of (range b mod n_ranges,
-// kv-head 0), for all its heads.
-template <class Pages>
-__device__ inline void mark_empty(int r, int n_ranges, int B, int Hq, int num_splits, int stride,
-                                  float* __restrict__ part_ml, Pages&& pages_of) {
-  for (int bb = r; bb < B; bb += n_ranges)
-    if (pages_of(bb) == 0)
-      for (int i = threadIdx.x & 63; i < Hq * num_splits; i += 64) {
-        const size_t row = ((size_t)bb * Hq + i / num_splits) * stride + i % num_splits;
-        part_ml[row * 2] = -INFINITY;
-        part_ml[row * 2 + 1] = 0.0f;
-      }
-}
 
 #ifndef OSCAR_SPLIT_TEAM_UNIT
 template <bool MIXED, bool BF, int NG, int NCH>
@@ -1536,7 +1457,7 @@ __global__ __launch_bounds__(64) __attribute__((
     run_piece(r, R, 0, R.npg, 0, true, 0, 1 << 20);
     return;
   }
-  const RangeStart s = range_start(r, n_ranges, B, max_pages, num_splits, pages_of);
+  const RangeStart s = range_start<kShortDiv>(r, n_ranges, B, max_pages, num_splits, pages_of);
   if (kvh == 0) mark_empty(r, n_ranges, B, Hq, num_splits, stride, part_ml, pages_of);
   if (s.npg == 0) return;
   int b = s.b, npg_b = s.npg;
@@ -1544,7 +1465,7 @@ __global__ __launch_bounds__(64) __attribute__((
   __builtin_amdgcn_s_setprio(3);  // lowered in bands as the wave's pages are done
   while (true) {
     const int64_t end = min(s.xe, before + npg_b);
-    const int piece = (int)(r - div64(before, s.pw));
+    const int piece = (int)(r - div64<kShortDiv>(before, s.pw));
     run_piece(b, range_of(b), (int)(x - before), (int)(end - before), piece, end == before + npg_b,
               (int)(x - s.x), (int)(s.xe - s.x));
     x = end;
@@ -1617,7 +1538,7 @@ __global__ __launch_bounds__(64 * kTeam) __attribute__((
       }
     }
   } else {
-    s = range_start(r, n_ranges, B, max_pages, num_splits, pages_of);
+    s = range_start<kShortDiv>(r, n_ranges, B, max_pages, num_splits, pages_of);
     if (kvh == 0 && w == 0) mark_empty(r, n_ranges, B, Hq, num_splits, stride, part_ml, pages_of);
   }
   if (s.npg == 0) return;  // the whole team
@@ -1625,7 +1546,7 @@ __global__ __launch_bounds__(64 * kTeam) __attribute__((
   int64_t x = s.x, before = s.before;
   while (true) {
     const int64_t end = min(s.xe, before + npg_b);
-    const int piece = num_splits == 1 ? 0 : (int)(r - div64(before, s.pw));
+    const int piece = num_splits == 1 ? 0 : (int)(r - div64<kShortDiv>(before, s.pw));
     const int p0 = (int)(x - before), n = (int)(end - x), per = (n + kTeam - 1) / kTeam;
     const int w0 = p0 + min(n, w * per), w1 = p0 + min(n, (w + 1) * per);
     const TeamSink mine{team_o<NCH>(L.wave[w]), L.ml[w]};

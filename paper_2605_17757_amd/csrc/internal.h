@@ -50,6 +50,18 @@ __host__ __device__ constexpr int kv4_v_off(int c, int t) {
 // that lane's write.
 __device__ inline void lane_exchange() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+// Inclusive prefix sum over the wave's lanes (DPP: shifts inside rows of 16 lanes, then the
+// rows' last lanes broadcast).
+__device__ inline int wave_prefix(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
 // Split kernel geometry: a wave handles all query heads of its kv-head in chunks
 // of 4, and the number of chunks sets its registers, hence the waves per CU.
 inline int split_chunks(int heads_per_kv) { return (heads_per_kv + 3) / 4; }

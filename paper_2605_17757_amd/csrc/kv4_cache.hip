@@ -226,18 +226,6 @@ __device__ inline uint32_t rank_key(float w, bool safe) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Inclusive prefix sum over the wave's lanes (DPP: shifts inside rows of 16 lanes, then the
-// rows' last lanes broadcast).
-__device__ inline int wave_prefix(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-  return v;
-}
-
 // The select in one block per row.  ITEMS: slots per thread at most; their keys are kept in
 // registers, the lists of holes and movers (at most S / 2 of each) in LDS.
 template <int ITEMS>

@@ -567,7 +567,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
     s.x = s.before = 0;
     s.xe = s.pw = (int64_t)1 << 40;
   } else {
-    s = range_start(r, n_ranges, B, max_pages, num_splits, pages_of);
+    s = range_start<true>(r, n_ranges, B, max_pages, num_splits, pages_of);
   }
   if (kvh == 0 && w == 0) mark_empty(r, n_ranges, B, Hq, num_splits, num_splits, part_ml, pages_of);
   if (!whole && s.npg == 0) return;
@@ -576,7 +576,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((
   while (b < B) {
     const int64_t end = min(s.xe, before + npg_b);
     if (end > x)
-      run_piece(b, (int)(x - before), (int)(end - before), whole ? 0 : (int)(r - div64(before, s.pw)),
+      run_piece(b, (int)(x - before), (int)(end - before), whole ? 0 : (int)(r - div64<true>(before, s.pw)),
                 end == before + npg_b);
     x = end;
     if (x >= s.xe) break;

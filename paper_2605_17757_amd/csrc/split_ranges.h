@@ -1,6 +1,6 @@
-// The 4-bit split's page ranges, cut as the 2-bit split cuts its own (decode_mfma.hip): the
-// pages of all sequences laid end to end, in equal ranges, as each wave works them out from
-// the sequences' page counts.
+// The split kernels' page ranges, of the 2-bit and the 4-bit cache: the pages of all
+// sequences laid end to end, in equal ranges, as each wave works them out from the
+// sequences' page counts.
 #pragma once
 
 #include "internal.h"
@@ -16,10 +16,11 @@ __device__ inline int wave_sum_i(int x) {
   return x;
 }
 
-// a / b for a >= 0, b > 0, in 32 bits where both fit (a 64-bit division is some 150
+// a / b for a >= 0, b > 0; SHORT: in 32 bits where both fit (a 64-bit division is some 150
 // dependent instructions).
+template <bool SHORT>
 __device__ inline int64_t div64(int64_t a, int64_t b) {
-  if (((a | b) >> 32) == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
+  if (SHORT && ((a | b) >> 32) == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
   return a / b;
 }
 
@@ -30,24 +31,16 @@ struct RangeStart {
   int64_t x, xe, before, pw;
   int b, npg;
 };
-template <class Pages>  // pages_of(b): pages of sequence b; called by whole waves
+template <bool SHORT, class Pages>  // pages_of(b): pages of sequence b; called by whole waves
 __device__ inline RangeStart range_start(int r, int n_ranges, int B, int max_pages, int num_splits,
                                          Pages&& pages_of) {
   const int l = threadIdx.x & 63;
   RangeStart s;
-  // pages of 64 sequences, and their inclusive prefix sum over the lanes (DPP: shifts
-  // inside rows of 16 lanes, then the rows' last lanes broadcast)
+  // pages of 64 sequences, and their inclusive prefix sum over the lanes
   auto scan = [&](int b0, int& np) {
     const int bb = b0 + l;
     np = bb < B ? pages_of(bb) : 0;
-    int v = np;
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-    return v;
+    return wave_prefix(np);
   };
   int np, incl = scan(0, np);
   int64_t T = __builtin_amdgcn_readlane(incl, 63);
@@ -55,7 +48,7 @@ __device__ inline RangeStart range_start(int r, int n_ranges, int B, int max_pag
     const int bb = b0 + l;
     T += __builtin_amdgcn_readfirstlane(wave_sum_i(bb < B ? pages_of(bb) : 0));
   }
-  s.pw = max(max(div64(T + n_ranges - 1, n_ranges),
+  s.pw = max(max(div64<SHORT>(T + n_ranges - 1, n_ranges),
                  (int64_t)((max_pages + num_splits - 2) / (num_splits - 1))),
              (int64_t)kMinRange);
   s.x = (int64_t)r * s.pw;
