@@ -35,7 +35,7 @@ __device__ inline float value_of(uint32_t x, int sh, float2 m) { return m.x * ((
 // Row by row against tiles, 8 heads: 1000 tokens in order 6.1 us against 6.9, 2048 8.0
 // against 7.2, 4200 13.2 against 10.2; of as many pages (a step's new tokens) 97 tokens 6.2
 // against 20, 4200 15 against 25, 131072 513 against 646.
-// 131072 tokens x 8 heads, fp32 (1.24 GB): 539 us row by row, 217 us (5.7 TB/s) by tiles
+// 131072 tokens x 8 heads, fp32 (1.24 GB): 539 us row by row, 224 us (5.5 TB/s) by tiles
 // at three waves per SIMD; at eight, whose half-written output lines do not fit the L2,
 // 307, at two 245, with non-temporal stores 450.
 // ---------------------------------------------------------------------------
@@ -208,11 +208,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
 //   move:   the moved rows' bytes (codes, scales, zeros) from page to page, one block per
 //           page that receives any.
 // Bounds: select the latency of its passes, one block per row: 32 x 8 rows of 8k to 16k
-// slots 32 us, 13 of them the two streams' bytes at the copy rate; 8 rows of 2k slots 9 us
+// slots 33 us, 13 of them the two streams' bytes at the copy rate; 8 rows of 2k slots 9 us
 // (40 and 11.4 with the lists in the workspace and every wave copying its own kept slots;
 // 73 with keys formed anew in every pass, two block-wide sums per 1024 slots).  Move the
 // cache lines of the sources' V codes, 64 bytes of a row in 8 lines: the same rows to 1024
-// slots, 240000 moves, 80 us for about 250 MB of lines (116 a wave per row).
+// slots, 240000 moves, 82 us for about 250 MB of lines (116 a wave per row).
 // ---------------------------------------------------------------------------
 constexpr int kSel = 1024;            // threads of a select block
 constexpr int kSelLds = 32 * kSel;    // slots up to which they fit into its registers and LDS

@@ -160,10 +160,11 @@ struct SplitSmem {
 // always on their way at 8 waves per CU.
 //
 // Bound: up to 4 heads per KV head HBM (64 sequences of 16k to 32k tokens, 32/8 heads:
-// 2.0 GB in 314 us, 6.4 TB/s; 555 vector instructions per page, VALU busy 61 %).  Beyond,
-// the VALU: per page about 310 instructions that all chunks share (unpacking 224, metadata
-// 84) and about 170 per chunk (scores 36, weights and their pieces 70, softmax 20, sums 8).
-// 12 heads (16 x 128k tokens): 828 a page, busy 74 %, matrix cores 28 %, 570 us, 4.7 TB/s.
+// 2.0 GB; 343 us in a trace, 310 at least, 5.9 and 6.5 TB/s; 554 vector instructions per
+// page, VALU busy 63 %).  Beyond, the VALU: per page about 310 instructions that all chunks
+// share (unpacking 224, metadata 84) and about 170 per chunk (scores 36, weights and their
+// pieces 70, softmax 20, sums 8).  12 heads (16 x 128k tokens): 828 a page, busy 74 %, matrix
+// cores 28 %, 625 us, 576 at least, 4.3 and 4.7 TB/s.
 // Two waves per SIMD: at three, which the 4-head instances allow, 342 us for 340.  With
 // the products' sums kept in the accumulators across pages (32 registers per chunk
 // instead of 8) more than 8 heads went to scratch: 16 heads 555 us, 310 now.  Rotating
