@@ -519,6 +519,123 @@ int oscar_bf16_decode_attn(const oscar_layout *L, const void *pages, const void 
                            oscar_dtype out_dtype, void *stream);
 
 /*
+ * New tokens' queries and keys on their way from the projection to a cache: RMS norm per
+ * head and rotation by position.  For a row x of d channels:
+ *   x^_c = x_c / sqrt(mean_c x_c^2 + eps) * w_c           (weight NULL: x^ = x)
+ *   each pair (a, b) of x^:  a' = f (a cos t - b sin t), b' = f (b cos t + a sin t)
+ * with the angle t = position * inv_freq[i] of pair i, f = attn_scale.  Steps in fp32 (the
+ * angle in fp64), one rounding to bf16 (nearest even) at the end.
+ */
+typedef struct {
+  int32_t rotary_dim;    /* channels that are rotated, the first of a head: a multiple of 16 up
+                            to d (0: none)                                                 */
+  int32_t interleaved;   /* pair i: channels (i, i + rotary_dim/2), or (2i, 2i + 1) if 1      */
+  float attn_scale;      /* f                                                                */
+  const float *inv_freq; /* device, fp32 [rotary_dim/2], 16-byte aligned                      */
+} oscar_rope;            /* host struct, read only */
+
+/* Frequencies for positions past the length that a model was trained on, f_i = base^(-2i/rotary_dim):
+ *   UNSCALED : f_i
+ *   LINEAR   : f_i / factor
+ *   BY_TURNS : keep f_i + (1 - keep) f_i / factor, keep = (r_i - low) / (high - low) clamped to
+ *              [0, 1], r_i = original_len f_i / (2 pi) the turns over the original length
+ *   BY_INDEX : the same blend with keep falling linearly over the pairs' indices, from 1 at
+ *              floor(index of `high` turns) to 0 at ceil(index of `low` turns) */
+typedef enum {
+  OSCAR_ROPE_UNSCALED = 0,
+  OSCAR_ROPE_LINEAR = 1,
+  OSCAR_ROPE_BY_TURNS = 2,
+  OSCAR_ROPE_BY_INDEX = 3
+} oscar_rope_scaling;
+
+/* oscar_rope_freqs -- fills inv_freq (HOST, fp32 [rotary_dim/2]); computed in fp64 and rounded
+ * once.  Arguments that the scaling does not name are ignored. */
+int oscar_rope_freqs(int32_t rotary_dim, double base, oscar_rope_scaling scaling, double factor,
+                     double original_len, double low, double high, float *inv_freq);
+
+/*
+ * oscar_qk_norm_rope -- norm and rotation of queries and keys into rows of their own, e.g.
+ * before a quantized cache's update and attention.  L: head_dim and num_kv_heads are used.
+ *   q, k         : bf16, token i's heads [Hq][d] (k: [Hkv][d]) contiguous at element
+ *                  i * q_stride (k_stride), e.g. parts of a fused projection's rows; strides
+ *                  multiples of 8, pointers 16-byte aligned
+ *   q_out, k_out : bf16 [n_tok][Hq][d], [n_tok][Hkv][d]; may be q (k) itself where its rows
+ *                  are contiguous (in place)
+ *   positions    : int64 [n_tok]
+ *   q_weight, k_weight : bf16 [d] or NULL (no norm); eps >= 0
+ * n_tok == 0 launches nothing.
+ */
+int oscar_qk_norm_rope(const oscar_layout *L, const oscar_rope *rope, const void *q, int64_t q_stride,
+                       void *q_out, int32_t Hq, const void *k, int64_t k_stride, void *k_out,
+                       const int64_t *positions, int32_t n_tok, const void *q_weight,
+                       const void *k_weight, float eps, void *stream);
+
+/*
+ * oscar_bf16_kv_append_rope -- oscar_bf16_kv_append with the norm and rotation on the way: keys
+ * as by oscar_qk_norm_rope and values as they are into the bf16 cache, and with Hq > 0 the
+ * queries as by oscar_qk_norm_rope into q_out, in one launch (Hq == 0: q, q_out, q_weight are
+ * unused).  Tokens with a negative slot are skipped (their queries are not).  v_new, v_stride as
+ * k_new, k_stride; other arguments as there.
+ */
+int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_rope *rope, const void *q,
+                              int64_t q_stride, void *q_out, int32_t Hq, const void *k_new,
+                              int64_t k_stride, const void *v_new, int64_t v_stride,
+                              const int64_t *slot_mapping, const int64_t *positions, int32_t n_tok,
+                              const void *q_weight, const void *k_weight, float eps, void *stream);
+
+/*
+ * oscar_bf16_chunk_attn, oscar_kv4_chunk_attn, oscar_chunk_attn -- causal attention of the
+ * newest tokens of every sequence, one or many each, over the bf16, 4-bit or 2-bit cache, which
+ * holds them already: chunked prefill, checking drafted tokens, and single tokens beside them.
+ * Sequence b has n_b = q_start[b+1] - q_start[b] new tokens, the last of its seq_lens[b]; the
+ * one of row q_start[b] + j is at position p = seq_lens[b] - n_b + j and sees the cached tokens
+ *   t <= p, and with window > 0 of them those with t > p - window or t < sinks.
+ * Per row and query head, over those tokens:
+ *   o = softmax(sm_scale * q K^T) V     (quantized caches: K^, V^ as in oscar_decode_attn)
+ * A row that sees no token (seq_lens[b] < n_b) is zero.  Rows from q_start[B] on are left as
+ * they were.  Pages of the block table that no new token of the sequence sees are not read, and
+ * their entries may be anything.  Slots past a sequence's length may hold anything.
+ * Products of bf16 values are exact, their sums, softmax statistics and outputs' sums are fp32.
+ * Softmax weights enter the value product rounded to bf16 (with at most 32 (token, head) rows per
+ * sequence and KV head on average: to two bf16 pieces); over a quantized cache weights, rotated
+ * queries and dequantized values enter as fp16, scaled by powers of two per row and page.  There
+ * |q~| log2(e) sm_scale and the scales must stay below 2^56.
+ *   q           : bf16 [n_q, Hq, d]; Hq % Hkv == 0, Hq/Hkv <= 16
+ *   q_start     : int32 [B + 1], ascending from 0, q_start[B] <= n_q; values outside [0, n_q] are
+ *                 clamped
+ *   block_table : int32 [B, max_pages_per_seq]; max_pages_per_seq * 64 <= 2^30
+ *   seq_lens    : int32 [B], the new tokens included; clamped to [0, max_pages_per_seq * 64]
+ *   window      : >= 0, 0: none; sinks >= 0, used with a window
+ *   num_splits  : pieces that a row's pages are cut into at most (>= 1, at most 1024), or 0 for
+ *                 oscar_chunk_default_splits; results do not depend on it beyond fp32 rounding
+ *   workspace   : >= oscar_chunk_workspace_bytes(L, n_q, B, Hq, max_pages_per_seq, num_splits,
+ *                 quantized) bytes, 256-byte aligned, contents need no initialization
+ *   out         : bf16 [n_q, Hq, d]
+ * q and out are 16-byte aligned.  n_q == 0 launches nothing.
+ */
+int32_t oscar_chunk_default_splits(const oscar_layout *L, int32_t n_q, int32_t B, int32_t Hq,
+                                   int32_t max_pages_per_seq);
+size_t oscar_chunk_workspace_bytes(const oscar_layout *L, int32_t n_q, int32_t B, int32_t Hq,
+                                   int32_t max_pages_per_seq, int32_t num_splits, int32_t quantized);
+int oscar_bf16_chunk_attn(const oscar_layout *L, const void *pages, const void *q, int32_t n_q,
+                          int32_t B, int32_t Hq, const int32_t *q_start, const int32_t *block_table,
+                          int32_t max_pages_per_seq, const int32_t *seq_lens, float sm_scale,
+                          int32_t window, int32_t sinks, int32_t num_splits, void *workspace,
+                          size_t workspace_bytes, void *out, void *stream);
+int oscar_kv4_chunk_attn(const oscar_layout *L, const void *pages, const void *q, int32_t n_q,
+                         int32_t B, int32_t Hq, const int32_t *q_start, const int32_t *block_table,
+                         int32_t max_pages_per_seq, const int32_t *seq_lens, const float *R_k,
+                         const float *R_v, float sm_scale, int32_t window, int32_t sinks,
+                         int32_t num_splits, void *workspace, size_t workspace_bytes, void *out,
+                         void *stream);
+int oscar_chunk_attn(const oscar_layout *L, const void *pages, const void *q, int32_t n_q, int32_t B,
+                     int32_t Hq, const int32_t *q_start, const int32_t *block_table,
+                     int32_t max_pages_per_seq, const int32_t *seq_lens, const float *R_k,
+                     const float *R_v, float sm_scale, int32_t window, int32_t sinks,
+                     int32_t num_splits, void *workspace, size_t workspace_bytes, void *out,
+                     void *stream);
+
+/*
  * Offline calibration (Sec. 3 "Algorithm Design: Offline Calibration and
  * Justification"; App. "Hadamard transform", "P_K" and the worked example;
  * Alg. 1 Calibrate).  From one layer's calibration activations (bf16

@@ -35,6 +35,9 @@ EXPORTS = (
     "oscar_kv4_evict_workspace_bytes", "oscar_kv4_evict",
     "oscar_bf16_page_bytes", "oscar_bf16_kv_append", "oscar_bf16_decode_workspace_bytes",
     "oscar_bf16_decode_attn",
+    "oscar_rope_freqs", "oscar_qk_norm_rope", "oscar_bf16_kv_append_rope",
+    "oscar_chunk_default_splits", "oscar_chunk_workspace_bytes", "oscar_bf16_chunk_attn",
+    "oscar_kv4_chunk_attn", "oscar_chunk_attn",
     "oscar_calib_workspace_bytes", "oscar_calib_query_cov", "oscar_calib_attn",
     "oscar_calib_score_cov", "oscar_calib_rotation_workspace_bytes", "oscar_calib_rotation",
     "oscar_calib_clip_workspace_bytes", "oscar_calib_clip",
@@ -70,6 +73,12 @@ class Layout(ctypes.Structure):
                          meta_dtype, rot_per_head)
 
 
+class _RopeArg(ctypes.Structure):
+    """Mirror of ``oscar_rope``."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("attn_scale", ctypes.c_float), ("inv_freq", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -83,7 +92,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         P, i32, i64, f32, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                                 ctypes.c_size_t)
-        LP = ctypes.POINTER(Layout)
+        f64, LP, RP = ctypes.c_double, ctypes.POINTER(Layout), ctypes.POINTER(_RopeArg)
         sigs = {
             "oscar_status_string": (ctypes.c_char_p, [ctypes.c_int]),
             "oscar_page_bytes": (sz, [LP]),
@@ -131,6 +140,19 @@ def lib() -> ctypes.CDLL:
             "oscar_bf16_decode_workspace_bytes": (sz, [LP, i32, i32, i32]),
             "oscar_bf16_decode_attn": (ctypes.c_int, [LP, P, P, i32, i32, P, i32, P, f32, i32, P,
                                                       sz, P, ctypes.c_int, P]),
+            "oscar_rope_freqs": (ctypes.c_int, [i32, f64, ctypes.c_int, f64, f64, f64, f64, P]),
+            "oscar_qk_norm_rope": (ctypes.c_int, [LP, RP, P, i64, P, i32, P, i64, P, P, i32, P, P, f32,
+                                                  P]),
+            "oscar_bf16_kv_append_rope": (ctypes.c_int, [LP, P, RP, P, i64, P, i32, P, i64, P, i64, P,
+                                                         P, i32, P, P, f32, P]),
+            "oscar_chunk_default_splits": (i32, [LP, i32, i32, i32, i32]),
+            "oscar_chunk_workspace_bytes": (sz, [LP, i32, i32, i32, i32, i32, i32]),
+            "oscar_bf16_chunk_attn": (ctypes.c_int, [LP, P, P, i32, i32, i32, P, P, i32, P, f32, i32,
+                                                     i32, i32, P, sz, P, P]),
+            "oscar_kv4_chunk_attn": (ctypes.c_int, [LP, P, P, i32, i32, i32, P, P, i32, P, P, P, f32,
+                                                    i32, i32, i32, P, sz, P, P]),
+            "oscar_chunk_attn": (ctypes.c_int, [LP, P, P, i32, i32, i32, P, P, i32, P, P, P, f32, i32,
+                                                i32, i32, P, sz, P, P]),
             "oscar_calib_workspace_bytes": (sz, [i64, i32, i32]),
             "oscar_calib_query_cov": (ctypes.c_int, [P, i64, i32, i32, P, P, sz, P]),
             "oscar_calib_attn": (ctypes.c_int, [P, P, P, i64, i32, i32, i32, P, P]),
@@ -669,6 +691,180 @@ def bf16_decode_attn(layout: Layout, pages, q, block_table, seq_lens, sm_scale: 
         _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
         _ptr(out, out.dtype, "out", B * Hq * d), out_dtype, _stream(stream))
     _check(st, "oscar_bf16_decode_attn")
+
+
+# ---------------------------------------------------------------------------
+# norm and rotation of new tokens' queries and keys
+# ---------------------------------------------------------------------------
+
+ROPE_UNSCALED, ROPE_LINEAR, ROPE_BY_TURNS, ROPE_BY_INDEX = range(4)
+
+
+def rope_freqs(rotary_dim: int, base: float, scaling: int = ROPE_UNSCALED, factor: float = 1.0,
+               original_len: float = 0.0, low: float = 1.0, high: float = 32.0,
+               device="cuda") -> torch.Tensor:
+    """fp32 [rotary_dim / 2] frequencies, scaled for positions past ``original_len``
+    (``oscar_rope_scaling``)."""
+    f = torch.empty(max(int(rotary_dim) // 2, 1), dtype=torch.float32)
+    _check(lib().oscar_rope_freqs(int(rotary_dim), float(base), int(scaling), float(factor),
+                                  float(original_len), float(low), float(high),
+                                  ctypes.c_void_p(f.data_ptr())), "oscar_rope_freqs")
+    return f.to(device)
+
+
+class Rope:
+    """How positions rotate a head: its first ``rotary_dim`` channels in pairs
+    (i, i + rotary_dim/2), or (2i, 2i + 1) if ``interleaved``, by position * inv_freq[i]
+    (fp32 GPU tensor), times ``attn_scale``."""
+
+    def __init__(self, rotary_dim: int, inv_freq, interleaved: bool = False, attn_scale: float = 1.0):
+        self.rotary_dim, self.inv_freq = int(rotary_dim), inv_freq
+        self.interleaved, self.attn_scale = bool(interleaved), float(attn_scale)
+
+    def _arg(self, dev: int) -> _RopeArg:
+        f = None
+        if self.rotary_dim > 0:
+            f = _arg(self.inv_freq, torch.float32, "inv_freq", self.rotary_dim // 2, dev)
+        return _RopeArg(self.rotary_dim, int(self.interleaved), self.attn_scale, f)
+
+
+def _rows_arg(x, name: str, n_tok: int, heads, dev: int):
+    """(address, token stride) of bf16 rows [n_tok, heads, d] whose heads are contiguous."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if x.dtype is not torch.bfloat16:
+        raise TypeError("%s must be torch.bfloat16, got %s" % (name, x.dtype))
+    if not x.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if x.get_device() != dev:
+        raise ValueError("%s is on %s, but the current device is cuda:%d" % (name, x.device, dev))
+    if x.dim() != 3 or x.shape[0] != n_tok or x.shape[2] != HEAD_DIM or (heads is not None and x.shape[1] != heads):
+        raise ValueError("%s must be [%d, %s, %d]" % (name, n_tok, "heads" if heads is None else heads, HEAD_DIM))
+    heads = int(x.shape[1])
+    if n_tok > 0 and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != HEAD_DIM)):
+        raise ValueError("%s must have a token's heads contiguous" % name)
+    return x.data_ptr(), (int(x.stride(0)) if n_tok > 1 else heads * HEAD_DIM)
+
+
+def _weight_arg(w, name: str, dev: int):
+    return None if w is None else _arg(w, torch.bfloat16, name, HEAD_DIM, dev)
+
+
+def qk_norm_rope(layout: Layout, rope: Rope, q, k, positions, q_out, k_out, q_weight=None,
+                 k_weight=None, eps: float = 1e-6, stream=None) -> None:
+    """RMS norm per head (``q_weight`` / ``k_weight`` bf16 [d]; None: none) and rotation by
+    position of q [n_tok, Hq, d] and k [n_tok, Hkv, d] (views of a fused projection will do)
+    into q_out, k_out (contiguous; q and k themselves if those are)."""
+    dev, st = _dev_stream(stream)
+    n_tok = int(positions.numel())
+    qp, qs = _rows_arg(q, "q", n_tok, None, dev)
+    kp, ks = _rows_arg(k, "k", n_tok, layout.num_kv_heads, dev)
+    Hq = int(q.shape[1])
+    r = rope._arg(dev)
+    _check(lib().oscar_qk_norm_rope(
+        ctypes.byref(layout), ctypes.byref(r), qp, qs,
+        _arg(q_out, torch.bfloat16, "q_out", n_tok * Hq * HEAD_DIM, dev), Hq, kp, ks,
+        _arg(k_out, torch.bfloat16, "k_out", n_tok * layout.num_kv_heads * HEAD_DIM, dev),
+        _arg(positions, torch.int64, "positions", None, dev), n_tok,
+        _weight_arg(q_weight, "q_weight", dev), _weight_arg(k_weight, "k_weight", dev), float(eps), st),
+        "oscar_qk_norm_rope")
+
+
+def bf16_kv_append_rope(layout: Layout, pages, rope: Rope, k_new, v_new, slot_mapping, positions,
+                        q=None, q_out=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                        stream=None) -> None:
+    """bf16_kv_append with the keys normalised and rotated on the way (qk_norm_rope), and the
+    queries too, into ``q_out``, if ``q`` is given.  Tokens with a negative slot are skipped."""
+    dev, st = _dev_stream(stream)
+    n_tok = int(slot_mapping.numel())
+    kp, ks = _rows_arg(k_new, "k_new", n_tok, layout.num_kv_heads, dev)
+    vp, vs = _rows_arg(v_new, "v_new", n_tok, layout.num_kv_heads, dev)
+    qp = qo = None
+    qs = Hq = 0
+    if q is not None:
+        qp, qs = _rows_arg(q, "q", n_tok, None, dev)
+        Hq = int(q.shape[1])
+        qo = _arg(q_out, torch.bfloat16, "q_out", n_tok * Hq * HEAD_DIM, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    r = rope._arg(dev)
+    _check(lib().oscar_bf16_kv_append_rope(
+        ctypes.byref(layout), _arg(pages, torch.bfloat16, "pages", bf16_pool_bytes(layout) // 2, dev),
+        ctypes.byref(r), qp, qs, qo, Hq, kp, ks, vp, vs,
+        _arg(slot_mapping, torch.int64, "slot_mapping", None, dev),
+        _arg(positions, torch.int64, "positions", n_tok, dev), n_tok,
+        _weight_arg(q_weight, "q_weight", dev), _weight_arg(k_weight, "k_weight", dev), float(eps), st),
+        "oscar_bf16_kv_append_rope")
+
+
+# ---------------------------------------------------------------------------
+# attention of chunks over a paged cache
+# ---------------------------------------------------------------------------
+
+def chunk_default_splits(layout: Layout, n_q: int, B: int, Hq: int, max_pages_per_seq: int) -> int:
+    return int(lib().oscar_chunk_default_splits(ctypes.byref(layout), n_q, B, Hq, max_pages_per_seq))
+
+
+def chunk_workspace_bytes(layout: Layout, n_q: int, B: int, Hq: int, max_pages_per_seq: int,
+                          num_splits: int = 0, quantized: bool = True) -> int:
+    return int(lib().oscar_chunk_workspace_bytes(ctypes.byref(layout), n_q, B, Hq, max_pages_per_seq,
+                                                 num_splits, int(bool(quantized))))
+
+
+def chunk_alloc_workspace(layout: Layout, n_q: int, B: int, Hq: int, max_pages_per_seq: int,
+                          num_splits: int = 0, quantized: bool = True, device="cuda"):
+    n = chunk_workspace_bytes(layout, n_q, B, Hq, max_pages_per_seq, num_splits, quantized)
+    if n == 0:
+        raise OscarError(ERR_INVALID_ARG, "chunk_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _chunk_call(name, layout, pool, q, q_start, block_table, seq_lens, rotations, sm_scale, window, sinks,
+                num_splits, workspace, out, dev, st):
+    if q.dim() != 3:
+        raise ValueError("q must be [n_q, Hq, d]")
+    n_q, Hq = int(q.shape[0]), int(q.shape[1])
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages_per_seq]")
+    B, mp = int(block_table.shape[0]), int(block_table.shape[1])
+    n = n_q * Hq * layout.head_dim
+    _check(getattr(lib(), name)(
+        ctypes.byref(layout), pool, _arg(q, torch.bfloat16, "q", n, dev), n_q, B, Hq,
+        _arg(q_start, torch.int32, "q_start", B + 1, dev),
+        _arg(block_table, torch.int32, "block_table", B * mp, dev), mp,
+        _arg(seq_lens, torch.int32, "seq_lens", B, dev), *rotations, float(sm_scale), int(window), int(sinks),
+        int(num_splits), _arg(workspace, torch.uint8, "workspace", None, dev), workspace.numel(),
+        _arg(out, torch.bfloat16, "out", n, dev), st), name)
+
+
+def bf16_chunk_attn(layout: Layout, pages, q, q_start, block_table, seq_lens, sm_scale: float,
+                    window: int, sinks: int, num_splits: int, workspace, out, stream=None) -> None:
+    """Causal attention of every sequence's newest tokens (rows q_start[b] .. q_start[b+1] of q
+    [n_q, Hq, d]) over the bf16 cache into ``out`` (bf16, like q).  ``window`` 0: none; with one,
+    the first ``sinks`` tokens stay visible."""
+    dev, st = _dev_stream(stream)
+    pool = _arg(pages, torch.bfloat16, "pages", bf16_pool_bytes(layout) // 2, dev)
+    _chunk_call("oscar_bf16_chunk_attn", layout, pool, q, q_start, block_table, seq_lens, (), sm_scale, window,
+                sinks, num_splits, workspace, out, dev, st)
+
+
+def kv4_chunk_attn(layout: Layout, pages, q, q_start, block_table, seq_lens, R_k, R_v, sm_scale: float,
+                   window: int, sinks: int, num_splits: int, workspace, out, stream=None) -> None:
+    """bf16_chunk_attn over the 4-bit cache (R_k / R_v None: identity)."""
+    dev, st = _dev_stream(stream)
+    rot = _rarg(R_k, "R_k", layout, dev), _rarg(R_v, "R_v", layout, dev)
+    _chunk_call("oscar_kv4_chunk_attn", layout, _kv4_pool(layout, pages, dev), q, q_start, block_table, seq_lens,
+                rot, sm_scale, window, sinks, num_splits, workspace, out, dev, st)
+
+
+def chunk_attn(layout: Layout, pages, q, q_start, block_table, seq_lens, R_k, R_v, sm_scale: float,
+               window: int, sinks: int, num_splits: int, workspace, out, stream=None) -> None:
+    """bf16_chunk_attn over the 2-bit cache (R_k / R_v None: identity)."""
+    dev, st = _dev_stream(stream)
+    rot = _rarg(R_k, "R_k", layout, dev), _rarg(R_v, "R_v", layout, dev)
+    pool = _arg(pages, torch.uint8, "pages", pool_bytes(layout), dev)
+    _chunk_call("oscar_chunk_attn", layout, pool, q, q_start, block_table, seq_lens, rot, sm_scale, window, sinks,
+                num_splits, workspace, out, dev, st)
 
 
 # ---------------------------------------------------------------------------

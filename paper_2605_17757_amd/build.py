@@ -38,6 +38,8 @@ SOURCES = {
     "kv4_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kv4_cache.hip": ["-ffp-contract=off"],
     "bf16_decode.hip": [],
+    "rope.hip": [],
+    "chunk_attn.hip": [],
     "mixed.hip": [],
     "calib.hip": ["-ffp-contract=off"],
     "probe.hip": [],

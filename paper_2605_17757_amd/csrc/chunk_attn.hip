@@ -1,0 +1,824 @@
+// Attention of the newest tokens of every sequence (a prompt's chunk, drafted tokens, one
+// token) over a paged cache that holds them already: bf16, 4-bit or 2-bit pages.
+//
+// A sequence's rows are its (token, query head) pairs of one KV head, token by token: a
+// tile of them shares every key and value read.  Per page of 64 tokens:
+//   S^T = K Q^T      two 32-token tiles, 8 steps of 16 channels
+//   p = 2^(S^T c - m), m a running reference per row, moved when a score exceeds it by kSlack
+//   O^T += V^T P^T   four 32-channel tiles, 4 steps of 16 tokens
+// both on 32x32x16 matrix products with the queries as columns (lane l: column l % 32,
+// half h = l / 32).  A lane then has 32 tokens' scores of one row in registers: maxima and
+// sums are per lane but for one exchange between the halves, and, since the order of tokens
+// inside a step is free, its p are P^T's operand as they are: with the rows of token tile T
+// taken as row r -> slot 4 (r % 16) + 2 T + r / 16, register i of tile T in half h is slot
+//   32 j0 + 16 h + 4 i4 + 2 T + b,   b = i / 8, j0 = i / 4 % 2, i4 = i % 4,
+// so half h has 8 consecutive slots 32 j0 + 16 h + 8 i2 .. + 7 for each step (j0, i2).
+//
+// What a lane gives the matrix cores of a page, 16 bytes a step, 8 values:
+//   K step ks of tile T: slot 4 lo + 2 T + b (l = lo + 16 b + 32 h), 8 channels
+//   V step (j0, i2) of tile C: one channel, 8 slots as above
+// bf16 pages hold these operands as they are.  Codes become fp16 with one packed
+// multiply-add: the 16-bit pattern of a code n is the fp16 subnormal n 2^-24, and
+//   x = s (n - z) = (n 2^-24) (s 2^24) - s z
+// with the scale and -s z rounded to fp16 (off by 2^-12 of s z at most; the scale is exact
+// unless it is 2^-14 of the page's largest) after division by a power of two, so that the
+// page's largest scale 2^24 and |s z| stay below 2^15: scores take it back as part of c, values
+// through the accumulators' exponent, which moves like m when a page needs more.
+#include "reduce_body.h"
+
+#include <type_traits>
+
+namespace oscar {
+namespace {
+
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+
+constexpr int kRows = 32;         // query rows of a wave
+constexpr int kWaves = 4;
+constexpr float kSlack = 8.0f;    // how far (log2) a score may exceed the reference before it moves
+constexpr int kNoWindow = 1 << 30;  // positions are below it
+// Least factor of scores: positive, so that a masked score stays -inf; below it scores are 0
+// to fp32's precision of exp.
+constexpr float kLeast = 0x1p-100f;
+constexpr int kBfBlock = 2 * kP * kD * 2;  // bytes of a bf16 page-head block
+
+template <int FMT>
+__device__ inline f16v mfma(const u4v& a, const u4v& b, const f16v& c) {
+  if (FMT == kBf16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0,
+                                                   0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+template <int FMT>
+__device__ inline uint32_t pack2(float a, float b) {  // to the operands' type, nearest even
+  if (FMT == kBf16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), h2));
+}
+__device__ inline float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Over the two halves of a wave: lanes l and l ^ 32.
+__device__ inline float half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ inline int wave_max_i(int v) {
+  auto dpp = [](int x, auto ctrl) {
+    return max(x, __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  v = dpp(v, std::integral_constant<int, 0x128>{});  // rows of 16 lanes, rotated by 8, 4, 2, 1
+  v = dpp(v, std::integral_constant<int, 0x124>{});
+  v = dpp(v, std::integral_constant<int, 0x122>{});
+  v = dpp(v, std::integral_constant<int, 0x121>{});
+  return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+// Exponent e of |x| < 2^(e + 1) (0 and subnormals: -127).
+__device__ inline int exp_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
+__device__ inline float pow2(int e) {  // clamped to fp32's normal range
+  return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23);
+}
+
+// ---------------------------------------------------------------------------
+// Tiles.  Sequence b's tiles have the numbers from floor(q_start[b] g / M) + b on: for any
+// chunk lengths at least as many as it has tiles, so that a block finds its sequence among
+// the numbers without a sum over the sequences before.
+// ---------------------------------------------------------------------------
+struct Tile {
+  int b;       // -1: none
+  int q0, n;   // the sequence's first row of q and its new tokens
+  int row0, rows;  // first (token, head) row of the tile, rows of the sequence
+  int len;
+};
+__device__ inline Tile find_tile(const ChunkArgs& a, int64_t id, int g, int M) {
+  const int l = threadIdx.x & 63;
+  auto start = [&](int b) { return min(max(a.q_start[b], 0), a.n_q); };
+  int lo = 0, n = a.B;  // the sequence is in [lo, lo + n)
+  while (n > 1) {       // 64 candidates at a time
+    const int step = (n + 63) / 64;
+    const int b = lo + l * step;
+    const bool le = l * step < n && (int64_t)start(b) * g / M + b <= id;
+    const int k = 63 - __clzll((unsigned long long)(__ballot(le) | 1ull));
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  Tile t;
+  t.b = __builtin_amdgcn_readfirstlane(lo);
+  t.q0 = start(t.b);
+  t.n = max(start(t.b + 1) - t.q0, 0);
+  t.rows = t.n * g;
+  const int64_t r0 = (id - ((int64_t)t.q0 * g / M + t.b)) * M;
+  t.len = min(max(a.seq_lens[t.b], 0), a.max_pages * kP);
+  t.row0 = (int)r0;
+  if (r0 < 0 || r0 >= t.rows) t.b = -1;
+  return t;
+}
+
+// Pages that rows [row0, row0 + M) of a tile see: `head` first ones, then from `from` on.
+struct Pages {
+  int head, from, count;
+  int p_min, p_max;  // positions of the first and the last row
+};
+__device__ inline Pages tile_pages(const Tile& t, int g, int M, int window, int sinks) {
+  Pages s;
+  const int base = t.len - t.n;
+  s.p_min = base + t.row0 / g;
+  s.p_max = base + (min(t.row0 + M, t.rows) - 1) / g;
+  const int start = max(s.p_min - window + 1, 0);
+  s.from = start / kP;
+  s.head = min((min(sinks, start) + kP - 1) / kP, s.from);
+  s.count = s.p_max < 0 ? 0 : s.head + s.p_max / kP + 1 - s.from;
+  return s;
+}
+
+// ---------------------------------------------------------------------------
+// One page's operands from the three formats.  Bytes of channels and slots: internal.h and
+// the headers of the formats' kernels.
+// ---------------------------------------------------------------------------
+// First channel of K step ks in half h, and channel of its element e.
+template <int FMT>
+__device__ inline int k_channel(int ks, int h, int e) {
+  if (FMT == kBf16) return 64 * (ks / 4) + 32 * h + 8 * (ks % 4) + e;  // ks = 4 X + kc
+  if (FMT == kInt4) return 32 * (ks % 4) + 16 * (ks / 4) + 8 * h + e;
+  return 64 * h + 16 * (ks / 2) + 4 * (ks % 2) + e / 2 + 8 * (e % 2);
+}
+// Slot (of 8) of element e of a V step.
+template <int FMT>
+__host__ __device__ constexpr int v_slot(int e) {
+  return FMT == kInt2 ? (e & 4) + (e % 4) / 2 + 2 * (e % 2) : e;
+}
+// Channels of rows 8 k + 4 h .. + 3 of the four V tiles: f(first channel, four values).
+template <int FMT, class F>
+__device__ inline void each_four(const f16v (&o)[4], int h, F&& f) {
+  if (FMT == kInt2) {  // row r of tile C: channel 4 r + C
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f(4 * (8 * (i / 4) + 4 * h + i % 4), o[0][i], o[1][i], o[2][i], o[3][i]);
+  } else {
+#pragma unroll
+    for (int C = 0; C < 4; ++C)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = 8 * k + 4 * h;
+        const int c = FMT == kBf16 ? 32 * C + r : 64 * (C / 2) + 32 * (r / 16) + 16 * (C % 2) + r % 16;
+        f(c, o[C][4 * k], o[C][4 * k + 1], o[C][4 * k + 2], o[C][4 * k + 3]);
+      }
+  }
+}
+
+// Codes of a page as a wave loads them: raw K and V codes of `NK`, `NV` 16-byte loads, and
+// lane l's slot l: scale and zero of every group.
+template <int FMT, int NG>
+struct Raw {
+  static constexpr int kLoads = FMT == kInt4 ? 4 : 2;
+  u4v k[kLoads], v[kLoads];
+  uint32_t ks[NG], vs[NG];
+};
+constexpr int block_bytes_of(int fmt, int ng) {
+  return fmt == kBf16 ? kBfBlock : fmt == kInt4 ? kv4_block_bytes(ng) : block_bytes(ng);
+}
+template <int FMT, int NG>
+__device__ inline u4v load_k(const uint8_t* blk, int i) {  // kInt4: (T, X) = (i / 2, i % 2); kInt2: T = i
+  const int l = threadIdx.x & 63, lo = l & 15, b = (l >> 4) & 1, h = l >> 5;
+  const int off = FMT == kInt4 ? (64 * (2 * (i / 2) + b) + 16 * (h + 2 * (i % 2)) + lo) * 16
+                               : (4 * lo + 2 * i + b) * 32 + 16 * h;
+  return *reinterpret_cast<const u4v*>(blk + off);
+}
+template <int FMT, int NG>
+__device__ inline u4v load_v(const uint8_t* blk, int i) {  // kInt4: (jp, i2) = (i / 2, i % 2); kInt2: j0 = i
+  const int l = threadIdx.x & 63, lo = l & 15, jj = (l >> 4) & 1, h = l >> 5;
+  const int off = FMT == kInt4 ? kKv4CodeBytes + (64 * (2 * (i / 2) + jj) + 16 * (2 * h + i % 2) + lo) * 16
+                               : kOffVCodes + (l & 31) * 64 + 32 * i + 16 * h;
+  return *reinterpret_cast<const u4v*>(blk + off);
+}
+template <int FMT, int NG>
+__device__ inline void load_entries(const uint8_t* blk, uint32_t (&ks)[NG], uint32_t (&vs)[NG]) {
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const int at = FMT == kInt4 ? l * NG + g : g * kP + l;
+    const int koff = FMT == kInt4 ? kv4_sz_off(NG, 0) : kOffKSz, voff = FMT == kInt4 ? kv4_sz_off(NG, 1) : off_vsz(NG);
+    ks[g] = reinterpret_cast<const uint32_t*>(blk + koff)[at];
+    vs[g] = reinterpret_cast<const uint32_t*>(blk + voff)[at];
+  }
+}
+__device__ inline float meta_f32(uint32_t half, int bf16) {
+  return bf16 ? __uint_as_float(half << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)half);
+}
+
+// Scales of a page in LDS, a wave's own: per group the slots' (s 2^24, -s z), divided by the
+// page's power of two.  K: both halves of a dword, by slot.  V: arrays of fp16, eight slots of a
+// step in 16 bytes, in the order of the step's elements.
+template <int NG>
+struct Scales {
+  uint32_t k[NG][kP];
+  __align__(16) uint16_t va[NG][kP], vb[NG][kP];
+};
+// The exponent that a (scale, zero) pair needs: s 2^24 and |s z| below 2^15 after division by 2^e.
+__device__ inline int entry_exp(float s, float z) {
+  const int es = exp_of(s), ez = exp_of(z);
+  return max(es + 24, es + ez + 1) + 1 - 15;
+}
+constexpr int kNoExp = -400;
+// Reads the entries of slots < ntok, writes the scales; e_k: the page's exponent of K; e_v: the
+// accumulators' exponent, raised where the page needs it.
+template <int FMT, int NG>
+__device__ inline void make_scales(const uint32_t (&ks)[NG], const uint32_t (&vs)[NG], int bf16, int ntok,
+                                   Scales<NG>& sc, int& e_k, int& e_v) {
+  const int l = threadIdx.x & 63;
+  float s[2][NG], z[2][NG];
+  int e[2] = {kNoExp, kNoExp};
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const uint32_t w = x ? vs[g] : ks[g];
+      s[x][g] = l < ntok ? meta_f32(w & 0xffffu, bf16) : 0.0f;  // slots never written
+      z[x][g] = l < ntok ? meta_f32(w >> 16, bf16) : 0.0f;
+      if (l < ntok) e[x] = max(e[x], entry_exp(s[x][g], z[x][g]));
+    }
+  e_k = wave_max_i(e[0]);
+  e_v = max(e_v, wave_max_i(e[1]));
+  const int at = FMT == kInt2 ? (l & ~3) + 2 * (l & 1) + ((l >> 1) & 1) : l;  // v_slot's inverse
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    // in two steps: 2^(24 - e) may pass fp32's range where s 2^(24 - e) does not
+    const float k0 = ldexpf(s[0][g], -e_k), v0 = ldexpf(s[1][g], -e_v);
+    sc.k[g][l] = pack2<kInt4>(k0 * 0x1p24f, -k0 * z[0][g]);
+    const uint32_t v = pack2<kInt4>(v0 * 0x1p24f, -v0 * z[1][g]);
+    sc.va[g][at] = (uint16_t)v;
+    sc.vb[g][at] = (uint16_t)(v >> 16);
+  }
+}
+__device__ inline uint32_t fma_h2(uint32_t n, uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2, n), __builtin_bit_cast(h2, a),
+                                                                __builtin_bit_cast(h2, b)));
+}
+// K operand of step ks, tile T from its raw load.
+template <int FMT, int NG>
+__device__ inline u4v k_operand(const u4v& raw, int T, int ks, const Scales<NG>& sc) {
+  const int l = threadIdx.x & 63, lo = l & 15, b = (l >> 4) & 1, h = l >> 5;
+  constexpr int G = kD / NG;
+  const int g = FMT == kInt4 ? 32 * (ks % 4) / G : (64 * h + 16 * (ks / 2)) / G;
+  const uint32_t ab = sc.k[g][4 * lo + 2 * T + b];
+  const uint32_t A = __builtin_amdgcn_perm(ab, ab, 0x01000100u), B = __builtin_amdgcn_perm(ab, ab, 0x03020302u);
+  const uint32_t d = FMT == kInt4 ? raw[ks % 4] : raw[ks / 2] >> (8 * (ks % 2));
+  u4v r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = FMT == kInt4 ? fma_h2((d >> (4 * i)) & 0x000f000fu, A, B) : fma_h2((d >> (2 * i)) & 0x00030003u, A, B);
+  return r;
+}
+// V operand of tile C, step (j0, i2) from its raw load.
+template <int FMT, int NG>
+__device__ inline u4v v_operand(const u4v& raw, int C, int j0, int i2, const Scales<NG>& sc) {
+  const int l = threadIdx.x & 63, jj = (l >> 4) & 1, h = l >> 5;
+  constexpr int G = kD / NG;
+  const int c = FMT == kInt4 ? 64 * (C / 2) + 32 * jj : 4 * (l & 31);  // a channel of the row's group
+  const int t0 = 32 * j0 + 16 * h + 8 * i2;
+  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[c / G][t0]), B = *reinterpret_cast<const u4v*>(&sc.vb[c / G][t0]);
+  u4v r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t d = raw[FMT == kInt4 ? 2 * j0 + i / 2 : 2 * i2 + i / 2] >> (8 * (i % 2));
+    r[i] = FMT == kInt4 ? fma_h2((d >> (4 * (C % 2))) & 0x000f000fu, A[i], B[i])
+                        : fma_h2((d >> (2 * C)) & 0x00030003u, A[i], B[i]);
+  }
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// A wave's 32 rows.
+// ---------------------------------------------------------------------------
+struct RowState {
+  int pos;         // of the row's token; -1: no row
+  float m, l;      // reference maximum; this lane's part of the sum
+  float c;         // factor of the scores (log2 units)
+};
+
+// The query operands of the wave's rows (row: this lane's, live or not).  Quantized caches:
+// fp16 rows divided by a power of two, which c takes back.
+template <int FMT>
+__device__ inline void load_queries(const ChunkArgs& a, size_t row, bool live, u4v (&q)[8], float& c) {
+  const int h = (threadIdx.x & 63) >> 5;
+  if (FMT == kBf16) {
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;  // scores are multiplied by |scale|
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      q[ks] = live ? *reinterpret_cast<const u4v*>(a.q + row * kD + k_channel<FMT>(ks, h, 0)) : u4v{0, 0, 0, 0};
+      q[ks] ^= flip;
+    }
+    c = fmaxf(fabsf(a.scale), kLeast);
+  } else {
+    const float* src = a.qt + row * kD;
+    float x[8][8], top = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[ks][e] = live ? src[k_channel<FMT>(ks, h, e)] : 0.0f;
+        top = fmaxf(top, fabsf(x[ks][e]));
+      }
+    const int e = max(exp_of(half_max(top)), -60) - 13;  // |q| < 2^14
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        q[ks][i] = pack2<FMT>(ldexpf(x[ks][2 * i], -e), ldexpf(x[ks][2 * i + 1], -e));
+    c = pow2(e);
+  }
+}
+
+// Scores of a page in s -> the operands of P^T (HL: a second, smaller piece of each p), m and l
+// and the accumulators' scale moved.  cp: c of this page; t0: the page's first token.
+template <int FMT, bool HL>
+__device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, float cp, bool masked, int t0,
+                                    int window, int sinks, u4v (&p)[4], u4v (&pl)[4]) {
+  if (masked) {
+    const int h = (threadIdx.x & 63) >> 5;
+    const int first = r.pos - (t0 + 16 * h);       // last visible slot, from the half's first
+    const int after = (r.pos - window) - (t0 + 16 * h);  // slots up to it lie before the window
+    const int sink = sinks - (t0 + 16 * h);
+#pragma unroll
+    for (int T = 0; T < 2; ++T)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int t = 32 * (i / 4 % 2) + 4 * (i % 4) + 2 * T + i / 8;
+        const bool ok = t <= first && (t > after || t < sink);
+        s[T][i] = ok ? s[T][i] : -INFINITY;
+      }
+  }
+  float mx = s[0][0];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+  mx = half_max(mx) * cp;
+  const bool need = mx > r.m + kSlack;
+  if (__ballot(need) != 0ull) {
+    const float mn = fmaxf(r.m, mx);
+    const float alpha = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - mn);
+    r.m = mn;
+    r.l *= alpha;
+#pragma unroll
+    for (int C = 0; C < 4; ++C) o[C] *= alpha;
+  }
+  const float ms = r.m == -INFINITY ? 0.0f : -r.m;
+  float sum = 0.0f;
+#pragma unroll
+  for (int T = 0; T < 2; ++T)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[T][i] = __builtin_amdgcn_exp2f(fmaf(s[T][i], cp, ms));
+      sum += s[T][i];
+    }
+  r.l += sum;
+  auto at = [&](int j0, int i2, int e) {  // p of slot 32 j0 + 16 h + 8 i2 + v_slot(e)
+    const int x = v_slot<FMT>(e), u = x % 4;
+    return s[u / 2][8 * (u % 2) + 4 * j0 + 2 * i2 + x / 4];
+  };
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = at(k / 2, k % 2, 2 * i), y = at(k / 2, k % 2, 2 * i + 1);
+      p[k][i] = pack2<FMT>(x, y);
+      if (HL) pl[k][i] = pack2<FMT>(x - bf_lo(p[k][i]), y - bf_hi(p[k][i]));
+    }
+}
+
+// The row's output, or its partial state in slot s of its num_splits.  scale: of the accumulators.
+template <int FMT>
+__device__ inline void store_row(const ChunkArgs& a, size_t row, int s, bool direct, const f16v (&o)[4], float m,
+                                 float l, float scale, int h) {
+  if (direct) {
+    const float il = l > 0.0f ? 1.0f / l : l != l ? l : 0.0f;
+    uint16_t* dst = a.out + row * kD;
+    each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
+      uint2 v;
+      v.x = pack2<kBf16>(x * il, y * il);
+      v.y = pack2<kBf16>(z * il, w * il);
+      *reinterpret_cast<uint2*>(dst + c) = v;
+    });
+    return;
+  }
+  const size_t at = row * a.num_splits + s;
+  float* dst = a.part_o + at * kD;
+  if (l != l) m = 0.0f;  // NaN in a row: its scores have no maximum, but the state is not empty
+  if (m != -INFINITY)    // of an empty state only that is read
+    each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
+      *reinterpret_cast<float4*>(dst + c) = make_float4(x * scale, y * scale, z * scale, w * scale);
+    });
+  if (h == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, l);
+}
+
+// Pieces that a tile's pages are cut into: at least `least` pages each.
+__device__ inline int piece_count(int pages, int num_splits, int least) {
+  return min(num_splits, max(1, (pages + least - 1) / least));
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: 4 waves of 32 rows share every page through LDS, two pages deep.
+// ---------------------------------------------------------------------------
+constexpr int kPageLds = 2 * kP * kD * 2;  // operands of a page
+template <int FMT, int NG>
+__global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
+  constexpr int M = kRows * kWaves;
+  __shared__ __align__(16) uint8_t lds[2 * kPageLds];
+  __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : kWaves];
+  const int g = a.Hq / a.Hkv;
+  const int kvh = blockIdx.x % a.Hkv;
+  const int64_t rest = blockIdx.x / a.Hkv;
+  const int split = (int)(rest % a.num_splits);
+  // a sequence's last tiles, which see most, first
+  const int64_t n_ids = (int64_t)a.n_q * g / M + a.B;
+  const Tile t = find_tile(a, n_ids - 1 - rest / a.num_splits, g, M);
+  if (t.b < 0) return;
+  const int window = a.window > 0 ? min(a.window, kNoWindow) : kNoWindow;
+  const Pages pg = tile_pages(t, g, M, window, a.sinks);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+  const int r = t.row0 + w * kRows + n;
+  const bool live = r < t.rows;
+  const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
+  const int pieces = piece_count(pg.count, a.num_splits, 4);
+  const bool direct = FMT == kBf16 && a.num_splits == 1;
+  RowState rs;
+  rs.pos = live ? t.len - t.n + r / g : -1;
+  rs.m = -INFINITY;
+  rs.l = 0.0f;
+  f16v o[4];
+#pragma unroll
+  for (int C = 0; C < 4; ++C)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
+  int e_v = kNoExp;
+  if (split < pieces && pg.count > 0) {
+    u4v q[8];
+    load_queries<FMT>(a, row, live, q, rs.c);
+    const int x0 = (int)((int64_t)pg.count * split / pieces), x1 = (int)((int64_t)pg.count * (split + 1) / pieces);
+    const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
+    auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
+    auto block_of = [&](int x) {
+      return a.pages + ((size_t)bt[page_of(x)] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
+    };
+    // what this wave brings of a page
+    u4v raw_k, raw_v;
+    uint32_t ks[NG], vs[NG];
+    auto fetch = [&](int x, int buf) {
+      const uint8_t* blk = block_of(x);
+      if (FMT == kBf16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int at = (w * 8 + i) * 1024;
+          __builtin_amdgcn_global_load_lds(
+              (const __attribute__((address_space(1))) void*)(blk + at + l * 16),
+              (__attribute__((address_space(3))) void*)(lds + buf * kPageLds + at), 16, 0, 0);
+        }
+      } else {
+        raw_k = load_k<FMT, NG>(blk, FMT == kInt4 ? w : w / 2);
+        raw_v = load_v<FMT, NG>(blk, FMT == kInt4 ? w : w / 2);
+        load_entries<FMT, NG>(blk, ks, vs);
+      }
+    };
+    int e_k = 0, e_old = kNoExp;
+    // quantized: the operands that this wave makes of its loads, (tile, step) in 1 KB each
+    auto expand = [&](int x, int buf) {
+      if (FMT == kBf16) return;
+      const int ntok = min(t.len - page_of(x) * kP, kP);
+      e_old = e_v;
+      make_scales<FMT, NG>(ks, vs, a.meta_bf16, ntok, reinterpret_cast<Scales<NG>*>(scales)[w], e_k, e_v);
+      lane_exchange();
+      const Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
+      uint8_t* dst = lds + buf * kPageLds + l * 16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int T = w / 2, kst = 4 * (w % 2) + i;
+        const u4v k = k_operand<FMT, NG>(raw_k, T, kst, sc);
+        *reinterpret_cast<u4v*>(dst + (T * 8 + kst) * 1024) = k;
+        const int C = FMT == kInt4 ? 2 * (w / 2) + i % 2 : i;
+        const int j0 = FMT == kInt4 ? i / 2 : w / 2, i2 = w % 2;
+        const u4v v = v_operand<FMT, NG>(raw_v, C, j0, i2, sc);
+        *reinterpret_cast<u4v*>(dst + kPageLds / 2 + (C * 4 + 2 * j0 + i2) * 1024) = v;
+      }
+      lane_exchange();
+    };
+    fetch(x0, 0);
+    expand(x0, 0);
+    __syncthreads();
+    for (int x = x0; x < x1; ++x) {
+      const int buf = (x - x0) & 1;
+      const int t0 = page_of(x) * kP;
+      const float cp = FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast);
+      if (FMT != kBf16 && e_v != e_old && e_old != kNoExp) {
+        const float f = pow2(max(e_old - e_v, -126));
+#pragma unroll
+        for (int C = 0; C < 4; ++C) o[C] *= f;
+      }
+      if (x + 1 < x1) fetch(x + 1, buf ^ 1);
+      uint8_t* base = lds + buf * kPageLds;
+      if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
+        const int ntok = t.len - t0;
+        for (int i = threadIdx.x; i < kP * kD / 8; i += 256) {  // 16 bytes: slots 16 hi + 8 kt + e
+          const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
+          u4v& v = reinterpret_cast<u4v*>(base + kPageLds / 2)[i];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
+        }
+        __syncthreads();
+      }
+      const int lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
+      const int vlane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
+      f16v s[2];
+#pragma unroll
+      for (int T = 0; T < 2; ++T)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int T = 0; T < 2; ++T) {
+          const int off = FMT == kBf16 ? T * 8192 + (k % 4) * 1024 + (k / 4) * 512 : (T * 8 + k) * 1024;
+          s[T] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + lane + off), q[k], s[T]);
+        }
+      const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
+      u4v p[4], unused[4];
+      softmax_page<FMT, false>(s, o, rs, cp, masked, t0, window, a.sinks, p, unused);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int C = 0; C < 4; ++C) {
+          const int off = FMT == kBf16 ? C * 4096 + (k % 2) * 1024 + (k / 2) * 512 : (C * 4 + k) * 1024;
+          o[C] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + kPageLds / 2 + vlane + off), p[k], o[C]);
+        }
+      if (x + 1 < x1) expand(x + 1, buf ^ 1);
+      __syncthreads();
+    }
+  }
+  const float lt = half_sum(rs.l);
+  if (!live) return;
+  store_row<FMT>(a, row, split, direct, o, rs.m, lt, FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v), h);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: a block takes one tile of 32 rows, its waves every fourth page each, from global
+// memory straight to the operands; the waves' states are merged in LDS.
+// ---------------------------------------------------------------------------
+template <int FMT, int NG>
+__global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
+  constexpr int M = kRows;
+  constexpr bool HL = FMT == kBf16;  // p in two bf16 pieces: costs nothing where the loads bound
+  __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : kWaves];
+  __shared__ float os[kWaves][4][16][64];
+  __shared__ float2 ml[kWaves][kRows];
+  const int g = a.Hq / a.Hkv;
+  const int kvh = blockIdx.x % a.Hkv;
+  const int64_t rest = blockIdx.x / a.Hkv;
+  const int split = (int)(rest % a.num_splits);
+  const Tile t = find_tile(a, rest / a.num_splits, g, M);
+  if (t.b < 0) return;
+  const int window = a.window > 0 ? min(a.window, kNoWindow) : kNoWindow;
+  const Pages pg = tile_pages(t, g, M, window, a.sinks);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+  const int lo = l & 15, b16 = (l >> 4) & 1;
+  const int r = t.row0 + n;
+  const bool live = r < t.rows;
+  const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
+  const int pieces = piece_count(pg.count, a.num_splits, 4);
+  const bool direct = FMT == kBf16 && a.num_splits == 1;
+  RowState rs;
+  rs.pos = live ? t.len - t.n + r / g : -1;
+  rs.m = -INFINITY;
+  rs.l = 0.0f;
+  f16v o[4];
+#pragma unroll
+  for (int C = 0; C < 4; ++C)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
+  int e_v = kNoExp;
+  const bool any = split < pieces && pg.count > 0;
+  const int x0 = any ? (int)((int64_t)pg.count * split / pieces) : 0;
+  const int x1 = any ? (int)((int64_t)pg.count * (split + 1) / pieces) : 0;
+  if (x0 + w < x1) {
+    const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
+    auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
+    auto block_of = [&](int x) {
+      return a.pages + ((size_t)bt[page_of(x)] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
+    };
+    constexpr int kL = FMT == kBf16 ? 16 : Raw<FMT, NG>::kLoads;
+    u4v rk[kL], rv[kL];
+    uint32_t ks[NG], vs[NG];
+    auto fetch_k = [&](const uint8_t* blk) {
+#pragma unroll
+      for (int i = 0; i < kL; ++i) {
+        if (FMT == kBf16) {  // (T, ks) = (i / 8, i % 8)
+          const int off = (i / 8) * 8192 + (i % 4) * 1024 + (i / 4 % 2) * 512 + b16 * 4096 + h * 256 + lo * 16;
+          rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
+        } else {
+          rk[i] = load_k<FMT, NG>(blk, i);
+        }
+      }
+    };
+    auto fetch_v = [&](const uint8_t* blk) {
+#pragma unroll
+      for (int i = 0; i < kL; ++i) {
+        if (FMT == kBf16) {  // (C, step) = (i / 4, i % 4)
+          const int off = kPageLds / 2 + (i / 4) * 4096 + (i % 2) * 1024 + (i / 2 % 2) * 512 + b16 * 2048 + h * 256 +
+                          lo * 16;
+          rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
+        } else {
+          rv[i] = load_v<FMT, NG>(blk, i);
+        }
+      }
+    };
+    const uint8_t* blk = block_of(x0 + w);
+    fetch_k(blk);
+    if (FMT != kBf16) {
+      fetch_v(blk);
+      load_entries<FMT, NG>(blk, ks, vs);
+    }
+    u4v q[8];
+    load_queries<FMT>(a, row, live, q, rs.c);
+    Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
+    for (int x = x0 + w; x < x1; x += kWaves) {
+      const int t0 = page_of(x) * kP, ntok = t.len - t0;
+      const bool more = x + kWaves < x1;
+      const uint8_t* next = more ? block_of(x + kWaves) : blk;
+      int e_k = 0;
+      if (FMT == kBf16) {
+        fetch_v(blk);
+      } else {
+        const int e_old = e_v;
+        lane_exchange();  // the last page's scales have been read
+        make_scales<FMT, NG>(ks, vs, a.meta_bf16, min(ntok, kP), sc, e_k, e_v);
+        lane_exchange();
+        if (e_v != e_old && e_old != kNoExp) {
+          const float f = pow2(max(e_old - e_v, -126));
+#pragma unroll
+          for (int C = 0; C < 4; ++C) o[C] *= f;
+        }
+      }
+      f16v s[2];
+#pragma unroll
+      for (int T = 0; T < 2; ++T)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int T = 0; T < 2; ++T) {
+          u4v ka;
+          if constexpr (FMT == kBf16) ka = rk[8 * T + k];
+          else ka = k_operand<FMT, NG>(rk[FMT == kInt4 ? 2 * T + k / 4 : T], T, k, sc);
+          s[T] = mfma<FMT>(ka, q[k], s[T]);
+        }
+      if (FMT == kBf16 && more) fetch_k(next);
+      const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
+      u4v p[4], pl[4];
+      softmax_page<FMT, HL>(s, o, rs, FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast), masked, t0, window, a.sinks, p, pl);
+      if (FMT == kBf16 && ntok < kP) {  // slots never written weigh 0: their values may be anything
+#pragma unroll
+        for (int i = 0; i < kL; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int ts = 32 * (i / 2 % 2) + 16 * h + 8 * (i % 2) + 2 * j;
+            rv[i][j] &= (ts < ntok ? 0xffffu : 0u) | (ts + 1 < ntok ? 0xffff0000u : 0u);
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int C = 0; C < 4; ++C) {
+          u4v va;
+          if constexpr (FMT == kBf16) va = rv[4 * C + k];
+          else va = v_operand<FMT, NG>(rv[FMT == kInt4 ? 2 * (C / 2) + k % 2 : k / 2], C, k / 2, k % 2, sc);
+          if (HL) o[C] = mfma<FMT>(va, pl[k], o[C]);
+          o[C] = mfma<FMT>(va, p[k], o[C]);
+        }
+      if (FMT != kBf16 && more) {
+        fetch_k(next);
+        fetch_v(next);
+        load_entries<FMT, NG>(next, ks, vs);
+      }
+      blk = next;
+    }
+  }
+  // merge: wave w sums tile C = w of the four states
+  const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
+  const float lt = half_sum(rs.l);
+  // (NaN in a row: its scores have no maximum, but the state is not empty)
+  if (h == 0) ml[w][n] = make_float2(lt != lt ? 0.0f : rs.m, lt);
+#pragma unroll
+  for (int C = 0; C < 4; ++C)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) os[w][C][i][l] = o[C][i] * unit;
+  __syncthreads();
+  float m = -INFINITY, L = 0.0f, f[kWaves];
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) m = fmaxf(m, ml[k][n].x);
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    f[k] = ml[k][n].x == -INFINITY ? 0.0f : exp2f(ml[k][n].x - m);
+    L += f[k] * ml[k][n].y;
+  }
+  if (!live) return;
+  // each wave stores a quarter of the channels: registers 4 w .. 4 w + 3 of every tile
+  f16v sum[4];
+#pragma unroll
+  for (int C = 0; C < 4; ++C)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) v += f[k] != 0.0f ? f[k] * os[k][C][4 * w + i][l] : 0.0f;
+      sum[C][i] = v;
+    }
+  const float il = L > 0.0f ? 1.0f / L : L != L ? L : 0.0f;
+  const size_t at = row * a.num_splits + split;
+  auto put = [&](int c, float x, float y, float z, float v) {
+    if (direct) {
+      uint2 d;
+      d.x = pack2<kBf16>(x * il, y * il);
+      d.y = pack2<kBf16>(z * il, v * il);
+      *reinterpret_cast<uint2*>(a.out + row * kD + c) = d;
+    } else if (m != -INFINITY) {  // of an empty state only that is read
+      *reinterpret_cast<float4*>(a.part_o + at * kD + c) = make_float4(x, y, z, v);
+    }
+  };
+  const int rr = 8 * w + 4 * h;
+  if (FMT == kInt2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(4 * (rr + i), sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
+  } else {
+#pragma unroll
+    for (int C = 0; C < 4; ++C)
+      put(FMT == kBf16 ? 32 * C + rr : 64 * (C / 2) + 32 * (rr / 16) + 16 * (C % 2) + rr % 16, sum[C][0], sum[C][1],
+          sum[C][2], sum[C][3]);
+  }
+  if (!direct && w == 0 && h == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, L);
+}
+
+// Merge of the splits and back-rotation, of the rows that belong to a sequence.
+template <int RB>
+__global__ __launch_bounds__(kRedThreads) void chunk_reduce_kernel(ChunkArgs a, int row0, int n_rows) {
+  const int64_t used = (int64_t)min(max(a.q_start[a.B], 0), a.n_q) * a.Hq - row0;
+  const int rows = (int)(used < n_rows ? used : n_rows);
+  if (rows <= 0) return;
+  reduce_body<false, RB>(blockIdx.x, rows, a.num_splits, a.part_o + (size_t)row0 * a.num_splits * kD,
+                         a.part_ml + (size_t)row0 * a.num_splits * 2, a.Rv, a.out + (size_t)row0 * kD, 0, a.rph, a.Hq,
+                         a.Hkv);
+}
+
+template <int FMT, int NG>
+hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
+  const int g = a.Hq / a.Hkv;
+  const int M = chunk_tile_rows(a.format, a.n_q, a.B, g);
+  const int64_t blocks = ((int64_t)a.n_q * g / M + a.B) * a.num_splits * a.Hkv;
+  if (blocks > 0xffffff) return hipErrorInvalidValue;
+  if (M == kRows)
+    hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((chunk_kernel<FMT, NG>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || (FMT == kBf16 && a.num_splits == 1)) return e;
+  // rows in parts of whole tokens that a launch holds
+  const int per = launch_seqs(a.Hq);
+  return by_seqs(a.n_q, per, [&](int t0, int n) {
+    const int row0 = t0 * a.Hq, rows = n * a.Hq;
+    auto go = [&](auto rb) {
+      constexpr int RB = decltype(rb)::value;
+      hipLaunchKernelGGL((chunk_reduce_kernel<RB>), dim3((unsigned)query_blocks(n, a.Hq, a.Hkv, a.rph, RB)),
+                         dim3(kRedThreads), 0, st, a, row0, rows);
+    };
+    switch (reduce_rows(rows)) {
+      case 16: go(std::integral_constant<int, 16>{}); break;
+      case 8: go(std::integral_constant<int, 8>{}); break;
+      case 4: go(std::integral_constant<int, 4>{}); break;
+      default: go(std::integral_constant<int, 2>{});
+    }
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
+
+// Few rows a sequence: one tile of 32 takes them.
+int chunk_tile_rows(int format, int64_t n_q, int B, int heads_per_kv) {
+  return n_q * heads_per_kv <= (int64_t)kRows * B ? kRows : kRows * kWaves;
+}
+
+hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st) {
+  if (a.format == kBf16) return launch_fmt<kBf16, 1>(a, st);
+  if (a.format == kInt4)
+    return a.ng == 4 ? launch_fmt<kInt4, 4>(a, st) : a.ng == 2 ? launch_fmt<kInt4, 2>(a, st) : launch_fmt<kInt4, 1>(a, st);
+  return a.ng == 4 ? launch_fmt<kInt2, 4>(a, st) : a.ng == 2 ? launch_fmt<kInt2, 2>(a, st) : launch_fmt<kInt2, 1>(a, st);
+}
+
+}  // namespace oscar

@@ -265,6 +265,55 @@ hipError_t launch_bf16_split(const uint16_t* pages, int Hkv, int B, int Hq,
                              const int32_t* seq_lens, int num_splits, const float* qt,
                              float* part_o, float* part_ml, hipStream_t st);
 
+// New tokens' queries and keys: RMS norm per head and rotation by position, to rows of their
+// own (k_out) or, keys with values, into bf16 pages.  Strides in elements between tokens.
+struct RopeRows {
+  const uint16_t* q;  // null (Hq = 0): no queries
+  int64_t q_stride;
+  uint16_t* q_out;
+  const uint16_t* k;
+  int64_t k_stride;
+  uint16_t* k_out;
+  const uint16_t* v;
+  int64_t v_stride;
+  uint16_t* pages;  // null: k_out
+  const int64_t* slots;
+  const int64_t* positions;
+  int n_tok, Hq, Hkv;
+  const uint16_t* q_weight;
+  const uint16_t* k_weight;
+  float eps;
+  int rotary, interleaved;
+  const float* freq;
+  float factor;
+};
+hipError_t launch_rope(const RopeRows& a, hipStream_t st);
+
+// Attention of the newest tokens of every sequence over a paged cache.
+enum CacheFormat { kBf16 = 0, kInt4 = 1, kInt2 = 2 };
+struct ChunkArgs {
+  const uint8_t* pages;
+  int format, ng, meta_bf16;
+  int Hkv, Hq, B, n_q;
+  const uint16_t* q;   // bf16 [n_q][Hq][128] (bf16 cache)
+  const float* qt;     // rotated, scaled by sm_scale log2 e (quantized caches)
+  const int32_t* q_start;
+  const int32_t* block_table;
+  int max_pages;
+  const int32_t* seq_lens;
+  float scale;         // bf16 cache: sm_scale log2 e
+  int window, sinks;   // window 0: none
+  int num_splits;
+  float* part_o;       // [n_q Hq][num_splits][128]; bf16 cache with one split: unused
+  float* part_ml;
+  uint16_t* out;       // bf16 [n_q][Hq][128]
+  const float* Rv;
+  int rph;
+};
+// Query rows (token, head) of a sequence and KV head that a block takes.
+int chunk_tile_rows(int format, int64_t n_q, int B, int heads_per_kv);
+hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st);
+
 // Offline calibration.
 // Waves per block of the calibration attention kernel (32 queries each); a block
 // covers 32 * kCalibAttnWaves / hc queries of hc query heads.

@@ -921,6 +921,369 @@ int oscar_bf16_decode_attn(const oscar_layout* L, const void* pages, const void*
 }  // extern "C"
 
 // ---------------------------------------------------------------------------
+// Norm and rotation of new tokens' queries and keys
+// ---------------------------------------------------------------------------
+
+namespace {
+
+int check_rope(const oscar_layout* L, const oscar_rope* r) {
+  if (!r || !isfinite(r->attn_scale) || (r->interleaved != 0 && r->interleaved != 1)) return OSCAR_ERR_INVALID_ARG;
+  if (r->rotary_dim < 0 || r->rotary_dim > L->head_dim) return OSCAR_ERR_INVALID_ARG;
+  if (r->rotary_dim % 16 != 0) return OSCAR_ERR_UNSUPPORTED;
+  if (r->rotary_dim > 0 && (!r->inv_freq || !aligned(r->inv_freq, 16))) return OSCAR_ERR_INVALID_ARG;
+  return OSCAR_OK;
+}
+
+// Rows [n_tok][heads][d], a token's heads contiguous, `stride` elements between tokens.
+int check_rows(const void* x, int64_t stride, int64_t heads, int64_t d) {
+  if (!x || !aligned(x, 16) || stride < heads * d) return OSCAR_ERR_INVALID_ARG;
+  if (stride % 8 != 0 || stride > (1LL << 40)) return OSCAR_ERR_UNSUPPORTED;
+  return OSCAR_OK;
+}
+size_t rows_bytes(int64_t n, int64_t stride, int64_t heads, int64_t d) {
+  return (size_t)((n - 1) * stride + heads * d) * sizeof(uint16_t);
+}
+
+// No array of the first `written` shares bytes with another (null or empty ones aside).
+bool apart(const Span* s, int n, int written) {
+  for (int i = 0; i < written; ++i)
+    for (int j = 0; j < n; ++j)
+      if (i != j && s[i].at && s[j].at && s[i].bytes && s[j].bytes && share_bytes(s[i], s[j])) return false;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int oscar_rope_freqs(int32_t rotary_dim, double base, oscar_rope_scaling scaling, double factor,
+                     double original_len, double low, double high, float* inv_freq) {
+  if (rotary_dim < 2 || rotary_dim % 2 != 0 || rotary_dim > 65536 || !inv_freq || !isfinite(base) || base <= 1.0)
+    return OSCAR_ERR_INVALID_ARG;
+  if (scaling != OSCAR_ROPE_UNSCALED && scaling != OSCAR_ROPE_LINEAR && scaling != OSCAR_ROPE_BY_TURNS &&
+      scaling != OSCAR_ROPE_BY_INDEX)
+    return OSCAR_ERR_INVALID_ARG;
+  if (scaling != OSCAR_ROPE_UNSCALED && !(isfinite(factor) && factor > 0.0)) return OSCAR_ERR_INVALID_ARG;
+  const bool parts = scaling == OSCAR_ROPE_BY_TURNS || scaling == OSCAR_ROPE_BY_INDEX;
+  if (parts && !(isfinite(original_len) && original_len > 0.0 && isfinite(low) && isfinite(high) && low > 0.0 &&
+                 high > low))
+    return OSCAR_ERR_INVALID_ARG;
+  const int32_t n = rotary_dim / 2;
+  const double two_pi = 6.283185307179586476925;
+  // the (fractional) index whose pair makes `turns` turns over the original length
+  auto index_of = [&](double turns) { return rotary_dim * log(original_len / (turns * two_pi)) / (2.0 * log(base)); };
+  double i0 = 0.0, i1 = 0.0;
+  if (scaling == OSCAR_ROPE_BY_INDEX) {
+    i0 = std::max(floor(index_of(high)), 0.0);
+    i1 = std::min(ceil(index_of(low)), (double)rotary_dim - 1.0);
+    if (i0 >= i1) i1 = i0 + 0.001;
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    const double f = pow(base, -2.0 * i / rotary_dim);
+    double keep = 1.0;  // share of the unscaled frequency
+    if (scaling == OSCAR_ROPE_LINEAR) keep = 0.0;
+    if (scaling == OSCAR_ROPE_BY_TURNS) keep = (original_len * f / two_pi - low) / (high - low);
+    if (scaling == OSCAR_ROPE_BY_INDEX) keep = 1.0 - (i - i0) / (i1 - i0);
+    keep = std::min(std::max(keep, 0.0), 1.0);
+    inv_freq[i] = (float)(scaling == OSCAR_ROPE_UNSCALED ? f : f * keep + f / factor * (1.0 - keep));
+  }
+  return OSCAR_OK;
+}
+
+int oscar_qk_norm_rope(const oscar_layout* L, const oscar_rope* rope, const void* q, int64_t q_stride,
+                       void* q_out, int32_t Hq, const void* k, int64_t k_stride, void* k_out,
+                       const int64_t* positions, int32_t n_tok, const void* q_weight,
+                       const void* k_weight, float eps, void* stream) {
+  int st = check_layout(L);
+  if (st) return st;
+  if ((st = check_rope(L, rope))) return st;
+  if (n_tok < 0 || Hq < 1 || !isfinite(eps) || eps < 0.0f) return OSCAR_ERR_INVALID_ARG;
+  if (n_tok == 0) return OSCAR_OK;
+  const int64_t d = L->head_dim, Hkv = L->num_kv_heads;
+  if (!q_out || !k_out || !positions || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(positions, 8) ||
+      !aligned(q_weight, 16) || !aligned(k_weight, 16))
+    return OSCAR_ERR_INVALID_ARG;
+  if ((st = check_rows(q, q_stride, Hq, d)) || (st = check_rows(k, k_stride, Hkv, d))) return st;
+  if (Hq > 65535) return OSCAR_ERR_UNSUPPORTED;
+  // in place: a row is read and written by the same lanes
+  const bool q_in_place = q == q_out && q_stride == Hq * d, k_in_place = k == k_out && k_stride == Hkv * d;
+  const Span spans[] = {{q_out, rows_bytes(n_tok, Hq * d, Hq, d)},
+                        {k_out, rows_bytes(n_tok, Hkv * d, Hkv, d)},
+                        {q_in_place ? nullptr : q, rows_bytes(n_tok, q_stride, Hq, d)},
+                        {k_in_place ? nullptr : k, rows_bytes(n_tok, k_stride, Hkv, d)},
+                        {positions, (size_t)n_tok * 8},
+                        {q_weight, (size_t)d * 2},
+                        {k_weight, (size_t)d * 2},
+                        {rope->rotary_dim ? rope->inv_freq : nullptr, (size_t)rope->rotary_dim * 2}};
+  if (!apart(spans, 8, 2)) return OSCAR_ERR_INVALID_ARG;
+  RopeRows a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_stride = q_stride;
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k = static_cast<const uint16_t*>(k);
+  a.k_stride = k_stride;
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.positions = positions;
+  a.n_tok = n_tok;
+  a.Hq = Hq;
+  a.Hkv = L->num_kv_heads;
+  a.q_weight = static_cast<const uint16_t*>(q_weight);
+  a.k_weight = static_cast<const uint16_t*>(k_weight);
+  a.eps = eps;
+  a.rotary = rope->rotary_dim;
+  a.interleaved = rope->interleaved;
+  a.freq = rope->inv_freq;
+  a.factor = rope->attn_scale;
+  return hip_status(launch_rope(a, static_cast<hipStream_t>(stream)));
+}
+
+int oscar_bf16_kv_append_rope(const oscar_layout* L, void* pages, const oscar_rope* rope, const void* q,
+                              int64_t q_stride, void* q_out, int32_t Hq, const void* k_new,
+                              int64_t k_stride, const void* v_new, int64_t v_stride,
+                              const int64_t* slot_mapping, const int64_t* positions, int32_t n_tok,
+                              const void* q_weight, const void* k_weight, float eps, void* stream) {
+  int st = check_layout(L);
+  if (st) return st;
+  if ((st = check_rope(L, rope))) return st;
+  if (n_tok < 0 || Hq < 0 || !isfinite(eps) || eps < 0.0f) return OSCAR_ERR_INVALID_ARG;
+  if (n_tok == 0) return OSCAR_OK;
+  const int64_t d = L->head_dim, Hkv = L->num_kv_heads;
+  if (!pages || !slot_mapping || !positions || !aligned(pages, 16) || !aligned(slot_mapping, 8) ||
+      !aligned(positions, 8) || !aligned(q_weight, 16) || !aligned(k_weight, 16))
+    return OSCAR_ERR_INVALID_ARG;
+  if ((st = check_rows(k_new, k_stride, Hkv, d)) || (st = check_rows(v_new, v_stride, Hkv, d))) return st;
+  if (Hq > 0 && (!q_out || !aligned(q_out, 16))) return OSCAR_ERR_INVALID_ARG;
+  if (Hq > 0 && (st = check_rows(q, q_stride, Hq, d))) return st;
+  if (Hq > 65535) return OSCAR_ERR_UNSUPPORTED;
+  const bool in_place = Hq > 0 && q == q_out && q_stride == Hq * d;
+  const Span spans[] = {{pages, oscar_bf16_page_bytes(L) * (size_t)L->num_pages},
+                        {Hq ? q_out : nullptr, rows_bytes(n_tok, Hq * d, Hq, d)},
+                        {Hq && !in_place ? q : nullptr, rows_bytes(n_tok, q_stride, Hq, d)},
+                        {k_new, rows_bytes(n_tok, k_stride, Hkv, d)},
+                        {v_new, rows_bytes(n_tok, v_stride, Hkv, d)},
+                        {slot_mapping, (size_t)n_tok * 8},
+                        {positions, (size_t)n_tok * 8},
+                        {q_weight, (size_t)d * 2},
+                        {k_weight, (size_t)d * 2},
+                        {rope->rotary_dim ? rope->inv_freq : nullptr, (size_t)rope->rotary_dim * 2}};
+  if (!apart(spans, 10, 2)) return OSCAR_ERR_INVALID_ARG;
+  st = debug_check(L, stream, 0, nullptr, 0, nullptr, slot_mapping, n_tok, nullptr, 0);
+  if (st) return st;
+  RopeRows a = {};
+  a.q = Hq ? static_cast<const uint16_t*>(q) : nullptr;
+  a.q_stride = q_stride;
+  a.q_out = Hq ? static_cast<uint16_t*>(q_out) : nullptr;
+  a.k = static_cast<const uint16_t*>(k_new);
+  a.k_stride = k_stride;
+  a.v = static_cast<const uint16_t*>(v_new);
+  a.v_stride = v_stride;
+  a.pages = static_cast<uint16_t*>(pages);
+  a.slots = slot_mapping;
+  a.positions = positions;
+  a.n_tok = n_tok;
+  a.Hq = Hq;
+  a.Hkv = L->num_kv_heads;
+  a.q_weight = static_cast<const uint16_t*>(q_weight);
+  a.k_weight = static_cast<const uint16_t*>(k_weight);
+  a.eps = eps;
+  a.rotary = rope->rotary_dim;
+  a.interleaved = rope->interleaved;
+  a.freq = rope->inv_freq;
+  a.factor = rope->attn_scale;
+  return hip_status(launch_rope(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Attention of chunks over a paged cache
+// ---------------------------------------------------------------------------
+
+namespace {
+
+// Sizes of a call; resolves num_splits (0: default).
+int check_chunk_sizes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq, int32_t max_pages_per_seq,
+                      int32_t* num_splits) {
+  int st = check_layout(L);
+  if (st) return st;
+  if (n_q < 0 || *num_splits < 0 || max_pages_per_seq < 1) return OSCAR_ERR_INVALID_ARG;
+  if ((st = check_decode_common(L, B, Hq, 1))) return st;
+  if ((int64_t)max_pages_per_seq * L->page_size > (1LL << 30) || (int64_t)n_q * Hq > 0x7fffffffLL ||
+      *num_splits > 1024)
+    return OSCAR_ERR_UNSUPPORTED;
+  if (*num_splits == 0) *num_splits = oscar_chunk_default_splits(L, n_q, B, Hq, max_pages_per_seq);
+  return OSCAR_OK;
+}
+
+struct ChunkWs {
+  size_t qt_off, po_off, pml_off, total;
+};
+ChunkWs chunk_ws(int64_t n_q, int64_t Hq, int64_t S, bool quantized) {
+  const bool parts = quantized || S > 1;
+  ChunkWs w;
+  w.qt_off = 0;
+  w.po_off = quantized ? align256((size_t)(n_q * Hq) * kD * sizeof(float)) : 0;
+  w.pml_off = align256(w.po_off + (parts ? (size_t)(n_q * Hq) * S * kD * sizeof(float) : 0));
+  w.total = align256(w.pml_off + (parts ? (size_t)(n_q * Hq) * S * 2 * sizeof(float) : 0));
+  if (w.total == 0) w.total = 256;
+  return w;
+}
+
+// OSCAR_DEBUG: chunk boundaries ascending within n_q, lengths within the table's rows, ids of the
+// pages that a sequence's new tokens see within the pool.
+int chunk_debug_check(const oscar_layout* L, void* stream, int32_t n_q, int32_t B, const int32_t* q_start,
+                      const int32_t* block_table, int32_t max_pages, const int32_t* seq_lens, int32_t window,
+                      int32_t sinks) {
+  if (!debug_on()) return OSCAR_OK;
+  int st = hip_status(hipStreamSynchronize(static_cast<hipStream_t>(stream)));
+  if (st) return st;
+  std::vector<int32_t> qs, lens, bt;
+  if ((st = copy_to_host(qs, q_start, (int64_t)B + 1)) || (st = copy_to_host(lens, seq_lens, B)) ||
+      (st = copy_to_host(bt, block_table, (int64_t)B * max_pages)))
+    return st;
+  if (qs[0] != 0 || qs[(size_t)B] > n_q) return OSCAR_ERR_INVALID_ARG;
+  const int64_t P = L->page_size;
+  for (int32_t b = 0; b < B; ++b) {
+    const int64_t n = (int64_t)qs[(size_t)b + 1] - qs[(size_t)b], len = lens[(size_t)b];
+    if (n < 0 || len < 0 || len > (int64_t)max_pages * P) return OSCAR_ERR_INVALID_ARG;
+    if (n == 0) continue;
+    const int64_t start = window > 0 ? std::max<int64_t>(0, len - n + 1 - window) : 0;
+    const int64_t from = start / P, head = std::min((std::min<int64_t>(sinks, start) + P - 1) / P, from);
+    for (int64_t i = 0; i < (len + P - 1) / P; ++i) {
+      if (i >= head && i < from) continue;
+      const int32_t pg = bt[(size_t)b * max_pages + (size_t)i];
+      if (pg < 0 || pg >= L->num_pages) return OSCAR_ERR_INVALID_ARG;
+    }
+  }
+  return OSCAR_OK;
+}
+
+int chunk_attn(int format, const oscar_layout* L, const void* pages, const void* q, int32_t n_q, int32_t B,
+               int32_t Hq, const int32_t* q_start, const int32_t* block_table, int32_t max_pages_per_seq,
+               const int32_t* seq_lens, const float* R_k, const float* R_v, float sm_scale, int32_t window,
+               int32_t sinks, int32_t num_splits, void* workspace, size_t workspace_bytes, void* out,
+               void* stream) {
+  int st = check_chunk_sizes(L, n_q, B, Hq, max_pages_per_seq, &num_splits);
+  if (st) return st;
+  if (!isfinite(sm_scale) || window < 0 || sinks < 0) return OSCAR_ERR_INVALID_ARG;
+  if (n_q == 0) return OSCAR_OK;
+  if (!pages || !q || !q_start || !block_table || !seq_lens || !workspace || !out) return OSCAR_ERR_INVALID_ARG;
+  if (!aligned(pages, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256) ||
+      !aligned(q_start, 4) || !aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(R_k, 16) ||
+      !aligned(R_v, 16))
+    return OSCAR_ERR_INVALID_ARG;
+  const bool quantized = format != kBf16;
+  const ChunkWs ws = chunk_ws(n_q, Hq, num_splits, quantized);
+  if (workspace_bytes < ws.total) return OSCAR_ERR_WORKSPACE_TOO_SMALL;
+  const int g = Hq / L->num_kv_heads, M = chunk_tile_rows(format, n_q, B, g);
+  if (((int64_t)n_q * g / M + B) * num_splits * L->num_kv_heads > 0xffffff) return OSCAR_ERR_UNSUPPORTED;
+  const size_t rows = (size_t)n_q * Hq * kD * sizeof(uint16_t), rot = (size_t)kD * kD * sizeof(float) *
+                                                                      (L->rot_per_head ? L->num_kv_heads : 1);
+  const size_t page = format == kBf16 ? oscar_bf16_page_bytes(L) : format == kInt4 ? oscar_kv4_page_bytes(L)
+                                                                                   : oscar_page_bytes(L);
+  const Span spans[] = {{out, rows},
+                        {workspace, ws.total},
+                        {q, rows},
+                        {pages, page * (size_t)L->num_pages},
+                        {q_start, ((size_t)B + 1) * 4},
+                        {block_table, (size_t)B * max_pages_per_seq * 4},
+                        {seq_lens, (size_t)B * 4},
+                        {R_k, rot},
+                        {R_v, rot}};
+  if (!apart(spans, 9, 2)) return OSCAR_ERR_INVALID_ARG;
+  st = chunk_debug_check(L, stream, n_q, B, q_start, block_table, max_pages_per_seq, seq_lens, window, sinks);
+  if (st) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  ChunkArgs a = {};
+  a.pages = static_cast<const uint8_t*>(pages);
+  a.format = format;
+  a.ng = groups(L);
+  a.meta_bf16 = meta_bf16(L);
+  a.Hkv = L->num_kv_heads;
+  a.Hq = Hq;
+  a.B = B;
+  a.n_q = n_q;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_start = q_start;
+  a.block_table = block_table;
+  a.max_pages = max_pages_per_seq;
+  a.seq_lens = seq_lens;
+  a.scale = sm_scale * kLog2e;
+  a.window = window;
+  a.sinks = sinks;
+  a.num_splits = num_splits;
+  a.part_o = reinterpret_cast<float*>(base + ws.po_off);
+  a.part_ml = reinterpret_cast<float*>(base + ws.pml_off);
+  a.out = static_cast<uint16_t*>(out);
+  a.Rv = R_v;
+  a.rph = L->rot_per_head;
+  if (quantized) {
+    float* qt = reinterpret_cast<float*>(base + ws.qt_off);
+    st = hip_status(launch_decode_prepare(a.q, n_q, Hq, R_k, a.scale, qt, hs, L->rot_per_head, L->num_kv_heads));
+    if (st) return st;
+    a.qt = qt;
+  }
+  return hip_status(launch_chunk_attn(a, hs));
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t oscar_chunk_default_splits(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
+                                   int32_t max_pages_per_seq) {
+  if (check_decode_common(L, B, Hq, 1) != OSCAR_OK || n_q < 1 || max_pages_per_seq < 1) return 1;
+  const int64_t g = Hq / L->num_kv_heads;
+  const int M = chunk_tile_rows(kBf16, n_q, B, (int)g);
+  // tiles as they come when the sequences' chunks are alike
+  const int64_t per_seq = (int64_t)n_q * g / B;
+  const int64_t tiles = B * std::max<int64_t>(1, (per_seq + M - 1) / M) * L->num_kv_heads;
+  // blocks: 4 for each that the GPU holds at once (one of the few-row kernel per CU, two of
+  // the other), and 16 pages at least for a block
+  const int64_t want = (int64_t)device_cus() * (M == 32 ? 4 : 8);
+  const int64_t s = std::min(want / tiles, (int64_t)max_pages_per_seq / 16);
+  return (int32_t)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
+}
+
+size_t oscar_chunk_workspace_bytes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
+                                   int32_t max_pages_per_seq, int32_t num_splits, int32_t quantized) {
+  if (check_chunk_sizes(L, n_q, B, Hq, max_pages_per_seq, &num_splits) != OSCAR_OK) return 0;
+  return chunk_ws(n_q, Hq, num_splits, quantized != 0).total;
+}
+
+int oscar_bf16_chunk_attn(const oscar_layout* L, const void* pages, const void* q, int32_t n_q, int32_t B,
+                          int32_t Hq, const int32_t* q_start, const int32_t* block_table,
+                          int32_t max_pages_per_seq, const int32_t* seq_lens, float sm_scale,
+                          int32_t window, int32_t sinks, int32_t num_splits, void* workspace,
+                          size_t workspace_bytes, void* out, void* stream) {
+  return chunk_attn(kBf16, L, pages, q, n_q, B, Hq, q_start, block_table, max_pages_per_seq, seq_lens, nullptr,
+                    nullptr, sm_scale, window, sinks, num_splits, workspace, workspace_bytes, out, stream);
+}
+
+int oscar_kv4_chunk_attn(const oscar_layout* L, const void* pages, const void* q, int32_t n_q, int32_t B,
+                         int32_t Hq, const int32_t* q_start, const int32_t* block_table,
+                         int32_t max_pages_per_seq, const int32_t* seq_lens, const float* R_k,
+                         const float* R_v, float sm_scale, int32_t window, int32_t sinks,
+                         int32_t num_splits, void* workspace, size_t workspace_bytes, void* out,
+                         void* stream) {
+  return chunk_attn(kInt4, L, pages, q, n_q, B, Hq, q_start, block_table, max_pages_per_seq, seq_lens, R_k, R_v,
+                    sm_scale, window, sinks, num_splits, workspace, workspace_bytes, out, stream);
+}
+
+int oscar_chunk_attn(const oscar_layout* L, const void* pages, const void* q, int32_t n_q, int32_t B,
+                     int32_t Hq, const int32_t* q_start, const int32_t* block_table,
+                     int32_t max_pages_per_seq, const int32_t* seq_lens, const float* R_k,
+                     const float* R_v, float sm_scale, int32_t window, int32_t sinks,
+                     int32_t num_splits, void* workspace, size_t workspace_bytes, void* out,
+                     void* stream) {
+  return chunk_attn(kInt2, L, pages, q, n_q, B, Hq, q_start, block_table, max_pages_per_seq, seq_lens, R_k, R_v,
+                    sm_scale, window, sinks, num_splits, workspace, workspace_bytes, out, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
 // Offline calibration
 // ---------------------------------------------------------------------------
 
