@@ -596,8 +596,8 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  * they were.  Pages of the block table that no new token of the sequence sees are not read, and
  * their entries may be anything.  Slots past a sequence's length may hold anything.
  * Products of bf16 values are exact, their sums, softmax statistics and outputs' sums are fp32.
- * Softmax weights enter the value product rounded to bf16 (with at most 32 (token, head) rows per
- * sequence and KV head on average: to two bf16 pieces); over a quantized cache weights, rotated
+ * Softmax weights enter the value product rounded to bf16 (to two bf16 pieces where n_q Hq/Hkv is
+ * at most 32 B); over a quantized cache weights, rotated
  * queries and dequantized values enter as fp16, scaled by powers of two per row and page.  There
  * |q~| log2(e) sm_scale and the scales must stay below 2^56.
  *   q           : bf16 [n_q, Hq, d]; Hq % Hkv == 0, Hq/Hkv <= 16

@@ -779,9 +779,8 @@ __global__ __launch_bounds__(kRedThreads) void chunk_reduce_kernel(ChunkArgs a, 
 template <int FMT, int NG>
 hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
   const int g = a.Hq / a.Hkv;
-  const int M = chunk_tile_rows(a.format, a.n_q, a.B, g);
+  const int M = chunk_tile_rows(a.n_q, a.B, g);
   const int64_t blocks = ((int64_t)a.n_q * g / M + a.B) * a.num_splits * a.Hkv;
-  if (blocks > 0xffffff) return hipErrorInvalidValue;
   if (M == kRows)
     hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3((unsigned)blocks), dim3(256), 0, st, a);
   else
@@ -810,7 +809,7 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
 }  // namespace
 
 // Few rows a sequence: one tile of 32 takes them.
-int chunk_tile_rows(int format, int64_t n_q, int B, int heads_per_kv) {
+int chunk_tile_rows(int64_t n_q, int B, int heads_per_kv) {
   return n_q * heads_per_kv <= (int64_t)kRows * B ? kRows : kRows * kWaves;
 }
 

@@ -311,7 +311,7 @@ struct ChunkArgs {
   int rph;
 };
 // Query rows (token, head) of a sequence and KV head that a block takes.
-int chunk_tile_rows(int format, int64_t n_q, int B, int heads_per_kv);
+int chunk_tile_rows(int64_t n_q, int B, int heads_per_kv);
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st);
 
 // Offline calibration.

@@ -1112,7 +1112,9 @@ int check_chunk_sizes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
       *num_splits > 1024)
     return OSCAR_ERR_UNSUPPORTED;
   if (*num_splits == 0) *num_splits = oscar_chunk_default_splits(L, n_q, B, Hq, max_pages_per_seq);
-  return OSCAR_OK;
+  // a launch holds fewer than 2^32 threads
+  const int64_t g = Hq / L->num_kv_heads, M = chunk_tile_rows(n_q, B, (int)g);
+  return (n_q * g / M + B) * *num_splits * L->num_kv_heads > 0xffffff ? OSCAR_ERR_UNSUPPORTED : OSCAR_OK;
 }
 
 struct ChunkWs {
@@ -1175,8 +1177,6 @@ int chunk_attn(int format, const oscar_layout* L, const void* pages, const void*
   const bool quantized = format != kBf16;
   const ChunkWs ws = chunk_ws(n_q, Hq, num_splits, quantized);
   if (workspace_bytes < ws.total) return OSCAR_ERR_WORKSPACE_TOO_SMALL;
-  const int g = Hq / L->num_kv_heads, M = chunk_tile_rows(format, n_q, B, g);
-  if (((int64_t)n_q * g / M + B) * num_splits * L->num_kv_heads > 0xffffff) return OSCAR_ERR_UNSUPPORTED;
   const size_t rows = (size_t)n_q * Hq * kD * sizeof(uint16_t), rot = (size_t)kD * kD * sizeof(float) *
                                                                       (L->rot_per_head ? L->num_kv_heads : 1);
   const size_t page = format == kBf16 ? oscar_bf16_page_bytes(L) : format == kInt4 ? oscar_kv4_page_bytes(L)
@@ -1235,7 +1235,7 @@ int32_t oscar_chunk_default_splits(const oscar_layout* L, int32_t n_q, int32_t B
                                    int32_t max_pages_per_seq) {
   if (check_decode_common(L, B, Hq, 1) != OSCAR_OK || n_q < 1 || max_pages_per_seq < 1) return 1;
   const int64_t g = Hq / L->num_kv_heads;
-  const int M = chunk_tile_rows(kBf16, n_q, B, (int)g);
+  const int M = chunk_tile_rows(n_q, B, (int)g);
   // tiles as they come when the sequences' chunks are alike
   const int64_t per_seq = (int64_t)n_q * g / B;
   const int64_t tiles = B * std::max<int64_t>(1, (per_seq + M - 1) / M) * L->num_kv_heads;
