@@ -175,14 +175,8 @@ __device__ inline void each_four(const f16v (&o)[4], int h, F&& f) {
   }
 }
 
-// Codes of a page as a wave loads them: raw K and V codes of `NK`, `NV` 16-byte loads, and
-// lane l's slot l: scale and zero of every group.
-template <int FMT, int NG>
-struct Raw {
-  static constexpr int kLoads = FMT == kInt4 ? 4 : 2;
-  u4v k[kLoads], v[kLoads];
-  uint32_t ks[NG], vs[NG];
-};
+template <int FMT>
+constexpr int raw_loads() { return FMT == kInt4 ? 4 : 2; }  // 16-byte loads of a wave for K's codes, and for V's
 constexpr int block_bytes_of(int fmt, int ng) {
   return fmt == kBf16 ? kBfBlock : fmt == kInt4 ? kv4_block_bytes(ng) : block_bytes(ng);
 }
@@ -200,15 +194,15 @@ __device__ inline u4v load_v(const uint8_t* blk, int i) {  // kInt4: (jp, i2) = 
                                : kOffVCodes + (l & 31) * 64 + 32 * i + 16 * h;
   return *reinterpret_cast<const u4v*>(blk + off);
 }
+// Lane l's slot l: scale and zero of every group, of K or of V.
 template <int FMT, int NG>
-__device__ inline void load_entries(const uint8_t* blk, uint32_t (&ks)[NG], uint32_t (&vs)[NG]) {
+__device__ inline void load_entries(const uint8_t* blk, int is_v, uint32_t (&x)[NG]) {
   const int l = threadIdx.x & 63;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const int at = FMT == kInt4 ? l * NG + g : g * kP + l;
-    const int koff = FMT == kInt4 ? kv4_sz_off(NG, 0) : kOffKSz, voff = FMT == kInt4 ? kv4_sz_off(NG, 1) : off_vsz(NG);
-    ks[g] = reinterpret_cast<const uint32_t*>(blk + koff)[at];
-    vs[g] = reinterpret_cast<const uint32_t*>(blk + voff)[at];
+    const int off = FMT == kInt4 ? kv4_sz_off(NG, is_v) : is_v ? off_vsz(NG) : kOffKSz;
+    x[g] = reinterpret_cast<const uint32_t*>(blk + off)[at];
   }
 }
 __device__ inline float meta_f32(uint32_t half, int bf16) {
@@ -229,34 +223,30 @@ __device__ inline int entry_exp(float s, float z) {
   return max(es + 24, es + ez + 1) + 1 - 15;
 }
 constexpr int kNoExp = -400;
-// Reads the entries of slots < ntok, writes the scales; e_k: the page's exponent of K; e_v: the
-// accumulators' exponent, raised where the page needs it.
+// The entries of slots < ntok to scales; e: the exponent, raised where the page needs it.
 template <int FMT, int NG>
-__device__ inline void make_scales(const uint32_t (&ks)[NG], const uint32_t (&vs)[NG], int bf16, int ntok,
-                                   Scales<NG>& sc, int& e_k, int& e_v) {
+__device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16, int ntok, Scales<NG>& sc, int& e) {
   const int l = threadIdx.x & 63;
-  float s[2][NG], z[2][NG];
-  int e[2] = {kNoExp, kNoExp};
+  float s[NG], z[NG];
+  int need = kNoExp;
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const uint32_t w = x ? vs[g] : ks[g];
-      s[x][g] = l < ntok ? meta_f32(w & 0xffffu, bf16) : 0.0f;  // slots never written
-      z[x][g] = l < ntok ? meta_f32(w >> 16, bf16) : 0.0f;
-      if (l < ntok) e[x] = max(e[x], entry_exp(s[x][g], z[x][g]));
-    }
-  e_k = wave_max_i(e[0]);
-  e_v = max(e_v, wave_max_i(e[1]));
+  for (int g = 0; g < NG; ++g) {
+    s[g] = l < ntok ? meta_f32(ent[g] & 0xffffu, bf16) : 0.0f;  // slots never written
+    z[g] = l < ntok ? meta_f32(ent[g] >> 16, bf16) : 0.0f;
+    if (l < ntok) need = max(need, entry_exp(s[g], z[g]));
+  }
+  e = max(e, wave_max_i(need));
   const int at = FMT == kInt2 ? (l & ~3) + 2 * (l & 1) + ((l >> 1) & 1) : l;  // v_slot's inverse
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    // in two steps: 2^(24 - e) may pass fp32's range where s 2^(24 - e) does not
-    const float k0 = ldexpf(s[0][g], -e_k), v0 = ldexpf(s[1][g], -e_v);
-    sc.k[g][l] = pack2<kInt4>(k0 * 0x1p24f, -k0 * z[0][g]);
-    const uint32_t v = pack2<kInt4>(v0 * 0x1p24f, -v0 * z[1][g]);
-    sc.va[g][at] = (uint16_t)v;
-    sc.vb[g][at] = (uint16_t)(v >> 16);
+    const float x = ldexpf(s[g], -e);
+    const uint32_t ab = pack2<kInt4>(x * 0x1p24f, -x * z[g]);
+    if (is_v) {
+      sc.va[g][at] = (uint16_t)ab;
+      sc.vb[g][at] = (uint16_t)(ab >> 16);
+    } else {
+      sc.k[g][l] = ab;
+    }
   }
 }
 __device__ inline uint32_t fma_h2(uint32_t n, uint32_t a, uint32_t b) {
@@ -338,25 +328,26 @@ __device__ inline void load_queries(const ChunkArgs& a, size_t row, bool live, u
   }
 }
 
+// Scores of tokens that the row does not see: -inf.  t0: the page's first token.
+__device__ inline void mask_page(f16v (&s)[2], int pos, int t0, int window, int sinks) {
+  const int h = (threadIdx.x & 63) >> 5;
+  const int last = pos - (t0 + 16 * h);              // last visible slot, from the half's first
+  const int before = (pos - window) - (t0 + 16 * h);  // slots up to it lie before the window
+  const int sink = sinks - (t0 + 16 * h);
+#pragma unroll
+  for (int T = 0; T < 2; ++T)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int t = 32 * (i / 4 % 2) + 4 * (i % 4) + 2 * T + i / 8;
+      const bool ok = t <= last && (t > before || t < sink);
+      s[T][i] = ok ? s[T][i] : -INFINITY;
+    }
+}
+
 // Scores of a page in s -> the operands of P^T (HL: a second, smaller piece of each p), m and l
-// and the accumulators' scale moved.  cp: c of this page; t0: the page's first token.
+// and the accumulators' scale moved.  cp: c of this page.
 template <int FMT, bool HL>
-__device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, float cp, bool masked, int t0,
-                                    int window, int sinks, u4v (&p)[4], u4v (&pl)[4]) {
-  if (masked) {
-    const int h = (threadIdx.x & 63) >> 5;
-    const int first = r.pos - (t0 + 16 * h);       // last visible slot, from the half's first
-    const int after = (r.pos - window) - (t0 + 16 * h);  // slots up to it lie before the window
-    const int sink = sinks - (t0 + 16 * h);
-#pragma unroll
-    for (int T = 0; T < 2; ++T)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int t = 32 * (i / 4 % 2) + 4 * (i % 4) + 2 * T + i / 8;
-        const bool ok = t <= first && (t > after || t < sink);
-        s[T][i] = ok ? s[T][i] : -INFINITY;
-      }
-  }
+__device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, float cp, u4v (&p)[4], u4v (&pl)[4]) {
   float mx = s[0][0];
 #pragma unroll
   for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
@@ -424,15 +415,40 @@ __device__ inline int piece_count(int pages, int num_splits, int least) {
   return min(num_splits, max(1, (pages + least - 1) / least));
 }
 
+// 16 bytes a lane from global memory to LDS, lane l's to dst + 16 l (dst: the wave's, a byte
+// address in LDS).  As inline asm, since the compiler, which cannot tell the slots of a buffer
+// apart, waits for every such load before the next LDS read of any of them; it has no outputs,
+// and the barrier that hands a slot over waits for it (wait_loads).
+__device__ inline void load_to_lds(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
+}
+// Waits until at most N of the wave's loads are under way.
+template <int N>
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// A barrier that waits for the waves' LDS accesses, and leaves loads under way alone.
+__device__ inline void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ inline uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
 // ---------------------------------------------------------------------------
-// Many rows: 4 waves of 32 rows share every page through LDS, two pages deep.
+// Many rows: W waves of 32 rows share every page through LDS.
 // ---------------------------------------------------------------------------
-constexpr int kPageLds = 2 * kP * kD * 2;  // operands of a page
-template <int FMT, int NG>
-__global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
-  constexpr int M = kRows * kWaves;
-  __shared__ __align__(16) uint8_t lds[2 * kPageLds];
-  __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : kWaves];
+constexpr int kHalfLds = kP * kD * 2;    // operands of a page's K or V
+constexpr int kPageLds = 2 * kHalfLds;
+template <int FMT, int NG, int W>
+__global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
+  constexpr int M = kRows * W;
+  constexpr int kSlots = FMT == kBf16 && W == 8 ? 3 : 2;
+  __shared__ __align__(16) uint8_t lds[kSlots * kPageLds];
+  __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : W];
+  __shared__ int exps[2][2];  // of the slots: K's exponent, the accumulators'
   const int g = a.Hq / a.Hkv;
   const int kvh = blockIdx.x % a.Hkv;
   const int64_t rest = blockIdx.x / a.Hkv;
@@ -458,7 +474,7 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
   for (int C = 0; C < 4; ++C)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
-  int e_v = kNoExp;
+  int e_o = kNoExp;  // the accumulators' exponent
   if (split < pieces && pg.count > 0) {
     u4v q[8];
     load_queries<FMT>(a, row, live, q, rs.c);
@@ -468,74 +484,101 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
     auto block_of = [&](int x) {
       return a.pages + ((size_t)bt[page_of(x)] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
     };
-    // what this wave brings of a page
-    u4v raw_k, raw_v;
-    uint32_t ks[NG], vs[NG];
-    auto fetch = [&](int x, int buf) {
+    // bf16: this wave's part of a page, straight to LDS
+    constexpr int kLoads = 32 / W;
+    auto fetch = [&](int x, int slot) {
+      const uint8_t* src = block_of(x) + w * kLoads * 1024 + l * 16;
+      const uint32_t dst = lds_address(lds) + slot * kPageLds + w * kLoads * 1024;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, __builtin_amdgcn_readfirstlane(dst + i * 1024));
+    };
+    // codes: a page in eight parts, K's four and V's four, of 4 operands of 1 KB each; a wave loads
+    // its parts to registers and a page later makes the operands
+    constexpr int kParts = 8 / W;
+    u4v raw[kParts];
+    uint32_t ent[kParts][NG];
+    int e_v = kNoExp;
+    auto load_codes = [&](int x) {
       const uint8_t* blk = block_of(x);
-      if (FMT == kBf16) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int at = (w * 8 + i) * 1024;
-          __builtin_amdgcn_global_load_lds(
-              (const __attribute__((address_space(1))) void*)(blk + at + l * 16),
-              (__attribute__((address_space(3))) void*)(lds + buf * kPageLds + at), 16, 0, 0);
-        }
-      } else {
-        raw_k = load_k<FMT, NG>(blk, FMT == kInt4 ? w : w / 2);
-        raw_v = load_v<FMT, NG>(blk, FMT == kInt4 ? w : w / 2);
-        load_entries<FMT, NG>(blk, ks, vs);
+      for (int j = 0; j < kParts; ++j) {
+        const int part = (W * j + w) % 4, is_v = (W * j + w) / 4;
+        const int i = FMT == kInt4 ? part : part / 2;
+        raw[j] = is_v ? load_v<FMT, NG>(blk, i) : load_k<FMT, NG>(blk, i);
+        load_entries<FMT, NG>(blk, is_v, ent[j]);
       }
     };
-    int e_k = 0, e_old = kNoExp;
-    // quantized: the operands that this wave makes of its loads, (tile, step) in 1 KB each
-    auto expand = [&](int x, int buf) {
-      if (FMT == kBf16) return;
+    auto expand = [&](int x, int slot) {
       const int ntok = min(t.len - page_of(x) * kP, kP);
-      e_old = e_v;
-      make_scales<FMT, NG>(ks, vs, a.meta_bf16, ntok, reinterpret_cast<Scales<NG>*>(scales)[w], e_k, e_v);
-      lane_exchange();
-      const Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
-      uint8_t* dst = lds + buf * kPageLds + l * 16;
+      Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
+      uint8_t* dst = lds + slot * kPageLds + l * 16;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int T = w / 2, kst = 4 * (w % 2) + i;
-        const u4v k = k_operand<FMT, NG>(raw_k, T, kst, sc);
-        *reinterpret_cast<u4v*>(dst + (T * 8 + kst) * 1024) = k;
-        const int C = FMT == kInt4 ? 2 * (w / 2) + i % 2 : i;
-        const int j0 = FMT == kInt4 ? i / 2 : w / 2, i2 = w % 2;
-        const u4v v = v_operand<FMT, NG>(raw_v, C, j0, i2, sc);
-        *reinterpret_cast<u4v*>(dst + kPageLds / 2 + (C * 4 + 2 * j0 + i2) * 1024) = v;
+      for (int j = 0; j < kParts; ++j) {
+        const int part = (W * j + w) % 4, is_v = (W * j + w) / 4;
+        lane_exchange();
+        int e = is_v ? e_v : kNoExp;
+        make_scales<FMT, NG>(ent[j], is_v, a.meta_bf16, ntok, sc, e);
+        if (is_v) e_v = e;
+        if (part == 0 && l == 0) exps[is_v][slot] = e;
+        lane_exchange();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (is_v) {
+            const int C = FMT == kInt4 ? 2 * (part / 2) + i % 2 : i;
+            const int j0 = FMT == kInt4 ? i / 2 : part / 2, i2 = part % 2;
+            *reinterpret_cast<u4v*>(dst + kHalfLds + (C * 4 + 2 * j0 + i2) * 1024) =
+                v_operand<FMT, NG>(raw[j], C, j0, i2, sc);
+          } else {
+            const int T = part / 2, ks = 4 * (part % 2) + i;
+            *reinterpret_cast<u4v*>(dst + (T * 8 + ks) * 1024) = k_operand<FMT, NG>(raw[j], T, ks, sc);
+          }
+        }
       }
-      lane_exchange();
     };
-    fetch(x0, 0);
-    expand(x0, 0);
-    __syncthreads();
+    if (FMT == kBf16) {
+      fetch(x0, 0);
+      wait_loads<0>();
+      if (kSlots == 3 && x0 + 1 < x1) fetch(x0 + 1, 1);
+    } else {
+      load_codes(x0);
+      expand(x0, 0);
+    }
+    lds_barrier();
+    int slot = 0;
     for (int x = x0; x < x1; ++x) {
-      const int buf = (x - x0) & 1;
       const int t0 = page_of(x) * kP;
-      const float cp = FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast);
-      if (FMT != kBf16 && e_v != e_old && e_old != kNoExp) {
-        const float f = pow2(max(e_old - e_v, -126));
-#pragma unroll
-        for (int C = 0; C < 4; ++C) o[C] *= f;
+      const bool next = x + 1 < x1;
+      const int ahead = slot + kSlots - 1 >= kSlots ? slot - 1 : slot + kSlots - 1;  // the slot that is free
+      if (FMT == kBf16) {
+        if (x + kSlots - 1 < x1) fetch(x + kSlots - 1, ahead);
+      } else if (next) {
+        load_codes(x + 1);
       }
-      if (x + 1 < x1) fetch(x + 1, buf ^ 1);
-      uint8_t* base = lds + buf * kPageLds;
+      float cp = rs.c;
+      if (FMT != kBf16) {
+        cp = fmaxf(rs.c * pow2(__builtin_amdgcn_readfirstlane(exps[0][slot])), kLeast);
+        const int e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
+        if (e != e_o && e_o != kNoExp) {
+          const float f = pow2(max(e_o - e, -126));
+#pragma unroll
+          for (int C = 0; C < 4; ++C) o[C] *= f;
+        }
+        e_o = e;
+      }
+      uint8_t* base = lds + slot * kPageLds;
       if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
         const int ntok = t.len - t0;
-        for (int i = threadIdx.x; i < kP * kD / 8; i += 256) {  // 16 bytes: slots 16 hi + 8 kt + e
+        for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
           const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
-          u4v& v = reinterpret_cast<u4v*>(base + kPageLds / 2)[i];
+          u4v& v = reinterpret_cast<u4v*>(base + kHalfLds)[i];
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
         }
-        __syncthreads();
+        lds_barrier();
       }
-      const int lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
-      const int vlane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
+      const int k_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
+      const int v_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
       f16v s[2];
 #pragma unroll
       for (int T = 0; T < 2; ++T)
@@ -546,25 +589,32 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
 #pragma unroll
         for (int T = 0; T < 2; ++T) {
           const int off = FMT == kBf16 ? T * 8192 + (k % 4) * 1024 + (k / 4) * 512 : (T * 8 + k) * 1024;
-          s[T] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + lane + off), q[k], s[T]);
+          s[T] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + k_lane + off), q[k], s[T]);
         }
-      const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
+      if (t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks))
+        mask_page(s, rs.pos, t0, window, a.sinks);
       u4v p[4], unused[4];
-      softmax_page<FMT, false>(s, o, rs, cp, masked, t0, window, a.sinks, p, unused);
+      softmax_page<FMT, false>(s, o, rs, cp, p, unused);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int C = 0; C < 4; ++C) {
           const int off = FMT == kBf16 ? C * 4096 + (k % 2) * 1024 + (k / 2) * 512 : (C * 4 + k) * 1024;
-          o[C] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + kPageLds / 2 + vlane + off), p[k], o[C]);
+          o[C] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + kHalfLds + v_lane + off), p[k], o[C]);
         }
-      if (x + 1 < x1) expand(x + 1, buf ^ 1);
-      __syncthreads();
+      if (FMT == kBf16) {  // page x + 1 has landed
+        if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
+        else wait_loads<0>();
+      } else if (next) {
+        expand(x + 1, ahead);
+      }
+      lds_barrier();
+      slot = slot + 1 == kSlots ? 0 : slot + 1;
     }
   }
   const float lt = half_sum(rs.l);
   if (!live) return;
-  store_row<FMT>(a, row, split, direct, o, rs.m, lt, FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v), h);
+  store_row<FMT>(a, row, split, direct, o, rs.m, lt, FMT == kBf16 || e_o == kNoExp ? 1.0f : ldexpf(1.0f, e_o), h);
 }
 
 // ---------------------------------------------------------------------------
@@ -572,7 +622,7 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(ChunkArgs a) {
 // memory straight to the operands; the waves' states are merged in LDS.
 // ---------------------------------------------------------------------------
 template <int FMT, int NG>
-__global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(ChunkArgs a) {
   constexpr int M = kRows;
   constexpr bool HL = FMT == kBf16;  // p in two bf16 pieces: costs nothing where the loads bound
   __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : kWaves];
@@ -612,7 +662,7 @@ __global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
     auto block_of = [&](int x) {
       return a.pages + ((size_t)bt[page_of(x)] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
     };
-    constexpr int kL = FMT == kBf16 ? 16 : Raw<FMT, NG>::kLoads;
+    constexpr int kL = FMT == kBf16 ? 16 : raw_loads<FMT>();
     u4v rk[kL], rv[kL];
     uint32_t ks[NG], vs[NG];
     auto fetch_k = [&](const uint8_t* blk) {
@@ -630,7 +680,7 @@ __global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
       for (int i = 0; i < kL; ++i) {
         if (FMT == kBf16) {  // (C, step) = (i / 4, i % 4)
-          const int off = kPageLds / 2 + (i / 4) * 4096 + (i % 2) * 1024 + (i / 2 % 2) * 512 + b16 * 2048 + h * 256 +
+          const int off = kHalfLds + (i / 4) * 4096 + (i % 2) * 1024 + (i / 2 % 2) * 512 + b16 * 2048 + h * 256 +
                           lo * 16;
           rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
         } else {
@@ -642,7 +692,8 @@ __global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
     fetch_k(blk);
     if (FMT != kBf16) {
       fetch_v(blk);
-      load_entries<FMT, NG>(blk, ks, vs);
+      load_entries<FMT, NG>(blk, 0, ks);
+      load_entries<FMT, NG>(blk, 1, vs);
     }
     u4v q[8];
     load_queries<FMT>(a, row, live, q, rs.c);
@@ -657,7 +708,9 @@ __global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
       } else {
         const int e_old = e_v;
         lane_exchange();  // the last page's scales have been read
-        make_scales<FMT, NG>(ks, vs, a.meta_bf16, min(ntok, kP), sc, e_k, e_v);
+        e_k = kNoExp;
+        make_scales<FMT, NG>(ks, 0, a.meta_bf16, min(ntok, kP), sc, e_k);
+        make_scales<FMT, NG>(vs, 1, a.meta_bf16, min(ntok, kP), sc, e_v);
         lane_exchange();
         if (e_v != e_old && e_old != kNoExp) {
           const float f = pow2(max(e_old - e_v, -126));
@@ -682,7 +735,8 @@ __global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
       if (FMT == kBf16 && more) fetch_k(next);
       const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
       u4v p[4], pl[4];
-      softmax_page<FMT, HL>(s, o, rs, FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast), masked, t0, window, a.sinks, p, pl);
+      if (masked) mask_page(s, rs.pos, t0, window, a.sinks);
+      softmax_page<FMT, HL>(s, o, rs, FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast), p, pl);
       if (FMT == kBf16 && ntok < kP) {  // slots never written weigh 0: their values may be anything
 #pragma unroll
         for (int i = 0; i < kL; ++i)
@@ -705,7 +759,8 @@ __global__ __launch_bounds__(256, 1) void chunk_few_kernel(ChunkArgs a) {
       if (FMT != kBf16 && more) {
         fetch_k(next);
         fetch_v(next);
-        load_entries<FMT, NG>(next, ks, vs);
+        load_entries<FMT, NG>(next, 0, ks);
+        load_entries<FMT, NG>(next, 1, vs);
       }
       blk = next;
     }
@@ -783,8 +838,10 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
   const int64_t blocks = ((int64_t)a.n_q * g / M + a.B) * a.num_splits * a.Hkv;
   if (M == kRows)
     hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  else if (M == 4 * kRows)
+    hipLaunchKernelGGL((chunk_kernel<FMT, NG, 4>), dim3((unsigned)blocks), dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL((chunk_kernel<FMT, NG>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((chunk_kernel<FMT, NG, 8>), dim3((unsigned)blocks), dim3(512), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || (FMT == kBf16 && a.num_splits == 1)) return e;
   // rows in parts of whole tokens that a launch holds
@@ -810,7 +867,8 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
 
 // Few rows a sequence: one tile of 32 takes them.
 int chunk_tile_rows(int64_t n_q, int B, int heads_per_kv) {
-  return n_q * heads_per_kv <= (int64_t)kRows * B ? kRows : kRows * kWaves;
+  const int64_t rows = n_q * heads_per_kv;
+  return rows <= (int64_t)kRows * B ? kRows : rows <= (int64_t)512 * B ? 4 * kRows : 8 * kRows;
 }
 
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st) {

@@ -1241,7 +1241,7 @@ int32_t oscar_chunk_default_splits(const oscar_layout* L, int32_t n_q, int32_t B
   const int64_t tiles = B * std::max<int64_t>(1, (per_seq + M - 1) / M) * L->num_kv_heads;
   // blocks: 4 for each that the GPU holds at once (one of the few-row kernel per CU, two of
   // the other), and 16 pages at least for a block
-  const int64_t want = (int64_t)device_cus() * (M == 32 ? 4 : 8);
+  const int64_t want = (int64_t)device_cus() * (M == 128 ? 8 : 4);
   const int64_t s = std::min(want / tiles, (int64_t)max_pages_per_seq / 16);
   return (int32_t)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
 }
