@@ -39,7 +39,7 @@ SOURCES = {
     "kv4_cache.hip": ["-ffp-contract=off"],
     "bf16_decode.hip": [],
     "rope.hip": [],
-    "chunk_attn.hip": [],
+    "chunk_attn.hip": ["-fno-honor-nans"],
     "mixed.hip": [],
     "calib.hip": ["-ffp-contract=off"],
     "probe.hip": [],

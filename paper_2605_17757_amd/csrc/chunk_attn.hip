@@ -46,6 +46,8 @@ constexpr int kNoWindow = 1 << 30;  // positions are below it
 // Least factor of scores: positive, so that a masked score stays -inf; below it scores are 0
 // to fp32's precision of exp.
 constexpr float kLeast = 0x1p-100f;
+constexpr int kHalfLds = kP * kD * 2;    // operands of a page's K or V
+constexpr int kPageLds = 2 * kHalfLds;
 constexpr int kBfBlock = 2 * kP * kD * 2;  // bytes of a bf16 page-head block
 
 template <int FMT>
@@ -85,6 +87,7 @@ __device__ inline int wave_max_i(int v) {
 }
 // Exponent e of |x| < 2^(e + 1) (0 and subnormals: -127).
 __device__ inline int exp_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
+__device__ inline bool is_nan(float x) { return (__float_as_uint(x) & 0x7fffffffu) > 0x7f800000u; }
 __device__ inline float pow2(int e) {  // clamped to fp32's normal range
   return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23);
 }
@@ -169,7 +172,7 @@ __device__ inline void each_four(const f16v (&o)[4], int h, F&& f) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int r = 8 * k + 4 * h;
-        const int c = FMT == kBf16 ? 32 * C + r : 64 * (C / 2) + 32 * (r / 16) + 16 * (C % 2) + r % 16;
+        const int c = FMT != kInt4 ? 32 * C + r : 64 * (C / 2) + 32 * (r / 16) + 16 * (C % 2) + r % 16;
         f(c, o[C][4 * k], o[C][4 * k + 1], o[C][4 * k + 2], o[C][4 * k + 3]);
       }
   }
@@ -344,13 +347,11 @@ __device__ inline void mask_page(f16v (&s)[2], int pos, int t0, int window, int 
     }
 }
 
-// Scores of a page in s -> the operands of P^T (HL: a second, smaller piece of each p), m and l
-// and the accumulators' scale moved.  cp: c of this page.
-template <int FMT, bool HL>
-__device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, float cp, u4v (&p)[4], u4v (&pl)[4]) {
+// The reference maximum for a page's scores, and the sums' scale with it.
+__device__ inline void move_reference(const f16v (&s)[2], f16v (&o)[4], RowState& r, float cp) {
   float mx = s[0][0];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+  for (int i = 0; i < 16; ++i) mx = fmaxf(fmaxf(mx, s[0][i]), s[1][i]);
   mx = half_max(mx) * cp;
   const bool need = mx > r.m + kSlack;
   if (__ballot(need) != 0ull) {
@@ -361,6 +362,13 @@ __device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, flo
 #pragma unroll
     for (int C = 0; C < 4; ++C) o[C] *= alpha;
   }
+}
+
+// Scores of a page in s -> the operands of P^T (HL: a second, smaller piece of each p), m and l
+// and the accumulators' scale moved.  cp: c of this page.
+template <int FMT, bool HL>
+__device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, float cp, u4v (&p)[4], u4v (&pl)[4]) {
+  move_reference(s, o, r, cp);
   const float ms = r.m == -INFINITY ? 0.0f : -r.m;
   float sum = 0.0f;
 #pragma unroll
@@ -390,7 +398,7 @@ template <int FMT>
 __device__ inline void store_row(const ChunkArgs& a, size_t row, int s, bool direct, const f16v (&o)[4], float m,
                                  float l, float scale, int h) {
   if (direct) {
-    const float il = l > 0.0f ? 1.0f / l : l != l ? l : 0.0f;
+    const float il = (l > 0.0f ? 1.0f / l : is_nan(l) ? l : 0.0f) * scale;
     uint16_t* dst = a.out + row * kD;
     each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
       uint2 v;
@@ -402,12 +410,23 @@ __device__ inline void store_row(const ChunkArgs& a, size_t row, int s, bool dir
   }
   const size_t at = row * a.num_splits + s;
   float* dst = a.part_o + at * kD;
-  if (l != l) m = 0.0f;  // NaN in a row: its scores have no maximum, but the state is not empty
+  if (is_nan(l)) m = 0.0f;  // NaN in a row: its scores have no maximum, but the state is not empty
   if (m != -INFINITY)    // of an empty state only that is read
     each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
       *reinterpret_cast<float4*>(dst + c) = make_float4(x * scale, y * scale, z * scale, w * scale);
     });
   if (h == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, l);
+}
+
+// A row's state of a piece without pages: nothing, or (direct) a zero row.
+__device__ inline void store_empty(const ChunkArgs& a, size_t row, int s, bool direct, int h) {
+  if (direct) {
+    u4v* dst = reinterpret_cast<u4v*>(a.out + row * kD) + 8 * h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dst[i] = u4v{0, 0, 0, 0};
+  } else if (h == 0) {
+    reinterpret_cast<float2*>(a.part_ml)[row * a.num_splits + s] = make_float2(-INFINITY, 0.0f);
+  }
 }
 
 // Pieces that a tile's pages are cut into: at least `least` pages each.
@@ -433,22 +452,207 @@ __device__ inline void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// A value that no one writes while the kernel runs, at an address that is the wave's: by a scalar
+// load, which the waits for vector loads do not meet.
+template <class T>
+__device__ inline T scalar_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)p;
+}
 __device__ inline uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
 // ---------------------------------------------------------------------------
+// Chunks of many rows over a quantized cache: every page is read by many blocks, and its codes
+// are expanded once, to what a wave gives the matrix cores, with R_k and R_v as operands beside
+// them (two fp16 pieces of each entry, so that the rotations cost no precision against q's and
+// o's own rounding).
+// ---------------------------------------------------------------------------
+// Part `part` (of four) of a page's K or V: four operands of 1 KB at dst; NATURAL: V's slots in
+// order within a step, whatever the codes' order.
+template <int FMT, int NG, bool NATURAL>
+__device__ inline void expand_part(const u4v& raw, int is_v, int part, const Scales<NG>& sc, uint8_t* dst) {
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (is_v) {
+      const int C = FMT == kInt4 ? 2 * (part / 2) + i % 2 : i;
+      const int j0 = FMT == kInt4 ? i / 2 : part / 2, i2 = part % 2;
+      u4v v = v_operand<FMT, NG>(raw, C, j0, i2, sc);
+      if (NATURAL && FMT == kInt2)  // slots (0, 2), (1, 3) -> (0, 1), (2, 3)
+        v = u4v{__builtin_amdgcn_perm(v.y, v.x, 0x05040100u), __builtin_amdgcn_perm(v.y, v.x, 0x07060302u),
+                __builtin_amdgcn_perm(v.w, v.z, 0x05040100u), __builtin_amdgcn_perm(v.w, v.z, 0x07060302u)};
+      *reinterpret_cast<u4v*>(dst + (C * 4 + 2 * j0 + i2) * 1024 + l * 16) = v;
+    } else {
+      const int T = part / 2, ks = 4 * (part % 2) + i;
+      *reinterpret_cast<u4v*>(dst + (T * 8 + ks) * 1024 + l * 16) = k_operand<FMT, NG>(raw, T, ks, sc);
+    }
+  }
+}
+// Channel that row r of output tile C (32 rows) of o~ V's products is.
+template <int FMT>
+__device__ inline int v_channel(int C, int r) {
+  return FMT == kInt2 ? 4 * r + C : FMT == kInt4 ? 64 * (C / 2) + 32 * (r / 16) + 16 * (C % 2) + r % 16 : 32 * C + r;
+}
+
+// Blocks: a page of a sequence's table and a KV head each; behind them one for each rotation.
+template <int FMT, int NG>
+__global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a) {
+  __shared__ Scales<NG> scales[4];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+  const int64_t pages = (int64_t)a.B * a.max_pages * a.Hkv;
+  if (blockIdx.x >= pages) {
+    // operand (tile, step, piece): R_k: rows the channels of q~ that the score steps take, 8 input
+    // channels of q each; R_v: rows 32 output channels, steps the channels of o~ in a lane
+    const int which = (int)(blockIdx.x - pages), is_v = which & 1;
+    const float* R = is_v ? a.Rv : a.Rk;
+    if (R) R += (size_t)(which >> 1) * kD * kD;
+    const int r = l & 31, h = l >> 5;
+    for (int i = w; i < 32; i += 4) {
+      const int C = i / 8, k = i % 8;
+      u4v hi, lo;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float x[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int e = 2 * j + u;
+          int from, to;  // R[from][to]
+          if (is_v) {    // o_c = sum_j o~_j R_v[c][j]; step k: row 16 (k % 2) + 8 (e / 4) + 4 h + e % 4 of tile k / 2
+            from = 32 * C + r;
+            to = v_channel<FMT>(k / 2, 16 * (k % 2) + 8 * (e / 4) + 4 * h + e % 4);
+          } else {       // q~_j = sum_c q_c R_k[c][j]; row r: element 4 (r / 8 % 2) + r % 4 of step 2 C + r / 16, half r / 4 % 2
+            from = 16 * k + 8 * h + e;
+            to = k_channel<FMT>(2 * C + r / 16, r / 4 % 2, 4 * (r / 8 % 2) + r % 4);
+          }
+          x[u] = R ? R[from * kD + to] : from == to ? 1.0f : 0.0f;
+        }
+        const uint32_t both = pack2<kInt4>(x[0], x[1]);
+        const h2 t = __builtin_bit_cast(h2, both);
+        hi[j] = both;
+        lo[j] = pack2<kInt4>(x[0] - (float)t.x, x[1] - (float)t.y);
+      }
+      uint8_t* dst = a.rot + (size_t)which * kRotBytes + (C * 8 + k) * 2048 + l * 16;
+      *reinterpret_cast<u4v*>(dst) = hi;
+      *reinterpret_cast<u4v*>(dst + 1024) = lo;
+    }
+    return;
+  }
+  const int kvh = blockIdx.x % a.Hkv;
+  const int64_t at = blockIdx.x / a.Hkv;
+  const int b = (int)(at / a.max_pages), i = (int)(at % a.max_pages);
+  const int q0 = min(max(a.q_start[b], 0), a.n_q), n = min(max(a.q_start[b + 1], 0), a.n_q) - q0;
+  const int len = min(max(a.seq_lens[b], 0), a.max_pages * kP);
+  if (n <= 0 || i * kP >= len) return;
+  const int window = a.window > 0 ? min(a.window, kNoWindow) : kNoWindow;
+  const int start = max(len - n - window + 1, 0), from = start / kP;
+  if (i >= min((min(a.sinks, start) + kP - 1) / kP, from) && i < from) return;  // no new token sees it
+  const uint8_t* blk = a.pages + ((size_t)a.block_table[at] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
+  const u4v rk = load_k<FMT, NG>(blk, FMT == kInt4 ? w : w / 2), rv = load_v<FMT, NG>(blk, FMT == kInt4 ? w : w / 2);
+  uint32_t ek[NG], ev[NG];
+  load_entries<FMT, NG>(blk, 0, ek);
+  load_entries<FMT, NG>(blk, 1, ev);
+  int e[2] = {kNoExp, kNoExp};
+  const int ntok = min(len - i * kP, kP);
+  make_scales<FMT, NG>(ek, 0, a.meta_bf16, ntok, scales[w], e[0]);
+  make_scales<FMT, NG>(ev, 1, a.meta_bf16, ntok, scales[w], e[1]);
+  lane_exchange();
+  uint8_t* dst = a.expanded + (size_t)blockIdx.x * kExpandedBytes;
+  expand_part<FMT, NG, true>(rk, 0, w, scales[w], dst);
+  expand_part<FMT, NG, true>(rv, 1, w, scales[w], dst + kExpandedBytes / 2);
+  if (threadIdx.x == 0) a.exps[blockIdx.x] = make_int2(e[0], e[1]);
+}
+
+// q~ = q R_k as the score products' operands, fp16 divided by a power of two that c takes; R_k's
+// operands at `rot` in LDS.
+__device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live, const uint8_t* rot, u4v (&q)[8],
+                                      float& c) {
+  const int l = threadIdx.x & 63, h = l >> 5;
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+  u4v x[8];
+  float top = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    x[k] = live ? *reinterpret_cast<const u4v*>(a.q + row * kD + 16 * k + 8 * h) : u4v{0, 0, 0, 0};
+    x[k] ^= flip;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf_lo(x[k][j])), fabsf(bf_hi(x[k][j]))));
+  }
+  const int e1 = max(exp_of(half_max(top)), -100) - 13;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[k][j] = pack2<kInt4>(ldexpf(bf_lo(x[k][j]), -e1), ldexpf(bf_hi(x[k][j]), -e1));
+  f16v y[4];
+  top = 0.0f;
+#pragma unroll
+  for (int C = 0; C < 4; ++C) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[C][i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const u4v* op = reinterpret_cast<const u4v*>(rot + (C * 8 + k) * 2048 + l * 16);
+      y[C] = mfma<kHalf>(op[64], x[k], y[C]);
+      y[C] = mfma<kHalf>(op[0], x[k], y[C]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(y[C][i]));
+  }
+  const int e2 = max(exp_of(half_max(top)), -60) - 13;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      q[k][j] = pack2<kHalf>(ldexpf(y[k / 2][8 * (k % 2) + 2 * j], -e2), ldexpf(y[k / 2][8 * (k % 2) + 2 * j + 1], -e2));
+  c = fabsf(a.scale) * pow2(e1 + e2);
+}
+// o = o~ R_v^T, o~ = the sums / l 2^e as fp16 (divided by a power of two): rows of the output's
+// channels in order; returns what they are still to be multiplied by to be the sums again.
+__device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_t* rot) {
+  const int lane = threadIdx.x & 63;
+  const float il = l > 0.0f ? 1.0f / l : is_nan(l) ? l : 0.0f;
+  float top = 0.0f;
+#pragma unroll
+  for (int C = 0; C < 4; ++C)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      o[C][i] *= il;
+      top = fmaxf(top, fabsf(o[C][i]));
+    }
+  const int e3 = max(exp_of(half_max(top)), -100) - 13;
+  u4v x[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      x[k][j] = pack2<kHalf>(ldexpf(o[k / 2][8 * (k % 2) + 2 * j], -e3), ldexpf(o[k / 2][8 * (k % 2) + 2 * j + 1], -e3));
+#pragma unroll
+  for (int C = 0; C < 4; ++C) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const u4v* op = reinterpret_cast<const u4v*>(rot + (C * 8 + k) * 2048 + lane * 16);
+      o[C] = mfma<kHalf>(op[64], x[k], o[C]);
+      o[C] = mfma<kHalf>(op[0], x[k], o[C]);
+    }
+  }
+  return ldexpf(l, e3 + e);
+}
+
+// ---------------------------------------------------------------------------
 // Many rows: W waves of 32 rows share every page through LDS.
 // ---------------------------------------------------------------------------
-constexpr int kHalfLds = kP * kD * 2;    // operands of a page's K or V
-constexpr int kPageLds = 2 * kHalfLds;
 template <int FMT, int NG, int W>
 __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   constexpr int M = kRows * W;
-  constexpr int kSlots = FMT == kBf16 && W == 8 ? 3 : 2;
+  constexpr bool CODES = FMT == kInt4 || FMT == kInt2;
+  constexpr int kSlots = W == 8 ? 3 : 2;
+  static_assert(W == 4 || (W == 8 && !CODES), "a block expands codes a part per wave");
+  static_assert(FMT != kHalf || kSlots * kPageLds >= kRotBytes, "a rotation's operands fit in the pages' slots");
   __shared__ __align__(16) uint8_t lds[kSlots * kPageLds];
-  __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : W];
-  __shared__ int exps[2][2];  // of the slots: K's exponent, the accumulators'
+  __shared__ Scales<CODES ? NG : 1> scales[CODES ? W : 1];
+  __shared__ int exps[2][2];  // CODES: of the slots: K's exponent, the accumulators'
   const int g = a.Hq / a.Hkv;
   const int kvh = blockIdx.x % a.Hkv;
   const int64_t rest = blockIdx.x / a.Hkv;
@@ -464,157 +668,230 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   const bool live = r < t.rows;
   const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
   const int pieces = piece_count(pg.count, a.num_splits, 4);
-  const bool direct = FMT == kBf16 && a.num_splits == 1;
+  const bool direct = !CODES && a.num_splits == 1;
+  if (split >= pieces || pg.count == 0) {
+    if (live) store_empty(a, row, split, direct, h);
+    return;
+  }
   RowState rs;
   rs.pos = live ? t.len - t.n + r / g : -1;
   rs.m = -INFINITY;
   rs.l = 0.0f;
+  // bytes from global memory to the start of the slots, by all waves; until all is there
+  auto fill = [&](const uint8_t* src, int bytes) {
+    for (int i = w; i < bytes / 1024; i += W)
+      load_to_lds(src + i * 1024 + l * 16, __builtin_amdgcn_readfirstlane(lds_address(lds) + i * 1024));
+    wait_loads<0>();
+    lds_barrier();
+  };
+  const uint8_t* rot = FMT == kHalf ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
+  u4v q[8];
+  if constexpr (FMT == kHalf) {
+    fill(rot, kRotBytes);
+    rotate_queries(a, row, live, lds, q, rs.c);
+    lds_barrier();
+  } else {
+    load_queries<FMT>(a, row, live, q, rs.c);
+  }
+  const int x0 = (int)((int64_t)pg.count * split / pieces), x1 = (int)((int64_t)pg.count * (split + 1) / pieces);
+  const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
+  auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
+  // index of a page's block: its number is loaded a page before it is needed
+  auto block_of = [&](int x) -> int64_t {
+    const int i = page_of(min(x, x1 - 1));
+    return (FMT == kHalf ? (int64_t)t.b * a.max_pages + i : (int64_t)scalar_load(bt + i)) * a.Hkv + kvh;
+  };
+  auto page_exps = [&](int x) {
+    const int* e = reinterpret_cast<const int*>(a.exps + block_of(x));
+    return make_int2(scalar_load(e), scalar_load(e + 1));
+  };
+  // bf16, kHalf: this wave's part of a page, straight to LDS
+  constexpr int kLoads = 32 / W;
+  auto fetch = [&](int64_t block, int slot) {
+    const uint8_t* src = (FMT == kHalf ? a.expanded : a.pages) + block * kPageLds + w * kLoads * 1024 + l * 16;
+    const uint32_t dst = lds_address(lds) + slot * kPageLds + w * kLoads * 1024;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, __builtin_amdgcn_readfirstlane(dst + i * 1024));
+  };
+  // codes: a wave takes a quarter of K's and of V's codes to registers, and a page later makes 4
+  // operands of 1 KB of each
+  u4v raw[2];
+  uint32_t ent[2][NG];
+  int e_v = kNoExp;
+  auto load_codes = [&](int64_t block) {
+    const uint8_t* blk = a.pages + block * block_bytes_of(FMT, NG);
+    const int i = FMT == kInt4 ? w : w / 2;
+    raw[0] = load_k<FMT, NG>(blk, i);
+    raw[1] = load_v<FMT, NG>(blk, i);
+    load_entries<FMT, NG>(blk, 0, ent[0]);
+    load_entries<FMT, NG>(blk, 1, ent[1]);
+  };
+  auto expand = [&](int x, int slot) {
+    const int ntok = min(t.len - page_of(x) * kP, kP);
+    Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
+    uint8_t* dst = lds + slot * kPageLds;
+    lane_exchange();
+    int e_k = kNoExp;
+    make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, ntok, sc, e_k);
+    make_scales<FMT, NG>(ent[1], 1, a.meta_bf16, ntok, sc, e_v);
+    if (threadIdx.x == 0) {
+      exps[0][slot] = e_k;
+      exps[1][slot] = e_v;
+    }
+    lane_exchange();
+    expand_part<FMT, NG, false>(raw[0], 0, w, sc, dst);
+    expand_part<FMT, NG, false>(raw[1], 1, w, sc, dst + kHalfLds);
+  };
   f16v o[4];
 #pragma unroll
   for (int C = 0; C < 4; ++C)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
   int e_o = kNoExp;  // the accumulators' exponent
-  if (split < pieces && pg.count > 0) {
-    u4v q[8];
-    load_queries<FMT>(a, row, live, q, rs.c);
-    const int x0 = (int)((int64_t)pg.count * split / pieces), x1 = (int)((int64_t)pg.count * (split + 1) / pieces);
-    const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
-    auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
-    auto block_of = [&](int x) {
-      return a.pages + ((size_t)bt[page_of(x)] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
-    };
-    // bf16: this wave's part of a page, straight to LDS
-    constexpr int kLoads = 32 / W;
-    auto fetch = [&](int x, int slot) {
-      const uint8_t* src = block_of(x) + w * kLoads * 1024 + l * 16;
-      const uint32_t dst = lds_address(lds) + slot * kPageLds + w * kLoads * 1024;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, __builtin_amdgcn_readfirstlane(dst + i * 1024));
-    };
-    // codes: a page in eight parts, K's four and V's four, of 4 operands of 1 KB each; a wave loads
-    // its parts to registers and a page later makes the operands
-    constexpr int kParts = 8 / W;
-    u4v raw[kParts];
-    uint32_t ent[kParts][NG];
-    int e_v = kNoExp;
-    auto load_codes = [&](int x) {
-      const uint8_t* blk = block_of(x);
-#pragma unroll
-      for (int j = 0; j < kParts; ++j) {
-        const int part = (W * j + w) % 4, is_v = (W * j + w) / 4;
-        const int i = FMT == kInt4 ? part : part / 2;
-        raw[j] = is_v ? load_v<FMT, NG>(blk, i) : load_k<FMT, NG>(blk, i);
-        load_entries<FMT, NG>(blk, is_v, ent[j]);
-      }
-    };
-    auto expand = [&](int x, int slot) {
-      const int ntok = min(t.len - page_of(x) * kP, kP);
-      Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
-      uint8_t* dst = lds + slot * kPageLds + l * 16;
-#pragma unroll
-      for (int j = 0; j < kParts; ++j) {
-        const int part = (W * j + w) % 4, is_v = (W * j + w) / 4;
-        lane_exchange();
-        int e = is_v ? e_v : kNoExp;
-        make_scales<FMT, NG>(ent[j], is_v, a.meta_bf16, ntok, sc, e);
-        if (is_v) e_v = e;
-        if (part == 0 && l == 0) exps[is_v][slot] = e;
-        lane_exchange();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (is_v) {
-            const int C = FMT == kInt4 ? 2 * (part / 2) + i % 2 : i;
-            const int j0 = FMT == kInt4 ? i / 2 : part / 2, i2 = part % 2;
-            *reinterpret_cast<u4v*>(dst + kHalfLds + (C * 4 + 2 * j0 + i2) * 1024) =
-                v_operand<FMT, NG>(raw[j], C, j0, i2, sc);
-          } else {
-            const int T = part / 2, ks = 4 * (part % 2) + i;
-            *reinterpret_cast<u4v*>(dst + (T * 8 + ks) * 1024) = k_operand<FMT, NG>(raw[j], T, ks, sc);
-          }
-        }
-      }
-    };
-    if (FMT == kBf16) {
-      fetch(x0, 0);
-      wait_loads<0>();
-      if (kSlots == 3 && x0 + 1 < x1) fetch(x0 + 1, 1);
-    } else {
-      load_codes(x0);
-      expand(x0, 0);
+  float unit = 1.0f;
+  int64_t ahead_block = block_of(x0 + kSlots - 1);
+  if (!CODES) {
+    fetch(block_of(x0), 0);
+    wait_loads<0>();
+    if (kSlots == 3 && x0 + 1 < x1) fetch(block_of(x0 + 1), 1);
+  } else {
+    load_codes(block_of(x0));
+    expand(x0, 0);
+  }
+  int2 ex_next = make_int2(0, 0);
+  if (FMT == kHalf) ex_next = page_exps(x0);
+  lds_barrier();
+  int slot = 0;
+  int x = x0;
+  do {
+    const int t0 = page_of(x) * kP;
+    const bool next = x + 1 < x1;
+    const int ahead = slot == 0 ? kSlots - 1 : slot - 1;  // the slot that is free
+    if (!CODES) {
+      if (x + kSlots - 1 < x1) fetch(ahead_block, ahead);
+    } else if (next) {
+      load_codes(ahead_block);
     }
-    lds_barrier();
-    int slot = 0;
-    for (int x = x0; x < x1; ++x) {
-      const int t0 = page_of(x) * kP;
-      const bool next = x + 1 < x1;
-      const int ahead = slot + kSlots - 1 >= kSlots ? slot - 1 : slot + kSlots - 1;  // the slot that is free
-      if (FMT == kBf16) {
-        if (x + kSlots - 1 < x1) fetch(x + kSlots - 1, ahead);
-      } else if (next) {
-        load_codes(x + 1);
+    ahead_block = block_of(x + kSlots);
+    float cp = rs.c, weight = 0.0f;  // weight (log2) of the page's values against the accumulators'
+    if (FMT != kBf16) {
+      int e_k, e;
+      if (FMT == kHalf) {
+        e_k = ex_next.x;
+        e = max(e_o, ex_next.y);
+        weight = (float)max(ex_next.y - e, -60);
+        if (next) ex_next = page_exps(x + 1);
+      } else {
+        e_k = __builtin_amdgcn_readfirstlane(exps[0][slot]);
+        e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
       }
-      float cp = rs.c;
-      if (FMT != kBf16) {
-        cp = fmaxf(rs.c * pow2(__builtin_amdgcn_readfirstlane(exps[0][slot])), kLeast);
-        const int e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
-        if (e != e_o && e_o != kNoExp) {
-          const float f = pow2(max(e_o - e, -126));
+      cp = fmaxf(rs.c * pow2(e_k), kLeast);
+      if (e != e_o && e_o != kNoExp) {
+        const float f = pow2(max(e_o - e, -126));
 #pragma unroll
-          for (int C = 0; C < 4; ++C) o[C] *= f;
-        }
-        e_o = e;
+        for (int C = 0; C < 4; ++C) o[C] *= f;
       }
-      uint8_t* base = lds + slot * kPageLds;
-      if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
-        const int ntok = t.len - t0;
-        for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
-          const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
-          u4v& v = reinterpret_cast<u4v*>(base + kHalfLds)[i];
+      e_o = e;
+    }
+    uint8_t* base = lds + slot * kPageLds;
+    if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
+      const int ntok = t.len - t0;
+      for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
+        const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
+        u4v& v = reinterpret_cast<u4v*>(base + kHalfLds)[i];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
-        }
-        lds_barrier();
+        for (int j = 0; j < 4; ++j)
+          v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
       }
-      const int k_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
-      const int v_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
-      f16v s[2];
+      lds_barrier();
+    }
+    const int k_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
+    const int v_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
+    // scores, the operands read three steps ahead
+    f16v s[2];
+    {
+      auto k_at = [&](int T, int k) {
+        const int off = FMT == kBf16 ? T * 8192 + (k % 4) * 1024 + (k / 4) * 512 : (T * 8 + k) * 1024;
+        return *reinterpret_cast<const u4v*>(base + k_lane + off);
+      };
+      u4v ka[4][2];
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int T = 0; T < 2; ++T) ka[k][T] = k_at(T, k);
 #pragma unroll
       for (int T = 0; T < 2; ++T)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < 8; ++k) {
+        if (k + 3 < 8)
 #pragma unroll
-        for (int T = 0; T < 2; ++T) {
-          const int off = FMT == kBf16 ? T * 8192 + (k % 4) * 1024 + (k / 4) * 512 : (T * 8 + k) * 1024;
-          s[T] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + k_lane + off), q[k], s[T]);
-        }
-      if (t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks))
-        mask_page(s, rs.pos, t0, window, a.sinks);
-      u4v p[4], unused[4];
-      softmax_page<FMT, false>(s, o, rs, cp, p, unused);
+          for (int T = 0; T < 2; ++T) ka[(k + 3) % 4][T] = k_at(T, k + 3);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int C = 0; C < 4; ++C) {
-          const int off = FMT == kBf16 ? C * 4096 + (k % 2) * 1024 + (k / 2) * 512 : (C * 4 + k) * 1024;
-          o[C] = mfma<FMT>(*reinterpret_cast<const u4v*>(base + kHalfLds + v_lane + off), p[k], o[C]);
-        }
-      if (FMT == kBf16) {  // page x + 1 has landed
-        if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
-        else wait_loads<0>();
-      } else if (next) {
-        expand(x + 1, ahead);
+        for (int T = 0; T < 2; ++T) s[T] = mfma<FMT>(ka[k % 4][T], q[k], s[T]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      lds_barrier();
-      slot = slot + 1 == kSlots ? 0 : slot + 1;
     }
+    auto v_at = [&](int C, int k) {
+      const int off = FMT == kBf16 ? C * 4096 + (k % 2) * 1024 + (k / 2) * 512 : (C * 4 + k) * 1024;
+      return *reinterpret_cast<const u4v*>(base + kHalfLds + v_lane + off);
+    };
+    u4v va[2][4];
+#pragma unroll
+    for (int C = 0; C < 4; ++C) va[0][C] = v_at(C, 0);
+    if (t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks))
+      mask_page(s, rs.pos, t0, window, a.sinks);
+    move_reference(s, o, rs, cp);
+    // weights of a step's operand, two at a time between the products of the step before
+    const float ms = (rs.m == -INFINITY ? 0.0f : -rs.m) + weight;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    u4v p[2];
+    auto weights = [&](int k, int i) {
+      auto one = [&](int e) {
+        const int y = v_slot<FMT>(e), u = y % 4;
+        return __builtin_amdgcn_exp2f(fmaf(s[u / 2][8 * (u % 2) + 4 * (k / 2) + 2 * (k % 2) + y / 4], cp, ms));
+      };
+      const float x = one(2 * i), y = one(2 * i + 1);
+      sum[i] += x;
+      sum[i] += y;
+      p[k % 2][i] = pack2<FMT>(x, y);
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) weights(0, i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k + 1 < 4)
+#pragma unroll
+        for (int C = 0; C < 4; ++C) va[(k + 1) % 2][C] = v_at(C, k + 1);
+#pragma unroll
+      for (int C = 0; C < 4; ++C) {
+        o[C] = mfma<FMT>(va[k % 2][C], p[k % 2], o[C]);
+        if (k + 1 < 4) weights(k + 1, C);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    asm volatile("" : "+v"(total));  // the additions stay among the products
+    rs.l = FMT == kHalf ? fmaf(total, __builtin_amdgcn_exp2f(-weight), rs.l) : rs.l + total;
+    if (!CODES) {  // page x + 1 has landed
+      if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
+      else wait_loads<0>();
+    } else if (next) {
+      expand(x + 1, ahead);
+    }
+    lds_barrier();
+    slot = slot + 1 == kSlots ? 0 : slot + 1;
+  } while (++x < x1);
+  rs.l = half_sum(rs.l);
+  if constexpr (FMT == kHalf) {
+    fill(rot + kRotBytes, kRotBytes);
+    unit = rotate_output(o, rs.l, e_o, lds);
+  } else if (FMT != kBf16) {
+    unit = ldexpf(1.0f, e_o);
   }
-  const float lt = half_sum(rs.l);
   if (!live) return;
-  store_row<FMT>(a, row, split, direct, o, rs.m, lt, FMT == kBf16 || e_o == kNoExp ? 1.0f : ldexpf(1.0f, e_o), h);
+  store_row<FMT>(a, row, split, direct, o, rs.m, rs.l, unit, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -769,7 +1046,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
   const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
   const float lt = half_sum(rs.l);
   // (NaN in a row: its scores have no maximum, but the state is not empty)
-  if (h == 0) ml[w][n] = make_float2(lt != lt ? 0.0f : rs.m, lt);
+  if (h == 0) ml[w][n] = make_float2(is_nan(lt) ? 0.0f : rs.m, lt);
 #pragma unroll
   for (int C = 0; C < 4; ++C)
 #pragma unroll
@@ -795,7 +1072,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
       for (int k = 0; k < kWaves; ++k) v += f[k] != 0.0f ? f[k] * os[k][C][4 * w + i][l] : 0.0f;
       sum[C][i] = v;
     }
-  const float il = L > 0.0f ? 1.0f / L : L != L ? L : 0.0f;
+  const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
   const size_t at = row * a.num_splits + split;
   auto put = [&](int c, float x, float y, float z, float v) {
     if (direct) {
@@ -834,16 +1111,30 @@ __global__ __launch_bounds__(kRedThreads) void chunk_reduce_kernel(ChunkArgs a, 
 template <int FMT, int NG>
 hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
   const int g = a.Hq / a.Hkv;
-  const int M = chunk_tile_rows(a.n_q, a.B, g);
-  const int64_t blocks = ((int64_t)a.n_q * g / M + a.B) * a.num_splits * a.Hkv;
-  if (M == kRows)
-    hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  else if (M == 4 * kRows)
-    hipLaunchKernelGGL((chunk_kernel<FMT, NG, 4>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((chunk_kernel<FMT, NG, 8>), dim3((unsigned)blocks), dim3(512), 0, st, a);
+  const bool quantized = FMT != kBf16;
+  const int64_t page_heads = (int64_t)a.B * a.max_pages * a.Hkv;
+  const int M = chunk_tile_rows(quantized, a.n_q, a.B, g, page_heads);
+  const unsigned blocks = (unsigned)(((int64_t)a.n_q * g / M + a.B) * a.num_splits * a.Hkv);
+  bool merged = !quantized && a.num_splits == 1, rotated = false;
+  if (M == kRows) {
+    hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3(blocks), dim3(256), 0, st, a);
+  } else if (M == 4 * kRows) {
+    hipLaunchKernelGGL((chunk_kernel<FMT, NG, 4>), dim3(blocks), dim3(256), 0, st, a);
+  } else if constexpr (FMT == kBf16) {
+    hipLaunchKernelGGL((chunk_kernel<kBf16, 1, 8>), dim3(blocks), dim3(512), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((expand_kernel<FMT, NG>), dim3((unsigned)(page_heads + 2 * (a.rph ? a.Hkv : 1))), dim3(256), 0,
+                       st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((chunk_kernel<kHalf, 1, 8>), dim3(blocks), dim3(512), 0, st, a);
+    merged = a.num_splits == 1;
+    rotated = true;
+  }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (FMT == kBf16 && a.num_splits == 1)) return e;
+  if (e != hipSuccess || merged) return e;
+  ChunkArgs m = a;
+  if (rotated) m.Rv = nullptr;
   // rows in parts of whole tokens that a launch holds
   const int per = launch_seqs(a.Hq);
   return by_seqs(a.n_q, per, [&](int t0, int n) {
@@ -851,7 +1142,7 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
     auto go = [&](auto rb) {
       constexpr int RB = decltype(rb)::value;
       hipLaunchKernelGGL((chunk_reduce_kernel<RB>), dim3((unsigned)query_blocks(n, a.Hq, a.Hkv, a.rph, RB)),
-                         dim3(kRedThreads), 0, st, a, row0, rows);
+                         dim3(kRedThreads), 0, st, m, row0, rows);
     };
     switch (reduce_rows(rows)) {
       case 16: go(std::integral_constant<int, 16>{}); break;
@@ -865,10 +1156,11 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Few rows a sequence: one tile of 32 takes them.
-int chunk_tile_rows(int64_t n_q, int B, int heads_per_kv) {
+int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int64_t page_heads) {
   const int64_t rows = n_q * heads_per_kv;
-  return rows <= (int64_t)kRows * B ? kRows : rows <= (int64_t)512 * B ? 4 * kRows : 8 * kRows;
+  if (rows <= (int64_t)kRows * B) return kRows;
+  // (expanded pages: 2 GiB at most)
+  return rows <= (int64_t)512 * B || (quantized && page_heads > 65536) ? 4 * kRows : kManyRows;
 }
 
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st) {

@@ -290,28 +290,40 @@ struct RopeRows {
 hipError_t launch_rope(const RopeRows& a, hipStream_t st);
 
 // Attention of the newest tokens of every sequence over a paged cache.
-enum CacheFormat { kBf16 = 0, kInt4 = 1, kInt2 = 2 };
+// (kHalf: pages that a call has expanded to fp16 operands.)
+enum CacheFormat { kBf16 = 0, kInt4 = 1, kInt2 = 2, kHalf = 3 };
 struct ChunkArgs {
   const uint8_t* pages;
   int format, ng, meta_bf16;
   int Hkv, Hq, B, n_q;
   const uint16_t* q;   // bf16 [n_q][Hq][128] (bf16 cache)
-  const float* qt;     // rotated, scaled by sm_scale log2 e (quantized caches)
+  const float* qt;     // rotated, scaled by sm_scale log2 e (quantized caches, pages not expanded)
   const int32_t* q_start;
   const int32_t* block_table;
   int max_pages;
   const int32_t* seq_lens;
-  float scale;         // bf16 cache: sm_scale log2 e
+  float scale;         // sm_scale log2 e
   int window, sinks;   // window 0: none
   int num_splits;
   float* part_o;       // [n_q Hq][num_splits][128]; bf16 cache with one split: unused
   float* part_ml;
   uint16_t* out;       // bf16 [n_q][Hq][128]
+  const float* Rk;
   const float* Rv;
   int rph;
+  // Quantized caches, chunks of many rows: the pages as fp16 operands, kExpandedBytes for each
+  // (sequence, page of its table, KV head), the exponents that they are divided by (K's, V's), and
+  // R_k, R_v as operands, kRotBytes each; null: expanded by the blocks that read them.
+  uint8_t* expanded;
+  int2* exps;
+  uint8_t* rot;
 };
-// Query rows (token, head) of a sequence and KV head that a block takes.
-int chunk_tile_rows(int64_t n_q, int B, int heads_per_kv);
+constexpr int kExpandedBytes = 2 * kP * kD * 2;
+constexpr int kRotBytes = 2 * kD * kD * 2;  // a rotation in two fp16 pieces
+// Query rows (token, head) of a sequence and KV head that a block takes; page_heads: pages of all
+// table rows times KV heads.
+int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int64_t page_heads);
+constexpr int kManyRows = 256;  // the largest: with quantized caches, pages are expanded once
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st);
 
 // Offline calibration.

@@ -1101,6 +1101,28 @@ int oscar_bf16_kv_append_rope(const oscar_layout* L, void* pages, const oscar_ro
 
 namespace {
 
+// Splits for tiles that see `pages` pages at most.
+int32_t chunk_splits(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq, int64_t pages) {
+  const int64_t g = Hq / L->num_kv_heads;
+  const int M = chunk_tile_rows(false, n_q, B, (int)g, 0);
+  // tiles as they come when the sequences' chunks are alike
+  const int64_t per_seq = (int64_t)n_q * g / B;
+  const int64_t tiles = B * std::max<int64_t>(1, (per_seq + M - 1) / M) * L->num_kv_heads;
+  // Blocks run in rounds of as many as the GPU holds; a block costs its pages, and what it does once
+  // and the partial state it leaves, about as much as 6 pages and (rows / 32) more.
+  const int64_t at_once = (int64_t)device_cus() * (M == kManyRows ? 1 : 2);
+  int64_t best = 1, least = 0;
+  for (int64_t s = 1; s == 1 || (s <= 64 && s * 16 <= pages); ++s) {
+    const int64_t rounds = (tiles * s + at_once - 1) / at_once;
+    const int64_t cost = rounds * (pages * 256 / s + (s == 1 ? 6 : 6 + M / 32) * 256);
+    if (s == 1 || cost < least) {
+      best = s;
+      least = cost;
+    }
+  }
+  return (int32_t)best;
+}
+
 // Sizes of a call; resolves num_splits (0: default).
 int check_chunk_sizes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq, int32_t max_pages_per_seq,
                       int32_t* num_splits) {
@@ -1113,21 +1135,37 @@ int check_chunk_sizes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
     return OSCAR_ERR_UNSUPPORTED;
   if (*num_splits == 0) *num_splits = oscar_chunk_default_splits(L, n_q, B, Hq, max_pages_per_seq);
   // a launch holds fewer than 2^32 threads
-  const int64_t g = Hq / L->num_kv_heads, M = chunk_tile_rows(n_q, B, (int)g);
+  const int64_t g = Hq / L->num_kv_heads;
+  const int64_t M = chunk_tile_rows(true, n_q, B, (int)g, (int64_t)B * max_pages_per_seq * L->num_kv_heads);
   return (n_q * g / M + B) * *num_splits * L->num_kv_heads > 0xffffff ? OSCAR_ERR_UNSUPPORTED : OSCAR_OK;
 }
 
+// quantized: the rotated queries, or (many rows) the expanded pages with their exponents and the
+// rotations; partial states where rows are split or rotated back afterwards.
 struct ChunkWs {
-  size_t qt_off, po_off, pml_off, total;
+  size_t qt_off, rot_off, exps_off, expanded_off, po_off, pml_off, total;
+  bool expands;
 };
-ChunkWs chunk_ws(int64_t n_q, int64_t Hq, int64_t S, bool quantized) {
-  const bool parts = quantized || S > 1;
+ChunkWs chunk_ws(const oscar_layout* L, int64_t n_q, int32_t B, int64_t Hq, int64_t max_pages, int64_t S,
+                 bool quantized) {
+  const size_t page_heads = (size_t)B * max_pages * L->num_kv_heads, rows = (size_t)(n_q * Hq);
   ChunkWs w;
-  w.qt_off = 0;
-  w.po_off = quantized ? align256((size_t)(n_q * Hq) * kD * sizeof(float)) : 0;
-  w.pml_off = align256(w.po_off + (parts ? (size_t)(n_q * Hq) * S * kD * sizeof(float) : 0));
-  w.total = align256(w.pml_off + (parts ? (size_t)(n_q * Hq) * S * 2 * sizeof(float) : 0));
-  if (w.total == 0) w.total = 256;
+  w.expands = quantized &&
+              chunk_tile_rows(true, n_q, B, (int)(Hq / L->num_kv_heads), (int64_t)page_heads) == kManyRows;
+  const bool parts = S > 1 || (quantized && !w.expands);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = align256(at + bytes);
+    return here;
+  };
+  w.qt_off = take(quantized && !w.expands ? rows * kD * sizeof(float) : 0);
+  w.rot_off = take(w.expands ? (size_t)2 * kRotBytes * (L->rot_per_head ? L->num_kv_heads : 1) : 0);
+  w.exps_off = take(w.expands ? page_heads * sizeof(int2) : 0);
+  w.expanded_off = take(w.expands ? page_heads * kExpandedBytes : 0);
+  w.po_off = take(parts ? rows * S * kD * sizeof(float) : 0);
+  w.pml_off = take(parts ? rows * S * 2 * sizeof(float) : 0);
+  w.total = at ? at : 256;
   return w;
 }
 
@@ -1165,6 +1203,7 @@ int chunk_attn(int format, const oscar_layout* L, const void* pages, const void*
                const int32_t* seq_lens, const float* R_k, const float* R_v, float sm_scale, int32_t window,
                int32_t sinks, int32_t num_splits, void* workspace, size_t workspace_bytes, void* out,
                void* stream) {
+  const bool choose = num_splits == 0;
   int st = check_chunk_sizes(L, n_q, B, Hq, max_pages_per_seq, &num_splits);
   if (st) return st;
   if (!isfinite(sm_scale) || window < 0 || sinks < 0) return OSCAR_ERR_INVALID_ARG;
@@ -1175,7 +1214,12 @@ int chunk_attn(int format, const oscar_layout* L, const void* pages, const void*
       !aligned(R_v, 16))
     return OSCAR_ERR_INVALID_ARG;
   const bool quantized = format != kBf16;
-  const ChunkWs ws = chunk_ws(n_q, Hq, num_splits, quantized);
+  if (choose && window > 0) {  // fewer where the window leaves few pages
+    const int64_t chunk = (n_q + B - 1) / B;
+    const int64_t seen = ((int64_t)window + sinks + std::min<int64_t>(chunk, kManyRows)) / L->page_size + 3;
+    num_splits = std::min(num_splits, chunk_splits(L, n_q, B, Hq, std::min<int64_t>(seen, max_pages_per_seq)));
+  }
+  const ChunkWs ws = chunk_ws(L, n_q, B, Hq, max_pages_per_seq, num_splits, quantized);
   if (workspace_bytes < ws.total) return OSCAR_ERR_WORKSPACE_TOO_SMALL;
   const size_t rows = (size_t)n_q * Hq * kD * sizeof(uint16_t), rot = (size_t)kD * kD * sizeof(float) *
                                                                       (L->rot_per_head ? L->num_kv_heads : 1);
@@ -1216,9 +1260,14 @@ int chunk_attn(int format, const oscar_layout* L, const void* pages, const void*
   a.part_o = reinterpret_cast<float*>(base + ws.po_off);
   a.part_ml = reinterpret_cast<float*>(base + ws.pml_off);
   a.out = static_cast<uint16_t*>(out);
+  a.Rk = R_k;
   a.Rv = R_v;
   a.rph = L->rot_per_head;
-  if (quantized) {
+  if (ws.expands) {
+    a.rot = base + ws.rot_off;
+    a.exps = reinterpret_cast<int2*>(base + ws.exps_off);
+    a.expanded = base + ws.expanded_off;
+  } else if (quantized) {
     float* qt = reinterpret_cast<float*>(base + ws.qt_off);
     st = hip_status(launch_decode_prepare(a.q, n_q, Hq, R_k, a.scale, qt, hs, L->rot_per_head, L->num_kv_heads));
     if (st) return st;
@@ -1234,22 +1283,13 @@ extern "C" {
 int32_t oscar_chunk_default_splits(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
                                    int32_t max_pages_per_seq) {
   if (check_decode_common(L, B, Hq, 1) != OSCAR_OK || n_q < 1 || max_pages_per_seq < 1) return 1;
-  const int64_t g = Hq / L->num_kv_heads;
-  const int M = chunk_tile_rows(n_q, B, (int)g);
-  // tiles as they come when the sequences' chunks are alike
-  const int64_t per_seq = (int64_t)n_q * g / B;
-  const int64_t tiles = B * std::max<int64_t>(1, (per_seq + M - 1) / M) * L->num_kv_heads;
-  // blocks: 4 for each that the GPU holds at once (one of the few-row kernel per CU, two of
-  // the other), and 16 pages at least for a block
-  const int64_t want = (int64_t)device_cus() * (M == 128 ? 8 : 4);
-  const int64_t s = std::min(want / tiles, (int64_t)max_pages_per_seq / 16);
-  return (int32_t)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
+  return chunk_splits(L, n_q, B, Hq, max_pages_per_seq);
 }
 
 size_t oscar_chunk_workspace_bytes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
                                    int32_t max_pages_per_seq, int32_t num_splits, int32_t quantized) {
   if (check_chunk_sizes(L, n_q, B, Hq, max_pages_per_seq, &num_splits) != OSCAR_OK) return 0;
-  return chunk_ws(n_q, Hq, num_splits, quantized != 0).total;
+  return chunk_ws(L, n_q, B, Hq, max_pages_per_seq, num_splits, quantized != 0).total;
 }
 
 int oscar_bf16_chunk_attn(const oscar_layout* L, const void* pages, const void* q, int32_t n_q, int32_t B,
