@@ -26,6 +26,7 @@
 // through the accumulators' exponent, which moves like m when a page needs more.
 #include "reduce_body.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace oscar {
@@ -92,6 +93,17 @@ __device__ inline float pow2(int e) {  // clamped to fp32's normal range
   return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23);
 }
 
+// A value that no one writes while the kernel runs, at an address that is the wave's: by a scalar
+// load, which the waits for vector loads do not meet.
+template <class T>
+__device__ inline T scalar_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)p;
+}
+__device__ inline int64_t uniform(int64_t x) {  // the same in all lanes: into scalar registers
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
 // ---------------------------------------------------------------------------
 // Tiles.  Sequence b's tiles have the numbers from floor(q_start[b] g / M) + b on: for any
 // chunk lengths at least as many as it has tiles, so that a block finds its sequence among
@@ -103,6 +115,17 @@ struct Tile {
   int row0, rows;  // first (token, head) row of the tile, rows of the sequence
   int len;
 };
+// Tile i of sequence b.
+__device__ inline Tile tile_at(const ChunkArgs& a, int b, int i, int g, int M) {  // (uniform)
+  Tile t;
+  t.b = b;
+  t.q0 = min(max(scalar_load(a.q_start + b), 0), a.n_q);
+  t.n = max(min(max(scalar_load(a.q_start + b + 1), 0), a.n_q) - t.q0, 0);
+  t.len = min(max(scalar_load(a.seq_lens + b), 0), a.max_pages * kP);
+  t.rows = t.n * g;
+  t.row0 = i * M;
+  return t;
+}
 __device__ inline Tile find_tile(const ChunkArgs& a, int64_t id, int g, int M) {
   const int l = threadIdx.x & 63;
   auto start = [&](int b) { return min(max(a.q_start[b], 0), a.n_q); };
@@ -115,15 +138,11 @@ __device__ inline Tile find_tile(const ChunkArgs& a, int64_t id, int g, int M) {
     lo += k * step;
     n = min(step, n - k * step);
   }
-  Tile t;
-  t.b = __builtin_amdgcn_readfirstlane(lo);
-  t.q0 = start(t.b);
-  t.n = max(start(t.b + 1) - t.q0, 0);
-  t.rows = t.n * g;
-  const int64_t r0 = (id - ((int64_t)t.q0 * g / M + t.b)) * M;
-  t.len = min(max(a.seq_lens[t.b], 0), a.max_pages * kP);
-  t.row0 = (int)r0;
-  if (r0 < 0 || r0 >= t.rows) t.b = -1;
+  const int b = __builtin_amdgcn_readfirstlane(lo);
+  Tile t = tile_at(a, b, 0, g, M);
+  const int64_t i = id - ((int64_t)t.q0 * g / M + b);
+  t.row0 = (int)(i * M);
+  if (i < 0 || i * M >= t.rows) t.b = -1;
   return t;
 }
 
@@ -315,12 +334,17 @@ __device__ inline void load_queries(const ChunkArgs& a, size_t row, bool live, u
     const float* src = a.qt + row * kD;
     float x[8][8], top = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
+    for (int ks = 0; ks < 8; ++ks) {
+      // (kInt2: the even elements four channels in order, the odd ones those eight further on)
+      const float4 lo = *reinterpret_cast<const float4*>(src + k_channel<FMT>(ks, h, 0));
+      const float4 hi = *reinterpret_cast<const float4*>(src + k_channel<FMT>(ks, h, FMT == kInt2 ? 1 : 4));
+      const float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[ks][e] = live ? src[k_channel<FMT>(ks, h, e)] : 0.0f;
+        x[ks][e] = live ? y[FMT == kInt2 ? e / 2 + 4 * (e % 2) : e] : 0.0f;
         top = fmaxf(top, fabsf(x[ks][e]));
       }
+    }
     const int e = max(exp_of(half_max(top)), -60) - 13;  // |q| < 2^14
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks)
@@ -393,10 +417,153 @@ __device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, flo
     }
 }
 
-// The row's output, or its partial state in slot s of its num_splits.  scale: of the accumulators.
+// ---------------------------------------------------------------------------
+// What a block does.  num_splits == 1: one tile, all of its pages.  Otherwise the pages of all
+// tiles of a KV head (as many for each of a sequence's tiles as the last one sees), laid end to
+// end, are cut into equal ranges, one for each block that the GPU holds at once; a tile's part of
+// a range leaves a partial state in the tile's slot for that range, counted from its first.
+// ---------------------------------------------------------------------------
+constexpr int kLeastPages = 4;  // of a range
+
+struct Segment {
+  Tile t;
+  Pages pg;
+  int x0, x1;   // pages of the tile
+  int slot;
+  bool last;    // no later range has pages of the tile
+  bool whole;   // no other range has
+};
+struct Walk {
+  int64_t x, xe, range;  // pages left, pages per range
+  int r, empty;          // the range; next sequence of those that see nothing
+  int empty_tile;
+};
+__device__ inline int64_t wave_sum_l(int64_t v) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+  return v;
+}
+// Tiles of sequence b, and the pages that its last one sees.
+__device__ inline int tiles_of(const ChunkArgs& a, int b, int g, int M, int window, int& pages) {
+  pages = 0;
+  if (b >= a.B) return 0;
+  Tile t;
+  t.q0 = min(max(a.q_start[b], 0), a.n_q);
+  t.n = max(min(max(a.q_start[b + 1], 0), a.n_q) - t.q0, 0);
+  t.len = min(max(a.seq_lens[b], 0), a.max_pages * kP);
+  t.rows = t.n * g;
+  const int tiles = (t.rows + M - 1) / M;
+  t.row0 = (tiles - 1) * M;
+  if (tiles > 0) pages = tile_pages(t, g, M, window, a.sinks).count;
+  return tiles;
+}
+__device__ inline Walk start_walk(const ChunkArgs& a, int g, int M, int window) {
+  Walk k = {};
+  k.r = (int)(blockIdx.x / a.Hkv);
+  if (a.num_splits == 1) return k;
+  const int l = threadIdx.x & 63, ranges = (int)(gridDim.x / a.Hkv);
+  int64_t all = 0;
+  int most = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int pages;
+    const int tiles = tiles_of(a, b0 + l, g, M, window, pages);
+    all += wave_sum_l((int64_t)tiles * pages);
+    most = max(most, wave_max_i(pages));
+  }
+  // (a tile meets ceil(pages / range) + 1 ranges at most)
+  k.range = uniform(max(max((all + ranges - 1) / ranges, (int64_t)((most + a.num_splits - 2) / (a.num_splits - 1))),
+                        (int64_t)kLeastPages));
+  k.x = k.r * k.range;
+  k.xe = min(uniform(all), k.x + k.range);
+  k.empty = k.r;
+  return k;
+}
+// The next segment.
+__device__ inline bool find_segment(const ChunkArgs& a, Walk& k, int g, int M, int window, Segment& s) {
+  if (a.num_splits == 1) {
+    if (k.empty) return false;
+    k.empty = 1;
+    // a sequence's last tiles, which see most, first
+    const int64_t n_ids = (int64_t)a.n_q * g / M + a.B;
+    s.t = find_tile(a, n_ids - 1 - k.r, g, M);
+    if (s.t.b < 0) return false;
+    s.pg = tile_pages(s.t, g, M, window, a.sinks);
+    s.x0 = s.slot = 0;
+    s.x1 = s.pg.count;
+    s.last = s.whole = true;
+    return true;
+  }
+  const int l = threadIdx.x & 63, ranges = (int)(gridDim.x / a.Hkv);
+  for (; k.empty < a.B; k.empty += ranges, k.empty_tile = 0) {  // rows that see nothing
+    Tile e = tile_at(a, k.empty, 0, g, M);
+    const int tiles = (e.rows + M - 1) / M;
+    if (k.empty_tile >= tiles) continue;
+    e.row0 = (tiles - 1) * M;
+    if (tile_pages(e, g, M, window, a.sinks).count > 0) continue;
+    e.row0 = k.empty_tile++ * M;
+    s.t = e;
+    s.pg = tile_pages(s.t, g, M, window, a.sinks);
+    s.x0 = s.x1 = s.slot = 0;
+    s.last = s.whole = true;
+    return true;
+  }
+  if (k.x >= k.xe) return false;
+  int64_t before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int pages;
+    const int tiles = tiles_of(a, b0 + l, g, M, window, pages);
+    const int64_t np = (int64_t)tiles * pages;
+    const int hi = wave_prefix((int)(np >> 16)), lo = wave_prefix((int)(np & 0xffff));  // lo < 2^22
+    const int64_t incl = before + ((int64_t)hi << 16) + lo;
+    const uint64_t hit = __ballot(np > 0 && incl - np <= k.x && k.x < incl);
+    if (hit) {
+      const int lane = __ffsll((unsigned long long)hit) - 1;
+      const int b = b0 + lane, count = __builtin_amdgcn_readlane(pages, lane);
+      const int64_t at = uniform(__shfl(incl - np, lane, 64));
+      const int tile = __builtin_amdgcn_readfirstlane((int)((k.x - at) / count));
+      const int64_t first = at + (int64_t)tile * count;
+      const int p0 = __builtin_amdgcn_readfirstlane((int)(k.x - first));
+      const int p1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)count, p0 + (k.xe - k.x)));
+      s.t = tile_at(a, b, tile, g, M);
+      s.pg = tile_pages(s.t, g, M, window, a.sinks);
+      s.x0 = min(p0, s.pg.count);
+      s.x1 = min(p1, s.pg.count);
+      s.slot = __builtin_amdgcn_readfirstlane((int)(k.r - first / k.range));
+      s.last = p1 == count;
+      s.whole = p0 == 0 && s.last;
+      k.x += p1 - p0;
+      return true;
+    }
+    before = uniform(__shfl(incl, 63, 64));
+  }
+  return false;  // not reached: page x lies in some tile
+}
+
+// The next segment, in scalar registers.
+__device__ inline bool next_segment(const ChunkArgs& a, Walk& k, int g, int M, int window, Segment& s) {
+  Segment x = {};
+  if (!__builtin_amdgcn_readfirstlane((int)find_segment(a, k, g, M, window, x))) return false;
+  auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  s.t = Tile{u(x.t.b), u(x.t.q0), u(x.t.n), u(x.t.row0), u(x.t.rows), u(x.t.len)};
+  s.pg = Pages{u(x.pg.head), u(x.pg.from), u(x.pg.count), u(x.pg.p_min), u(x.pg.p_max)};
+  s.x0 = u(x.x0);
+  s.x1 = u(x.x1);
+  s.slot = u(x.slot);
+  s.last = u(x.last);
+  s.whole = u(x.whole);
+  return true;
+}
+
+// Marks in slot 0 a row that has its output already.
+constexpr float kDone = INFINITY;
+
+// The row's output (direct), or its partial state in the segment's slot.  scale: of the
+// accumulators.
 template <int FMT>
-__device__ inline void store_row(const ChunkArgs& a, size_t row, int s, bool direct, const f16v (&o)[4], float m,
-                                 float l, float scale, int h) {
+__device__ inline void store_row(const ChunkArgs& a, size_t row, const Segment& s, bool direct, const f16v (&o)[4],
+                                 float m, float l, float scale, int h) {
+  const size_t at = row * a.num_splits + s.slot;
+  float2* ml = reinterpret_cast<float2*>(a.part_ml);
   if (direct) {
     const float il = (l > 0.0f ? 1.0f / l : is_nan(l) ? l : 0.0f) * scale;
     uint16_t* dst = a.out + row * kD;
@@ -406,32 +573,32 @@ __device__ inline void store_row(const ChunkArgs& a, size_t row, int s, bool dir
       v.y = pack2<kBf16>(z * il, w * il);
       *reinterpret_cast<uint2*>(dst + c) = v;
     });
+    if (a.num_splits > 1 && h == 0) ml[at] = make_float2(kDone, 0.0f);
     return;
   }
-  const size_t at = row * a.num_splits + s;
   float* dst = a.part_o + at * kD;
   if (is_nan(l)) m = 0.0f;  // NaN in a row: its scores have no maximum, but the state is not empty
   if (m != -INFINITY)    // of an empty state only that is read
     each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
       *reinterpret_cast<float4*>(dst + c) = make_float4(x * scale, y * scale, z * scale, w * scale);
     });
-  if (h == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, l);
+  if (h == 0) {
+    ml[at] = make_float2(m, l);
+    if (s.last)
+      for (int i = s.slot + 1; i < a.num_splits; ++i) ml[row * a.num_splits + i] = make_float2(-INFINITY, 0.0f);
+  }
 }
-
-// A row's state of a piece without pages: nothing, or (direct) a zero row.
-__device__ inline void store_empty(const ChunkArgs& a, size_t row, int s, bool direct, int h) {
+// A segment without pages.
+__device__ inline void store_empty(const ChunkArgs& a, size_t row, const Segment& s, bool direct, int h) {
+  float2* ml = reinterpret_cast<float2*>(a.part_ml) + row * a.num_splits;
   if (direct) {
     u4v* dst = reinterpret_cast<u4v*>(a.out + row * kD) + 8 * h;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dst[i] = u4v{0, 0, 0, 0};
+    if (a.num_splits > 1 && h == 0) ml[0] = make_float2(kDone, 0.0f);
   } else if (h == 0) {
-    reinterpret_cast<float2*>(a.part_ml)[row * a.num_splits + s] = make_float2(-INFINITY, 0.0f);
+    for (int i = s.slot; i < (s.last ? a.num_splits : s.slot + 1); ++i) ml[i] = make_float2(-INFINITY, 0.0f);
   }
-}
-
-// Pieces that a tile's pages are cut into: at least `least` pages each.
-__device__ inline int piece_count(int pages, int num_splits, int least) {
-  return min(num_splits, max(1, (pages + least - 1) / least));
 }
 
 // 16 bytes a lane from global memory to LDS, lane l's to dst + 16 l (dst: the wave's, a byte
@@ -451,12 +618,6 @@ __device__ inline void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-}
-// A value that no one writes while the kernel runs, at an address that is the wave's: by a scalar
-// load, which the waits for vector loads do not meet.
-template <class T>
-__device__ inline T scalar_load(const T* p) {
-  return *(const __attribute__((address_space(4))) T*)p;
 }
 __device__ inline uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
@@ -655,23 +816,20 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   __shared__ int exps[2][2];  // CODES: of the slots: K's exponent, the accumulators'
   const int g = a.Hq / a.Hkv;
   const int kvh = blockIdx.x % a.Hkv;
-  const int64_t rest = blockIdx.x / a.Hkv;
-  const int split = (int)(rest % a.num_splits);
-  // a sequence's last tiles, which see most, first
-  const int64_t n_ids = (int64_t)a.n_q * g / M + a.B;
-  const Tile t = find_tile(a, n_ids - 1 - rest / a.num_splits, g, M);
-  if (t.b < 0) return;
   const int window = a.window > 0 ? min(a.window, kNoWindow) : kNoWindow;
-  const Pages pg = tile_pages(t, g, M, window, a.sinks);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+  Walk walk = start_walk(a, g, M, window);
+  for (Segment sg; next_segment(a, walk, g, M, window, sg);) {
+  const Tile& t = sg.t;
+  const Pages& pg = sg.pg;
   const int r = t.row0 + w * kRows + n;
   const bool live = r < t.rows;
   const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
-  const int pieces = piece_count(pg.count, a.num_splits, 4);
-  const bool direct = !CODES && a.num_splits == 1;
-  if (split >= pieces || pg.count == 0) {
-    if (live) store_empty(a, row, split, direct, h);
-    return;
+  const bool direct = !CODES && sg.whole;
+  const int x0 = sg.x0, x1 = sg.x1;
+  if (x0 >= x1) {
+    if (live) store_empty(a, row, sg, direct, h);
+    continue;
   }
   RowState rs;
   rs.pos = live ? t.len - t.n + r / g : -1;
@@ -693,7 +851,6 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   } else {
     load_queries<FMT>(a, row, live, q, rs.c);
   }
-  const int x0 = (int)((int64_t)pg.count * split / pieces), x1 = (int)((int64_t)pg.count * (split + 1) / pieces);
   const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
   auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
   // index of a page's block: its number is loaded a page before it is needed
@@ -762,6 +919,9 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   if (FMT == kHalf) ex_next = page_exps(x0);
   lds_barrier();
   int slot = 0;
+  // positions of the wave's first and last row (none: nothing is seen)
+  const int wr0 = t.row0 + w * kRows, wr1 = min(wr0 + kRows, t.rows) - 1;
+  const int w_min = t.len - t.n + wr0 / g, w_max = wr0 <= wr1 ? t.len - t.n + wr1 / g : -1;
   int x = x0;
   do {
     const int t0 = page_of(x) * kP;
@@ -807,6 +967,9 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     }
     const int k_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
     const int v_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
+    // the wave's rows see something of the page
+    const bool seen = t0 <= w_max && (t0 + kP - 1 > w_min - window || t0 < a.sinks);
+    if (seen) {
     // scores, the operands read three steps ahead
     f16v s[2];
     {
@@ -840,7 +1003,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     u4v va[2][4];
 #pragma unroll
     for (int C = 0; C < 4; ++C) va[0][C] = v_at(C, 0);
-    if (t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks))
+    if (t0 + kP - 1 > w_min || (t0 <= w_max - window && t0 + kP > a.sinks))
       mask_page(s, rs.pos, t0, window, a.sinks);
     move_reference(s, o, rs, cp);
     // weights of a step's operand, two at a time between the products of the step before
@@ -874,6 +1037,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     asm volatile("" : "+v"(total));  // the additions stay among the products
     rs.l = FMT == kHalf ? fmaf(total, __builtin_amdgcn_exp2f(-weight), rs.l) : rs.l + total;
+    }
     if (!CODES) {  // page x + 1 has landed
       if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
       else wait_loads<0>();
@@ -890,8 +1054,9 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   } else if (FMT != kBf16) {
     unit = ldexpf(1.0f, e_o);
   }
-  if (!live) return;
-  store_row<FMT>(a, row, split, direct, o, rs.m, rs.l, unit, h);
+  if (live) store_row<FMT>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
+  lds_barrier();  // the slots are free again
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -903,23 +1068,22 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
   constexpr int M = kRows;
   constexpr bool HL = FMT == kBf16;  // p in two bf16 pieces: costs nothing where the loads bound
   __shared__ Scales<FMT == kBf16 ? 1 : NG> scales[FMT == kBf16 ? 1 : kWaves];
-  __shared__ float os[kWaves][4][16][64];
+  __shared__ float4 os[kWaves][4][4][64];
   __shared__ float2 ml[kWaves][kRows];
   const int g = a.Hq / a.Hkv;
   const int kvh = blockIdx.x % a.Hkv;
-  const int64_t rest = blockIdx.x / a.Hkv;
-  const int split = (int)(rest % a.num_splits);
-  const Tile t = find_tile(a, rest / a.num_splits, g, M);
-  if (t.b < 0) return;
   const int window = a.window > 0 ? min(a.window, kNoWindow) : kNoWindow;
-  const Pages pg = tile_pages(t, g, M, window, a.sinks);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
   const int lo = l & 15, b16 = (l >> 4) & 1;
+  Walk walk = start_walk(a, g, M, window);
+  for (Segment sg; next_segment(a, walk, g, M, window, sg);) {
+  const Tile& t = sg.t;
+  const Pages& pg = sg.pg;
   const int r = t.row0 + n;
   const bool live = r < t.rows;
   const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
-  const int pieces = piece_count(pg.count, a.num_splits, 4);
-  const bool direct = FMT == kBf16 && a.num_splits == 1;
+  const bool direct = FMT == kBf16 && sg.whole;
+  const int x0 = sg.x0, x1 = sg.x1;
   RowState rs;
   rs.pos = live ? t.len - t.n + r / g : -1;
   rs.m = -INFINITY;
@@ -930,17 +1094,14 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
   int e_v = kNoExp;
-  const bool any = split < pieces && pg.count > 0;
-  const int x0 = any ? (int)((int64_t)pg.count * split / pieces) : 0;
-  const int x1 = any ? (int)((int64_t)pg.count * (split + 1) / pieces) : 0;
   if (x0 + w < x1) {
     const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
     auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
     auto block_of = [&](int x) {
-      return a.pages + ((size_t)bt[page_of(x)] * a.Hkv + kvh) * block_bytes_of(FMT, NG);
+      return a.pages + ((size_t)scalar_load(bt + page_of(x)) * a.Hkv + kvh) * block_bytes_of(FMT, NG);
     };
     constexpr int kL = FMT == kBf16 ? 16 : raw_loads<FMT>();
-    u4v rk[kL], rv[kL];
+    u4v rk[kL], rv[kL], rv_next[kL];  // (codes: V's of the next page beside the page's)
     uint32_t ks[NG], vs[NG];
     auto fetch_k = [&](const uint8_t* blk) {
 #pragma unroll
@@ -953,7 +1114,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
         }
       }
     };
-    auto fetch_v = [&](const uint8_t* blk) {
+    auto fetch_v = [&](const uint8_t* blk, u4v (&rv)[kL]) {
 #pragma unroll
       for (int i = 0; i < kL; ++i) {
         if (FMT == kBf16) {  // (C, step) = (i / 4, i % 4)
@@ -968,20 +1129,21 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     const uint8_t* blk = block_of(x0 + w);
     fetch_k(blk);
     if (FMT != kBf16) {
-      fetch_v(blk);
+      fetch_v(blk, rv);
       load_entries<FMT, NG>(blk, 0, ks);
       load_entries<FMT, NG>(blk, 1, vs);
     }
     u4v q[8];
     load_queries<FMT>(a, row, live, q, rs.c);
     Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
-    for (int x = x0 + w; x < x1; x += kWaves) {
+    int x = x0 + w;
+    do {
       const int t0 = page_of(x) * kP, ntok = t.len - t0;
       const bool more = x + kWaves < x1;
       const uint8_t* next = more ? block_of(x + kWaves) : blk;
       int e_k = 0;
       if (FMT == kBf16) {
-        fetch_v(blk);
+        fetch_v(blk, rv);
       } else {
         const int e_old = e_v;
         lane_exchange();  // the last page's scales have been read
@@ -1009,7 +1171,14 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
           else ka = k_operand<FMT, NG>(rk[FMT == kInt4 ? 2 * T + k / 4 : T], T, k, sc);
           s[T] = mfma<FMT>(ka, q[k], s[T]);
         }
-      if (FMT == kBf16 && more) fetch_k(next);
+      if (more) {  // the next page's loads, as soon as there is room for them
+        fetch_k(next);
+        if (FMT != kBf16) {
+          fetch_v(next, rv_next);
+          load_entries<FMT, NG>(next, 0, ks);
+          load_entries<FMT, NG>(next, 1, vs);
+        }
+      }
       const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
       u4v p[4], pl[4];
       if (masked) mask_page(s, rs.pos, t0, window, a.sinks);
@@ -1033,14 +1202,12 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
           if (HL) o[C] = mfma<FMT>(va, pl[k], o[C]);
           o[C] = mfma<FMT>(va, p[k], o[C]);
         }
-      if (FMT != kBf16 && more) {
-        fetch_k(next);
-        fetch_v(next);
-        load_entries<FMT, NG>(next, 0, ks);
-        load_entries<FMT, NG>(next, 1, vs);
-      }
+      if (FMT != kBf16)
+#pragma unroll
+        for (int i = 0; i < kL; ++i) rv[i] = rv_next[i];
       blk = next;
-    }
+      x += kWaves;
+    } while (x < x1);
   }
   // merge: wave w sums tile C = w of the four states
   const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
@@ -1050,7 +1217,8 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
 #pragma unroll
   for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) os[w][C][i][l] = o[C][i] * unit;
+    for (int i = 0; i < 4; ++i)
+      os[w][C][i][l] = make_float4(o[C][4 * i] * unit, o[C][4 * i + 1] * unit, o[C][4 * i + 2] * unit, o[C][4 * i + 3] * unit);
   __syncthreads();
   float m = -INFINITY, L = 0.0f, f[kWaves];
 #pragma unroll
@@ -1060,41 +1228,82 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     f[k] = ml[k][n].x == -INFINITY ? 0.0f : exp2f(ml[k][n].x - m);
     L += f[k] * ml[k][n].y;
   }
-  if (!live) return;
   // each wave stores a quarter of the channels: registers 4 w .. 4 w + 3 of every tile
-  f16v sum[4];
+  float sum[4][4] = {};
 #pragma unroll
   for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float v = 0.0f;
+    for (int k = 0; k < kWaves; ++k)
+      if (f[k] != 0.0f) {
+        const float4 v = os[k][C][w][l];
+        sum[C][0] = fmaf(f[k], v.x, sum[C][0]);
+        sum[C][1] = fmaf(f[k], v.y, sum[C][1]);
+        sum[C][2] = fmaf(f[k], v.z, sum[C][2]);
+        sum[C][3] = fmaf(f[k], v.w, sum[C][3]);
+      }
+  if (live) {
+    const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
+    const size_t at = row * a.num_splits + sg.slot;
+    auto put = [&](int c, float x, float y, float z, float v) {
+      if (direct) {
+        uint2 d;
+        d.x = pack2<kBf16>(x * il, y * il);
+        d.y = pack2<kBf16>(z * il, v * il);
+        *reinterpret_cast<uint2*>(a.out + row * kD + c) = d;
+      } else if (m != -INFINITY) {  // of an empty state only that is read
+        *reinterpret_cast<float4*>(a.part_o + at * kD + c) = make_float4(x, y, z, v);
+      }
+    };
+    const int rr = 8 * w + 4 * h;
+    if (FMT == kInt2) {
 #pragma unroll
-      for (int k = 0; k < kWaves; ++k) v += f[k] != 0.0f ? f[k] * os[k][C][4 * w + i][l] : 0.0f;
-      sum[C][i] = v;
+      for (int i = 0; i < 4; ++i) put(4 * (rr + i), sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
+    } else {
+#pragma unroll
+      for (int C = 0; C < 4; ++C)
+        put(FMT == kBf16 ? 32 * C + rr : 64 * (C / 2) + 32 * (rr / 16) + 16 * (C % 2) + rr % 16, sum[C][0], sum[C][1],
+            sum[C][2], sum[C][3]);
     }
-  const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
-  const size_t at = row * a.num_splits + split;
-  auto put = [&](int c, float x, float y, float z, float v) {
-    if (direct) {
-      uint2 d;
-      d.x = pack2<kBf16>(x * il, y * il);
-      d.y = pack2<kBf16>(z * il, v * il);
-      *reinterpret_cast<uint2*>(a.out + row * kD + c) = d;
-    } else if (m != -INFINITY) {  // of an empty state only that is read
-      *reinterpret_cast<float4*>(a.part_o + at * kD + c) = make_float4(x, y, z, v);
+    if (w == 0 && h == 0 && (!direct || a.num_splits > 1)) {
+      float2* dst = reinterpret_cast<float2*>(a.part_ml) + row * a.num_splits;
+      dst[sg.slot] = direct ? make_float2(kDone, 0.0f) : make_float2(m, L);
+      if (sg.last && !direct)
+        for (int i = sg.slot + 1; i < a.num_splits; ++i) dst[i] = make_float2(-INFINITY, 0.0f);
     }
-  };
-  const int rr = 8 * w + 4 * h;
-  if (FMT == kInt2) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) put(4 * (rr + i), sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
-  } else {
-#pragma unroll
-    for (int C = 0; C < 4; ++C)
-      put(FMT == kBf16 ? 32 * C + rr : 64 * (C / 2) + 32 * (rr / 16) + 16 * (C % 2) + rr % 16, sum[C][0], sum[C][1],
-          sum[C][2], sum[C][3]);
   }
-  if (!direct && w == 0 && h == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, L);
+  __syncthreads();  // os, ml and the scales are free again
+  }
+}
+
+// Merge of the partial states in the output's basis, of the rows that belong to a sequence and have
+// no output yet: 32 lanes a row, four channels each; a live state follows no empty one.
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int64_t row0) {
+  const int64_t row = row0 + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int c = threadIdx.x & 31, S = a.num_splits;
+  if (row >= (int64_t)min(max(a.q_start[a.B], 0), a.n_q) * a.Hq) return;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + row * S;
+  if (ml[0].x == kDone) return;
+  float M = -INFINITY;
+  for (int s = 0; s < S; ++s) M = fmaxf(M, ml[s].x);
+  const float4* po = reinterpret_cast<const float4*>(a.part_o + row * S * kD) + c;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float L = 0.0f;
+  for (int s = 0; s < S; ++s) {
+    const float2 x = ml[s];
+    if (x.x == -INFINITY) continue;  // (pages that the row does not see)
+    const float e = __builtin_amdgcn_exp2f(x.x - M);
+    const float4 v = po[(size_t)s * (kD / 4)];
+    L = fmaf(e, x.y, L);
+    o.x = fmaf(e, v.x, o.x);
+    o.y = fmaf(e, v.y, o.y);
+    o.z = fmaf(e, v.z, o.z);
+    o.w = fmaf(e, v.w, o.w);
+  }
+  const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
+  uint2 d;
+  d.x = pack2<kBf16>(o.x * il, o.y * il);
+  d.y = pack2<kBf16>(o.z * il, o.w * il);
+  reinterpret_cast<uint2*>(a.out + row * kD)[c] = d;
 }
 
 // Merge of the splits and back-rotation, of the rows that belong to a sequence.
@@ -1109,12 +1318,15 @@ __global__ __launch_bounds__(kRedThreads) void chunk_reduce_kernel(ChunkArgs a, 
 }
 
 template <int FMT, int NG>
-hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
-  const int g = a.Hq / a.Hkv;
+hipError_t launch_fmt(const ChunkArgs& args, hipStream_t st) {
+  const int g = args.Hq / args.Hkv;
   const bool quantized = FMT != kBf16;
-  const int64_t page_heads = (int64_t)a.B * a.max_pages * a.Hkv;
-  const int M = chunk_tile_rows(quantized, a.n_q, a.B, g, page_heads);
-  const unsigned blocks = (unsigned)(((int64_t)a.n_q * g / M + a.B) * a.num_splits * a.Hkv);
+  const int64_t page_heads = (int64_t)args.B * args.max_pages * args.Hkv;
+  const int M = chunk_tile_rows(quantized, args.n_q, args.B, g, page_heads);
+  const ChunkArgs& a = args;
+  const int64_t tiles = (int64_t)a.n_q * g / M + a.B;
+  const int ranges = std::max(1, chunk_blocks(quantized, M) / a.Hkv);
+  const unsigned blocks = (unsigned)((a.num_splits == 1 ? tiles : ranges) * a.Hkv);
   bool merged = !quantized && a.num_splits == 1, rotated = false;
   if (M == kRows) {
     hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3(blocks), dim3(256), 0, st, a);
@@ -1133,8 +1345,12 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || merged) return e;
-  ChunkArgs m = a;
-  if (rotated) m.Rv = nullptr;
+  if (!quantized || rotated)
+    return by_seqs(a.n_q, launch_seqs(a.Hq), [&](int t0, int n) {
+      hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)(((int64_t)n * a.Hq + 7) / 8)), dim3(256), 0, st, a,
+                         (int64_t)t0 * a.Hq);
+      return hipGetLastError();
+    });
   // rows in parts of whole tokens that a launch holds
   const int per = launch_seqs(a.Hq);
   return by_seqs(a.n_q, per, [&](int t0, int n) {
@@ -1142,7 +1358,7 @@ hipError_t launch_fmt(const ChunkArgs& a, hipStream_t st) {
     auto go = [&](auto rb) {
       constexpr int RB = decltype(rb)::value;
       hipLaunchKernelGGL((chunk_reduce_kernel<RB>), dim3((unsigned)query_blocks(n, a.Hq, a.Hkv, a.rph, RB)),
-                         dim3(kRedThreads), 0, st, m, row0, rows);
+                         dim3(kRedThreads), 0, st, a, row0, rows);
     };
     switch (reduce_rows(rows)) {
       case 16: go(std::integral_constant<int, 16>{}); break;
@@ -1161,6 +1377,11 @@ int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int64_
   if (rows <= (int64_t)kRows * B) return kRows;
   // (expanded pages: 2 GiB at most)
   return rows <= (int64_t)512 * B || (quantized && page_heads > 65536) ? 4 * kRows : kManyRows;
+}
+
+// Blocks that the GPU holds at once.
+int chunk_blocks(bool quantized, int tile_rows) {
+  return device_cus() * (tile_rows == kManyRows || (tile_rows == kRows && !quantized) ? 1 : 2);
 }
 
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st) {

@@ -1103,24 +1103,20 @@ namespace {
 
 // Splits for tiles that see `pages` pages at most.
 int32_t chunk_splits(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq, int64_t pages) {
-  const int64_t g = Hq / L->num_kv_heads;
+  const int64_t g = Hq / L->num_kv_heads, Hkv = L->num_kv_heads;
   const int M = chunk_tile_rows(false, n_q, B, (int)g, 0);
-  // tiles as they come when the sequences' chunks are alike
-  const int64_t per_seq = (int64_t)n_q * g / B;
-  const int64_t tiles = B * std::max<int64_t>(1, (per_seq + M - 1) / M) * L->num_kv_heads;
-  // Blocks run in rounds of as many as the GPU holds; a block costs its pages, and what it does once
-  // and the partial state it leaves, about as much as 6 pages and (rows / 32) more.
-  const int64_t at_once = (int64_t)device_cus() * (M == kManyRows ? 1 : 2);
-  int64_t best = 1, least = 0;
-  for (int64_t s = 1; s == 1 || (s <= 64 && s * 16 <= pages); ++s) {
-    const int64_t rounds = (tiles * s + at_once - 1) / at_once;
-    const int64_t cost = rounds * (pages * 256 / s + (s == 1 ? 6 : 6 + M / 32) * 256);
-    if (s == 1 || cost < least) {
-      best = s;
-      least = cost;
-    }
-  }
-  return (int32_t)best;
+  // tiles of a KV head as they come when the sequences' chunks are alike
+  const int64_t tiles = B * std::max<int64_t>(1, ((int64_t)n_q * g / B + M - 1) / M);
+  const int64_t at_once = chunk_blocks(true, M), ranges = std::max<int64_t>(1, at_once / Hkv);
+  // Whole tiles run in rounds of as many blocks as the GPU holds; ranges are even, but tiles that two
+  // ranges share are begun twice and leave partial states.  A tile's begin takes about 6 pages' time,
+  // a block's share of the states (6 + rows / 32) three times.
+  const int64_t rounds = (tiles * Hkv + at_once - 1) / at_once, whole = rounds * (pages + 6);
+  const int64_t cut = tiles * (pages + 6) / ranges + 3 * (6 + M / 32);
+  if (pages <= 16 || rounds > 4 || whole <= cut) return 1;
+  // slots for the longest sequence when the average one is half as long
+  const int64_t range = std::max<int64_t>(4, tiles * pages / 2 / ranges);
+  return (int32_t)std::min<int64_t>(pages / range + 2, 64);
 }
 
 // Sizes of a call; resolves num_splits (0: default).
