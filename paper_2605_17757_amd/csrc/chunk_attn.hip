@@ -227,10 +227,6 @@ __device__ inline void load_entries(const uint8_t* blk, int is_v, uint32_t (&x)[
     x[g] = reinterpret_cast<const uint32_t*>(blk + off)[at];
   }
 }
-__device__ inline float meta_f32(uint32_t half, int bf16) {
-  return bf16 ? __uint_as_float(half << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)half);
-}
-
 // Scales of a page in LDS, a wave's own: per group the slots' (s 2^24, -s z), divided by the
 // page's power of two.  K: both halves of a dword, by slot.  V: arrays of fp16, eight slots of a
 // step in 16 bytes, in the order of the step's elements.
@@ -249,14 +245,26 @@ constexpr int kNoExp = -400;
 template <int FMT, int NG>
 __device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16, int ntok, Scales<NG>& sc, int& e) {
   const int l = threadIdx.x & 63;
+  const uint32_t written = l < ntok ? 0xffffffffu : 0u;  // slots never written: scale 0
   float s[NG], z[NG];
+  if (bf16) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      s[g] = bf_lo(ent[g] & written);
+      z[g] = bf_hi(ent[g] & written);
+    }
+  } else {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const uint32_t both = ent[g] & written;
+      const h2 x = __builtin_bit_cast(h2, both);
+      s[g] = (float)x.x;
+      z[g] = (float)x.y;
+    }
+  }
   int need = kNoExp;
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    s[g] = l < ntok ? meta_f32(ent[g] & 0xffffu, bf16) : 0.0f;  // slots never written
-    z[g] = l < ntok ? meta_f32(ent[g] >> 16, bf16) : 0.0f;
-    if (l < ntok) need = max(need, entry_exp(s[g], z[g]));
-  }
+  for (int g = 0; g < NG; ++g) need = max(need, entry_exp(s[g], z[g]));
   e = max(e, wave_max_i(need));
   const int at = FMT == kInt2 ? (l & ~3) + 2 * (l & 1) + ((l >> 1) & 1) : l;  // v_slot's inverse
 #pragma unroll
@@ -1101,7 +1109,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
       return a.pages + ((size_t)scalar_load(bt + page_of(x)) * a.Hkv + kvh) * block_bytes_of(FMT, NG);
     };
     constexpr int kL = FMT == kBf16 ? 16 : raw_loads<FMT>();
-    u4v rk[kL], rv[kL], rv_next[kL];  // (codes: V's of the next page beside the page's)
+    u4v rk[kL], rv0[kL], rv1[FMT == kBf16 ? 1 : kL];  // codes: V's of the next page beside the page's
     uint32_t ks[NG], vs[NG];
     auto fetch_k = [&](const uint8_t* blk) {
 #pragma unroll
@@ -1114,7 +1122,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
         }
       }
     };
-    auto fetch_v = [&](const uint8_t* blk, u4v (&rv)[kL]) {
+    auto fetch_v = [&](const uint8_t* blk, auto& rv) {
 #pragma unroll
       for (int i = 0; i < kL; ++i) {
         if (FMT == kBf16) {  // (C, step) = (i / 4, i % 4)
@@ -1129,7 +1137,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     const uint8_t* blk = block_of(x0 + w);
     fetch_k(blk);
     if (FMT != kBf16) {
-      fetch_v(blk, rv);
+      fetch_v(blk, rv0);
       load_entries<FMT, NG>(blk, 0, ks);
       load_entries<FMT, NG>(blk, 1, vs);
     }
@@ -1137,7 +1145,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     load_queries<FMT>(a, row, live, q, rs.c);
     Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
     int x = x0 + w;
-    do {
+    auto page = [&](auto& rv, auto& rv_next) {
       const int t0 = page_of(x) * kP, ntok = t.len - t0;
       const bool more = x + kWaves < x1;
       const uint8_t* next = more ? block_of(x + kWaves) : blk;
@@ -1202,12 +1210,19 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
           if (HL) o[C] = mfma<FMT>(va, pl[k], o[C]);
           o[C] = mfma<FMT>(va, p[k], o[C]);
         }
-      if (FMT != kBf16)
-#pragma unroll
-        for (int i = 0; i < kL; ++i) rv[i] = rv_next[i];
       blk = next;
       x += kWaves;
-    } while (x < x1);
+    };
+    if constexpr (FMT == kBf16) {
+      do page(rv0, rv0);
+      while (x < x1);
+    } else {
+      do {
+        page(rv0, rv1);
+        if (x >= x1) break;
+        page(rv1, rv0);
+      } while (x < x1);
+    }
   }
   // merge: wave w sums tile C = w of the four states
   const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
