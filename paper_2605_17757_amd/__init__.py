@@ -718,14 +718,22 @@ class Rope:
     (fp32 GPU tensor), times ``attn_scale``."""
 
     def __init__(self, rotary_dim: int, inv_freq, interleaved: bool = False, attn_scale: float = 1.0):
-        self.rotary_dim, self.inv_freq = int(rotary_dim), inv_freq
-        self.interleaved, self.attn_scale = bool(interleaved), float(attn_scale)
+        self._rotary_dim, self._inv_freq = int(rotary_dim), inv_freq
+        self._interleaved, self._attn_scale = bool(interleaved), float(attn_scale)
+        self._struct = None
+
+    rotary_dim = property(lambda self: self._rotary_dim)
+    inv_freq = property(lambda self: self._inv_freq)
+    interleaved = property(lambda self: self._interleaved)
+    attn_scale = property(lambda self: self._attn_scale)
 
     def _arg(self, dev: int) -> _RopeArg:
         f = None
-        if self.rotary_dim > 0:
-            f = _arg(self.inv_freq, torch.float32, "inv_freq", self.rotary_dim // 2, dev)
-        return _RopeArg(self.rotary_dim, int(self.interleaved), self.attn_scale, f)
+        if self._rotary_dim > 0:
+            f = _arg(self._inv_freq, torch.float32, "inv_freq", self._rotary_dim // 2, dev)
+        if self._struct is None or self._struct.inv_freq != f:
+            self._struct = _RopeArg(self._rotary_dim, int(self._interleaved), self._attn_scale, f)
+        return self._struct
 
 
 def _rows_arg(x, name: str, n_tok: int, heads, dev: int):
@@ -734,16 +742,17 @@ def _rows_arg(x, name: str, n_tok: int, heads, dev: int):
         raise TypeError("%s must be a torch.Tensor" % name)
     if x.dtype is not torch.bfloat16:
         raise TypeError("%s must be torch.bfloat16, got %s" % (name, x.dtype))
-    if not x.is_cuda:
-        raise ValueError("%s must be a GPU tensor" % name)
     if x.get_device() != dev:
+        if not x.is_cuda:
+            raise ValueError("%s must be a GPU tensor" % name)
         raise ValueError("%s is on %s, but the current device is cuda:%d" % (name, x.device, dev))
-    if x.dim() != 3 or x.shape[0] != n_tok or x.shape[2] != HEAD_DIM or (heads is not None and x.shape[1] != heads):
+    shape = tuple(x.shape)
+    if len(shape) != 3 or shape[0] != n_tok or shape[2] != HEAD_DIM or (heads is not None and shape[1] != heads):
         raise ValueError("%s must be [%d, %s, %d]" % (name, n_tok, "heads" if heads is None else heads, HEAD_DIM))
-    heads = int(x.shape[1])
-    if n_tok > 0 and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != HEAD_DIM)):
+    st = x.stride()
+    if n_tok > 0 and (st[2] != 1 or (st[1] != HEAD_DIM and shape[1] > 1)):
         raise ValueError("%s must have a token's heads contiguous" % name)
-    return x.data_ptr(), (int(x.stride(0)) if n_tok > 1 else heads * HEAD_DIM)
+    return x.data_ptr(), (st[0] if n_tok > 1 else shape[1] * HEAD_DIM)
 
 
 def _weight_arg(w, name: str, dev: int):

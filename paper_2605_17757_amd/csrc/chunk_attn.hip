@@ -291,11 +291,20 @@ __device__ inline u4v k_operand(const u4v& raw, int T, int ks, const Scales<NG>&
   const int g = FMT == kInt4 ? 32 * (ks % 4) / G : (64 * h + 16 * (ks / 2)) / G;
   const uint32_t ab = sc.k[g][4 * lo + 2 * T + b];
   const uint32_t A = __builtin_amdgcn_perm(ab, ab, 0x01000100u), B = __builtin_amdgcn_perm(ab, ab, 0x03020302u);
-  const uint32_t d = FMT == kInt4 ? raw[ks % 4] : raw[ks / 2] >> (8 * (ks % 2));
   u4v r;
+  if (FMT == kInt4) {
+    const uint32_t d = raw[ks % 4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = FMT == kInt4 ? fma_h2((d >> (4 * i)) & 0x000f000fu, A, B) : fma_h2((d >> (2 * i)) & 0x00030003u, A, B);
+    for (int i = 0; i < 4; ++i) r[i] = fma_h2((d >> (4 * i)) & 0x000f000fu, A, B);
+  } else {  // codes in place: n 4^i 2^-24, with the scale divided by 4^i
+    const uint32_t d = raw[ks / 2] >> (8 * (ks % 2));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const _Float16 m = (_Float16)(1.0f / (1 << (2 * i)));
+      const uint32_t Ai = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, A) * h2{m, m});
+      r[i] = fma_h2(d & (0x00030003u << (2 * i)), Ai, B);
+    }
+  }
   return r;
 }
 // V operand of tile C, step (j0, i2) from its raw load.

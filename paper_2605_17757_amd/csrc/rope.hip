@@ -10,7 +10,11 @@
 // hardware's sine and cosine take turns.
 // Eight lanes hold a (token, head) row, two chunks of 8 channels each, so chosen that a
 // lane has both channels of its pairs; the norm's sum is three DPP steps.
+// Bound: memory.  8191 tokens of 32 + 8 heads, 168 MB read and written: 30 us, 5.6 TB/s; with
+// pages, 16503 tokens of 64 + 8 heads, 676 MB: 147 us, 4.6 TB/s (a copy of 2 GiB: 4.9).
 #include "internal.h"
+
+#include <type_traits>
 
 namespace oscar {
 namespace {
@@ -59,74 +63,120 @@ __device__ inline void lane_chunks(int j, int rotary, int interleaved, int& c0, 
   }
 }
 
-// One wave's unit: heads [8 u, 8 u + 8) of the Hq + Hkv query and key heads of a token.
-template <bool PAGES>
-__device__ inline void rows_unit(const RopeRows& a, int64_t unit, int per_tok) {
-  const int l = threadIdx.x & 63, j = l & 7;
-  const int64_t tok = unit / per_tok;
-  const int head = (int)(unit - tok * per_tok) * kUnitHeads + (l >> 3);
-  const int heads = a.Hq + a.Hkv;
-  const bool is_k = head >= a.Hq, live = head < heads;
-  const int kvh = head - a.Hq;
-  const uint16_t* src = is_k ? a.k + (size_t)tok * a.k_stride + (size_t)kvh * kD
-                             : a.q + (size_t)tok * a.q_stride + (size_t)head * kD;
-  int c0, c1;
-  lane_chunks(j, a.rotary, a.interleaved, c0, c1);
-  u4v w0{0, 0, 0, 0}, w1{0, 0, 0, 0};
-  if (live) {
-    w0 = *reinterpret_cast<const u4v*>(src + 8 * c0);
-    w1 = *reinterpret_cast<const u4v*>(src + 8 * c1);
+// What a lane does with its 16 channels of a row: the angles of its pairs (cos 1, sin 0 where it
+// rotates nothing), norm, rotation.
+__device__ inline void angles(const RopeRows& a, int j, int64_t position, float (&cs)[8], float (&sn)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = 1.0f;
+    sn[i] = 0.0f;
   }
+  if (j >= a.rotary / 16) return;
+  const double pos = (double)position * 0.15915494309189533577;  // 1 / 2 pi
+  const float4* fp = reinterpret_cast<const float4*>(a.freq + 8 * j);
+  const float4 f0 = fp[0], f1 = fp[1];
+  const float fr[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double turns = pos * (double)fr[i];
+    const float t = (float)(turns - __builtin_rint(turns));
+    cs[i] = __builtin_amdgcn_cosf(t) * a.factor;
+    sn[i] = __builtin_amdgcn_sinf(t) * a.factor;
+  }
+}
+__device__ inline void norm_rotate(const RopeRows& a, const uint16_t* weight, int j, int c0, int c1,
+                                   const float (&cs)[8], const float (&sn)[8], u4v& w0, u4v& w1) {
   float x[16];
   unpack8(w0, x);
   unpack8(w1, x + 8);
-  const uint16_t* wt = is_k ? a.k_weight : a.q_weight;
-  if (wt) {
+  if (weight) {
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s = fmaf(x[i], x[i], s);
     const float r = 1.0f / sqrtf(sum8(s) * (1.0f / kD) + a.eps);
     float g[16];
-    unpack8(*reinterpret_cast<const u4v*>(wt + 8 * c0), g);
-    unpack8(*reinterpret_cast<const u4v*>(wt + 8 * c1), g + 8);
+    unpack8(*reinterpret_cast<const u4v*>(weight + 8 * c0), g);
+    unpack8(*reinterpret_cast<const u4v*>(weight + 8 * c1), g + 8);
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = x[i] * r * g[i];
   }
   if (j < a.rotary / 16) {
-    const double pos = (double)a.positions[tok] * 0.15915494309189533577;  // 1 / 2 pi
-    float fr[8];  // frequencies of the lane's pairs
-    const float4* fp = reinterpret_cast<const float4*>(a.freq + 8 * j);
-    const float4 f0 = fp[0], f1 = fp[1];
-    fr[0] = f0.x; fr[1] = f0.y; fr[2] = f0.z; fr[3] = f0.w;
-    fr[4] = f1.x; fr[5] = f1.y; fr[6] = f1.z; fr[7] = f1.w;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const double turns = pos * (double)fr[i];
-      const float t = (float)(turns - __builtin_rint(turns));
-      const float c = __builtin_amdgcn_cosf(t) * a.factor, s = __builtin_amdgcn_sinf(t) * a.factor;
       float& p = a.interleaved ? x[2 * i] : x[i];
       float& q = a.interleaved ? x[2 * i + 1] : x[8 + i];
-      const float u = p * c - q * s, v = q * c + p * s;
-      p = u;
+      const float y = p * cs[i] - q * sn[i], v = q * cs[i] + p * sn[i];
+      p = y;
       q = v;
     }
   }
   w0 = pack8(x);
   w1 = pack8(x + 8);
-  if (!live) return;
-  if (PAGES && is_k) {
+}
+
+// A wave takes up to `units` units of a token, 8 of its query and (without pages) key heads each,
+// with the sines and cosines in registers.
+template <bool PAGES>
+__device__ inline void rows_units(const RopeRows& a, int64_t item, int units, int per_tok) {
+  const int l = threadIdx.x & 63, j = l & 7;
+  const int parts = (per_tok + units - 1) / units;
+  const int64_t tok = item / parts;
+  const int u0 = (int)(item - tok * parts) * units, u1 = min(u0 + units, per_tok);
+  const int heads = a.Hq + (PAGES ? 0 : a.Hkv);
+  int c0, c1;
+  lane_chunks(j, a.rotary, a.interleaved, c0, c1);
+  u4v w0{0, 0, 0, 0}, w1{0, 0, 0, 0};
+  auto load = [&](int u) {
+    const int head = u * kUnitHeads + (l >> 3);
+    if (head >= heads) return;
+    const uint16_t* src = !PAGES && head >= a.Hq ? a.k + (size_t)tok * a.k_stride + (size_t)(head - a.Hq) * kD
+                                                 : a.q + (size_t)tok * a.q_stride + (size_t)head * kD;
+    w0 = *reinterpret_cast<const u4v*>(src + 8 * c0);
+    w1 = *reinterpret_cast<const u4v*>(src + 8 * c1);
+  };
+  load(u0);
+  float cs[8], sn[8];
+  angles(a, j, a.positions[tok], cs, sn);
+  for (int u = u0; u < u1; ++u) {
+    const int head = u * kUnitHeads + (l >> 3);
+    const bool is_k = !PAGES && head >= a.Hq;
+    u4v y0 = w0, y1 = w1;
+    if (u + 1 < u1) load(u + 1);
+    norm_rotate(a, is_k ? a.k_weight : a.q_weight, j, c0, c1, cs, sn, y0, y1);
+    if (head >= heads) continue;
+    uint16_t* dst = is_k ? a.k_out + ((size_t)tok * a.Hkv + head - a.Hq) * kD
+                         : a.q_out + ((size_t)tok * a.Hq + head) * kD;
+    *reinterpret_cast<u4v*>(dst + 8 * c0) = y0;
+    *reinterpret_cast<u4v*>(dst + 8 * c1) = y1;
+  }
+}
+
+// Keys of TOK tokens of one KV head into the pages, eight tokens a wave at a time.  A page's 128
+// bytes hold 16 of eight slots each (every fourth slot): from one block, and so one L2, they go to
+// memory as whole lines (a token's heads in one wave: 16503 tokens of 64 + 8 heads took 154 us, 147 now).
+template <int TOK>
+__device__ inline void keys_tile(const RopeRows& a, int64_t tile) {
+  const int kvh = (int)(tile % a.Hkv);
+  const int64_t tok0 = tile / a.Hkv * TOK;
+  const int l = threadIdx.x & 63, j = l & 7;
+  int c0, c1;
+  lane_chunks(j, a.rotary, a.interleaved, c0, c1);
+  for (int r = (threadIdx.x >> 6) * 8 + (l >> 3); r < TOK; r += 32) {
+    const bool live = tok0 + r < a.n_tok;
+    const int64_t tok = live ? tok0 + r : a.n_tok - 1;
+    const uint16_t* src = a.k + (size_t)tok * a.k_stride + (size_t)kvh * kD;
+    u4v w0 = *reinterpret_cast<const u4v*>(src + 8 * c0), w1 = *reinterpret_cast<const u4v*>(src + 8 * c1);
+    float cs[8], sn[8];
+    angles(a, j, a.positions[tok], cs, sn);
+    norm_rotate(a, a.k_weight, j, c0, c1, cs, sn, w0, w1);
     const int64_t slot = a.slots[tok];
-    if (slot < 0) return;
+    if (!live || slot < 0) continue;
     const int t = (int)(slot % kP);
     u4v* blk = reinterpret_cast<u4v*>(a.pages + ((size_t)(slot / kP) * a.Hkv + kvh) * kBlockElems);
     // chunk c: channels 32 hi + 8 kc of slot 4 lo + u
     blk[((t & 3) * 4 + (c0 & 3)) * 64 + (t >> 2) + 16 * (c0 >> 2)] = w0;
     blk[((t & 3) * 4 + (c1 & 3)) * 64 + (t >> 2) + 16 * (c1 >> 2)] = w1;
-    return;
   }
-  uint16_t* dst = is_k ? a.k_out + ((size_t)tok * a.Hkv + kvh) * kD : a.q_out + ((size_t)tok * a.Hq + head) * kD;
-  *reinterpret_cast<u4v*>(dst + 8 * c0) = w0;
-  *reinterpret_cast<u4v*>(dst + 8 * c1) = w1;
 }
 
 // Values of TOK tokens of one KV head into the pages.  A page holds eight slots of a
@@ -185,20 +235,23 @@ __device__ inline void values_tile(const RopeRows& a, int64_t tile, uint8_t* sme
 }
 
 template <bool PAGES, int TOK>
-__global__ __launch_bounds__(256) void rope_kernel(RopeRows a, int64_t row_blocks, int per_tok) {
+__global__ __launch_bounds__(256) void rope_kernel(RopeRows a, int64_t row_blocks, int units, int per_tok) {
   __shared__ __align__(16) uint8_t smem[PAGES ? TOK * (kD + 2) * 2 + TOK * 8 + TOK * 4 : 16];
   if (!PAGES || blockIdx.x < row_blocks) {
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit < (int64_t)a.n_tok * per_tok) rows_unit<PAGES>(a, unit, per_tok);
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (item < (int64_t)a.n_tok * ((per_tok + units - 1) / units)) rows_units<PAGES>(a, item, units, per_tok);
     return;
   }
-  if (PAGES) values_tile<TOK>(a, (int64_t)blockIdx.x - row_blocks, smem);
+  if (PAGES) {
+    keys_tile<TOK>(a, (int64_t)blockIdx.x - row_blocks);
+    values_tile<TOK>(a, (int64_t)blockIdx.x - row_blocks, smem);
+  }
 }
 
 template <bool PAGES, int TOK>
 hipError_t launch(const RopeRows& a, hipStream_t st) {
   // a launch holds fewer than 2^32 threads: the tokens in parts where they need more
-  const int per_tok = (a.Hq + a.Hkv + kUnitHeads - 1) / kUnitHeads;
+  const int per_tok = (a.Hq + (PAGES ? 0 : a.Hkv) + kUnitHeads - 1) / kUnitHeads;
   const int64_t per = (int64_t)per_tok + (PAGES ? a.Hkv : 0);
   int64_t most = ((int64_t)1 << 23) / per / 64 * 64;
   if (most < 64) most = 64;
@@ -212,10 +265,14 @@ hipError_t launch(const RopeRows& a, hipStream_t st) {
     if (p.v) p.v += t0 * a.v_stride;
     p.positions += t0;
     if (p.slots) p.slots += t0;
-    const int64_t rows = ((int64_t)p.n_tok * per_tok + 3) / 4;
+    // Two units a wave where that leaves each SIMD eight waves: 8191 tokens of 32 + 8 heads take 35 us
+    // with one, 30 with two, 29 with all five; 16503 of 64 heads (more than the caches hold) 146,
+    // 147 and, with eight, 154.
+    const int units = (int64_t)p.n_tok * per_tok >= 64 * device_cus() ? 2 : 1;
+    const int64_t rows = per_tok ? ((int64_t)p.n_tok * ((per_tok + units - 1) / units) + 3) / 4 : 0;
     const int64_t tiles = PAGES ? (int64_t)((p.n_tok + TOK - 1) / TOK) * a.Hkv : 0;
     hipLaunchKernelGGL((rope_kernel<PAGES, TOK>), dim3((unsigned)(rows + tiles)), dim3(256), 0, st, p, rows,
-                       per_tok);
+                       units, per_tok);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
