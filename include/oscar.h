@@ -594,7 +594,9 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  *   o = softmax(sm_scale * q K^T) V     (quantized caches: K^, V^ as in oscar_decode_attn)
  * A row that sees no token (seq_lens[b] < n_b) is zero.  Rows from q_start[B] on are left as
  * they were.  Pages of the block table that no new token of the sequence sees are not read, and
- * their entries may be anything.  Slots past a sequence's length may hold anything.
+ * their entries may be anything.  Slots past a sequence's length may hold anything; a NaN or an
+ * infinity among the values that some new token of the sequence sees may reach the rows of others.
+ * A NaN in a query row gives NaN in its own output row only.
  * Products of bf16 values are exact, their sums, softmax statistics and outputs' sums are fp32.
  * Softmax weights enter the value product rounded to bf16 (to two bf16 pieces where n_q Hq/Hkv is
  * at most 32 B); over a quantized cache weights, rotated
@@ -607,9 +609,14 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  *   seq_lens    : int32 [B], the new tokens included; clamped to [0, max_pages_per_seq * 64]
  *   window      : >= 0, 0: none; sinks >= 0, used with a window
  *   num_splits  : pieces that a row's pages are cut into at most (>= 1, at most 1024), or 0 for
- *                 oscar_chunk_default_splits; results do not depend on it beyond fp32 rounding
+ *                 oscar_chunk_default_splits, or fewer where a window leaves few pages or the
+ *                 workspace room for fewer; results do not depend on it beyond fp32 rounding
  *   workspace   : >= oscar_chunk_workspace_bytes(L, n_q, B, Hq, max_pages_per_seq, num_splits,
- *                 quantized) bytes, 256-byte aligned, contents need no initialization
+ *                 quantized) bytes, 256-byte aligned, contents need no initialization.  With
+ *                 num_splits 0 one for the largest n_q serves smaller ones too.  Over a quantized
+ *                 cache, chunks of more than 512 (token, head) rows per sequence and KV head on
+ *                 average have their pages expanded to 16 bits there (32 KiB for a page of
+ *                 block_table and KV head) while these are at most 65536.
  *   out         : bf16 [n_q, Hq, d]
  * q and out are 16-byte aligned.  n_q == 0 launches nothing.
  */

@@ -436,8 +436,8 @@ __device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, flo
 
 // ---------------------------------------------------------------------------
 // What a block does.  num_splits == 1: one tile, all of its pages.  Otherwise the pages of all
-// tiles of a KV head (as many for each of a sequence's tiles as the last one sees), laid end to
-// end, are cut into equal ranges, one for each block that the GPU holds at once; a tile's part of
+// tiles of a KV head (as many for each of a sequence's tiles as one sees at most), laid end to end,
+// are cut into equal ranges, one for each block that the GPU holds at once; a tile's part of
 // a range leaves a partial state in the tile's slot for that range, counted from its first.
 // ---------------------------------------------------------------------------
 constexpr int kLeastPages = 4;  // of a range
@@ -460,7 +460,7 @@ __device__ inline int64_t wave_sum_l(int64_t v) {
   for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
   return v;
 }
-// Tiles of sequence b, and the pages that its last one sees.
+// Tiles of sequence b, and the pages that one of them sees at most: none without cached tokens.
 __device__ inline int tiles_of(const ChunkArgs& a, int b, int g, int M, int window, int& pages) {
   pages = 0;
   if (b >= a.B) return 0;
@@ -469,9 +469,15 @@ __device__ inline int tiles_of(const ChunkArgs& a, int b, int g, int M, int wind
   t.n = max(min(max(a.q_start[b + 1], 0), a.n_q) - t.q0, 0);
   t.len = min(max(a.seq_lens[b], 0), a.max_pages * kP);
   t.rows = t.n * g;
+  t.row0 = 0;
   const int tiles = (t.rows + M - 1) / M;
-  t.row0 = (tiles - 1) * M;
-  if (tiles > 0) pages = tile_pages(t, g, M, window, a.sinks).count;
+  if (tiles == 1) {
+    pages = tile_pages(t, g, M, window, a.sinks).count;
+  } else if (tiles > 1) {
+    // a window's and a tile's tokens lie in so many pages at most, the first tokens in the others
+    const int64_t span = (int64_t)window + (M - 1) / g + 1;
+    pages = (int)min((span + kP - 2) / kP + 1 + ((int64_t)a.sinks + kP - 1) / kP, (int64_t)(t.len + kP - 1) / kP);
+  }
   return tiles;
 }
 __device__ inline Walk start_walk(const ChunkArgs& a, int g, int M, int window) {
@@ -513,10 +519,7 @@ __device__ inline bool find_segment(const ChunkArgs& a, Walk& k, int g, int M, i
   const int l = threadIdx.x & 63, ranges = (int)(gridDim.x / a.Hkv);
   for (; k.empty < a.B; k.empty += ranges, k.empty_tile = 0) {  // rows that see nothing
     Tile e = tile_at(a, k.empty, 0, g, M);
-    const int tiles = (e.rows + M - 1) / M;
-    if (k.empty_tile >= tiles) continue;
-    e.row0 = (tiles - 1) * M;
-    if (tile_pages(e, g, M, window, a.sinks).count > 0) continue;
+    if (e.len > 0 || k.empty_tile >= (e.rows + M - 1) / M) continue;
     e.row0 = k.empty_tile++ * M;
     s.t = e;
     s.pg = tile_pages(s.t, g, M, window, a.sinks);

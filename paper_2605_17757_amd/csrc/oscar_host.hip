@@ -1162,6 +1162,8 @@ ChunkWs chunk_ws(const oscar_layout* L, int64_t n_q, int32_t B, int64_t Hq, int6
   w.po_off = take(parts ? rows * S * kD * sizeof(float) : 0);
   w.pml_off = take(parts ? rows * S * 2 * sizeof(float) : 0);
   w.total = at ? at : 256;
+  // chunks of fewer tokens need no more: those of the most rows that are not expanded
+  if (w.expands) w.total = std::max(w.total, (size_t)512 * B * L->num_kv_heads * (2 * kD + 2) * sizeof(float) + 768);
   return w;
 }
 
@@ -1215,6 +1217,9 @@ int chunk_attn(int format, const oscar_layout* L, const void* pages, const void*
     const int64_t seen = ((int64_t)window + sinks + std::min<int64_t>(chunk, kManyRows)) / L->page_size + 3;
     num_splits = std::min(num_splits, chunk_splits(L, n_q, B, Hq, std::min<int64_t>(seen, max_pages_per_seq)));
   }
+  while (choose && num_splits > 1 &&
+         chunk_ws(L, n_q, B, Hq, max_pages_per_seq, num_splits, quantized).total > workspace_bytes)
+    --num_splits;
   const ChunkWs ws = chunk_ws(L, n_q, B, Hq, max_pages_per_seq, num_splits, quantized);
   if (workspace_bytes < ws.total) return OSCAR_ERR_WORKSPACE_TOO_SMALL;
   const size_t rows = (size_t)n_q * Hq * kD * sizeof(uint16_t), rot = (size_t)kD * kD * sizeof(float) *

@@ -149,6 +149,120 @@ def test_splits(fmt, new, splits):
     c.check(q, new, c.run(q, new, 200, 70, splits=splits), 200, 70)
 
 
+MANY = 512   # (token, head) rows per sequence past which 256 rows share a page, and codes are expanded first
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "kv4", "kv2"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (90, 5), (300, 200)])
+@pytest.mark.parametrize("new,lens,Hq,Hkv", [([600], [600], 1, 1), ([515, 0, 600], [900, 64, 610], 2, 1),
+                                             ([200], [331], 16, 4), ([100, 170], [1000, 170], 16, 2)])
+@pytest.mark.parametrize("splits", [0, 1, 6])
+def test_many_rows(fmt, window, sinks, new, lens, Hq, Hkv, splits):
+    assert sum(new) * Hq // Hkv > MANY * len(new)
+    c = Cache(fmt, lens, Hkv, seed=window + sinks + Hq)
+    q = _q(new, Hq)
+    for b, (n, length) in enumerate(zip(new, lens)):
+        seen = R.visible(n, length, window, sinks).any(0)
+        for i in range(c.mp):
+            if not seen[i * P:(i + 1) * P].any():
+                c.block_table[b, i] = 0
+    out = c.run(q, new, window, sinks, splits=splits)
+    c.check(q, new, out, window, sinks)
+    assert torch.equal(out, c.run(q, new, window, sinks, splits=splits))
+
+
+@pytest.mark.parametrize("fmt", ["kv4", "kv2"])
+@pytest.mark.parametrize("G", [32, 64, 128])
+@pytest.mark.parametrize("meta,per_head,rot", [(0, False, True), (1, True, True), (1, False, False)])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_many_rows_formats(fmt, G, meta, per_head, rot, splits):
+    new, lens = [300, 260], [640, 261]
+    c = Cache(fmt, lens, 3, seed=G, G=G, meta=meta, per_head=per_head, rot=rot)
+    q = _q(new, 6)
+    q[3] = 0
+    q[5] *= 1e-20
+    q[6] *= 40
+    c.check(q, new, c.run(q, new, splits=splits))
+
+
+@pytest.mark.parametrize("fmt", ["kv4", "kv2"])
+@pytest.mark.parametrize("new", [[600], [80], [3]])
+def test_tables_past_what_is_expanded(fmt, new):
+    # more than 65536 (page, KV head) pairs in the table: codes are expanded by the blocks that read them
+    c = Cache(fmt, [700], 1, seed=16)
+    wide = torch.zeros(1, 66000, dtype=torch.int32, device="cuda")
+    wide[:, :c.mp] = c.block_table
+    c.block_table, c.mp = wide, 66000
+    q = _q(new, 2)
+    for splits in (0, 1):
+        c.check(q, new, c.run(q, new, splits=splits))
+
+
+@pytest.mark.parametrize("fmt,meta", [("kv4", 0), ("kv4", 1), ("kv2", 0), ("kv2", 1)])
+@pytest.mark.parametrize("new", [[2], [90], [520]])
+def test_rows_of_zeros_and_of_one_value(fmt, meta, new):
+    """What the quantizer stores of rows without a range: scale 1, zero point -value, codes 0."""
+    c = Cache(fmt, [600], 1, seed=17, meta=meta)
+    Hkv, L = 1, c.L
+    pool = ok.kv4_alloc_pool(L) if fmt == "kv4" else ok.alloc_pool(L)
+    k = torch.zeros(600, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    k[200:] = 0.75
+    v[100:400] = -2.5
+    v[400:] = 1e-3
+    at = torch.arange(600, device="cuda")
+    slots = c.block_table[0].long()[at // P] * P + at % P
+    (ok.kv4_append if fmt == "kv4" else ok.kv_append)(L, pool, k, v, slots, None, None, 1.0, 1.0)
+    c.pool, c.Rk, c.Rv = pool, None, None
+    M = (lambda x: x.to(torch.bfloat16 if meta else torch.float16).double())
+    c.k, c.v = [M(k.float())], [M(v.float())]
+    c.koff, c.voff = [c.k[0].abs()], [c.v[0].abs()]
+    q = _q(new, 2)
+    c.check(q, new, c.run(q, new))
+
+
+def test_one_workspace_for_smaller_chunks():
+    for fmt in ("bf16", "kv4"):
+        c = Cache(fmt, [3000], 2, seed=18)
+        ws = ok.chunk_alloc_workspace(c.L, 1100, 1, 4, c.mp, 0, quantized=fmt != "bf16")
+        for n in (1100, 600, 250, 30, 1):
+            q = _q([n], 4)
+            c.check(q, [n], c.run(q, [n], ws=ws))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "kv4", "kv2"])
+def test_debug_checks(fmt, monkeypatch):
+    monkeypatch.setenv("OSCAR_DEBUG", "1")
+    new, lens = [2, 3], [200, 64]
+    c = Cache(fmt, lens, 1, seed=19)
+    q = _q(new, 2)
+    out = torch.full_like(q, 3.0)
+    c.run(q, new, out=out)
+    c.check(q, new, out)
+    table, lens_t = c.block_table.clone(), c.seq_lens.clone()
+    out.fill_(3.0)
+
+    def refused(**kw):
+        with pytest.raises(ok.OscarError) as e:
+            c.run(q, kw.pop("new", new), out=out, **kw)
+        assert e.value.status == ok.ERR_INVALID_ARG and (out == 3.0).all()
+    c.block_table[1, 0] = c.L.num_pages        # (never dereferenced)
+    refused()
+    c.block_table[1, 0] = -1
+    refused()
+    c.block_table.copy_(table)
+    c.block_table[0, 0] = -1                    # outside the window: not looked at
+    refused()
+    c.run(q, new, window=70, out=out)
+    c.block_table.copy_(table)
+    out.fill_(3.0)
+    c.seq_lens[0] = c.mp * P + 1
+    refused()
+    c.seq_lens.copy_(lens_t)
+    refused(new=[4, 2])                          # 6 rows of 5
+    refused(new=[3, -1])                         # descending
+
+
 @pytest.mark.parametrize("fmt", ["kv4", "kv2"])
 @pytest.mark.parametrize("G", [32, 64, 128])
 @pytest.mark.parametrize("meta,per_head,rot", [(0, False, True), (1, True, True), (1, False, False)])
