@@ -644,10 +644,10 @@ __device__ inline uint32_t lds_address(const void* p) {
 }
 
 // ---------------------------------------------------------------------------
-// Chunks of many rows over a quantized cache: every page is read by many blocks, and its codes
-// are expanded once, to what a wave gives the matrix cores, with R_k and R_v as operands beside
-// them (two fp16 pieces of each entry, so that the rotations cost no precision against q's and
-// o's own rounding).
+// Chunks over a quantized cache: R_k and R_v as operands (two fp16 pieces of each entry, so that the
+// rotations cost no precision against q's and o's own rounding), for the blocks to rotate their
+// rows; and where a page is read by many blocks, its codes expanded once to what a wave gives the
+// matrix cores.
 // ---------------------------------------------------------------------------
 // Part `part` (of four) of a page's K or V: four operands of 1 KB at dst; NATURAL: V's slots in
 // order within a step, whatever the codes' order.
@@ -676,20 +676,21 @@ __device__ inline int v_channel(int C, int r) {
   return FMT == kInt2 ? 4 * r + C : FMT == kInt4 ? 64 * (C / 2) + 32 * (r / 16) + 16 * (C % 2) + r % 16 : 32 * C + r;
 }
 
-// Blocks: a page of a sequence's table and a KV head each; behind them one for each rotation.
+// Blocks: a page of a sequence's table and a KV head each (`pages` of them, or none); behind them
+// kRotParts for each rotation.
+constexpr int kRotParts = 8;
 template <int FMT, int NG>
-__global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages) {
   __shared__ Scales<NG> scales[4];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
-  const int64_t pages = (int64_t)a.B * a.max_pages * a.Hkv;
   if (blockIdx.x >= pages) {
     // operand (tile, step, piece): R_k: rows the channels of q~ that the score steps take, 8 input
     // channels of q each; R_v: rows 32 output channels, steps the channels of o~ in a lane
-    const int which = (int)(blockIdx.x - pages), is_v = which & 1;
+    const int which = (int)(blockIdx.x - pages) / kRotParts, is_v = which & 1;
     const float* R = is_v ? a.Rv : a.Rk;
     if (R) R += (size_t)(which >> 1) * kD * kD;
     const int r = l & 31, h = l >> 5;
-    for (int i = w; i < 32; i += 4) {
+    for (int i = 4 * (int)((blockIdx.x - pages) % kRotParts) + w; i < 32; i += 4 * kRotParts) {
       const int C = i / 8, k = i % 8;
       u4v hi, lo;
 #pragma unroll
@@ -830,7 +831,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   constexpr bool CODES = FMT == kInt4 || FMT == kInt2;
   constexpr int kSlots = W == 8 ? 3 : 2;
   static_assert(W == 4 || (W == 8 && !CODES), "a block expands codes a part per wave");
-  static_assert(FMT != kHalf || kSlots * kPageLds >= kRotBytes, "a rotation's operands fit in the pages' slots");
+  static_assert(kSlots * kPageLds >= kRotBytes, "a rotation's operands fit in the pages' slots");
   __shared__ __align__(16) uint8_t lds[kSlots * kPageLds];
   __shared__ Scales<CODES ? NG : 1> scales[CODES ? W : 1];
   __shared__ int exps[2][2];  // CODES: of the slots: K's exponent, the accumulators'
@@ -845,7 +846,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   const int r = t.row0 + w * kRows + n;
   const bool live = r < t.rows;
   const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
-  const bool direct = !CODES && sg.whole;
+  const bool direct = sg.whole;
   const int x0 = sg.x0, x1 = sg.x1;
   if (x0 >= x1) {
     if (live) store_empty(a, row, sg, direct, h);
@@ -862,9 +863,9 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     wait_loads<0>();
     lds_barrier();
   };
-  const uint8_t* rot = FMT == kHalf ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
+  const uint8_t* rot = FMT != kBf16 ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
   u4v q[8];
-  if constexpr (FMT == kHalf) {
+  if constexpr (FMT != kBf16) {
     fill(rot, kRotBytes);
     rotate_queries(a, row, live, lds, q, rs.c);
     lds_barrier();
@@ -1068,13 +1069,11 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     slot = slot + 1 == kSlots ? 0 : slot + 1;
   } while (++x < x1);
   rs.l = half_sum(rs.l);
-  if constexpr (FMT == kHalf) {
+  if constexpr (FMT != kBf16) {
     fill(rot + kRotBytes, kRotBytes);
     unit = rotate_output(o, rs.l, e_o, lds);
-  } else if (FMT != kBf16) {
-    unit = ldexpf(1.0f, e_o);
   }
-  if (live) store_row<FMT>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
+  if (live) store_row<kBf16>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
   lds_barrier();  // the slots are free again
   }
 }
@@ -1303,28 +1302,51 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
 }
 
 // Merge of the partial states in the output's basis, of the rows that belong to a sequence and have
-// no output yet: 32 lanes a row, four channels each; a live state follows no empty one.
+// no output yet: 32 lanes a row, four channels each.  A lane reads the maximum and sum of one slot in
+// 32; the states' loads are issued eight slots at a time (empty ones, at the end but for pages that
+// the row does not see, weigh 0).
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int64_t row0) {
   const int64_t row = row0 + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int c = threadIdx.x & 31, S = a.num_splits;
-  if (row >= (int64_t)min(max(a.q_start[a.B], 0), a.n_q) * a.Hq) return;
+  if (row >= (int64_t)min(max(scalar_load(a.q_start + a.B), 0), a.n_q) * a.Hq) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + row * S;
-  if (ml[0].x == kDone) return;
+  const float2 first = ml[min(c, S - 1)];
+  if (__shfl(first.x, 0, 32) == kDone) return;
   float M = -INFINITY;
-  for (int s = 0; s < S; ++s) M = fmaxf(M, ml[s].x);
+  int live = 0;  // one past the last state that is not empty
+  for (int s0 = 0; s0 < S; s0 += 32) {
+    const float2 x = s0 == 0 ? first : ml[min(s0 + c, S - 1)];
+    const bool is = s0 + c < S && x.x != -INFINITY;
+    M = fmaxf(M, is ? x.x : -INFINITY);
+    live = max(live, is ? s0 + c + 1 : 0);
+  }
+#pragma unroll
+  for (int m = 16; m >= 1; m >>= 1) {
+    M = fmaxf(M, __shfl_xor(M, m, 32));
+    live = max(live, __shfl_xor(live, m, 32));
+  }
   const float4* po = reinterpret_cast<const float4*>(a.part_o + row * S * kD) + c;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float L = 0.0f;
-  for (int s = 0; s < S; ++s) {
-    const float2 x = ml[s];
-    if (x.x == -INFINITY) continue;  // (pages that the row does not see)
-    const float e = __builtin_amdgcn_exp2f(x.x - M);
-    const float4 v = po[(size_t)s * (kD / 4)];
-    L = fmaf(e, x.y, L);
-    o.x = fmaf(e, v.x, o.x);
-    o.y = fmaf(e, v.y, o.y);
-    o.z = fmaf(e, v.z, o.z);
-    o.w = fmaf(e, v.w, o.w);
+  for (int s0 = 0; s0 < live; s0 += 8) {
+    float2 x[8];
+    float4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int s = min(s0 + k, live - 1);
+      x[k] = ml[s];
+      v[k] = po[(size_t)s * (kD / 4)];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (s0 + k >= live || x[k].x == -INFINITY) continue;  // (nothing but -inf is written of an empty state)
+      const float e = __builtin_amdgcn_exp2f(x[k].x - M);
+      L = fmaf(e, x[k].y, L);
+      o.x = fmaf(e, v[k].x, o.x);
+      o.y = fmaf(e, v[k].y, o.y);
+      o.z = fmaf(e, v[k].z, o.z);
+      o.w = fmaf(e, v[k].w, o.w);
+    }
   }
   const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
   uint2 d;
@@ -1354,25 +1376,24 @@ hipError_t launch_fmt(const ChunkArgs& args, hipStream_t st) {
   const int64_t tiles = (int64_t)a.n_q * g / M + a.B;
   const int ranges = std::max(1, chunk_blocks(quantized, M) / a.Hkv);
   const unsigned blocks = (unsigned)((a.num_splits == 1 ? tiles : ranges) * a.Hkv);
-  bool merged = !quantized && a.num_splits == 1, rotated = false;
-  if (M == kRows) {
+  if constexpr (FMT != kBf16)
+    if (M != kRows) {  // the rotations' operands, and (256 rows) the pages'
+      const int64_t pages = M == kManyRows ? page_heads : 0;
+      hipLaunchKernelGGL((expand_kernel<FMT, NG>), dim3((unsigned)(pages + kRotParts * 2 * (a.rph ? a.Hkv : 1))),
+                         dim3(256), 0, st, a, pages);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  if (M == kRows)
     hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3(blocks), dim3(256), 0, st, a);
-  } else if (M == 4 * kRows) {
+  else if (M == 4 * kRows)
     hipLaunchKernelGGL((chunk_kernel<FMT, NG, 4>), dim3(blocks), dim3(256), 0, st, a);
-  } else if constexpr (FMT == kBf16) {
-    hipLaunchKernelGGL((chunk_kernel<kBf16, 1, 8>), dim3(blocks), dim3(512), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((expand_kernel<FMT, NG>), dim3((unsigned)(page_heads + 2 * (a.rph ? a.Hkv : 1))), dim3(256), 0,
-                       st, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((chunk_kernel<kHalf, 1, 8>), dim3(blocks), dim3(512), 0, st, a);
-    merged = a.num_splits == 1;
-    rotated = true;
-  }
+  else
+    hipLaunchKernelGGL((chunk_kernel<FMT == kBf16 ? kBf16 : kHalf, 1, 8>), dim3(blocks), dim3(512), 0, st, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || merged) return e;
-  if (!quantized || rotated)
+  const bool rotated = quantized && M == kRows;  // partial states in the rotated basis
+  if (e != hipSuccess || (a.num_splits == 1 && !rotated)) return e;
+  if (!rotated)
     return by_seqs(a.n_q, launch_seqs(a.Hq), [&](int t0, int n) {
       hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)(((int64_t)n * a.Hq + 7) / 8)), dim3(256), 0, st, a,
                          (int64_t)t0 * a.Hq);

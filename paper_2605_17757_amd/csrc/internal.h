@@ -297,7 +297,7 @@ struct ChunkArgs {
   int format, ng, meta_bf16;
   int Hkv, Hq, B, n_q;
   const uint16_t* q;   // bf16 [n_q][Hq][128] (bf16 cache)
-  const float* qt;     // rotated, scaled by sm_scale log2 e (quantized caches, pages not expanded)
+  const float* qt;     // rotated, scaled by sm_scale log2 e (quantized caches, tiles of 32 rows)
   const int32_t* q_start;
   const int32_t* block_table;
   int max_pages;
@@ -311,9 +311,9 @@ struct ChunkArgs {
   const float* Rk;
   const float* Rv;
   int rph;
-  // Quantized caches, chunks of many rows: the pages as fp16 operands, kExpandedBytes for each
-  // (sequence, page of its table, KV head), the exponents that they are divided by (K's, V's), and
-  // R_k, R_v as operands, kRotBytes each; null: expanded by the blocks that read them.
+  // Quantized caches, larger tiles: R_k, R_v as operands, kRotBytes each; with kManyRows the pages as
+  // fp16 operands, kExpandedBytes for each (sequence, page of its table, KV head), and the exponents
+  // that they are divided by (K's, V's).
   uint8_t* expanded;
   int2* exps;
   uint8_t* rot;

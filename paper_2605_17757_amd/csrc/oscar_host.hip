@@ -1136,34 +1136,34 @@ int check_chunk_sizes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
   return (n_q * g / M + B) * *num_splits * L->num_kv_heads > 0xffffff ? OSCAR_ERR_UNSUPPORTED : OSCAR_OK;
 }
 
-// quantized: the rotated queries, or (many rows) the expanded pages with their exponents and the
-// rotations; partial states where rows are split or rotated back afterwards.
+// quantized: the rotated queries (few rows: 32 a tile), or the rotations and (256) the expanded pages
+// with their exponents; partial states where rows are split, or rotated back afterwards.
 struct ChunkWs {
   size_t qt_off, rot_off, exps_off, expanded_off, po_off, pml_off, total;
-  bool expands;
+  int tile_rows;
 };
 ChunkWs chunk_ws(const oscar_layout* L, int64_t n_q, int32_t B, int64_t Hq, int64_t max_pages, int64_t S,
                  bool quantized) {
   const size_t page_heads = (size_t)B * max_pages * L->num_kv_heads, rows = (size_t)(n_q * Hq);
   ChunkWs w;
-  w.expands = quantized &&
-              chunk_tile_rows(true, n_q, B, (int)(Hq / L->num_kv_heads), (int64_t)page_heads) == kManyRows;
-  const bool parts = S > 1 || (quantized && !w.expands);
+  w.tile_rows = chunk_tile_rows(quantized, n_q, B, (int)(Hq / L->num_kv_heads), (int64_t)page_heads);
+  const bool few = quantized && w.tile_rows == 32, expands = quantized && w.tile_rows == kManyRows;
+  const bool parts = S > 1 || few;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
     at = align256(at + bytes);
     return here;
   };
-  w.qt_off = take(quantized && !w.expands ? rows * kD * sizeof(float) : 0);
-  w.rot_off = take(w.expands ? (size_t)2 * kRotBytes * (L->rot_per_head ? L->num_kv_heads : 1) : 0);
-  w.exps_off = take(w.expands ? page_heads * sizeof(int2) : 0);
-  w.expanded_off = take(w.expands ? page_heads * kExpandedBytes : 0);
+  w.qt_off = take(few ? rows * kD * sizeof(float) : 0);
+  w.rot_off = take(quantized && !few ? (size_t)2 * kRotBytes * (L->rot_per_head ? L->num_kv_heads : 1) : 0);
+  w.exps_off = take(expands ? page_heads * sizeof(int2) : 0);
+  w.expanded_off = take(expands ? page_heads * kExpandedBytes : 0);
   w.po_off = take(parts ? rows * S * kD * sizeof(float) : 0);
   w.pml_off = take(parts ? rows * S * 2 * sizeof(float) : 0);
   w.total = at ? at : 256;
-  // chunks of fewer tokens need no more: those of the most rows that are not expanded
-  if (w.expands) w.total = std::max(w.total, (size_t)512 * B * L->num_kv_heads * (2 * kD + 2) * sizeof(float) + 768);
+  // chunks of fewer tokens need no more: those of the most rows that are rotated apart
+  if (quantized && !few) w.total = std::max(w.total, (size_t)32 * B * L->num_kv_heads * (2 * kD + 2) * sizeof(float) + 768);
   return w;
 }
 
@@ -1264,15 +1264,15 @@ int chunk_attn(int format, const oscar_layout* L, const void* pages, const void*
   a.Rk = R_k;
   a.Rv = R_v;
   a.rph = L->rot_per_head;
-  if (ws.expands) {
-    a.rot = base + ws.rot_off;
-    a.exps = reinterpret_cast<int2*>(base + ws.exps_off);
-    a.expanded = base + ws.expanded_off;
-  } else if (quantized) {
+  if (quantized && ws.tile_rows == 32) {
     float* qt = reinterpret_cast<float*>(base + ws.qt_off);
     st = hip_status(launch_decode_prepare(a.q, n_q, Hq, R_k, a.scale, qt, hs, L->rot_per_head, L->num_kv_heads));
     if (st) return st;
     a.qt = qt;
+  } else if (quantized) {
+    a.rot = base + ws.rot_off;
+    a.exps = reinterpret_cast<int2*>(base + ws.exps_off);
+    a.expanded = base + ws.expanded_off;
   }
   return hip_status(launch_chunk_attn(a, hs));
 }

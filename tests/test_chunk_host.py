@@ -139,7 +139,9 @@ def test_workspace_and_splits():
     size = lambda *a: ok.chunk_workspace_bytes(lay, *a)
     assert size(100, 4, 32, 100, 1, False) == 256
     assert 100 * 32 * 520 * 3 <= size(100, 4, 32, 100, 3, False) <= 100 * 32 * 520 * 3 + 512
-    assert 100 * 32 * (512 + 520) <= size(100, 4, 32, 100, 1, True) <= 100 * 32 * (512 + 520) + 768
+    # codes: 32 rows of a KV head to a sequence are rotated apart, more by the blocks that take them
+    assert 32 * 32 * (512 + 520) <= size(32, 4, 32, 100, 1, True) <= 32 * 32 * (512 + 520) + 768
+    assert size(32, 4, 32, 100, 1, True) <= size(100, 4, 32, 100, 1, True) <= size(1000, 4, 32, 100, 1, True)
     assert size(0, 4, 32, 100, 1, True) == 256 and size(100, 4, 12, 100, 1, True) == 0
     s = ok.chunk_default_splits
     assert s(lay, 1, 1, 32, 8) == 1                    # a short table: one piece
