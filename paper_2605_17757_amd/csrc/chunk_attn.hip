@@ -198,6 +198,8 @@ __device__ inline void each_four(const f16v (&o)[4], int h, F&& f) {
 }
 
 template <int FMT>
+constexpr int kBits = FMT == kInt4 ? 4 : 2;  // of a code
+template <int FMT>
 constexpr int raw_loads() { return FMT == kInt4 ? 4 : 2; }  // 16-byte loads of a wave for K's codes, and for V's
 constexpr int block_bytes_of(int fmt, int ng) {
   return fmt == kBf16 ? kBfBlock : fmt == kInt4 ? kv4_block_bytes(ng) : block_bytes(ng);
@@ -229,17 +231,14 @@ __device__ inline void load_entries(const uint8_t* blk, int is_v, uint32_t (&x)[
 }
 // Scales of a page in LDS, a wave's own: per group the slots' (s 2^24, -s z), divided by the
 // page's power of two.  K: both halves of a dword, by slot.  V: arrays of fp16, eight slots of a
-// step in 16 bytes, in the order of the step's elements.
+// step in 16 bytes, in the order of the step's elements; the scales also divided by 2^(bits i), for
+// codes that lie i places up in their 16 bits.
+constexpr int kPlaces = 4;
 template <int NG>
 struct Scales {
   uint32_t k[NG][kP];
-  __align__(16) uint16_t va[NG][kP], vb[NG][kP];
+  __align__(16) uint16_t va[kPlaces][NG][kP], vb[NG][kP];
 };
-// The exponent that a (scale, zero) pair needs: s 2^24 and |s z| below 2^15 after division by 2^e.
-__device__ inline int entry_exp(float s, float z) {
-  const int es = exp_of(s), ez = exp_of(z);
-  return max(es + 24, es + ez + 1) + 1 - 15;
-}
 constexpr int kNoExp = -400;
 // The entries of slots < ntok to scales; e: the exponent, raised where the page needs it.
 template <int FMT, int NG>
@@ -262,17 +261,20 @@ __device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16
       z[g] = (float)x.y;
     }
   }
-  int need = kNoExp;
+  float top = 0.0f;  // s 2^24 and |s z| are below 2^15 after division by 2^e
 #pragma unroll
-  for (int g = 0; g < NG; ++g) need = max(need, entry_exp(s[g], z[g]));
-  e = max(e, wave_max_i(need));
+  for (int g = 0; g < NG; ++g) top = fmaxf(fmaxf(top, fabsf(s[g])), fabsf(s[g] * (z[g] * 0x1p-24f)));
+  e = max(e, wave_max_i(exp_of(top) + 24 + 1 - 15));
   const int at = FMT == kInt2 ? (l & ~3) + 2 * (l & 1) + ((l >> 1) & 1) : l;  // v_slot's inverse
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const float x = ldexpf(s[g], -e);
     const uint32_t ab = pack2<kInt4>(x * 0x1p24f, -x * z[g]);
     if (is_v) {
-      sc.va[g][at] = (uint16_t)ab;
+#pragma unroll
+      for (int i = 0; i < (FMT == kInt2 ? 4 : 2); ++i)
+        sc.va[i][g][at] = __builtin_bit_cast(
+            uint16_t, (_Float16)(__builtin_bit_cast(_Float16, (uint16_t)ab) * (_Float16)(1.0f / (1 << (kBits<FMT> * i)))));
       sc.vb[g][at] = (uint16_t)(ab >> 16);
     } else {
       sc.k[g][l] = ab;
@@ -291,12 +293,15 @@ __device__ inline u4v k_operand(const u4v& raw, int T, int ks, const Scales<NG>&
   const int g = FMT == kInt4 ? 32 * (ks % 4) / G : (64 * h + 16 * (ks / 2)) / G;
   const uint32_t ab = sc.k[g][4 * lo + 2 * T + b];
   const uint32_t A = __builtin_amdgcn_perm(ab, ab, 0x01000100u), B = __builtin_amdgcn_perm(ab, ab, 0x03020302u);
-  u4v r;
+  u4v r;  // codes in place: n 2^(bits i) 2^-24, with the scale divided by 2^(bits i)
   if (FMT == kInt4) {
     const uint32_t d = raw[ks % 4];
+    const _Float16 m = (_Float16)(1.0f / 16);
+    const uint32_t A1 = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, A) * h2{m, m});
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = fma_h2((d >> (4 * i)) & 0x000f000fu, A, B);
-  } else {  // codes in place: n 4^i 2^-24, with the scale divided by 4^i
+    for (int i = 0; i < 4; ++i)
+      r[i] = fma_h2((d >> (8 * (i / 2))) & (0x000f000fu << (4 * (i % 2))), i % 2 ? A1 : A, B);
+  } else {
     const uint32_t d = raw[ks / 2] >> (8 * (ks % 2));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -314,13 +319,14 @@ __device__ inline u4v v_operand(const u4v& raw, int C, int j0, int i2, const Sca
   constexpr int G = kD / NG;
   const int c = FMT == kInt4 ? 64 * (C / 2) + 32 * jj : 4 * (l & 31);  // a channel of the row's group
   const int t0 = 32 * j0 + 16 * h + 8 * i2;
-  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[c / G][t0]), B = *reinterpret_cast<const u4v*>(&sc.vb[c / G][t0]);
+  constexpr int bits = kBits<FMT>;
+  const int place = FMT == kInt4 ? C % 2 : C;
+  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[place][c / G][t0]), B = *reinterpret_cast<const u4v*>(&sc.vb[c / G][t0]);
   u4v r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t d = raw[FMT == kInt4 ? 2 * j0 + i / 2 : 2 * i2 + i / 2] >> (8 * (i % 2));
-    r[i] = FMT == kInt4 ? fma_h2((d >> (4 * (C % 2))) & 0x000f000fu, A[i], B[i])
-                        : fma_h2((d >> (2 * C)) & 0x00030003u, A[i], B[i]);
+    r[i] = fma_h2(d & (((1u << bits) - 1) * 0x00010001u << (bits * place)), A[i], B[i]);
   }
   return r;
 }
