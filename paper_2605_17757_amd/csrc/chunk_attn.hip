@@ -447,6 +447,12 @@ __device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, flo
 // a range leaves a partial state in the tile's slot for that range, counted from its first.
 // ---------------------------------------------------------------------------
 constexpr int kLeastPages = 4;  // of a range
+// Sequences whose tiles every block counts; of more it looks for the tile's number in q_start, which
+// leaves numbers without a tile: blocks that end at once, but where they are as far apart as a
+// shader engine's blocks, that engine's share of the work is missing.  64 sequences of 4k tokens of
+// bf16, 8 new ones each: counted 174 us, looked for 222; 512 of 300: 253, 349, one new: 198, 181;
+// 2048 of 300, one new: 1041, 724.
+constexpr int kCounted = 256;
 
 struct Segment {
   Tile t;
@@ -507,14 +513,31 @@ __device__ inline Walk start_walk(const ChunkArgs& a, int g, int M, int window) 
   k.empty = k.r;
   return k;
 }
+// Tile r of all sequences', counted from the last one's last.
+__device__ inline Tile count_tile(const ChunkArgs& a, int r, int g, int M) {
+  auto start = [&](int b) { return min(max(a.q_start[min(b, a.B)], 0), a.n_q); };
+  int before = 0;
+  for (int b0 = (a.B - 1) & ~63; b0 >= 0; b0 -= 64) {
+    const int b = b0 + 63 - (threadIdx.x & 63);
+    const int tiles = (max(start(b + 1) - start(b), 0) * g + M - 1) / M;
+    const int incl = before + wave_prefix(tiles);
+    const uint64_t hit = __ballot(incl - tiles <= r && r < incl);
+    if (hit) {
+      const int lane = __ffsll((unsigned long long)hit) - 1;
+      return tile_at(a, b0 + 63 - lane, __builtin_amdgcn_readlane(incl, lane) - 1 - r, g, M);
+    }
+    before = __builtin_amdgcn_readlane(incl, 63);
+  }
+  Tile t = {};
+  t.b = -1;
+  return t;
+}
 // The next segment.
 __device__ inline bool find_segment(const ChunkArgs& a, Walk& k, int g, int M, int window, Segment& s) {
   if (a.num_splits == 1) {
     if (k.empty) return false;
     k.empty = 1;
-    // a sequence's last tiles, which see most, first
-    const int64_t n_ids = (int64_t)a.n_q * g / M + a.B;
-    s.t = find_tile(a, n_ids - 1 - k.r, g, M);
+    s.t = a.B > 1 && a.B <= kCounted ? count_tile(a, k.r, g, M) : find_tile(a, (int64_t)a.n_q * g / M + a.B - 1 - k.r, g, M);
     if (s.t.b < 0) return false;
     s.pg = tile_pages(s.t, g, M, window, a.sinks);
     s.x0 = s.slot = 0;
@@ -831,7 +854,7 @@ __device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_
 // ---------------------------------------------------------------------------
 // Many rows: W waves of 32 rows share every page through LDS.
 // ---------------------------------------------------------------------------
-template <int FMT, int NG, int W>
+template <int FMT, int NG, int W, bool HL = false>  // HL: p in two pieces
 __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   constexpr int M = kRows * W;
   constexpr bool CODES = FMT == kInt4 || FMT == kInt2;
@@ -847,16 +870,16 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
   Walk walk = start_walk(a, g, M, window);
   for (Segment sg; next_segment(a, walk, g, M, window, sg);) {
-  const Tile& t = sg.t;
-  const Pages& pg = sg.pg;
-  const int r = t.row0 + w * kRows + n;
-  const bool live = r < t.rows;
-  const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
-  const bool direct = sg.whole;
-  const int x0 = sg.x0, x1 = sg.x1;
-  if (x0 >= x1) {
-    if (live) store_empty(a, row, sg, direct, h);
-    continue;
+    const Tile& t = sg.t;
+    const Pages& pg = sg.pg;
+    const int r = t.row0 + w * kRows + n;
+    const bool live = r < t.rows;
+    const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
+    const bool direct = sg.whole;
+    const int x0 = sg.x0, x1 = sg.x1;
+    if (x0 >= x1) {
+      if (live) store_empty(a, row, sg, direct, h);
+      continue;
   }
   RowState rs;
   rs.pos = live ? t.len - t.n + r / g : -1;
@@ -1036,7 +1059,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     // weights of a step's operand, two at a time between the products of the step before
     const float ms = (rs.m == -INFINITY ? 0.0f : -rs.m) + weight;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    u4v p[2];
+    u4v p[2], pl[2];
     auto weights = [&](int k, int i) {
       auto one = [&](int e) {
         const int y = v_slot<FMT>(e), u = y % 4;
@@ -1046,6 +1069,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       sum[i] += x;
       sum[i] += y;
       p[k % 2][i] = pack2<FMT>(x, y);
+      if (HL) pl[k % 2][i] = pack2<FMT>(x - bf_lo(p[k % 2][i]), y - bf_hi(p[k % 2][i]));
     };
 #pragma unroll
     for (int i = 0; i < 4; ++i) weights(0, i);
@@ -1056,6 +1080,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
         for (int C = 0; C < 4; ++C) va[(k + 1) % 2][C] = v_at(C, k + 1);
 #pragma unroll
       for (int C = 0; C < 4; ++C) {
+        if (HL) o[C] = mfma<FMT>(va[k % 2][C], pl[k % 2], o[C]);
         o[C] = mfma<FMT>(va[k % 2][C], p[k % 2], o[C]);
         if (k + 1 < 4) weights(k + 1, C);
         __builtin_amdgcn_sched_barrier(0);
@@ -1102,208 +1127,208 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
   const int lo = l & 15, b16 = (l >> 4) & 1;
   Walk walk = start_walk(a, g, M, window);
   for (Segment sg; next_segment(a, walk, g, M, window, sg);) {
-  const Tile& t = sg.t;
-  const Pages& pg = sg.pg;
-  const int r = t.row0 + n;
-  const bool live = r < t.rows;
-  const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
-  const bool direct = FMT == kBf16 && sg.whole;
-  const int x0 = sg.x0, x1 = sg.x1;
-  RowState rs;
-  rs.pos = live ? t.len - t.n + r / g : -1;
-  rs.m = -INFINITY;
-  rs.l = 0.0f;
-  f16v o[4];
+    const Tile& t = sg.t;
+    const Pages& pg = sg.pg;
+    const int r = t.row0 + n;
+    const bool live = r < t.rows;
+    const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
+    const bool direct = FMT == kBf16 && sg.whole;
+    const int x0 = sg.x0, x1 = sg.x1;
+    RowState rs;
+    rs.pos = live ? t.len - t.n + r / g : -1;
+    rs.m = -INFINITY;
+    rs.l = 0.0f;
+    f16v o[4];
 #pragma unroll
-  for (int C = 0; C < 4; ++C)
+    for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
-  int e_v = kNoExp;
-  if (x0 + w < x1) {
-    const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
-    auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
-    auto block_of = [&](int x) {
-      return a.pages + ((size_t)scalar_load(bt + page_of(x)) * a.Hkv + kvh) * block_bytes_of(FMT, NG);
-    };
-    constexpr int kL = FMT == kBf16 ? 16 : raw_loads<FMT>();
-    u4v rk[kL], rv0[kL], rv1[FMT == kBf16 ? 1 : kL];  // codes: V's of the next page beside the page's
-    uint32_t ks[NG], vs[NG];
-    auto fetch_k = [&](const uint8_t* blk) {
+      for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
+    int e_v = kNoExp;
+    if (x0 + w < x1) {
+      const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
+      auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
+      auto block_of = [&](int x) {
+        return a.pages + ((size_t)scalar_load(bt + page_of(x)) * a.Hkv + kvh) * block_bytes_of(FMT, NG);
+      };
+      constexpr int kL = FMT == kBf16 ? 16 : raw_loads<FMT>();
+      u4v rk[kL], rv0[kL], rv1[FMT == kBf16 ? 1 : kL];  // codes: V's of the next page beside the page's
+      uint32_t ks[NG], vs[NG];
+      auto fetch_k = [&](const uint8_t* blk) {
 #pragma unroll
-      for (int i = 0; i < kL; ++i) {
-        if (FMT == kBf16) {  // (T, ks) = (i / 8, i % 8)
-          const int off = (i / 8) * 8192 + (i % 4) * 1024 + (i / 4 % 2) * 512 + b16 * 4096 + h * 256 + lo * 16;
-          rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
-        } else {
-          rk[i] = load_k<FMT, NG>(blk, i);
-        }
-      }
-    };
-    auto fetch_v = [&](const uint8_t* blk, auto& rv) {
-#pragma unroll
-      for (int i = 0; i < kL; ++i) {
-        if (FMT == kBf16) {  // (C, step) = (i / 4, i % 4)
-          const int off = kHalfLds + (i / 4) * 4096 + (i % 2) * 1024 + (i / 2 % 2) * 512 + b16 * 2048 + h * 256 +
-                          lo * 16;
-          rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
-        } else {
-          rv[i] = load_v<FMT, NG>(blk, i);
-        }
-      }
-    };
-    const uint8_t* blk = block_of(x0 + w);
-    fetch_k(blk);
-    if (FMT != kBf16) {
-      fetch_v(blk, rv0);
-      load_entries<FMT, NG>(blk, 0, ks);
-      load_entries<FMT, NG>(blk, 1, vs);
-    }
-    u4v q[8];
-    load_queries<FMT>(a, row, live, q, rs.c);
-    Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
-    int x = x0 + w;
-    auto page = [&](auto& rv, auto& rv_next) {
-      const int t0 = page_of(x) * kP, ntok = t.len - t0;
-      const bool more = x + kWaves < x1;
-      const uint8_t* next = more ? block_of(x + kWaves) : blk;
-      int e_k = 0;
-      if (FMT == kBf16) {
-        fetch_v(blk, rv);
-      } else {
-        const int e_old = e_v;
-        lane_exchange();  // the last page's scales have been read
-        e_k = kNoExp;
-        make_scales<FMT, NG>(ks, 0, a.meta_bf16, min(ntok, kP), sc, e_k);
-        make_scales<FMT, NG>(vs, 1, a.meta_bf16, min(ntok, kP), sc, e_v);
-        lane_exchange();
-        if (e_v != e_old && e_old != kNoExp) {
-          const float f = pow2(max(e_old - e_v, -126));
-#pragma unroll
-          for (int C = 0; C < 4; ++C) o[C] *= f;
-        }
-      }
-      f16v s[2];
-#pragma unroll
-      for (int T = 0; T < 2; ++T)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-#pragma unroll
-        for (int T = 0; T < 2; ++T) {
-          u4v ka;
-          if constexpr (FMT == kBf16) ka = rk[8 * T + k];
-          else ka = k_operand<FMT, NG>(rk[FMT == kInt4 ? 2 * T + k / 4 : T], T, k, sc);
-          s[T] = mfma<FMT>(ka, q[k], s[T]);
-        }
-      if (more) {  // the next page's loads, as soon as there is room for them
-        fetch_k(next);
-        if (FMT != kBf16) {
-          fetch_v(next, rv_next);
-          load_entries<FMT, NG>(next, 0, ks);
-          load_entries<FMT, NG>(next, 1, vs);
-        }
-      }
-      const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
-      u4v p[4], pl[4];
-      if (masked) mask_page(s, rs.pos, t0, window, a.sinks);
-      softmax_page<FMT, HL>(s, o, rs, FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast), p, pl);
-      if (FMT == kBf16 && ntok < kP) {  // slots never written weigh 0: their values may be anything
-#pragma unroll
-        for (int i = 0; i < kL; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int ts = 32 * (i / 2 % 2) + 16 * h + 8 * (i % 2) + 2 * j;
-            rv[i][j] &= (ts < ntok ? 0xffffu : 0u) | (ts + 1 < ntok ? 0xffff0000u : 0u);
+        for (int i = 0; i < kL; ++i) {
+          if (FMT == kBf16) {  // (T, ks) = (i / 8, i % 8)
+            const int off = (i / 8) * 8192 + (i % 4) * 1024 + (i / 4 % 2) * 512 + b16 * 4096 + h * 256 + lo * 16;
+            rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
+          } else {
+            rk[i] = load_k<FMT, NG>(blk, i);
           }
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int C = 0; C < 4; ++C) {
-          u4v va;
-          if constexpr (FMT == kBf16) va = rv[4 * C + k];
-          else va = v_operand<FMT, NG>(rv[FMT == kInt4 ? 2 * (C / 2) + k % 2 : k / 2], C, k / 2, k % 2, sc);
-          if (HL) o[C] = mfma<FMT>(va, pl[k], o[C]);
-          o[C] = mfma<FMT>(va, p[k], o[C]);
         }
-      blk = next;
-      x += kWaves;
-    };
-    if constexpr (FMT == kBf16) {
-      do page(rv0, rv0);
-      while (x < x1);
-    } else {
-      do {
-        page(rv0, rv1);
-        if (x >= x1) break;
-        page(rv1, rv0);
-      } while (x < x1);
+      };
+      auto fetch_v = [&](const uint8_t* blk, auto& rv) {
+#pragma unroll
+        for (int i = 0; i < kL; ++i) {
+          if (FMT == kBf16) {  // (C, step) = (i / 4, i % 4)
+            const int off = kHalfLds + (i / 4) * 4096 + (i % 2) * 1024 + (i / 2 % 2) * 512 + b16 * 2048 + h * 256 +
+                            lo * 16;
+            rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u4v*>(blk + off));
+          } else {
+            rv[i] = load_v<FMT, NG>(blk, i);
+          }
+        }
+      };
+      const uint8_t* blk = block_of(x0 + w);
+      fetch_k(blk);
+      if (FMT != kBf16) {
+        fetch_v(blk, rv0);
+        load_entries<FMT, NG>(blk, 0, ks);
+        load_entries<FMT, NG>(blk, 1, vs);
+      }
+      u4v q[8];
+      load_queries<FMT>(a, row, live, q, rs.c);
+      Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
+      int x = x0 + w;
+      auto page = [&](auto& rv, auto& rv_next) {
+        const int t0 = page_of(x) * kP, ntok = t.len - t0;
+        const bool more = x + kWaves < x1;
+        const uint8_t* next = more ? block_of(x + kWaves) : blk;
+        int e_k = 0;
+        if (FMT == kBf16) {
+          fetch_v(blk, rv);
+        } else {
+          const int e_old = e_v;
+          lane_exchange();  // the last page's scales have been read
+          e_k = kNoExp;
+          make_scales<FMT, NG>(ks, 0, a.meta_bf16, min(ntok, kP), sc, e_k);
+          make_scales<FMT, NG>(vs, 1, a.meta_bf16, min(ntok, kP), sc, e_v);
+          lane_exchange();
+          if (e_v != e_old && e_old != kNoExp) {
+            const float f = pow2(max(e_old - e_v, -126));
+#pragma unroll
+            for (int C = 0; C < 4; ++C) o[C] *= f;
+          }
+        }
+        f16v s[2];
+#pragma unroll
+        for (int T = 0; T < 2; ++T)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+          for (int T = 0; T < 2; ++T) {
+            u4v ka;
+            if constexpr (FMT == kBf16) ka = rk[8 * T + k];
+            else ka = k_operand<FMT, NG>(rk[FMT == kInt4 ? 2 * T + k / 4 : T], T, k, sc);
+            s[T] = mfma<FMT>(ka, q[k], s[T]);
+          }
+        if (more) {  // the next page's loads, as soon as there is room for them
+          fetch_k(next);
+          if (FMT != kBf16) {
+            fetch_v(next, rv_next);
+            load_entries<FMT, NG>(next, 0, ks);
+            load_entries<FMT, NG>(next, 1, vs);
+          }
+        }
+        const bool masked = t0 + kP - 1 > pg.p_min || (t0 <= pg.p_max - window && t0 + kP > a.sinks);
+        u4v p[4], pl[4];
+        if (masked) mask_page(s, rs.pos, t0, window, a.sinks);
+        softmax_page<FMT, HL>(s, o, rs, FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast), p, pl);
+        if (FMT == kBf16 && ntok < kP) {  // slots never written weigh 0: their values may be anything
+#pragma unroll
+          for (int i = 0; i < kL; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int ts = 32 * (i / 2 % 2) + 16 * h + 8 * (i % 2) + 2 * j;
+              rv[i][j] &= (ts < ntok ? 0xffffu : 0u) | (ts + 1 < ntok ? 0xffff0000u : 0u);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int C = 0; C < 4; ++C) {
+            u4v va;
+            if constexpr (FMT == kBf16) va = rv[4 * C + k];
+            else va = v_operand<FMT, NG>(rv[FMT == kInt4 ? 2 * (C / 2) + k % 2 : k / 2], C, k / 2, k % 2, sc);
+            if (HL) o[C] = mfma<FMT>(va, pl[k], o[C]);
+            o[C] = mfma<FMT>(va, p[k], o[C]);
+          }
+        blk = next;
+        x += kWaves;
+      };
+      if constexpr (FMT == kBf16) {
+        do page(rv0, rv0);
+        while (x < x1);
+      } else {
+        do {
+          page(rv0, rv1);
+          if (x >= x1) break;
+          page(rv1, rv0);
+        } while (x < x1);
+      }
     }
-  }
-  // merge: wave w sums tile C = w of the four states
-  const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
-  const float lt = half_sum(rs.l);
-  // (NaN in a row: its scores have no maximum, but the state is not empty)
-  if (h == 0) ml[w][n] = make_float2(is_nan(lt) ? 0.0f : rs.m, lt);
+    // merge: wave w sums tile C = w of the four states
+    const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
+    const float lt = half_sum(rs.l);
+    // (NaN in a row: its scores have no maximum, but the state is not empty)
+    if (h == 0) ml[w][n] = make_float2(is_nan(lt) ? 0.0f : rs.m, lt);
 #pragma unroll
-  for (int C = 0; C < 4; ++C)
+    for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      os[w][C][i][l] = make_float4(o[C][4 * i] * unit, o[C][4 * i + 1] * unit, o[C][4 * i + 2] * unit, o[C][4 * i + 3] * unit);
-  __syncthreads();
-  float m = -INFINITY, L = 0.0f, f[kWaves];
+      for (int i = 0; i < 4; ++i)
+        os[w][C][i][l] = make_float4(o[C][4 * i] * unit, o[C][4 * i + 1] * unit, o[C][4 * i + 2] * unit, o[C][4 * i + 3] * unit);
+    __syncthreads();
+    float m = -INFINITY, L = 0.0f, f[kWaves];
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) m = fmaxf(m, ml[k][n].x);
+    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, ml[k][n].x);
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) {
-    f[k] = ml[k][n].x == -INFINITY ? 0.0f : exp2f(ml[k][n].x - m);
-    L += f[k] * ml[k][n].y;
-  }
-  // each wave stores a quarter of the channels: registers 4 w .. 4 w + 3 of every tile
-  float sum[4][4] = {};
+    for (int k = 0; k < kWaves; ++k) {
+      f[k] = ml[k][n].x == -INFINITY ? 0.0f : exp2f(ml[k][n].x - m);
+      L += f[k] * ml[k][n].y;
+    }
+    // each wave stores a quarter of the channels: registers 4 w .. 4 w + 3 of every tile
+    float sum[4][4] = {};
 #pragma unroll
-  for (int C = 0; C < 4; ++C)
+    for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k)
-      if (f[k] != 0.0f) {
+      for (int k = 0; k < kWaves; ++k) {
         const float4 v = os[k][C][w][l];
-        sum[C][0] = fmaf(f[k], v.x, sum[C][0]);
-        sum[C][1] = fmaf(f[k], v.y, sum[C][1]);
-        sum[C][2] = fmaf(f[k], v.z, sum[C][2]);
-        sum[C][3] = fmaf(f[k], v.w, sum[C][3]);
+        const bool counts = f[k] != 0.0f;
+        sum[C][0] = fmaf(f[k], counts ? v.x : 0.0f, sum[C][0]);
+        sum[C][1] = fmaf(f[k], counts ? v.y : 0.0f, sum[C][1]);
+        sum[C][2] = fmaf(f[k], counts ? v.z : 0.0f, sum[C][2]);
+        sum[C][3] = fmaf(f[k], counts ? v.w : 0.0f, sum[C][3]);
       }
-  if (live) {
-    const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
-    const size_t at = row * a.num_splits + sg.slot;
-    auto put = [&](int c, float x, float y, float z, float v) {
-      if (direct) {
-        uint2 d;
-        d.x = pack2<kBf16>(x * il, y * il);
-        d.y = pack2<kBf16>(z * il, v * il);
-        *reinterpret_cast<uint2*>(a.out + row * kD + c) = d;
-      } else if (m != -INFINITY) {  // of an empty state only that is read
-        *reinterpret_cast<float4*>(a.part_o + at * kD + c) = make_float4(x, y, z, v);
+    if (live) {
+      const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
+      const size_t at = row * a.num_splits + sg.slot;
+      auto put = [&](int c, float x, float y, float z, float v) {
+        if (direct) {
+          uint2 d;
+          d.x = pack2<kBf16>(x * il, y * il);
+          d.y = pack2<kBf16>(z * il, v * il);
+          *reinterpret_cast<uint2*>(a.out + row * kD + c) = d;
+        } else if (m != -INFINITY) {  // of an empty state only that is read
+          *reinterpret_cast<float4*>(a.part_o + at * kD + c) = make_float4(x, y, z, v);
+        }
+      };
+      const int rr = 8 * w + 4 * h;
+      if (FMT == kInt2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(4 * (rr + i), sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
+      } else {
+#pragma unroll
+        for (int C = 0; C < 4; ++C)
+          put(FMT == kBf16 ? 32 * C + rr : 64 * (C / 2) + 32 * (rr / 16) + 16 * (C % 2) + rr % 16, sum[C][0], sum[C][1],
+              sum[C][2], sum[C][3]);
       }
-    };
-    const int rr = 8 * w + 4 * h;
-    if (FMT == kInt2) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) put(4 * (rr + i), sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
-    } else {
-#pragma unroll
-      for (int C = 0; C < 4; ++C)
-        put(FMT == kBf16 ? 32 * C + rr : 64 * (C / 2) + 32 * (rr / 16) + 16 * (C % 2) + rr % 16, sum[C][0], sum[C][1],
-            sum[C][2], sum[C][3]);
+      if (w == 0 && h == 0 && (!direct || a.num_splits > 1)) {
+        float2* dst = reinterpret_cast<float2*>(a.part_ml) + row * a.num_splits;
+        dst[sg.slot] = direct ? make_float2(kDone, 0.0f) : make_float2(m, L);
+        if (sg.last && !direct)
+          for (int i = sg.slot + 1; i < a.num_splits; ++i) dst[i] = make_float2(-INFINITY, 0.0f);
+      }
     }
-    if (w == 0 && h == 0 && (!direct || a.num_splits > 1)) {
-      float2* dst = reinterpret_cast<float2*>(a.part_ml) + row * a.num_splits;
-      dst[sg.slot] = direct ? make_float2(kDone, 0.0f) : make_float2(m, L);
-      if (sg.last && !direct)
-        for (int i = sg.slot + 1; i < a.num_splits; ++i) dst[i] = make_float2(-INFINITY, 0.0f);
-    }
-  }
-  __syncthreads();  // os, ml and the scales are free again
+    __syncthreads();  // os, ml and the scales are free again
   }
 }
 
@@ -1377,7 +1402,7 @@ hipError_t launch_fmt(const ChunkArgs& args, hipStream_t st) {
   const int g = args.Hq / args.Hkv;
   const bool quantized = FMT != kBf16;
   const int64_t page_heads = (int64_t)args.B * args.max_pages * args.Hkv;
-  const int M = chunk_tile_rows(quantized, args.n_q, args.B, g, page_heads);
+  const int M = chunk_tile_rows(quantized, args.n_q, args.B, g, args.Hkv, args.max_pages);
   const ChunkArgs& a = args;
   const int64_t tiles = (int64_t)a.n_q * g / M + a.B;
   const int ranges = std::max(1, chunk_blocks(quantized, M) / a.Hkv);
@@ -1392,6 +1417,8 @@ hipError_t launch_fmt(const ChunkArgs& args, hipStream_t st) {
     }
   if (M == kRows)
     hipLaunchKernelGGL((chunk_few_kernel<FMT, NG>), dim3(blocks), dim3(256), 0, st, a);
+  else if (FMT == kBf16 && (int64_t)a.n_q * g <= (int64_t)kRows * a.B)  // two pieces, as in tiles of 32
+    hipLaunchKernelGGL((chunk_kernel<kBf16, 1, 4, true>), dim3(blocks), dim3(256), 0, st, a);
   else if (M == 4 * kRows)
     hipLaunchKernelGGL((chunk_kernel<FMT, NG, 4>), dim3(blocks), dim3(256), 0, st, a);
   else
@@ -1426,11 +1453,24 @@ hipError_t launch_fmt(const ChunkArgs& args, hipStream_t st) {
 
 }  // namespace
 
-int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int64_t page_heads) {
-  const int64_t rows = n_q * heads_per_kv;
-  if (rows <= (int64_t)kRows * B) return kRows;
-  // (expanded pages: 2 GiB at most)
-  return rows <= (int64_t)512 * B || (quantized && page_heads > 65536) ? 4 * kRows : kManyRows;
+// Rows of a tile, by the rows that a sequence and KV head have on average (32 query and 8 KV heads
+// below; us with the smaller tile, with the larger).
+//  32, blocks whose waves take pages of their own: codes are then expanded by every wave for itself,
+//      and no wave idles.  8 sequences of 8k tokens in 4 bits, 36 rows each: 57, 68 with 128; 64 rows:
+//      53, 71; 128 rows: 87, 84; 32 sequences of 2k, 64 rows: 85, 100; 128 rows: 128, 111.  Of bf16
+//      pages every wave has a whole page's loads in flight, but a CU holds one block and the next
+//      one's start is seen: 64 sequences of 4k tokens, 4 rows each: 167, 184; of 1k: 48, 43; 128 of
+//      300: 50, 37; 32 of 2k: 46, 49; one of 1k: 14, 26.
+// 128 or 256 (one block of 8 waves to a CU instead of two of 4; codes expanded beforehand, to 2 GiB
+//      at most): 8 sequences of 8k, 4 bits, 512 rows: 236, 242; 768: 347, 325; 1024: 403, 368; 2048:
+//      779, 624.  32 of 2k: 235, 288; 356, 370; 433, 404; 802, 693.  bf16, 32 of 2k: 151, 192; 231, 254;
+//      285, 282; 540, 526.
+int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int Hkv, int64_t max_pages) {
+  const int64_t rows = n_q * heads_per_kv, heads = (int64_t)B * Hkv;
+  if (quantized ? rows <= (int64_t)2 * kRows * B
+                : rows <= (int64_t)kRows * B && (max_pages > 24 || heads < 2 * device_cus()))
+    return kRows;
+  return rows <= (int64_t)512 * B || (quantized && heads * max_pages > 65536) ? 4 * kRows : kManyRows;
 }
 
 // Blocks that the GPU holds at once.

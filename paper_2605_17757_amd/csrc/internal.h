@@ -320,9 +320,8 @@ struct ChunkArgs {
 };
 constexpr int kExpandedBytes = 2 * kP * kD * 2;
 constexpr int kRotBytes = 2 * kD * kD * 2;  // a rotation in two fp16 pieces
-// Query rows (token, head) of a sequence and KV head that a block takes; page_heads: pages of all
-// table rows times KV heads.
-int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int64_t page_heads);
+// Query rows (token, head) of a sequence and KV head that a block takes.
+int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int Hkv, int64_t max_pages);
 int chunk_blocks(bool quantized, int tile_rows);  // that the GPU holds at once
 constexpr int kManyRows = 256;  // the largest: with quantized caches, pages are expanded once
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st);

@@ -1104,7 +1104,7 @@ namespace {
 // Splits for tiles that see `pages` pages at most.
 int32_t chunk_splits(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq, int64_t pages) {
   const int64_t g = Hq / L->num_kv_heads, Hkv = L->num_kv_heads;
-  const int M = chunk_tile_rows(false, n_q, B, (int)g, 0);
+  const int M = chunk_tile_rows(false, n_q, B, (int)g, (int)Hkv, pages);
   // tiles of a KV head as they come when the sequences' chunks are alike
   const int64_t tiles = B * std::max<int64_t>(1, ((int64_t)n_q * g / B + M - 1) / M);
   const int64_t at_once = chunk_blocks(true, M), ranges = std::max<int64_t>(1, at_once / Hkv);
@@ -1132,7 +1132,7 @@ int check_chunk_sizes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
   if (*num_splits == 0) *num_splits = oscar_chunk_default_splits(L, n_q, B, Hq, max_pages_per_seq);
   // a launch holds fewer than 2^32 threads
   const int64_t g = Hq / L->num_kv_heads;
-  const int64_t M = chunk_tile_rows(true, n_q, B, (int)g, (int64_t)B * max_pages_per_seq * L->num_kv_heads);
+  const int64_t M = chunk_tile_rows(true, n_q, B, (int)g, L->num_kv_heads, max_pages_per_seq);
   return (n_q * g / M + B) * *num_splits * L->num_kv_heads > 0xffffff ? OSCAR_ERR_UNSUPPORTED : OSCAR_OK;
 }
 
@@ -1146,7 +1146,7 @@ ChunkWs chunk_ws(const oscar_layout* L, int64_t n_q, int32_t B, int64_t Hq, int6
                  bool quantized) {
   const size_t page_heads = (size_t)B * max_pages * L->num_kv_heads, rows = (size_t)(n_q * Hq);
   ChunkWs w;
-  w.tile_rows = chunk_tile_rows(quantized, n_q, B, (int)(Hq / L->num_kv_heads), (int64_t)page_heads);
+  w.tile_rows = chunk_tile_rows(quantized, n_q, B, (int)(Hq / L->num_kv_heads), L->num_kv_heads, max_pages);
   const bool few = quantized && w.tile_rows == 32, expands = quantized && w.tile_rows == kManyRows;
   const bool parts = S > 1 || few;
   size_t at = 0;
@@ -1163,7 +1163,7 @@ ChunkWs chunk_ws(const oscar_layout* L, int64_t n_q, int32_t B, int64_t Hq, int6
   w.pml_off = take(parts ? rows * S * 2 * sizeof(float) : 0);
   w.total = at ? at : 256;
   // chunks of fewer tokens need no more: those of the most rows that are rotated apart
-  if (quantized && !few) w.total = std::max(w.total, (size_t)32 * B * L->num_kv_heads * (2 * kD + 2) * sizeof(float) + 768);
+  if (quantized && !few) w.total = std::max(w.total, (size_t)64 * B * L->num_kv_heads * (2 * kD + 2) * sizeof(float) + 768);
   return w;
 }
 

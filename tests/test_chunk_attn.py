@@ -366,6 +366,22 @@ def test_many_sequences(fmt):
     c.check(q, new, c.run(q, new))
 
 
+@pytest.mark.parametrize("fmt,Hkv", [("bf16", 8), ("bf16", 1), ("kv4", 8), ("kv2", 1)])
+@pytest.mark.parametrize("B,most", [(33, 4), (64, 90), (65, 8), (129, 9), (256, 2), (257, 40)])
+def test_tiles_of_many_sequences(fmt, Hkv, B, most):
+    # each block finds its tile among the sequences'; none, one or more of a sequence, some without new tokens
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, 150, B).tolist()
+    new = [int(rng.integers(0, min(n, most) + 1)) for n in lens]
+    new[0], new[B // 2], new[B - 1] = 0, min(lens[B // 2], most), 0
+    c = Cache(fmt, lens, Hkv, seed=B, spare=0)
+    q = _q(new, 4 * Hkv, seed=B, more=3)
+    out = torch.full_like(q, 7.0)
+    c.run(q, new, splits=1, out=out)
+    c.check(q, new, out)
+    assert bool((out[sum(new):] == 7.0).all())
+
+
 def test_thousands_of_sequences():
     B = 5000
     c = Cache("bf16", [3], 1, seed=11)
