@@ -20,10 +20,19 @@
 // bf16 pages hold these operands as they are.  Codes become fp16 with one packed
 // multiply-add: the 16-bit pattern of a code n is the fp16 subnormal n 2^-24, and
 //   x = s (n - z) = (n 2^-24) (s 2^24) - s z
-// with the scale and -s z rounded to fp16 (off by 2^-12 of s z at most; the scale is exact
+// with the scale and -s z rounded to fp16 (off by 2^-11 of s z at most; the scale is exact
 // unless it is 2^-14 of the page's largest) after division by a power of two, so that the
 // page's largest scale 2^24 and |s z| stay below 2^15: scores take it back as part of c, values
-// through the accumulators' exponent, which moves like m when a page needs more.
+// through the accumulators' exponent, which moves like m when a page needs more.  A code that lies
+// some places up in its 16 bits stays there, and its scale is divided by 2^places.
+//
+// Three kernels, by the rows of a tile (chunk_tile_rows, with both sides of each choice measured):
+//   chunk_few_kernel   32 rows, waves share a tile's pages among them: bound by the bytes over bf16,
+//                      by each page's chain of instructions over codes
+//   chunk_kernel       128 or 256 rows, waves share every page through LDS: bound by the matrix
+//                      products and the power limit
+//   expand_kernel      (with 256 rows over codes) pages to fp16 operands, once: bound by the bytes
+// and a merge of the partial states where the pages of a tile are shared among blocks.
 #include "reduce_body.h"
 
 #include <algorithm>
@@ -66,6 +75,9 @@ __device__ inline uint32_t pack2(float a, float b) {  // to the operands' type, 
 __device__ inline float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// x itself, by a move that the compiler does not see through.
+__device__ inline int stay(int x) { return __builtin_amdgcn_update_dpp(x, x, 0xE4, 0xF, 0xF, false); }
+__device__ inline float stay(float x) { return __uint_as_float((uint32_t)stay((int)__float_as_uint(x))); }
 // Over the two halves of a wave: lanes l and l ^ 32.
 __device__ inline float half_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -650,26 +662,26 @@ __device__ inline void store_empty(const ChunkArgs& a, size_t row, const Segment
   }
 }
 
-// 16 bytes a lane from global memory to LDS, lane l's to dst + 16 l (dst: the wave's, a byte
-// address in LDS).  As inline asm, since the compiler, which cannot tell the slots of a buffer
-// apart, waits for every such load before the next LDS read of any of them; it has no outputs,
-// and the barrier that hands a slot over waits for it (wait_loads).
-__device__ inline void load_to_lds(const void* src, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
+// 16 bytes a lane from global memory to LDS, lane l's to dst + 16 l (dst: the wave's).  The compiler
+// waits for such a load before it reads LDS that may be the load's: a kernel that reads one page
+// while others come in has an array of its own for each.
+__device__ inline void load_to_lds(const void* src, uint8_t* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 // Waits until at most N of the wave's loads are under way.
 template <int N>
 __device__ inline void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xf70);  // vmcnt alone
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 // A barrier that waits for the waves' LDS accesses, and leaves loads under way alone.
 __device__ inline void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt alone
   __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-__device__ inline uint32_t lds_address(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
 // ---------------------------------------------------------------------------
@@ -706,7 +718,9 @@ __device__ inline int v_channel(int C, int r) {
 }
 
 // Blocks: a page of a sequence's table and a KV head each (`pages` of them, or none); behind them
-// kRotParts for each rotation.
+// kRotParts for each rotation.  Bound by the bytes written: 8192 pages of a head, 54 MB of 2-bit
+// codes read and 269 MB written, 54 us (5.9 TB/s).  Expanded by the blocks that read them instead, 2 x
+// 513 tokens over 32k took 870 us, with this launch 700.
 constexpr int kRotParts = 8;
 template <int FMT, int NG>
 __global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages) {
@@ -774,10 +788,27 @@ __global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages)
   if (threadIdx.x == 0) a.exps[blockIdx.x] = make_int2(e[0], e[1]);
 }
 
+// The product of a rotation's operands in LDS, half at rot, half at rot2, with x.  (Operands read
+// ahead of their products changed nothing: other waves' products fill the gaps.)
+__device__ inline void rotate(const u4v (&x)[8], f16v (&y)[4], const uint8_t* rot, const uint8_t* rot2) {
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int C = 0; C < 4; ++C) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[C][i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const u4v* op = reinterpret_cast<const u4v*>((C < 2 ? rot : rot2) + (C % 2 * 8 + k) * 2048 + l * 16);
+      y[C] = mfma<kHalf>(op[64], x[k], y[C]);
+      y[C] = mfma<kHalf>(op[0], x[k], y[C]);
+    }
+  }
+}
+
 // q~ = q R_k as the score products' operands, fp16 divided by a power of two that c takes; R_k's
-// operands at `rot` in LDS.
-__device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live, const uint8_t* rot, u4v (&q)[8],
-                                      float& c) {
+// operands in LDS (rotate).
+__device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live, const uint8_t* rot,
+                                      const uint8_t* rot2, u4v (&q)[8], float& c) {
   const int l = threadIdx.x & 63, h = l >> 5;
   const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
   u4v x[8];
@@ -795,20 +826,12 @@ __device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live,
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[k][j] = pack2<kInt4>(ldexpf(bf_lo(x[k][j]), -e1), ldexpf(bf_hi(x[k][j]), -e1));
   f16v y[4];
+  rotate(x, y, rot, rot2);
   top = 0.0f;
 #pragma unroll
-  for (int C = 0; C < 4; ++C) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[C][i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const u4v* op = reinterpret_cast<const u4v*>(rot + (C * 8 + k) * 2048 + l * 16);
-      y[C] = mfma<kHalf>(op[64], x[k], y[C]);
-      y[C] = mfma<kHalf>(op[0], x[k], y[C]);
-    }
+  for (int C = 0; C < 4; ++C)
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(y[C][i]));
-  }
   const int e2 = max(exp_of(half_max(top)), -60) - 13;
 #pragma unroll
   for (int k = 0; k < 8; ++k)
@@ -819,8 +842,7 @@ __device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live,
 }
 // o = o~ R_v^T, o~ = the sums / l 2^e as fp16 (divided by a power of two): rows of the output's
 // channels in order; returns what they are still to be multiplied by to be the sums again.
-__device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_t* rot) {
-  const int lane = threadIdx.x & 63;
+__device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_t* rot, const uint8_t* rot2) {
   const float il = l > 0.0f ? 1.0f / l : is_nan(l) ? l : 0.0f;
   float top = 0.0f;
 #pragma unroll
@@ -837,22 +859,25 @@ __device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       x[k][j] = pack2<kHalf>(ldexpf(o[k / 2][8 * (k % 2) + 2 * j], -e3), ldexpf(o[k / 2][8 * (k % 2) + 2 * j + 1], -e3));
-#pragma unroll
-  for (int C = 0; C < 4; ++C) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const u4v* op = reinterpret_cast<const u4v*>(rot + (C * 8 + k) * 2048 + lane * 16);
-      o[C] = mfma<kHalf>(op[64], x[k], o[C]);
-      o[C] = mfma<kHalf>(op[0], x[k], o[C]);
-    }
-  }
+  rotate(x, o, rot, rot2);
   return ldexpf(l, e3 + e);
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: W waves of 32 rows share every page through LDS.
+// Many rows: W waves of 32 rows share every page through LDS.  4 D flops per (row, token), on the
+// matrix cores; per page and wave 32 products (1024 cycles of a SIMD's matrix core) beside 32
+// exponentials a lane and their fp32 steps, which are issued between the value products.
+//   A page's 32 KiB come by loads straight to LDS, issued W = 8: two pages, 4: one page before their
+// use, so that no registers hold them; the next operands are read from LDS three steps ahead of the
+// score products, one ahead of the value products.  One barrier a page: the slot that it frees is
+// the one filled next.  Codes (W = 4) come to registers a page ahead, and each wave makes a quarter of
+// the page's operands.
+//   8 waves read a page once where 4 do twice, and hide the loads two pages deep: a prompt of 8192
+// tokens, 32 query heads on 8: 510 us (1.08 PFLOP/s, of 1.36 that a large library product reaches
+// here), by 4 waves 530 to 600; 2048 tokens over 16k in 4 bits 555 (expanded beforehand), by 4 waves 770.
+// Without reads from LDS the prompt takes 90 % of its time, without loads 86, without the softmax 85,
+// the products alone 60.  Matrix cores are busy 50 to 54 % of it at 1.9 to 2.1 GHz, the clock that
+// the power limit leaves (in the library product: 73 % at 1.4 to 1.8).
 // ---------------------------------------------------------------------------
 template <int FMT, int NG, int W, bool HL = false>  // HL: p in two pieces
 __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
@@ -860,10 +885,21 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   constexpr bool CODES = FMT == kInt4 || FMT == kInt2;
   constexpr int kSlots = W == 8 ? 3 : 2;
   static_assert(W == 4 || (W == 8 && !CODES), "a block expands codes a part per wave");
-  static_assert(kSlots * kPageLds >= kRotBytes, "a rotation's operands fit in the pages' slots");
-  __shared__ __align__(16) uint8_t lds[kSlots * kPageLds];
+  static_assert(2 * kPageLds == kRotBytes, "a rotation's operands fit in two pages' slots");
+  // (codes: no loads to LDS, one array; a loop without copies of itself for the slots needs fewer registers)
+  __shared__ __align__(16) uint8_t slot0[CODES ? 2 * kPageLds : kPageLds], slot1[CODES ? 16 : kPageLds],
+      slot2[kSlots == 3 ? kPageLds : 16];
+  auto lds_of = [&](auto s) -> uint8_t* {
+    if constexpr (CODES) return slot0 + s * kPageLds;
+    else return s.value == 0 ? slot0 : s.value == 1 ? slot1 : slot2;
+  };
+  auto ahead_of = [](auto s) {  // the slot that is free
+    if constexpr (CODES) return 1 - s;
+    else return std::integral_constant<int, s.value == 0 ? kSlots - 1 : s.value - 1>{};
+  };
+  uint8_t* const second = CODES ? slot0 + kPageLds : slot1;
   __shared__ Scales<CODES ? NG : 1> scales[CODES ? W : 1];
-  __shared__ int exps[2][2];  // CODES: of the slots: K's exponent, the accumulators'
+  __shared__ int exps[2][kSlots];  // CODES: of the slots: K's exponent, the accumulators'
   const int g = a.Hq / a.Hkv;
   const int kvh = blockIdx.x % a.Hkv;
   const int window = a.window > 0 ? min(a.window, kNoWindow) : kNoWindow;
@@ -885,18 +921,22 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   rs.pos = live ? t.len - t.n + r / g : -1;
   rs.m = -INFINITY;
   rs.l = 0.0f;
-  // bytes from global memory to the start of the slots, by all waves; until all is there
-  auto fill = [&](const uint8_t* src, int bytes) {
-    for (int i = w; i < bytes / 1024; i += W)
-      load_to_lds(src + i * 1024 + l * 16, __builtin_amdgcn_readfirstlane(lds_address(lds) + i * 1024));
+  // a rotation's operands from global memory to slots 0 and 1, by all waves; until all is there
+  auto fill = [&](const uint8_t* src) {
+#pragma unroll 1
+    for (int i = 0; i < kPageLds / 1024 / W; ++i) {
+      const int at = (w + i * W) * 1024;
+      load_to_lds(src + at + l * 16, slot0 + at);
+      load_to_lds(src + kPageLds + at + l * 16, second + at);
+    }
     wait_loads<0>();
     lds_barrier();
   };
   const uint8_t* rot = FMT != kBf16 ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
   u4v q[8];
   if constexpr (FMT != kBf16) {
-    fill(rot, kRotBytes);
-    rotate_queries(a, row, live, lds, q, rs.c);
+    fill(rot);
+    rotate_queries(a, row, live, slot0, second, q, rs.c);
     lds_barrier();
   } else {
     load_queries<FMT>(a, row, live, q, rs.c);
@@ -914,11 +954,10 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   };
   // bf16, kHalf: this wave's part of a page, straight to LDS
   constexpr int kLoads = 32 / W;
-  auto fetch = [&](int64_t block, int slot) {
+  auto fetch = [&](int64_t block, uint8_t* dst) {
     const uint8_t* src = (FMT == kHalf ? a.expanded : a.pages) + block * kPageLds + w * kLoads * 1024 + l * 16;
-    const uint32_t dst = lds_address(lds) + slot * kPageLds + w * kLoads * 1024;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, __builtin_amdgcn_readfirstlane(dst + i * 1024));
+    for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, dst + (w * kLoads + i) * 1024);
   };
   // codes: a wave takes a quarter of K's and of V's codes to registers, and a page later makes 4
   // operands of 1 KB of each
@@ -936,7 +975,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   auto expand = [&](int x, int slot) {
     const int ntok = min(t.len - page_of(x) * kP, kP);
     Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
-    uint8_t* dst = lds + slot * kPageLds;
+    uint8_t* dst = slot0 + slot * kPageLds;
     lane_exchange();
     int e_k = kNoExp;
     make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, ntok, sc, e_k);
@@ -958,9 +997,9 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   float unit = 1.0f;
   int64_t ahead_block = block_of(x0 + kSlots - 1);
   if (!CODES) {
-    fetch(block_of(x0), 0);
+    fetch(block_of(x0), slot0);
     wait_loads<0>();
-    if (kSlots == 3 && x0 + 1 < x1) fetch(block_of(x0 + 1), 1);
+    if (kSlots == 3 && x0 + 1 < x1) fetch(block_of(x0 + 1), slot1);
   } else {
     load_codes(block_of(x0));
     expand(x0, 0);
@@ -968,17 +1007,20 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
   int2 ex_next = make_int2(0, 0);
   if (FMT == kHalf) ex_next = page_exps(x0);
   lds_barrier();
-  int slot = 0;
   // positions of the wave's first and last row (none: nothing is seen)
   const int wr0 = t.row0 + w * kRows, wr1 = min(wr0 + kRows, t.rows) - 1;
   const int w_min = t.len - t.n + wr0 / g, w_max = wr0 <= wr1 ? t.len - t.n + wr1 / g : -1;
+  // a lane's offset among a step's operands, a sum's part for the compiler (as the low bits of an
+  // address past the reads' offsets it was put in again for each read)
+  const int k_lane = stay(FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16);
+  const int v_lane = FMT == kBf16 ? stay((l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256) : k_lane;
   int x = x0;
-  do {
+  auto page = [&](auto slot) {
+    const auto ahead = ahead_of(slot);
     const int t0 = page_of(x) * kP;
     const bool next = x + 1 < x1;
-    const int ahead = slot == 0 ? kSlots - 1 : slot - 1;  // the slot that is free
     if (!CODES) {
-      if (x + kSlots - 1 < x1) fetch(ahead_block, ahead);
+      if (x + kSlots - 1 < x1) fetch(ahead_block, lds_of(ahead));
     } else if (next) {
       load_codes(ahead_block);
     }
@@ -1003,7 +1045,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       }
       e_o = e;
     }
-    uint8_t* base = lds + slot * kPageLds;
+    uint8_t* base = lds_of(slot);
     if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
       const int ntok = t.len - t0;
       for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
@@ -1015,8 +1057,6 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       }
       lds_barrier();
     }
-    const int k_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16;
-    const int v_lane = FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256 : l * 16;
     // the wave's rows see something of the page
     const bool seen = t0 <= w_max && (t0 + kP - 1 > w_min - window || t0 < a.sinks);
     if (seen) {
@@ -1087,22 +1127,38 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       }
     }
     float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    asm volatile("" : "+v"(total));  // the additions stay among the products
+    total = stay(total);  // the additions stay among the products
     rs.l = FMT == kHalf ? fmaf(total, __builtin_amdgcn_exp2f(-weight), rs.l) : rs.l + total;
     }
     if (!CODES) {  // page x + 1 has landed
       if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
       else wait_loads<0>();
-    } else if (next) {
-      expand(x + 1, ahead);
+    }
+    if constexpr (CODES) {
+      if (next) expand(x + 1, ahead);
     }
     lds_barrier();
-    slot = slot + 1 == kSlots ? 0 : slot + 1;
-  } while (++x < x1);
+    ++x;
+  };
+  if constexpr (CODES) {
+    int slot = 0;
+    do {
+      page(slot);
+      slot = 1 - slot;
+    } while (x < x1);
+  } else do {
+    page(std::integral_constant<int, 0>{});
+    if (x >= x1) break;
+    page(std::integral_constant<int, 1>{});
+    if constexpr (kSlots == 3) {
+      if (x >= x1) break;
+      page(std::integral_constant<int, 2>{});
+    }
+  } while (x < x1);
   rs.l = half_sum(rs.l);
   if constexpr (FMT != kBf16) {
-    fill(rot + kRotBytes, kRotBytes);
-    unit = rotate_output(o, rs.l, e_o, lds);
+    fill(rot + kRotBytes);
+    unit = rotate_output(o, rs.l, e_o, slot0, second);
   }
   if (live) store_row<kBf16>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
   lds_barrier();  // the slots are free again
@@ -1112,6 +1168,15 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
 // ---------------------------------------------------------------------------
 // Few rows: a block takes one tile of 32 rows, its waves every fourth page each, from global
 // memory straight to the operands; the waves' states are merged in LDS.
+//   bf16: bound by the bytes.  A page's 16 KiB of K are loaded while the page before is multiplied,
+// its V while its scores are: one wave a SIMD with 400 registers.  64 sequences of 16k to 32k tokens,
+// one new each in a window of 4096, 32 query heads on 8: 174 us, 6.2 TB/s.
+//   Codes: bound by a page's chain (scales, scores, maximum, exponentials, values) of two waves a
+// SIMD: 500 (2 bits, one group) to 700 (4 bits, four groups) vector instructions, 256 of them to
+// expand the codes (a mask and a multiply-add for two), 150 the softmax of 32 rows; vector ALUs are busy
+// 50 to 75 % of the time, matrix cores 20.  K and V are loaded a page ahead, V's codes into registers of
+// their own.  32 sequences of 4k to 16k tokens, 5 new each, 32 heads on 8, 4 bits: 114 us and, with
+// rotations and merge, 126; 16 of up to 32k, 4 new, 64 heads, 2 bits: 84 and 94.
 // ---------------------------------------------------------------------------
 template <int FMT, int NG>
 __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(ChunkArgs a) {
@@ -1335,7 +1400,8 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
 // Merge of the partial states in the output's basis, of the rows that belong to a sequence and have
 // no output yet: 32 lanes a row, four channels each.  A lane reads the maximum and sum of one slot in
 // 32; the states' loads are issued eight slots at a time (empty ones, at the end but for pages that
-// the row does not see, weigh 0).
+// the row does not see, weigh 0).  Bound by the states' latency: a call with one token of 32
+// heads over 16k of bf16 took 40 us slot by slot, 23 now.
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int64_t row0) {
   const int64_t row = row0 + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int c = threadIdx.x & 31, S = a.num_splits;
