@@ -285,8 +285,8 @@ __device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16
     if (is_v) {
 #pragma unroll
       for (int i = 0; i < (FMT == kInt2 ? 4 : 2); ++i)
-        sc.va[i][g][at] = __builtin_bit_cast(
-            uint16_t, (_Float16)(__builtin_bit_cast(_Float16, (uint16_t)ab) * (_Float16)(1.0f / (1 << (kBits<FMT> * i)))));
+        sc.va[i][g][at] = __builtin_bit_cast(uint16_t, (_Float16)(__builtin_bit_cast(_Float16, (uint16_t)ab) *
+                                                                  (_Float16)(1.0f / (1 << (kBits<FMT> * i)))));
       sc.vb[g][at] = (uint16_t)(ab >> 16);
     } else {
       sc.k[g][l] = ab;
@@ -333,7 +333,8 @@ __device__ inline u4v v_operand(const u4v& raw, int C, int j0, int i2, const Sca
   const int t0 = 32 * j0 + 16 * h + 8 * i2;
   constexpr int bits = kBits<FMT>;
   const int place = FMT == kInt4 ? C % 2 : C;
-  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[place][c / G][t0]), B = *reinterpret_cast<const u4v*>(&sc.vb[c / G][t0]);
+  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[place][c / G][t0]);
+  const u4v B = *reinterpret_cast<const u4v*>(&sc.vb[c / G][t0]);
   u4v r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -549,7 +550,8 @@ __device__ inline bool find_segment(const ChunkArgs& a, Walk& k, int g, int M, i
   if (a.num_splits == 1) {
     if (k.empty) return false;
     k.empty = 1;
-    s.t = a.B > 1 && a.B <= kCounted ? count_tile(a, k.r, g, M) : find_tile(a, (int64_t)a.n_q * g / M + a.B - 1 - k.r, g, M);
+    s.t = a.B > 1 && a.B <= kCounted ? count_tile(a, k.r, g, M)
+                                     : find_tile(a, (int64_t)a.n_q * g / M + a.B - 1 - k.r, g, M);
     if (s.t.b < 0) return false;
     s.pg = tile_pages(s.t, g, M, window, a.sinks);
     s.x0 = s.slot = 0;
@@ -746,7 +748,8 @@ __global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages)
           if (is_v) {    // o_c = sum_j o~_j R_v[c][j]; step k: row 16 (k % 2) + 8 (e / 4) + 4 h + e % 4 of tile k / 2
             from = 32 * C + r;
             to = v_channel<FMT>(k / 2, 16 * (k % 2) + 8 * (e / 4) + 4 * h + e % 4);
-          } else {       // q~_j = sum_c q_c R_k[c][j]; row r: element 4 (r / 8 % 2) + r % 4 of step 2 C + r / 16, half r / 4 % 2
+          } else {       // q~_j = sum_c q_c R_k[c][j]; row r: element 4 (r / 8 % 2) + r % 4 of step
+                         // 2 C + r / 16, half r / 4 % 2
             from = 16 * k + 8 * h + e;
             to = k_channel<FMT>(2 * C + r / 16, r / 4 % 2, 4 * (r / 8 % 2) + r % 4);
           }
@@ -837,7 +840,8 @@ __device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live,
   for (int k = 0; k < 8; ++k)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      q[k][j] = pack2<kHalf>(ldexpf(y[k / 2][8 * (k % 2) + 2 * j], -e2), ldexpf(y[k / 2][8 * (k % 2) + 2 * j + 1], -e2));
+      q[k][j] = pack2<kHalf>(ldexpf(y[k / 2][8 * (k % 2) + 2 * j], -e2),
+                             ldexpf(y[k / 2][8 * (k % 2) + 2 * j + 1], -e2));
   c = fabsf(a.scale) * pow2(e1 + e2);
 }
 // o = o~ R_v^T, o~ = the sums / l 2^e as fp16 (divided by a power of two): rows of the output's
@@ -858,7 +862,8 @@ __device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_
   for (int k = 0; k < 8; ++k)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      x[k][j] = pack2<kHalf>(ldexpf(o[k / 2][8 * (k % 2) + 2 * j], -e3), ldexpf(o[k / 2][8 * (k % 2) + 2 * j + 1], -e3));
+      x[k][j] = pack2<kHalf>(ldexpf(o[k / 2][8 * (k % 2) + 2 * j], -e3),
+                             ldexpf(o[k / 2][8 * (k % 2) + 2 * j + 1], -e3));
   rotate(x, o, rot, rot2);
   return ldexpf(l, e3 + e);
 }
@@ -916,252 +921,254 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     if (x0 >= x1) {
       if (live) store_empty(a, row, sg, direct, h);
       continue;
-  }
-  RowState rs;
-  rs.pos = live ? t.len - t.n + r / g : -1;
-  rs.m = -INFINITY;
-  rs.l = 0.0f;
-  // a rotation's operands from global memory to slots 0 and 1, by all waves; until all is there
-  auto fill = [&](const uint8_t* src) {
+    }
+    RowState rs;
+    rs.pos = live ? t.len - t.n + r / g : -1;
+    rs.m = -INFINITY;
+    rs.l = 0.0f;
+    // a rotation's operands from global memory to slots 0 and 1, by all waves; until all is there
+    auto fill = [&](const uint8_t* src) {
 #pragma unroll 1
-    for (int i = 0; i < kPageLds / 1024 / W; ++i) {
-      const int at = (w + i * W) * 1024;
-      load_to_lds(src + at + l * 16, slot0 + at);
-      load_to_lds(src + kPageLds + at + l * 16, second + at);
+      for (int i = 0; i < kPageLds / 1024 / W; ++i) {
+        const int at = (w + i * W) * 1024;
+        load_to_lds(src + at + l * 16, slot0 + at);
+        load_to_lds(src + kPageLds + at + l * 16, second + at);
+      }
+      wait_loads<0>();
+      lds_barrier();
+    };
+    const uint8_t* rot = FMT != kBf16 ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
+    u4v q[8];
+    if constexpr (FMT != kBf16) {
+      fill(rot);
+      rotate_queries(a, row, live, slot0, second, q, rs.c);
+      lds_barrier();
+    } else {
+      load_queries<FMT>(a, row, live, q, rs.c);
     }
-    wait_loads<0>();
-    lds_barrier();
-  };
-  const uint8_t* rot = FMT != kBf16 ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
-  u4v q[8];
-  if constexpr (FMT != kBf16) {
-    fill(rot);
-    rotate_queries(a, row, live, slot0, second, q, rs.c);
-    lds_barrier();
-  } else {
-    load_queries<FMT>(a, row, live, q, rs.c);
-  }
-  const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
-  auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
-  // index of a page's block: its number is loaded a page before it is needed
-  auto block_of = [&](int x) -> int64_t {
-    const int i = page_of(min(x, x1 - 1));
-    return (FMT == kHalf ? (int64_t)t.b * a.max_pages + i : (int64_t)scalar_load(bt + i)) * a.Hkv + kvh;
-  };
-  auto page_exps = [&](int x) {
-    const int* e = reinterpret_cast<const int*>(a.exps + block_of(x));
-    return make_int2(scalar_load(e), scalar_load(e + 1));
-  };
-  // bf16, kHalf: this wave's part of a page, straight to LDS
-  constexpr int kLoads = 32 / W;
-  auto fetch = [&](int64_t block, uint8_t* dst) {
-    const uint8_t* src = (FMT == kHalf ? a.expanded : a.pages) + block * kPageLds + w * kLoads * 1024 + l * 16;
+    const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
+    auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
+    // index of a page's block: its number is loaded a page before it is needed
+    auto block_of = [&](int x) -> int64_t {
+      const int i = page_of(min(x, x1 - 1));
+      return (FMT == kHalf ? (int64_t)t.b * a.max_pages + i : (int64_t)scalar_load(bt + i)) * a.Hkv + kvh;
+    };
+    auto page_exps = [&](int x) {
+      const int* e = reinterpret_cast<const int*>(a.exps + block_of(x));
+      return make_int2(scalar_load(e), scalar_load(e + 1));
+    };
+    // bf16, kHalf: this wave's part of a page, straight to LDS
+    constexpr int kLoads = 32 / W;
+    auto fetch = [&](int64_t block, uint8_t* dst) {
+      const uint8_t* src = (FMT == kHalf ? a.expanded : a.pages) + block * kPageLds + w * kLoads * 1024 + l * 16;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, dst + (w * kLoads + i) * 1024);
-  };
-  // codes: a wave takes a quarter of K's and of V's codes to registers, and a page later makes 4
-  // operands of 1 KB of each
-  u4v raw[2];
-  uint32_t ent[2][NG];
-  int e_v = kNoExp;
-  auto load_codes = [&](int64_t block) {
-    const uint8_t* blk = a.pages + block * block_bytes_of(FMT, NG);
-    const int i = FMT == kInt4 ? w : w / 2;
-    raw[0] = load_k<FMT, NG>(blk, i);
-    raw[1] = load_v<FMT, NG>(blk, i);
-    load_entries<FMT, NG>(blk, 0, ent[0]);
-    load_entries<FMT, NG>(blk, 1, ent[1]);
-  };
-  auto expand = [&](int x, int slot) {
-    const int ntok = min(t.len - page_of(x) * kP, kP);
-    Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
-    uint8_t* dst = slot0 + slot * kPageLds;
-    lane_exchange();
-    int e_k = kNoExp;
-    make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, ntok, sc, e_k);
-    make_scales<FMT, NG>(ent[1], 1, a.meta_bf16, ntok, sc, e_v);
-    if (threadIdx.x == 0) {
-      exps[0][slot] = e_k;
-      exps[1][slot] = e_v;
-    }
-    lane_exchange();
-    expand_part<FMT, NG, false>(raw[0], 0, w, sc, dst);
-    expand_part<FMT, NG, false>(raw[1], 1, w, sc, dst + kHalfLds);
-  };
-  f16v o[4];
+      for (int i = 0; i < kLoads; ++i) load_to_lds(src + i * 1024, dst + (w * kLoads + i) * 1024);
+    };
+    // codes: a wave takes a quarter of K's and of V's codes to registers, and a page later makes 4
+    // operands of 1 KB of each
+    u4v raw[2];
+    uint32_t ent[2][NG];
+    int e_v = kNoExp;
+    auto load_codes = [&](int64_t block) {
+      const uint8_t* blk = a.pages + block * block_bytes_of(FMT, NG);
+      const int i = FMT == kInt4 ? w : w / 2;
+      raw[0] = load_k<FMT, NG>(blk, i);
+      raw[1] = load_v<FMT, NG>(blk, i);
+      load_entries<FMT, NG>(blk, 0, ent[0]);
+      load_entries<FMT, NG>(blk, 1, ent[1]);
+    };
+    auto expand = [&](int x, int slot) {
+      const int ntok = min(t.len - page_of(x) * kP, kP);
+      Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
+      uint8_t* dst = slot0 + slot * kPageLds;
+      lane_exchange();
+      int e_k = kNoExp;
+      make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, ntok, sc, e_k);
+      make_scales<FMT, NG>(ent[1], 1, a.meta_bf16, ntok, sc, e_v);
+      if (threadIdx.x == 0) {
+        exps[0][slot] = e_k;
+        exps[1][slot] = e_v;
+      }
+      lane_exchange();
+      expand_part<FMT, NG, false>(raw[0], 0, w, sc, dst);
+      expand_part<FMT, NG, false>(raw[1], 1, w, sc, dst + kHalfLds);
+    };
+    f16v o[4];
 #pragma unroll
-  for (int C = 0; C < 4; ++C)
+    for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
-  int e_o = kNoExp;  // the accumulators' exponent
-  float unit = 1.0f;
-  int64_t ahead_block = block_of(x0 + kSlots - 1);
-  if (!CODES) {
-    fetch(block_of(x0), slot0);
-    wait_loads<0>();
-    if (kSlots == 3 && x0 + 1 < x1) fetch(block_of(x0 + 1), slot1);
-  } else {
-    load_codes(block_of(x0));
-    expand(x0, 0);
-  }
-  int2 ex_next = make_int2(0, 0);
-  if (FMT == kHalf) ex_next = page_exps(x0);
-  lds_barrier();
-  // positions of the wave's first and last row (none: nothing is seen)
-  const int wr0 = t.row0 + w * kRows, wr1 = min(wr0 + kRows, t.rows) - 1;
-  const int w_min = t.len - t.n + wr0 / g, w_max = wr0 <= wr1 ? t.len - t.n + wr1 / g : -1;
-  // a lane's offset among a step's operands, a sum's part for the compiler (as the low bits of an
-  // address past the reads' offsets it was put in again for each read)
-  const int k_lane = stay(FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16);
-  const int v_lane = FMT == kBf16 ? stay((l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256) : k_lane;
-  int x = x0;
-  auto page = [&](auto slot) {
-    const auto ahead = ahead_of(slot);
-    const int t0 = page_of(x) * kP;
-    const bool next = x + 1 < x1;
+      for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
+    int e_o = kNoExp;  // the accumulators' exponent
+    float unit = 1.0f;
+    int64_t ahead_block = block_of(x0 + kSlots - 1);
     if (!CODES) {
-      if (x + kSlots - 1 < x1) fetch(ahead_block, lds_of(ahead));
-    } else if (next) {
-      load_codes(ahead_block);
+      fetch(block_of(x0), slot0);
+      wait_loads<0>();
+      if (kSlots == 3 && x0 + 1 < x1) fetch(block_of(x0 + 1), slot1);
+    } else {
+      load_codes(block_of(x0));
+      expand(x0, 0);
     }
-    ahead_block = block_of(x + kSlots);
-    float cp = rs.c, weight = 0.0f;  // weight (log2) of the page's values against the accumulators'
-    if (FMT != kBf16) {
-      int e_k, e;
-      if (FMT == kHalf) {
-        e_k = ex_next.x;
-        e = max(e_o, ex_next.y);
-        weight = (float)max(ex_next.y - e, -60);
-        if (next) ex_next = page_exps(x + 1);
-      } else {
-        e_k = __builtin_amdgcn_readfirstlane(exps[0][slot]);
-        e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
+    int2 ex_next = make_int2(0, 0);
+    if (FMT == kHalf) ex_next = page_exps(x0);
+    lds_barrier();
+    // positions of the wave's first and last row (none: nothing is seen)
+    const int wr0 = t.row0 + w * kRows, wr1 = min(wr0 + kRows, t.rows) - 1;
+    const int w_min = t.len - t.n + wr0 / g, w_max = wr0 <= wr1 ? t.len - t.n + wr1 / g : -1;
+    // a lane's offset among a step's operands, a sum's part for the compiler (as the low bits of an
+    // address past the reads' offsets it was put in again for each read)
+    const int k_lane = stay(FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16);
+    const int v_lane = FMT == kBf16 ? stay((l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256) : k_lane;
+    int x = x0;
+    auto page = [&](auto slot) {
+      const auto ahead = ahead_of(slot);
+      const int t0 = page_of(x) * kP;
+      const bool next = x + 1 < x1;
+      if (!CODES) {
+        if (x + kSlots - 1 < x1) fetch(ahead_block, lds_of(ahead));
+      } else if (next) {
+        load_codes(ahead_block);
       }
-      cp = fmaxf(rs.c * pow2(e_k), kLeast);
-      if (e != e_o && e_o != kNoExp) {
-        const float f = pow2(max(e_o - e, -126));
+      ahead_block = block_of(x + kSlots);
+      float cp = rs.c, weight = 0.0f;  // weight (log2) of the page's values against the accumulators'
+      if (FMT != kBf16) {
+        int e_k, e;
+        if (FMT == kHalf) {
+          e_k = ex_next.x;
+          e = max(e_o, ex_next.y);
+          weight = (float)max(ex_next.y - e, -60);
+          if (next) ex_next = page_exps(x + 1);
+        } else {
+          e_k = __builtin_amdgcn_readfirstlane(exps[0][slot]);
+          e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
+        }
+        cp = fmaxf(rs.c * pow2(e_k), kLeast);
+        if (e != e_o && e_o != kNoExp) {
+          const float f = pow2(max(e_o - e, -126));
 #pragma unroll
-        for (int C = 0; C < 4; ++C) o[C] *= f;
+          for (int C = 0; C < 4; ++C) o[C] *= f;
+        }
+        e_o = e;
       }
-      e_o = e;
-    }
-    uint8_t* base = lds_of(slot);
-    if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
-      const int ntok = t.len - t0;
-      for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
-        const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
-        u4v& v = reinterpret_cast<u4v*>(base + kHalfLds)[i];
+      uint8_t* base = lds_of(slot);
+      if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
+        const int ntok = t.len - t0;
+        for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
+          const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
+          u4v& v = reinterpret_cast<u4v*>(base + kHalfLds)[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
+          for (int j = 0; j < 4; ++j)
+            v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
+        }
+        lds_barrier();
+      }
+      // the wave's rows see something of the page
+      const bool seen = t0 <= w_max && (t0 + kP - 1 > w_min - window || t0 < a.sinks);
+      if (seen) {
+        // scores, the operands read three steps ahead
+        f16v s[2];
+        {
+          auto k_at = [&](int T, int k) {
+            const int off = FMT == kBf16 ? T * 8192 + (k % 4) * 1024 + (k / 4) * 512 : (T * 8 + k) * 1024;
+            return *reinterpret_cast<const u4v*>(base + k_lane + off);
+          };
+          u4v ka[4][2];
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int T = 0; T < 2; ++T) ka[k][T] = k_at(T, k);
+#pragma unroll
+          for (int T = 0; T < 2; ++T)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (k + 3 < 8)
+#pragma unroll
+              for (int T = 0; T < 2; ++T) ka[(k + 3) % 4][T] = k_at(T, k + 3);
+#pragma unroll
+            for (int T = 0; T < 2; ++T) s[T] = mfma<FMT>(ka[k % 4][T], q[k], s[T]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        auto v_at = [&](int C, int k) {
+          const int off = FMT == kBf16 ? C * 4096 + (k % 2) * 1024 + (k / 2) * 512 : (C * 4 + k) * 1024;
+          return *reinterpret_cast<const u4v*>(base + kHalfLds + v_lane + off);
+        };
+        u4v va[2][4];
+#pragma unroll
+        for (int C = 0; C < 4; ++C) va[0][C] = v_at(C, 0);
+        if (t0 + kP - 1 > w_min || (t0 <= w_max - window && t0 + kP > a.sinks))
+          mask_page(s, rs.pos, t0, window, a.sinks);
+        move_reference(s, o, rs, cp);
+        // weights of a step's operand, two at a time between the products of the step before
+        const float ms = (rs.m == -INFINITY ? 0.0f : -rs.m) + weight;
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        u4v p[2], pl[2];
+        auto weights = [&](int k, int i) {
+          auto one = [&](int e) {
+            const int y = v_slot<FMT>(e), u = y % 4;
+            return __builtin_amdgcn_exp2f(fmaf(s[u / 2][8 * (u % 2) + 4 * (k / 2) + 2 * (k % 2) + y / 4], cp, ms));
+          };
+          const float x = one(2 * i), y = one(2 * i + 1);
+          sum[i] += x;
+          sum[i] += y;
+          p[k % 2][i] = pack2<FMT>(x, y);
+          if (HL) pl[k % 2][i] = pack2<FMT>(x - bf_lo(p[k % 2][i]), y - bf_hi(p[k % 2][i]));
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weights(0, i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (k + 1 < 4)
+#pragma unroll
+            for (int C = 0; C < 4; ++C) va[(k + 1) % 2][C] = v_at(C, k + 1);
+#pragma unroll
+          for (int C = 0; C < 4; ++C) {
+            if (HL) o[C] = mfma<FMT>(va[k % 2][C], pl[k % 2], o[C]);
+            o[C] = mfma<FMT>(va[k % 2][C], p[k % 2], o[C]);
+            if (k + 1 < 4) weights(k + 1, C);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        total = stay(total);  // the additions stay among the products
+        rs.l = FMT == kHalf ? fmaf(total, __builtin_amdgcn_exp2f(-weight), rs.l) : rs.l + total;
+      }
+      if (!CODES) {  // page x + 1 has landed
+        if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
+        else wait_loads<0>();
+      }
+      if constexpr (CODES) {
+        if (next) expand(x + 1, ahead);
       }
       lds_barrier();
-    }
-    // the wave's rows see something of the page
-    const bool seen = t0 <= w_max && (t0 + kP - 1 > w_min - window || t0 < a.sinks);
-    if (seen) {
-    // scores, the operands read three steps ahead
-    f16v s[2];
-    {
-      auto k_at = [&](int T, int k) {
-        const int off = FMT == kBf16 ? T * 8192 + (k % 4) * 1024 + (k / 4) * 512 : (T * 8 + k) * 1024;
-        return *reinterpret_cast<const u4v*>(base + k_lane + off);
-      };
-      u4v ka[4][2];
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-#pragma unroll
-        for (int T = 0; T < 2; ++T) ka[k][T] = k_at(T, k);
-#pragma unroll
-      for (int T = 0; T < 2; ++T)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[T][i] = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (k + 3 < 8)
-#pragma unroll
-          for (int T = 0; T < 2; ++T) ka[(k + 3) % 4][T] = k_at(T, k + 3);
-#pragma unroll
-        for (int T = 0; T < 2; ++T) s[T] = mfma<FMT>(ka[k % 4][T], q[k], s[T]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    auto v_at = [&](int C, int k) {
-      const int off = FMT == kBf16 ? C * 4096 + (k % 2) * 1024 + (k / 2) * 512 : (C * 4 + k) * 1024;
-      return *reinterpret_cast<const u4v*>(base + kHalfLds + v_lane + off);
+      ++x;
     };
-    u4v va[2][4];
-#pragma unroll
-    for (int C = 0; C < 4; ++C) va[0][C] = v_at(C, 0);
-    if (t0 + kP - 1 > w_min || (t0 <= w_max - window && t0 + kP > a.sinks))
-      mask_page(s, rs.pos, t0, window, a.sinks);
-    move_reference(s, o, rs, cp);
-    // weights of a step's operand, two at a time between the products of the step before
-    const float ms = (rs.m == -INFINITY ? 0.0f : -rs.m) + weight;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    u4v p[2], pl[2];
-    auto weights = [&](int k, int i) {
-      auto one = [&](int e) {
-        const int y = v_slot<FMT>(e), u = y % 4;
-        return __builtin_amdgcn_exp2f(fmaf(s[u / 2][8 * (u % 2) + 4 * (k / 2) + 2 * (k % 2) + y / 4], cp, ms));
-      };
-      const float x = one(2 * i), y = one(2 * i + 1);
-      sum[i] += x;
-      sum[i] += y;
-      p[k % 2][i] = pack2<FMT>(x, y);
-      if (HL) pl[k % 2][i] = pack2<FMT>(x - bf_lo(p[k % 2][i]), y - bf_hi(p[k % 2][i]));
-    };
-#pragma unroll
-    for (int i = 0; i < 4; ++i) weights(0, i);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (k + 1 < 4)
-#pragma unroll
-        for (int C = 0; C < 4; ++C) va[(k + 1) % 2][C] = v_at(C, k + 1);
-#pragma unroll
-      for (int C = 0; C < 4; ++C) {
-        if (HL) o[C] = mfma<FMT>(va[k % 2][C], pl[k % 2], o[C]);
-        o[C] = mfma<FMT>(va[k % 2][C], p[k % 2], o[C]);
-        if (k + 1 < 4) weights(k + 1, C);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    total = stay(total);  // the additions stay among the products
-    rs.l = FMT == kHalf ? fmaf(total, __builtin_amdgcn_exp2f(-weight), rs.l) : rs.l + total;
-    }
-    if (!CODES) {  // page x + 1 has landed
-      if (kSlots == 3 && x + 2 < x1) wait_loads<kLoads>();
-      else wait_loads<0>();
-    }
     if constexpr (CODES) {
-      if (next) expand(x + 1, ahead);
+      int slot = 0;
+      do {
+        page(slot);
+        slot = 1 - slot;
+      } while (x < x1);
+    } else {
+      do {
+        page(std::integral_constant<int, 0>{});
+        if (x >= x1) break;
+        page(std::integral_constant<int, 1>{});
+        if constexpr (kSlots == 3) {
+          if (x >= x1) break;
+          page(std::integral_constant<int, 2>{});
+        }
+      } while (x < x1);
     }
-    lds_barrier();
-    ++x;
-  };
-  if constexpr (CODES) {
-    int slot = 0;
-    do {
-      page(slot);
-      slot = 1 - slot;
-    } while (x < x1);
-  } else do {
-    page(std::integral_constant<int, 0>{});
-    if (x >= x1) break;
-    page(std::integral_constant<int, 1>{});
-    if constexpr (kSlots == 3) {
-      if (x >= x1) break;
-      page(std::integral_constant<int, 2>{});
+    rs.l = half_sum(rs.l);
+    if constexpr (FMT != kBf16) {
+      fill(rot + kRotBytes);
+      unit = rotate_output(o, rs.l, e_o, slot0, second);
     }
-  } while (x < x1);
-  rs.l = half_sum(rs.l);
-  if constexpr (FMT != kBf16) {
-    fill(rot + kRotBytes);
-    unit = rotate_output(o, rs.l, e_o, slot0, second);
-  }
-  if (live) store_row<kBf16>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
-  lds_barrier();  // the slots are free again
+    if (live) store_row<kBf16>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
+    lds_barrier();  // the slots are free again
   }
 }
 
@@ -1340,7 +1347,8 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     for (int C = 0; C < 4; ++C)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        os[w][C][i][l] = make_float4(o[C][4 * i] * unit, o[C][4 * i + 1] * unit, o[C][4 * i + 2] * unit, o[C][4 * i + 3] * unit);
+        os[w][C][i][l] = make_float4(o[C][4 * i] * unit, o[C][4 * i + 1] * unit, o[C][4 * i + 2] * unit,
+                                     o[C][4 * i + 3] * unit);
     __syncthreads();
     float m = -INFINITY, L = 0.0f, f[kWaves];
 #pragma unroll
@@ -1547,8 +1555,12 @@ int chunk_blocks(bool quantized, int tile_rows) {
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t st) {
   if (a.format == kBf16) return launch_fmt<kBf16, 1>(a, st);
   if (a.format == kInt4)
-    return a.ng == 4 ? launch_fmt<kInt4, 4>(a, st) : a.ng == 2 ? launch_fmt<kInt4, 2>(a, st) : launch_fmt<kInt4, 1>(a, st);
-  return a.ng == 4 ? launch_fmt<kInt2, 4>(a, st) : a.ng == 2 ? launch_fmt<kInt2, 2>(a, st) : launch_fmt<kInt2, 1>(a, st);
+    return a.ng == 4   ? launch_fmt<kInt4, 4>(a, st)
+           : a.ng == 2 ? launch_fmt<kInt4, 2>(a, st)
+                       : launch_fmt<kInt4, 1>(a, st);
+  return a.ng == 4   ? launch_fmt<kInt2, 4>(a, st)
+         : a.ng == 2 ? launch_fmt<kInt2, 2>(a, st)
+                     : launch_fmt<kInt2, 1>(a, st);
 }
 
 }  // namespace oscar
