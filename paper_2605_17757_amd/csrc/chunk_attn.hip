@@ -191,22 +191,14 @@ template <int FMT>
 __host__ __device__ constexpr int v_slot(int e) {
   return FMT == kInt2 ? (e & 4) + (e % 4) / 2 + 2 * (e % 2) : e;
 }
-// Channels of rows 8 k + 4 h .. + 3 of the four V tiles: f(first channel, four values).
-template <int FMT, class F>
+// Rows 8 k + 4 h .. + 3 of the four tiles, row r of tile C channel 32 C + r: f(first channel, four values).
+template <class F>
 __device__ inline void each_four(const f16v (&o)[4], int h, F&& f) {
-  if (FMT == kInt2) {  // row r of tile C: channel 4 r + C
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f(4 * (8 * (i / 4) + 4 * h + i % 4), o[0][i], o[1][i], o[2][i], o[3][i]);
-  } else {
+  for (int C = 0; C < 4; ++C)
 #pragma unroll
-    for (int C = 0; C < 4; ++C)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = 8 * k + 4 * h;
-        const int c = FMT != kInt4 ? 32 * C + r : 64 * (C / 2) + 32 * (r / 16) + 16 * (C % 2) + r % 16;
-        f(c, o[C][4 * k], o[C][4 * k + 1], o[C][4 * k + 2], o[C][4 * k + 3]);
-      }
-  }
+    for (int k = 0; k < 4; ++k)
+      f(32 * C + 8 * k + 4 * h, o[C][4 * k], o[C][4 * k + 1], o[C][4 * k + 2], o[C][4 * k + 3]);
 }
 
 template <int FMT>
@@ -622,7 +614,6 @@ constexpr float kDone = INFINITY;
 
 // The row's output (direct), or its partial state in the segment's slot.  scale: of the
 // accumulators.
-template <int FMT>
 __device__ inline void store_row(const ChunkArgs& a, size_t row, const Segment& s, bool direct, const f16v (&o)[4],
                                  float m, float l, float scale, int h) {
   const size_t at = row * a.num_splits + s.slot;
@@ -630,7 +621,7 @@ __device__ inline void store_row(const ChunkArgs& a, size_t row, const Segment& 
   if (direct) {
     const float il = (l > 0.0f ? 1.0f / l : is_nan(l) ? l : 0.0f) * scale;
     uint16_t* dst = a.out + row * kD;
-    each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
+    each_four(o, h, [&](int c, float x, float y, float z, float w) {
       uint2 v;
       v.x = pack2<kBf16>(x * il, y * il);
       v.y = pack2<kBf16>(z * il, w * il);
@@ -642,7 +633,7 @@ __device__ inline void store_row(const ChunkArgs& a, size_t row, const Segment& 
   float* dst = a.part_o + at * kD;
   if (is_nan(l)) m = 0.0f;  // NaN in a row: its scores have no maximum, but the state is not empty
   if (m != -INFINITY)    // of an empty state only that is read
-    each_four<FMT>(o, h, [&](int c, float x, float y, float z, float w) {
+    each_four(o, h, [&](int c, float x, float y, float z, float w) {
       *reinterpret_cast<float4*>(dst + c) = make_float4(x * scale, y * scale, z * scale, w * scale);
     });
   if (h == 0) {
@@ -1167,7 +1158,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       fill(rot + kRotBytes);
       unit = rotate_output(o, rs.l, e_o, slot0, second);
     }
-    if (live) store_row<kBf16>(a, row, sg, direct, o, rs.m, rs.l, unit, h);
+    if (live) store_row(a, row, sg, direct, o, rs.m, rs.l, unit, h);
     lds_barrier();  // the slots are free again
   }
 }
