@@ -611,7 +611,7 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  *   window      : >= 0, 0: none; sinks >= 0, used with a window
  *   num_splits  : pieces that a row's pages are cut into at most (>= 1, at most 1024), or 0 for
  *                 oscar_chunk_default_splits, or fewer where a window leaves few pages or the
- *                 workspace room for fewer; results do not depend on it beyond fp32 rounding
+ *                 workspace room for fewer; results depend on it only in the roundings named above
  *   workspace   : >= oscar_chunk_workspace_bytes(L, n_q, B, Hq, max_pages_per_seq, num_splits,
  *                 quantized) bytes, 256-byte aligned, contents need no initialization.  With
  *                 num_splits 0 one for the largest n_q serves smaller ones too.  Over a quantized
