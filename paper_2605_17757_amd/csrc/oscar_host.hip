@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <exception>
 #include <mutex>
 #include <vector>
 
@@ -76,7 +77,11 @@ bool debug_on() {
 
 template <class T>
 int copy_to_host(std::vector<T>& h, const T* d, int64_t n) {
-  h.resize((size_t)n);
+  try {
+    h.resize((size_t)n);
+  } catch (const std::exception&) {  // more than host memory holds: no exception leaves a C entry
+    return OSCAR_ERR_UNSUPPORTED;
+  }
   if (n == 0) return OSCAR_OK;
   return hip_status(hipMemcpy(h.data(), d, (size_t)n * sizeof(T), hipMemcpyDeviceToHost));
 }
