@@ -1006,8 +1006,8 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     // positions of the wave's first and last row (none: nothing is seen)
     const int wr0 = t.row0 + w * kRows, wr1 = min(wr0 + kRows, t.rows) - 1;
     const int w_min = t.len - t.n + wr0 / g, w_max = wr0 <= wr1 ? t.len - t.n + wr1 / g : -1;
-    // a lane's offset among a step's operands, a sum's part for the compiler (as the low bits of an
-    // address past the reads' offsets it was put in again for each read)
+    // A lane's offset among a step's operands; the compiler does not see that its low bits are 0, and so
+    // adds a slot's address to it once (it put the address' bits in before each read otherwise).
     const int k_lane = stay(FMT == kBf16 ? (l & 15) * 16 + ((l >> 4) & 1) * 4096 + h * 256 : l * 16);
     const int v_lane = FMT == kBf16 ? stay((l & 15) * 16 + ((l >> 4) & 1) * 2048 + h * 256) : k_lane;
     int x = x0;
