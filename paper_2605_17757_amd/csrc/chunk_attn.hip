@@ -52,6 +52,11 @@ typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 constexpr int kRows = 32;         // query rows of a wave
 constexpr int kWaves = 4;
 constexpr float kSlack = 8.0f;    // how far (log2) a score may exceed the reference before it moves
+// Weights that become fp16 are 2^7 times larger, in the sums of values and of weights alike: up to
+// 2^(7 + kSlack) of fp16's 2^16, and its least step is 2^-31 of the reference's weight.  (Without, 131072
+// tokens of 2^-25 of the largest weight, together 0.4 %, were 0 in the sums of values.)
+template <int FMT>
+constexpr float kWeightUp = FMT == kBf16 ? 0.0f : 7.0f;
 constexpr int kNoWindow = 1 << 30;  // positions are below it
 // Least factor of scores: positive, so that a masked score stays -inf; below it scores are 0
 // to fp32's precision of exp.
@@ -421,7 +426,7 @@ __device__ inline void move_reference(const f16v (&s)[2], f16v (&o)[4], RowState
 template <int FMT, bool HL>
 __device__ inline void softmax_page(f16v (&s)[2], f16v (&o)[4], RowState& r, float cp, u4v (&p)[4], u4v (&pl)[4]) {
   move_reference(s, o, r, cp);
-  const float ms = r.m == -INFINITY ? 0.0f : -r.m;
+  const float ms = (r.m == -INFINITY ? 0.0f : -r.m) + kWeightUp<FMT>;
   float sum = 0.0f;
 #pragma unroll
   for (int T = 0; T < 2; ++T)
@@ -1093,7 +1098,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
           mask_page(s, rs.pos, t0, window, a.sinks);
         move_reference(s, o, rs, cp);
         // weights of a step's operand, two at a time between the products of the step before
-        const float ms = (rs.m == -INFINITY ? 0.0f : -rs.m) + weight;
+        const float ms = (rs.m == -INFINITY ? 0.0f : -rs.m) + kWeightUp<FMT> + weight;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         u4v p[2], pl[2];
         auto weights = [&](int k, int i) {
