@@ -600,11 +600,13 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  * Products of bf16 values are exact, their sums, softmax statistics and outputs' sums are fp32.
  * Softmax weights enter the value product rounded to bf16 (to two bf16 pieces where n_q Hq/Hkv is
  * at most 32 B); over a quantized cache weights, rotated queries and dequantized values enter as
- * fp16, scaled by powers of two per row and page: a weight is off by 2^-11 of itself at most, or,
- * for small ones over pages of like scales, by 2^-30 of its row's largest weight (as much as the
- * output's own rounding where 2^22 cached tokens all have such weights).  There |q~| log2(e) sm_scale and the scales must
- * stay below 2^56, and with n_q Hq/Hkv above 64 B the rotations' entries below 2^15: they enter as
- * two fp16 pieces, and a row of o~ as fp16, scaled by a power of two.
+ * fp16, scaled by powers of two per row and page.  A weight is off by 2^-11 of itself at most, or,
+ * for small ones, by 2^-30 of its row's largest weight (as much as the output's own rounding where
+ * 2^22 cached tokens all have such weights); a value s (n - z) by 2^-11 of itself and of |s z|, or,
+ * for small ones, by 2^-31 of the largest s (levels - 1) and |s z| among its page's cached tokens and
+ * groups; pages of values below 2^-60 of another's lose them.  There |q~| log2(e) sm_scale and the
+ * scales must stay below 2^56, and with n_q Hq/Hkv above 64 B the rotations' entries below 2^15: they
+ * enter as two fp16 pieces, and a row of o~ as fp16, scaled by a power of two.
  *   q           : bf16 [n_q, Hq, d]; Hq % Hkv == 0, Hq/Hkv <= 16
  *   q_start     : int32 [B + 1], ascending from 0, q_start[B] <= n_q; values outside [0, n_q] are
  *                 clamped

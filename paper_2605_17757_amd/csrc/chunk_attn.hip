@@ -17,14 +17,18 @@
 // What a lane gives the matrix cores of a page, 16 bytes a step, 8 values:
 //   K step ks of tile T: slot 4 lo + 2 T + b (l = lo + 16 b + 32 h), 8 channels
 //   V step (j0, i2) of tile C: one channel, 8 slots as above
-// bf16 pages hold these operands as they are.  Codes become fp16 with one packed
-// multiply-add: the 16-bit pattern of a code n is the fp16 subnormal n 2^-24, and
-//   x = s (n - z) = (n 2^-24) (s 2^24) - s z
-// with the scale and -s z rounded to fp16 (off by 2^-11 of s z at most; the scale is exact
-// unless it is 2^-14 of the page's largest) after division by a power of two, so that the
-// page's largest scale 2^24 and |s z| stay below 2^15: scores take it back as part of c, values
-// through the accumulators' exponent, which moves like m when a page needs more.  A code that lies
-// some places up in its 16 bits stays there, and its scale is divided by 2^places.
+// bf16 pages hold these operands as they are.  Codes become fp16 numbers n by the conversions of
+// small floating point types, two codes an instruction: as E4M3 the bytes 0 to 15 are n 2^-9 (subnormals
+// up to 7, and on without a gap), as E2M1 the nibbles 0 to 3 are n / 2.  One packed multiply-add gives
+//   x = s (n - z) = n s - s z
+// with the scale and -s z rounded to fp16 after division by a power of two, so that the largest
+// values that the page's scales and zero points allow, s times the largest code and |s z|, stay
+// below 2^14: off by 2^-11 of |x| and of |s z| at most, or by 2^-31 of that largest (17 half steps of
+// fp16's subnormals: one of the scale times 15, two of s z and x).  The range matters: a row without
+// a range is stored with scale 1 whatever its value.  (Codes as the subnormals n 2^-24 need no
+// conversion, but the scale times 2^24 then has to stay below 2^15: beside a scale of 1, 1e-3 was 2.4 %
+// off and 2e-5 became 0.)  Scores take the power of two back as part of c, values through the
+// accumulators' exponent, which follows the pages'.
 //
 // Three kernels, by the rows of a tile (chunk_tile_rows, with both sides of each choice measured):
 //   chunk_few_kernel   32 rows, waves share a tile's pages among them: bound by the bytes over bf16,
@@ -188,13 +192,13 @@ __device__ inline Pages tile_pages(const Tile& t, int g, int M, int window, int 
 template <int FMT>
 __device__ inline int k_channel(int ks, int h, int e) {
   if (FMT == kBf16) return 64 * (ks / 4) + 32 * h + 8 * (ks % 4) + e;  // ks = 4 X + kc
-  if (FMT == kInt4) return 32 * (ks % 4) + 16 * (ks / 4) + 8 * h + e;
-  return 64 * h + 16 * (ks / 2) + 4 * (ks % 2) + e / 2 + 8 * (e % 2);
+  if (FMT == kInt4) return 32 * (ks % 4) + 16 * (ks / 4) + 8 * h + e / 2 + 4 * (e % 2);
+  return 64 * h + 16 * (ks / 2) + ks % 2 + 2 * e;
 }
 // Slot (of 8) of element e of a V step.
 template <int FMT>
 __host__ __device__ constexpr int v_slot(int e) {
-  return FMT == kInt2 ? (e & 4) + (e % 4) / 2 + 2 * (e % 2) : e;
+  return FMT == kInt4 ? (e & 4) + (e % 4) / 2 + 2 * (e % 2) : e;
 }
 // Rows 8 k + 4 h .. + 3 of the four tiles, row r of tile C channel 32 C + r: f(first channel, four values).
 template <class F>
@@ -238,20 +242,31 @@ __device__ inline void load_entries(const uint8_t* blk, int is_v, uint32_t (&x)[
     x[g] = reinterpret_cast<const uint32_t*>(blk + off)[at];
   }
 }
-// Scales of a page in LDS, a wave's own: per group the slots' (s 2^24, -s z), divided by the
-// page's power of two.  K: both halves of a dword, by slot.  V: arrays of fp16, eight slots of a
-// step in 16 bytes, in the order of the step's elements; the scales also divided by 2^(bits i), for
-// codes that lie i places up in their 16 bits.
-constexpr int kPlaces = 4;
+// Scales of a page in LDS, a wave's own: per group the slots' (s, -s z), divided by a power of two.
+// K: both halves of a dword, by slot.  V: arrays of fp16, eight slots of a step in 16 bytes, in the
+// order of the step's elements.
 template <int NG>
 struct Scales {
   uint32_t k[NG][kP];
-  __align__(16) uint16_t va[kPlaces][NG][kP], vb[NG][kP];
+  __align__(16) uint16_t va[NG][kP], vb[NG][kP];
 };
 constexpr int kNoExp = -400;
-// The entries of slots < ntok to scales; e: the exponent, raised where the page needs it.
+// Exponents of operands that sums run over: with them the accumulators change their unit.
+constexpr int kRoom = 2;   // a page that needs up to so much less takes the accumulators'
+constexpr int kDeep = 60;  // no exponent lies further below the largest: 2^30 tokens' sums stay below 2^120
+struct Exponent {
+  int e = kNoExp, most = kNoExp;
+  __device__ void follow(int need) {
+    most = max(most, need);
+    if (need > e || need < e - kRoom) e = max(need, most - kDeep);
+  }
+};
+// What sums in units of 2^from are multiplied by to be in units of 2^to.
+__device__ inline float unit_change(int from, int to) { return ldexpf(1.0f, from - to); }
+// The entries of slots < ntok to scales; e: the exponent that the page brings its operands to.
 template <int FMT, int NG>
-__device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16, int ntok, Scales<NG>& sc, int& e) {
+__device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16, int ntok, Scales<NG>& sc,
+                                   Exponent& ex) {
   const int l = threadIdx.x & 63;
   const uint32_t written = l < ntok ? 0xffffffffu : 0u;  // slots never written: scale 0
   float s[NG], z[NG];
@@ -270,20 +285,18 @@ __device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16
       z[g] = (float)x.y;
     }
   }
-  float top = 0.0f;  // s 2^24 and |s z| are below 2^15 after division by 2^e
+  float top = 0.0f;  // of the values' two parts, below 2^14 after division by 2^e
 #pragma unroll
-  for (int g = 0; g < NG; ++g) top = fmaxf(fmaxf(top, fabsf(s[g])), fabsf(s[g] * (z[g] * 0x1p-24f)));
-  e = max(e, wave_max_i(exp_of(top) + 24 + 1 - 15));
-  const int at = FMT == kInt2 ? (l & ~3) + 2 * (l & 1) + ((l >> 1) & 1) : l;  // v_slot's inverse
+  for (int g = 0; g < NG; ++g)
+    top = fmaxf(fmaxf(top, fabsf(s[g]) * (float)((1 << kBits<FMT>) - 1)), fabsf(s[g] * z[g]));
+  ex.follow(max(wave_max_i(exp_of(top)) + 1 - 14, -120));
+  const int at = FMT == kInt4 ? (l & ~3) + 2 * (l & 1) + ((l >> 1) & 1) : l;  // v_slot's inverse
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    const float x = ldexpf(s[g], -e);
-    const uint32_t ab = pack2<kInt4>(x * 0x1p24f, -x * z[g]);
+    const float x = ldexpf(s[g], -ex.e);
+    const uint32_t ab = pack2<kInt4>(x, -x * z[g]);
     if (is_v) {
-#pragma unroll
-      for (int i = 0; i < (FMT == kInt2 ? 4 : 2); ++i)
-        sc.va[i][g][at] = __builtin_bit_cast(uint16_t, (_Float16)(__builtin_bit_cast(_Float16, (uint16_t)ab) *
-                                                                  (_Float16)(1.0f / (1 << (kBits<FMT> * i)))));
+      sc.va[g][at] = (uint16_t)ab;
       sc.vb[g][at] = (uint16_t)(ab >> 16);
     } else {
       sc.k[g][l] = ab;
@@ -294,6 +307,17 @@ __device__ inline uint32_t fma_h2(uint32_t n, uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2, n), __builtin_bit_cast(h2, a),
                                                                 __builtin_bit_cast(h2, b)));
 }
+// Codes as fp16: of bytes 0 and 1 or (hi) 2 and 3, each the code times `unit`, at most 15; of the two
+// nibbles of byte `byte`, at most 3 each.
+__device__ inline uint32_t bytes_h2(uint32_t codes, int unit, bool hi) {
+  const float scale = 512.0f / unit;
+  return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)codes, scale, true))
+            : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)codes, scale, false));
+}
+template <int BYTE>
+__device__ inline uint32_t nibbles_h2(uint32_t codes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, BYTE));
+}
 // K operand of step ks, tile T from its raw load.
 template <int FMT, int NG>
 __device__ inline u4v k_operand(const u4v& raw, int T, int ks, const Scales<NG>& sc) {
@@ -302,23 +326,18 @@ __device__ inline u4v k_operand(const u4v& raw, int T, int ks, const Scales<NG>&
   const int g = FMT == kInt4 ? 32 * (ks % 4) / G : (64 * h + 16 * (ks / 2)) / G;
   const uint32_t ab = sc.k[g][4 * lo + 2 * T + b];
   const uint32_t A = __builtin_amdgcn_perm(ab, ab, 0x01000100u), B = __builtin_amdgcn_perm(ab, ab, 0x03020302u);
-  u4v r;  // codes in place: n 2^(bits i) 2^-24, with the scale divided by 2^(bits i)
-  if (FMT == kInt4) {
+  u4v n;
+  if (FMT == kInt4) {  // low nibbles: channels 0, 4, 1, 5; high ones: 2, 6, 3, 7
     const uint32_t d = raw[ks % 4];
-    const _Float16 m = (_Float16)(1.0f / 16);
-    const uint32_t A1 = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, A) * h2{m, m});
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      r[i] = fma_h2((d >> (8 * (i / 2))) & (0x000f000fu << (4 * (i % 2))), i % 2 ? A1 : A, B);
-  } else {
-    const uint32_t d = raw[ks / 2] >> (8 * (ks % 2));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const _Float16 m = (_Float16)(1.0f / (1 << (2 * i)));
-      const uint32_t Ai = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, A) * h2{m, m});
-      r[i] = fma_h2(d & (0x00030003u << (2 * i)), Ai, B);
-    }
+    for (int i = 0; i < 4; ++i) n[i] = bytes_h2((d >> (4 * (i / 2))) & 0x0f0f0f0fu, 1, i % 2);
+  } else {  // even codes, odd codes
+    const uint32_t d = (raw[ks / 2] >> (2 * (ks % 2))) & 0x33333333u;
+    n = u4v{nibbles_h2<0>(d), nibbles_h2<1>(d), nibbles_h2<2>(d), nibbles_h2<3>(d)};
   }
+  u4v r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = fma_h2(n[i], A, B);
   return r;
 }
 // V operand of tile C, step (j0, i2) from its raw load.
@@ -328,15 +347,15 @@ __device__ inline u4v v_operand(const u4v& raw, int C, int j0, int i2, const Sca
   constexpr int G = kD / NG;
   const int c = FMT == kInt4 ? 64 * (C / 2) + 32 * jj : 4 * (l & 31);  // a channel of the row's group
   const int t0 = 32 * j0 + 16 * h + 8 * i2;
-  constexpr int bits = kBits<FMT>;
-  const int place = FMT == kInt4 ? C % 2 : C;
-  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[place][c / G][t0]);
+  const u4v A = *reinterpret_cast<const u4v*>(&sc.va[c / G][t0]);
   const u4v B = *reinterpret_cast<const u4v*>(&sc.vb[c / G][t0]);
   u4v r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t d = raw[FMT == kInt4 ? 2 * j0 + i / 2 : 2 * i2 + i / 2] >> (8 * (i % 2));
-    r[i] = fma_h2(d & (((1u << bits) - 1) * 0x00010001u << (bits * place)), A[i], B[i]);
+    // a byte: two channels of a slot, slots 0, 2, 1, 3; four channels of a slot, slots in order
+    const uint32_t d = FMT == kInt4 ? (raw[2 * j0 + i / 2] >> (4 * (C % 2))) & 0x0f0f0f0fu
+                                    : (raw[2 * i2 + i / 2] >> (4 * (C / 2))) & (C % 2 ? 0x0c0c0c0cu : 0x03030303u);
+    r[i] = fma_h2(bytes_h2(d, FMT == kInt2 && C % 2 ? 4 : 1, i % 2), A[i], B[i]);
   }
   return r;
 }
@@ -367,16 +386,22 @@ __device__ inline void load_queries(const ChunkArgs& a, size_t row, bool live, u
     const float* src = a.qt + row * kD;
     float x[8][8], top = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      // (kInt2: the even elements four channels in order, the odd ones those eight further on)
-      const float4 lo = *reinterpret_cast<const float4*>(src + k_channel<FMT>(ks, h, 0));
-      const float4 hi = *reinterpret_cast<const float4*>(src + k_channel<FMT>(ks, h, FMT == kInt2 ? 1 : 4));
-      const float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    for (int i = 0; i < 4; ++i) {  // 16 channels: two steps
+      float y[16];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[ks][e] = live ? y[FMT == kInt2 ? e / 2 + 4 * (e % 2) : e] : 0.0f;
-        top = fmaxf(top, fabsf(x[ks][e]));
+      for (int j = 0; j < 4; ++j) {
+        const int from = FMT == kInt4 ? k_channel<FMT>(i + 4 * (j / 2), h, 0) + 4 * (j % 2) : k_channel<FMT>(2 * i, h, 2 * j);
+        const float4 v = *reinterpret_cast<const float4*>(src + from);
+        y[4 * j] = v.x, y[4 * j + 1] = v.y, y[4 * j + 2] = v.z, y[4 * j + 3] = v.w;
       }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float& to = x[FMT == kInt4 ? i + 4 * j : 2 * i + j][e];
+          to = live ? y[FMT == kInt4 ? 8 * j + e / 2 + 4 * (e % 2) : 2 * e + j] : 0.0f;
+          top = fmaxf(top, fabsf(to));
+        }
     }
     const int e = max(exp_of(half_max(top)), -60) - 13;  // |q| < 2^14
 #pragma unroll
@@ -699,7 +724,7 @@ __device__ inline void expand_part(const u4v& raw, int is_v, int part, const Sca
       const int C = FMT == kInt4 ? 2 * (part / 2) + i % 2 : i;
       const int j0 = FMT == kInt4 ? i / 2 : part / 2, i2 = part % 2;
       u4v v = v_operand<FMT, NG>(raw, C, j0, i2, sc);
-      if (NATURAL && FMT == kInt2)  // slots (0, 2), (1, 3) -> (0, 1), (2, 3)
+      if (NATURAL && FMT == kInt4)  // slots (0, 2), (1, 3) -> (0, 1), (2, 3)
         v = u4v{__builtin_amdgcn_perm(v.y, v.x, 0x05040100u), __builtin_amdgcn_perm(v.y, v.x, 0x07060302u),
                 __builtin_amdgcn_perm(v.w, v.z, 0x05040100u), __builtin_amdgcn_perm(v.w, v.z, 0x07060302u)};
       *reinterpret_cast<u4v*>(dst + (C * 4 + 2 * j0 + i2) * 1024 + l * 16) = v;
@@ -776,7 +801,7 @@ __global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages)
   uint32_t ek[NG], ev[NG];
   load_entries<FMT, NG>(blk, 0, ek);
   load_entries<FMT, NG>(blk, 1, ev);
-  int e[2] = {kNoExp, kNoExp};
+  Exponent e[2];
   const int ntok = min(len - i * kP, kP);
   make_scales<FMT, NG>(ek, 0, a.meta_bf16, ntok, scales[w], e[0]);
   make_scales<FMT, NG>(ev, 1, a.meta_bf16, ntok, scales[w], e[1]);
@@ -784,7 +809,7 @@ __global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages)
   uint8_t* dst = a.expanded + (size_t)blockIdx.x * kExpandedBytes;
   expand_part<FMT, NG, true>(rk, 0, w, scales[w], dst);
   expand_part<FMT, NG, true>(rv, 1, w, scales[w], dst + kExpandedBytes / 2);
-  if (threadIdx.x == 0) a.exps[blockIdx.x] = make_int2(e[0], e[1]);
+  if (threadIdx.x == 0) a.exps[blockIdx.x] = make_int2(e[0].e, e[1].e);
 }
 
 // The product of a rotation's operands in LDS, half at rot, half at rot2, with x.  (Operands read
@@ -964,7 +989,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     // operands of 1 KB of each
     u4v raw[2];
     uint32_t ent[2][NG];
-    int e_v = kNoExp;
+    Exponent e_v;
     auto load_codes = [&](int64_t block) {
       const uint8_t* blk = a.pages + block * block_bytes_of(FMT, NG);
       const int i = FMT == kInt4 ? w : w / 2;
@@ -978,12 +1003,12 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
       uint8_t* dst = slot0 + slot * kPageLds;
       lane_exchange();
-      int e_k = kNoExp;
+      Exponent e_k;
       make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, ntok, sc, e_k);
       make_scales<FMT, NG>(ent[1], 1, a.meta_bf16, ntok, sc, e_v);
       if (threadIdx.x == 0) {
-        exps[0][slot] = e_k;
-        exps[1][slot] = e_v;
+        exps[0][slot] = e_k.e;
+        exps[1][slot] = e_v.e;
       }
       lane_exchange();
       expand_part<FMT, NG, false>(raw[0], 0, w, sc, dst);
@@ -994,7 +1019,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     for (int C = 0; C < 4; ++C)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
-    int e_o = kNoExp;  // the accumulators' exponent
+    Exponent e_o;  // the accumulators'
     float unit = 1.0f;
     int64_t ahead_block = block_of(x0 + kSlots - 1);
     if (!CODES) {
@@ -1028,23 +1053,23 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       ahead_block = block_of(x + kSlots);
       float cp = rs.c, weight = 0.0f;  // weight (log2) of the page's values against the accumulators'
       if (FMT != kBf16) {
-        int e_k, e;
+        int e_k;
+        const int e_old = e_o.e;
         if (FMT == kHalf) {
           e_k = ex_next.x;
-          e = max(e_o, ex_next.y);
-          weight = (float)max(ex_next.y - e, -60);
+          e_o.follow(ex_next.y);
+          weight = (float)max(ex_next.y - e_o.e, -60);
           if (next) ex_next = page_exps(x + 1);
         } else {
           e_k = __builtin_amdgcn_readfirstlane(exps[0][slot]);
-          e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
+          e_o.e = __builtin_amdgcn_readfirstlane(exps[1][slot]);
         }
         cp = fmaxf(rs.c * pow2(e_k), kLeast);
-        if (e != e_o && e_o != kNoExp) {
-          const float f = pow2(max(e_o - e, -126));
+        if (e_o.e != e_old && e_old != kNoExp) {
+          const float f = unit_change(e_old, e_o.e);
 #pragma unroll
           for (int C = 0; C < 4; ++C) o[C] *= f;
         }
-        e_o = e;
       }
       uint8_t* base = lds_of(slot);
       if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
@@ -1161,7 +1186,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     rs.l = half_sum(rs.l);
     if constexpr (FMT != kBf16) {
       fill(rot + kRotBytes);
-      unit = rotate_output(o, rs.l, e_o, slot0, second);
+      unit = rotate_output(o, rs.l, e_o.e, slot0, second);
     }
     if (live) store_row(a, row, sg, direct, o, rs.m, rs.l, unit, h);
     lds_barrier();  // the slots are free again
@@ -1175,8 +1200,8 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
 // its V while its scores are: one wave a SIMD with 400 registers.  64 sequences of 16k to 32k tokens,
 // one new each in a window of 4096, 32 query heads on 8: 174 us, 6.2 TB/s.
 //   Codes: bound by a page's chain (scales, scores, maximum, exponentials, values) of two waves a
-// SIMD: 500 (2 bits, one group) to 700 (4 bits, four groups) vector instructions, 256 of them to
-// expand the codes (a mask and a multiply-add for two), 150 the softmax of 32 rows; vector ALUs are busy
+// SIMD: 600 (2 bits, one group) to 800 (4 bits, four groups) vector instructions, 320 to 350 of them to
+// expand the codes (a conversion and a multiply-add for two, and masks), 150 the softmax of 32 rows; vector ALUs are busy
 // 50 to 75 % of the time, matrix cores 20.  K and V are loaded a page ahead, V's codes into registers of
 // their own.  32 sequences of 4k to 16k tokens, 5 new each, 32 heads on 8, 4 bits: 114 us and, with
 // rotations and merge, 126; 16 of up to 32k, 4 new, 64 heads, 2 bits: 84 and 94.
@@ -1211,7 +1236,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     for (int C = 0; C < 4; ++C)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[C][i] = 0.0f;
-    int e_v = kNoExp;
+    Exponent e_v;
     if (x0 + w < x1) {
       const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
       auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
@@ -1263,14 +1288,15 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
         if (FMT == kBf16) {
           fetch_v(blk, rv);
         } else {
-          const int e_old = e_v;
+          const int e_old = e_v.e;
+          Exponent page_k;
           lane_exchange();  // the last page's scales have been read
-          e_k = kNoExp;
-          make_scales<FMT, NG>(ks, 0, a.meta_bf16, min(ntok, kP), sc, e_k);
+          make_scales<FMT, NG>(ks, 0, a.meta_bf16, min(ntok, kP), sc, page_k);
           make_scales<FMT, NG>(vs, 1, a.meta_bf16, min(ntok, kP), sc, e_v);
           lane_exchange();
-          if (e_v != e_old && e_old != kNoExp) {
-            const float f = pow2(max(e_old - e_v, -126));
+          e_k = page_k.e;
+          if (e_v.e != e_old && e_old != kNoExp) {
+            const float f = unit_change(e_old, e_v.e);
 #pragma unroll
             for (int C = 0; C < 4; ++C) o[C] *= f;
           }
@@ -1335,7 +1361,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
       }
     }
     // merge: wave w sums tile C = w of the four states
-    const float unit = FMT == kBf16 || e_v == kNoExp ? 1.0f : ldexpf(1.0f, e_v);
+    const float unit = FMT == kBf16 || e_v.e == kNoExp ? 1.0f : ldexpf(1.0f, e_v.e);
     const float lt = half_sum(rs.l);
     // (NaN in a row: its scores have no maximum, but the state is not empty)
     if (h == 0) ml[w][n] = make_float2(is_nan(lt) ? 0.0f : rs.m, lt);
