@@ -594,8 +594,9 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  *   o = softmax(sm_scale * q K^T) V     (quantized caches: K^, V^ as in oscar_decode_attn)
  * A row that sees no token (seq_lens[b] < n_b) is zero.  Rows from q_start[B] on are left as
  * they were.  Pages of the block table that no new token of the sequence sees are not read, and
- * their entries may be anything.  Slots past a sequence's length may hold anything; a NaN or an
- * infinity among the values that some new token of the sequence sees may reach the rows of others.
+ * their entries may be anything.  Slots past a sequence's length and cached tokens that none of its
+ * new ones sees may hold anything; a NaN or an infinity among the values that some new token of the
+ * sequence sees may reach the rows of others.
  * A NaN in a query row gives NaN in its own output row only.
  * Products of bf16 values are exact, their sums, softmax statistics and outputs' sums are fp32.
  * Softmax weights enter the value product rounded to bf16 (to two bf16 pieces where n_q Hq/Hkv is

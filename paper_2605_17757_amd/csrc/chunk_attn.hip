@@ -184,6 +184,24 @@ __device__ inline Pages tile_pages(const Tile& t, int g, int M, int window, int 
   return s;
 }
 
+// Cached tokens that some row of a sequence sees: t < end, and t >= start or t < sinks.  The others of a page that is
+// read may hold anything: their weights are 0, and so are their values and scales made (0 times a NaN
+// or an infinity is not, and a scale counts in the page's exponent).
+struct Seen {
+  int end, start, sinks;
+  __device__ bool operator()(int t) const { return t < end && (t >= start || t < sinks); }
+  __device__ bool whole_page(int t0) const { return t0 + kP <= end && (t0 >= start || t0 + kP <= sinks); }
+  // The halves of a dword that belong to tokens t and t + 1.
+  __device__ uint32_t pair(int t) const { return ((*this)(t) ? 0xffffu : 0u) | ((*this)(t + 1) ? 0xffff0000u : 0u); }
+};
+// Of a sequence's rows, where clearing takes instructions of its own (bf16: for the tile's rows alone
+// chunks of seven sequences in a window took 2 % longer); of the tile's, where scales are made anyway.
+template <int FMT>
+__device__ inline Seen seen_by_rows(const Tile& t, const Pages& s, int window, int sinks) {
+  return FMT == kBf16 ? Seen{t.len, max(t.len - t.n - window + 1, 0), sinks}
+                      : Seen{s.p_max + 1, max(s.p_min - window + 1, 0), sinks};
+}
+
 // ---------------------------------------------------------------------------
 // One page's operands from the three formats.  Bytes of channels and slots: internal.h and
 // the headers of the formats' kernels.
@@ -263,12 +281,13 @@ struct Exponent {
 };
 // What sums in units of 2^from are multiplied by to be in units of 2^to.
 __device__ inline float unit_change(int from, int to) { return ldexpf(1.0f, from - to); }
-// The entries of slots < ntok to scales; e: the exponent that the page brings its operands to.
+// A page's entries to scales, of slots that no row sees 0; e: the exponent that the page brings its
+// operands to.
 template <int FMT, int NG>
-__device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16, int ntok, Scales<NG>& sc,
+__device__ inline void make_scales(const uint32_t (&ent)[NG], int is_v, int bf16, bool seen, Scales<NG>& sc,
                                    Exponent& ex) {
   const int l = threadIdx.x & 63;
-  const uint32_t written = l < ntok ? 0xffffffffu : 0u;  // slots never written: scale 0
+  const uint32_t written = seen ? 0xffffffffu : 0u;
   float s[NG], z[NG];
   if (bf16) {
 #pragma unroll
@@ -802,9 +821,9 @@ __global__ __launch_bounds__(256) void expand_kernel(ChunkArgs a, int64_t pages)
   load_entries<FMT, NG>(blk, 0, ek);
   load_entries<FMT, NG>(blk, 1, ev);
   Exponent e[2];
-  const int ntok = min(len - i * kP, kP);
-  make_scales<FMT, NG>(ek, 0, a.meta_bf16, ntok, scales[w], e[0]);
-  make_scales<FMT, NG>(ev, 1, a.meta_bf16, ntok, scales[w], e[1]);
+  const bool seen = Seen{len, start, a.sinks}(i * kP + l);
+  make_scales<FMT, NG>(ek, 0, a.meta_bf16, seen, scales[w], e[0]);
+  make_scales<FMT, NG>(ev, 1, a.meta_bf16, seen, scales[w], e[1]);
   lane_exchange();
   uint8_t* dst = a.expanded + (size_t)blockIdx.x * kExpandedBytes;
   expand_part<FMT, NG, true>(rk, 0, w, scales[w], dst);
@@ -938,6 +957,7 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     const bool live = r < t.rows;
     const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
     const bool direct = sg.whole;
+    const Seen seen_by = seen_by_rows<FMT>(t, pg, window, a.sinks);
     const int x0 = sg.x0, x1 = sg.x1;
     if (x0 >= x1) {
       if (live) store_empty(a, row, sg, direct, h);
@@ -999,13 +1019,13 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
       load_entries<FMT, NG>(blk, 1, ent[1]);
     };
     auto expand = [&](int x, int slot) {
-      const int ntok = min(t.len - page_of(x) * kP, kP);
+      const bool seen = seen_by(page_of(x) * kP + l);
       Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[w];
       uint8_t* dst = slot0 + slot * kPageLds;
       lane_exchange();
       Exponent e_k;
-      make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, ntok, sc, e_k);
-      make_scales<FMT, NG>(ent[1], 1, a.meta_bf16, ntok, sc, e_v);
+      make_scales<FMT, NG>(ent[0], 0, a.meta_bf16, seen, sc, e_k);
+      make_scales<FMT, NG>(ent[1], 1, a.meta_bf16, seen, sc, e_v);
       if (threadIdx.x == 0) {
         exps[0][slot] = e_k.e;
         exps[1][slot] = e_v.e;
@@ -1072,14 +1092,12 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
         }
       }
       uint8_t* base = lds_of(slot);
-      if (FMT == kBf16 && t.len - t0 < kP) {  // slots never written weigh 0: their values may be anything
-        const int ntok = t.len - t0;
+      if (FMT == kBf16 && !seen_by.whole_page(t0)) {
         for (int i = threadIdx.x; i < kP * kD / 8; i += 64 * W) {  // 16 bytes: slots 16 hi + 8 kt + e
           const int first = 16 * ((i >> 4) & 3) + 8 * ((i >> 6) & 1);
           u4v& v = reinterpret_cast<u4v*>(base + kHalfLds)[i];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            v[j] &= (first + 2 * j < ntok ? 0xffffu : 0u) | (first + 2 * j + 1 < ntok ? 0xffff0000u : 0u);
+          for (int j = 0; j < 4; ++j) v[j] &= seen_by.pair(t0 + first + 2 * j);
         }
         lds_barrier();
       }
@@ -1226,6 +1244,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
     const bool live = r < t.rows;
     const size_t row = (size_t)(t.q0 + (live ? r / g : 0)) * a.Hq + kvh * g + (live ? r % g : 0);
     const bool direct = FMT == kBf16 && sg.whole;
+    const Seen seen_by = seen_by_rows<FMT>(t, pg, window, a.sinks);
     const int x0 = sg.x0, x1 = sg.x1;
     RowState rs;
     rs.pos = live ? t.len - t.n + r / g : -1;
@@ -1281,7 +1300,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
       Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
       int x = x0 + w;
       auto page = [&](auto& rv, auto& rv_next) {
-        const int t0 = page_of(x) * kP, ntok = t.len - t0;
+        const int t0 = page_of(x) * kP;
         const bool more = x + kWaves < x1;
         const uint8_t* next = more ? block_of(x + kWaves) : blk;
         int e_k = 0;
@@ -1289,10 +1308,11 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
           fetch_v(blk, rv);
         } else {
           const int e_old = e_v.e;
+          const bool seen = seen_by(t0 + l);
           Exponent page_k;
           lane_exchange();  // the last page's scales have been read
-          make_scales<FMT, NG>(ks, 0, a.meta_bf16, min(ntok, kP), sc, page_k);
-          make_scales<FMT, NG>(vs, 1, a.meta_bf16, min(ntok, kP), sc, e_v);
+          make_scales<FMT, NG>(ks, 0, a.meta_bf16, seen, sc, page_k);
+          make_scales<FMT, NG>(vs, 1, a.meta_bf16, seen, sc, e_v);
           lane_exchange();
           e_k = page_k.e;
           if (e_v.e != e_old && e_old != kNoExp) {
@@ -1327,14 +1347,12 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
         u4v p[4], pl[4];
         if (masked) mask_page(s, rs.pos, t0, window, a.sinks);
         softmax_page<FMT, HL>(s, o, rs, FMT == kBf16 ? rs.c : fmaxf(rs.c * pow2(e_k), kLeast), p, pl);
-        if (FMT == kBf16 && ntok < kP) {  // slots never written weigh 0: their values may be anything
+        if (FMT == kBf16 && !seen_by.whole_page(t0)) {
 #pragma unroll
           for (int i = 0; i < kL; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int ts = 32 * (i / 2 % 2) + 16 * h + 8 * (i % 2) + 2 * j;
-              rv[i][j] &= (ts < ntok ? 0xffffu : 0u) | (ts + 1 < ntok ? 0xffff0000u : 0u);
-            }
+            for (int j = 0; j < 4; ++j)
+              rv[i][j] &= seen_by.pair(t0 + 32 * (i / 2 % 2) + 16 * h + 8 * (i % 2) + 2 * j);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
