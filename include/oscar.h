@@ -619,7 +619,8 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  *                 workspace room for fewer; results depend on it only in the roundings named above
  *   workspace   : >= oscar_chunk_workspace_bytes(L, n_q, B, Hq, max_pages_per_seq, num_splits,
  *                 quantized) bytes, 256-byte aligned, contents need no initialization.  With
- *                 num_splits 0 one for the largest n_q serves smaller ones too.  Over a quantized
+ *                 num_splits 0 that is the most that any chunk of up to n_q tokens needs, each in its
+ *                 own default number of pieces: one workspace serves them all.  Over a quantized
  *                 cache, chunks of more than 512 (token, head) rows per sequence and KV head on
  *                 average have their pages expanded to 16 bits there (32 KiB for a page of
  *                 block_table and KV head) while these are at most 65536.

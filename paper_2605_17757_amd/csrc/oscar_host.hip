@@ -1172,6 +1172,26 @@ ChunkWs chunk_ws(const oscar_layout* L, int64_t n_q, int32_t B, int64_t Hq, int6
   return w;
 }
 
+// For every chunk of up to n_q tokens, in as many pieces as it is cut into by default: a long chunk is
+// cut into none, a token into many.  The size grows with the tokens where tiles' rows and number stay, so
+// that the ends of those ranges do, up to the chunks that are never cut.
+size_t chunk_ws_most(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq, int64_t max_pages, bool quantized) {
+  const int64_t g = Hq / L->num_kv_heads;
+  size_t most = 0;
+  auto with = [&](int64_t n) {
+    if (n < 0 || n > n_q) return;
+    const int32_t S = oscar_chunk_default_splits(L, (int32_t)n, B, Hq, (int32_t)max_pages);
+    most = std::max(most, chunk_ws(L, n, B, Hq, max_pages, S, quantized).total);
+  };
+  with(n_q);
+  for (const int64_t rows : {32, 64, 512}) with(rows * B / g);  // borders of chunk_tile_rows
+  for (const int M : {4 * 32, kManyRows}) {
+    const int64_t tiles = 4 * (int64_t)chunk_blocks(true, M) / ((int64_t)B * L->num_kv_heads) + 1;
+    for (int64_t k = 1; k <= tiles; ++k) with(((k * M + 1) * B - 1) / g);
+  }
+  return most;
+}
+
 // OSCAR_DEBUG: chunk boundaries ascending within n_q, lengths within the table's rows, ids of the
 // pages that a sequence's new tokens see within the pool.
 int chunk_debug_check(const oscar_layout* L, void* stream, int32_t n_q, int32_t B, const int32_t* q_start,
@@ -1294,8 +1314,10 @@ int32_t oscar_chunk_default_splits(const oscar_layout* L, int32_t n_q, int32_t B
 
 size_t oscar_chunk_workspace_bytes(const oscar_layout* L, int32_t n_q, int32_t B, int32_t Hq,
                                    int32_t max_pages_per_seq, int32_t num_splits, int32_t quantized) {
+  const bool choose = num_splits == 0;
   if (check_chunk_sizes(L, n_q, B, Hq, max_pages_per_seq, &num_splits) != OSCAR_OK) return 0;
-  return chunk_ws(L, n_q, B, Hq, max_pages_per_seq, num_splits, quantized != 0).total;
+  return choose ? chunk_ws_most(L, n_q, B, Hq, max_pages_per_seq, quantized != 0)
+                : chunk_ws(L, n_q, B, Hq, max_pages_per_seq, num_splits, quantized != 0).total;
 }
 
 int oscar_bf16_chunk_attn(const oscar_layout* L, const void* pages, const void* q, int32_t n_q, int32_t B,
