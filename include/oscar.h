@@ -597,7 +597,7 @@ int oscar_bf16_kv_append_rope(const oscar_layout *L, void *pages, const oscar_ro
  * their entries may be anything.  Slots past a sequence's length and cached tokens that none of its
  * new ones sees may hold anything; a NaN or an infinity among the values that some new token of the
  * sequence sees may reach the rows of others.
- * A NaN in a query row gives NaN in its own output row only.
+ * A NaN or an infinity in a query row gives NaN in its own output row only.
  * Products of bf16 values are exact, their sums, softmax statistics and outputs' sums are fp32.
  * Softmax weights enter the value product rounded to bf16 (to two bf16 pieces where n_q Hq/Hkv is
  * at most 32 B); over a quantized cache weights, rotated queries and dequantized values enter as

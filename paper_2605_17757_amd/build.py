@@ -39,8 +39,7 @@ SOURCES = {
     "kv4_cache.hip": ["-ffp-contract=off"],
     "bf16_decode.hip": [],
     "rope.hip": [],
-    # maxima without an instruction that quiets each operand; NaN is looked for by its bits there
-    "chunk_attn.hip": ["-fno-honor-nans"],
+    "chunk_attn.hip": [],
     "mixed.hip": [],
     "calib.hip": ["-ffp-contract=off"],
     "probe.hip": [],

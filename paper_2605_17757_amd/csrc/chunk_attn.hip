@@ -87,10 +87,12 @@ __device__ inline float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff000
 // x itself, by a move that the compiler does not see through.
 __device__ inline int stay(int x) { return __builtin_amdgcn_update_dpp(x, x, 0xE4, 0xF, 0xF, false); }
 __device__ inline float stay(float x) { return __uint_as_float((uint32_t)stay((int)__float_as_uint(x))); }
+// The larger one, NaN if one is: a single instruction, where fmaxf quiets each operand first.
+__device__ inline float maximum(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 // Over the two halves of a wave: lanes l and l ^ 32.
 __device__ inline float half_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ inline float half_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -106,6 +108,20 @@ __device__ inline int wave_max_i(int v) {
   v = dpp(v, std::integral_constant<int, 0x121>{});
   return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
              max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+// The same of what is ordered as its bits are: magnitudes.
+__device__ inline float half_max_bits(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __uint_as_float(max((uint32_t)r[0], (uint32_t)r[1]));
+}
+// The largest magnitude of x's fp32 bits and eight bf16 values.
+constexpr uint32_t kInfBits = 0x7f800000u;  // (NaN above it)
+__device__ inline uint32_t top_bf16(uint32_t x, const u4v& w) {
+  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+  us2 t = us2{0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(us2, w[i] & 0x7fff7fffu));
+  return max(x, (uint32_t)max(t.x, t.y) << 16);
 }
 // Exponent e of |x| < 2^(e + 1) (0 and subnormals: -127).
 __device__ inline int exp_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
@@ -389,21 +405,27 @@ struct RowState {
 };
 
 // The query operands of the wave's rows (row: this lane's, live or not).  Quantized caches:
-// fp16 rows divided by a power of two, which c takes back.
+// fp16 rows divided by a power of two, which c takes back.  Returns whether a NaN or an infinity is
+// among this lane's channels: the row's sum then begins as NaN, and so does the row end, also where
+// its scores are all -infinity.
 template <int FMT>
-__device__ inline void load_queries(const ChunkArgs& a, size_t row, bool live, u4v (&q)[8], float& c) {
+__device__ inline bool load_queries(const ChunkArgs& a, size_t row, bool live, u4v (&q)[8], float& c) {
   const int h = (threadIdx.x & 63) >> 5;
   if (FMT == kBf16) {
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;  // scores are multiplied by |scale|
+    uint32_t top = 0;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
       q[ks] = live ? *reinterpret_cast<const u4v*>(a.q + row * kD + k_channel<FMT>(ks, h, 0)) : u4v{0, 0, 0, 0};
+      top = top_bf16(top, q[ks]);
       q[ks] ^= flip;
     }
     c = fmaxf(fabsf(a.scale), kLeast);
+    return top >= kInfBits;
   } else {
     const float* src = a.qt + row * kD;
-    float x[8][8], top = 0.0f;
+    float x[8][8];
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // 16 channels: two steps
       float y[16];
@@ -419,16 +441,17 @@ __device__ inline void load_queries(const ChunkArgs& a, size_t row, bool live, u
         for (int e = 0; e < 8; ++e) {
           float& to = x[FMT == kInt4 ? i + 4 * j : 2 * i + j][e];
           to = live ? y[FMT == kInt4 ? 8 * j + e / 2 + 4 * (e % 2) : 2 * e + j] : 0.0f;
-          top = fmaxf(top, fabsf(to));
+          top = max(top, __float_as_uint(to) & 0x7fffffffu);
         }
     }
-    const int e = max(exp_of(half_max(top)), -60) - 13;  // |q| < 2^14
+    const int e = max(exp_of(half_max_bits(top)), -60) - 13;  // |q| < 2^14
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         q[ks][i] = pack2<FMT>(ldexpf(x[ks][2 * i], -e), ldexpf(x[ks][2 * i + 1], -e));
     c = pow2(e);
+    return top >= kInfBits;
   }
 }
 
@@ -452,11 +475,11 @@ __device__ inline void mask_page(f16v (&s)[2], int pos, int t0, int window, int 
 __device__ inline void move_reference(const f16v (&s)[2], f16v (&o)[4], RowState& r, float cp) {
   float mx = s[0][0];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) mx = fmaxf(fmaxf(mx, s[0][i]), s[1][i]);
+  for (int i = 0; i < 16; ++i) mx = maximum(maximum(mx, s[0][i]), s[1][i]);
   mx = half_max(mx) * cp;
   const bool need = mx > r.m + kSlack;
   if (__ballot(need) != 0ull) {
-    const float mn = fmaxf(r.m, mx);
+    const float mn = mx > r.m ? mx : r.m;  // (mx may be NaN)
     const float alpha = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - mn);
     r.m = mn;
     r.l *= alpha;
@@ -849,28 +872,27 @@ __device__ inline void rotate(const u4v (&x)[8], f16v (&y)[4], const uint8_t* ro
 }
 
 // q~ = q R_k as the score products' operands, fp16 divided by a power of two that c takes; R_k's
-// operands in LDS (rotate).
-__device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live, const uint8_t* rot,
+// operands in LDS (rotate).  Returns as load_queries.
+__device__ inline bool rotate_queries(const ChunkArgs& a, size_t row, bool live, const uint8_t* rot,
                                       const uint8_t* rot2, u4v (&q)[8], float& c) {
   const int l = threadIdx.x & 63, h = l >> 5;
   const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
   u4v x[8];
-  float top = 0.0f;
+  uint32_t top_q = 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     x[k] = live ? *reinterpret_cast<const u4v*>(a.q + row * kD + 16 * k + 8 * h) : u4v{0, 0, 0, 0};
+    top_q = top_bf16(top_q, x[k]);
     x[k] ^= flip;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf_lo(x[k][j])), fabsf(bf_hi(x[k][j]))));
   }
-  const int e1 = max(exp_of(half_max(top)), -100) - 13;
+  const int e1 = max(exp_of(half_max_bits(top_q)), -100) - 13;
 #pragma unroll
   for (int k = 0; k < 8; ++k)
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[k][j] = pack2<kInt4>(ldexpf(bf_lo(x[k][j]), -e1), ldexpf(bf_hi(x[k][j]), -e1));
   f16v y[4];
   rotate(x, y, rot, rot2);
-  top = 0.0f;
+  float top = 0.0f;
 #pragma unroll
   for (int C = 0; C < 4; ++C)
 #pragma unroll
@@ -883,6 +905,7 @@ __device__ inline void rotate_queries(const ChunkArgs& a, size_t row, bool live,
       q[k][j] = pack2<kHalf>(ldexpf(y[k / 2][8 * (k % 2) + 2 * j], -e2),
                              ldexpf(y[k / 2][8 * (k % 2) + 2 * j + 1], -e2));
   c = fabsf(a.scale) * pow2(e1 + e2);
+  return top_q >= kInfBits;
 }
 // o = o~ R_v^T, o~ = the sums / l 2^e as fp16 (divided by a power of two): rows of the output's
 // channels in order; returns what they are still to be multiplied by to be the sums again.
@@ -980,13 +1003,15 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
     };
     const uint8_t* rot = FMT != kBf16 ? a.rot + (size_t)(a.rph ? kvh : 0) * 2 * kRotBytes : nullptr;
     u4v q[8];
+    bool lost;
     if constexpr (FMT != kBf16) {
       fill(rot);
-      rotate_queries(a, row, live, slot0, second, q, rs.c);
+      lost = rotate_queries(a, row, live, slot0, second, q, rs.c);
       lds_barrier();
     } else {
-      load_queries<FMT>(a, row, live, q, rs.c);
+      lost = load_queries<FMT>(a, row, live, q, rs.c);
     }
+    if (lost && rs.pos >= 0) rs.l = __uint_as_float(0x7fc00000u);
     const int32_t* bt = a.block_table + (size_t)t.b * a.max_pages;
     auto page_of = [&](int x) { return x < pg.head ? x : pg.from + x - pg.head; };
     // index of a page's block: its number is loaded a page before it is needed
@@ -1296,7 +1321,7 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
         load_entries<FMT, NG>(blk, 1, vs);
       }
       u4v q[8];
-      load_queries<FMT>(a, row, live, q, rs.c);
+      if (load_queries<FMT>(a, row, live, q, rs.c) && rs.pos >= 0) rs.l = __uint_as_float(0x7fc00000u);
       Scales<NG>& sc = reinterpret_cast<Scales<NG>*>(scales)[FMT == kBf16 ? 0 : w];
       int x = x0 + w;
       auto page = [&](auto& rv, auto& rv_next) {
@@ -1411,6 +1436,11 @@ __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(Ch
         sum[C][2] = fmaf(f[k], counts ? v.z : 0.0f, sum[C][2]);
         sum[C][3] = fmaf(f[k], counts ? v.w : 0.0f, sum[C][3]);
       }
+    if (is_nan(L))  // the values as well: a merge may look at them alone
+#pragma unroll
+      for (int C = 0; C < 4; ++C)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[C][i] = L;
     if (live) {
       const float il = L > 0.0f ? 1.0f / L : is_nan(L) ? L : 0.0f;
       const size_t at = row * a.num_splits + sg.slot;
