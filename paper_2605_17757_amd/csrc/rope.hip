@@ -8,6 +8,8 @@
 // the exact fp64 product of an integer and an fp32 number, brought to turns and reduced to
 // its fraction in fp64, since an fp32 angle of position 10^5 is off by 0.004 already.  The
 // hardware's sine and cosine take turns.
+// Rows whose mean square is outside [2^-100, 2^100] are divided by a power of two first (bf16 values
+// reach 3e38, the sum of their squares would leave fp32's range).
 // Eight lanes hold a (token, head) row, two chunks of 8 channels each, so chosen that a
 // lane has both channels of its pairs; the norm's sum is three DPP steps.
 // Bound: memory.  8191 tokens of 32 + 8 heads, 168 MB read and written: 30 us, 5.6 TB/s; with
@@ -84,16 +86,34 @@ __device__ inline void angles(const RopeRows& a, int j, int64_t position, float 
     sn[i] = __builtin_amdgcn_sinf(t) * a.factor;
   }
 }
+// A row divided by a power of two that brings its largest magnitude, or the root of eps, near 1; what
+// eps is there.
+__device__ inline float rescale(float (&x)[16], float eps) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int m = 1; m < 8; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, 8));
+  const int e_eps = (int)(__float_as_uint(eps) >> 23) - 127, e = max((int)(top >> 23) - 127, e_eps >> 1);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = ldexpf(x[i], -e);
+  return ldexpf(eps, -2 * e);
+}
 __device__ inline void norm_rotate(const RopeRows& a, const uint16_t* weight, int j, int c0, int c1,
                                    const float (&cs)[8], const float (&sn)[8], u4v& w0, u4v& w1) {
   float x[16];
   unpack8(w0, x);
   unpack8(w1, x + 8);
   if (weight) {
-    float s = 0.0f;
+    auto mean_square = [&]() {
+      float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s = fmaf(x[i], x[i], s);
-    const float r = 1.0f / sqrtf(sum8(s) * (1.0f / kD) + a.eps);
+      for (int i = 0; i < 16; ++i) s = fmaf(x[i], x[i], s);
+      return sum8(s) * (1.0f / kD);
+    };
+    float mean = mean_square() + a.eps;
+    if (!(mean >= 0x1p-100f && mean <= 0x1p100f)) mean = rescale(x, a.eps) + mean_square();
+    const float r = 1.0f / sqrtf(mean);
     float g[16];
     unpack8(*reinterpret_cast<const u4v*>(weight + 8 * c0), g);
     unpack8(*reinterpret_cast<const u4v*>(weight + 8 * c1), g + 8);
