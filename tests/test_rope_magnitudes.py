@@ -67,3 +67,23 @@ def test_rows_of_zeros_and_of_nan():
             want[1, 2] = eps == 0.0
             assert torch.equal(nan, want)
             assert eps == 0.0 or not o[1, 2].any()
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-45, 1e-40])
+def test_rows_of_subnormal_numbers(eps):
+    """Elements of 2^-133 to 2^-126: normalised to numbers near 1 unless eps outweighs them."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    n, H = 600, 8
+    x = torch.randint(1, 128, (n, H, D), generator=g, device="cuda").to(torch.int16)      # bf16 bits
+    x[::2] //= 16
+    x[1::4, :, ::3] = 0
+    x[..., 0] = 3                                       # (no row of zeros: 0 / 0)
+    x = x.view(torch.bfloat16)
+    w = _weights(8)[0]
+    pos = torch.arange(n, device="cuda")
+    out = [torch.empty_like(x) for _ in range(2)]
+    ok.qk_norm_rope(ok.Layout(H, 1), ok.Rope(0, None), x, x, pos, *out, q_weight=w, k_weight=w, eps=eps)
+    ref, tol = R.rope(x, w, float(torch.tensor(eps, dtype=torch.float32)), pos, None, 0, False, 1.0)
+    assert bool(torch.isfinite(ref).all())
+    for o in out:
+        _close(o, ref, tol, "row")
