@@ -4,16 +4,16 @@
 //   x^_c = x_c / sqrt(mean_c x_c^2 + eps) w_c             (without weights: x^ = x)
 //   pair (a, b) of x^ -> f (a cos t - b sin t, b cos t + a sin t),  t = pos * freq_i
 // for the rotary / 2 pairs of the head's first channels, the others as they are.
-// All steps in fp32 and one rounding to bf16 at the end, but for the angle: pos * freq is
-// the exact fp64 product of an integer and an fp32 number, brought to turns and reduced to
-// its fraction in fp64, since an fp32 angle of position 10^5 is off by 0.004 already.  The
-// hardware's sine and cosine take turns.
+// All steps in fp32 and one rounding to bf16 at the end, but for the angle: its turns,
+// (pos / 2 pi) * freq, and their fraction are fp64 (each rounded to 2^-53 of itself), since an
+// fp32 angle of position 10^5 is off by 0.004 already.  The hardware's sine and cosine take turns.
 // Rows whose mean square is outside [2^-100, 2^100] are divided by a power of two first (bf16 values
 // reach 3e38, the sum of their squares would leave fp32's range).
 // Eight lanes hold a (token, head) row, two chunks of 8 channels each, so chosen that a
 // lane has both channels of its pairs; the norm's sum is three DPP steps.
-// Bound: memory.  8191 tokens of 32 + 8 heads, 168 MB read and written: 30 us, 5.6 TB/s; with
-// pages, 16503 tokens of 64 + 8 heads, 676 MB: 147 us, 4.6 TB/s (a copy of 2 GiB: 4.9).
+// Bound: memory.  8191 tokens of 32 + 8 heads, 168 MB read and written: 35 us, 4.7 TB/s, inputs new to
+// the caches (the same again and again, which the last-level cache holds: 30); with pages, 16503 tokens
+// of 64 + 8 heads, 676 MB: 146 us, 4.6 TB/s (a copy of 2 GiB: 4.9).
 #include "internal.h"
 
 #include <type_traits>
@@ -94,7 +94,8 @@ __device__ inline float rescale(float (&x)[16], float eps) {
   for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
 #pragma unroll
   for (int m = 1; m < 8; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, 8));
-  const int e_eps = (int)(__float_as_uint(eps) >> 23) - 127, e = max((int)(top >> 23) - 127, e_eps >> 1);
+  const int e_eps = eps > 0.0f ? (int)(__float_as_uint(eps) >> 23) - 127 : -400;
+  const int e = max((int)(top >> 23) - 127, e_eps >> 1);
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = ldexpf(x[i], -e);
   return ldexpf(eps, -2 * e);
@@ -285,9 +286,9 @@ hipError_t launch(const RopeRows& a, hipStream_t st) {
     if (p.v) p.v += t0 * a.v_stride;
     p.positions += t0;
     if (p.slots) p.slots += t0;
-    // Two units a wave where that leaves each SIMD eight waves: 8191 tokens of 32 + 8 heads take 35 us
-    // with one, 30 with two, 29 with all five; 16503 of 64 heads (more than the caches hold) 146,
-    // 147 and, with eight, 154.
+    // Two units a wave where that leaves each SIMD eight waves.  8191 tokens of 32 + 8 heads that the
+    // last-level cache holds take 35 us with one, 30 with two, 29 with all five; from memory 35.5, 35.5
+    // and 38.7; 16503 of 64 heads into pages 144, 145 and, with eight, 154.
     const int units = (int64_t)p.n_tok * per_tok >= 64 * device_cus() ? 2 : 1;
     const int64_t rows = per_tok ? ((int64_t)p.n_tok * ((per_tok + units - 1) / units) + 3) / 4 : 0;
     const int64_t tiles = PAGES ? (int64_t)((p.n_tok + TOK - 1) / TOK) * a.Hkv : 0;
