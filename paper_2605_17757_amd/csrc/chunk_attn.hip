@@ -30,6 +30,13 @@
 // off and 2e-5 became 0.)  Scores take the power of two back as part of c, values through the
 // accumulators' exponent, which follows the pages'.
 //
+// What becomes 16 bits, beside the output (whose own rounding is 1.6e-3 to 1.7e-3 of its 2-norm):
+//   weights over bf16, in tiles of 128 and 256 rows past 32 rows a sequence: one bf16 value, errors
+//     2.0e-3 to 2.3e-3.  Two pieces are half of the matrix products again: a prompt of 8192 tokens 734 us
+//     for 548, chunks of seven sequences 259 for 202 (same card).  32 rows take two, their loads bound them.
+//   over codes: weights, K^, V^ and q~ one fp16 value each (o~ too in the larger tiles), of 11 bits: 1.8e-3.
+//     They are the matrix cores' operands; fp32 ones run at a sixteenth of the rate.
+//
 // Three kernels, by the rows of a tile (chunk_tile_rows, with both sides of each choice measured):
 //   chunk_few_kernel   32 rows, waves share a tile's pages among them: bound by the bytes over bf16,
 //                      by each page's chain of instructions over codes
@@ -941,10 +948,10 @@ __device__ inline float rotate_output(f16v (&o)[4], float l, int e, const uint8_
 // the one filled next.  Codes (W = 4) come to registers a page ahead, and each wave makes a quarter of
 // the page's operands.
 //   8 waves read a page once where 4 do twice, and hide the loads two pages deep: a prompt of 8192
-// tokens, 32 query heads on 8: 510 us (1.08 PFLOP/s, of 1.36 that a large library product reaches
-// here), by 4 waves 530 to 600; 2048 tokens over 16k in 4 bits 555 (expanded beforehand), by 4 waves 770.
+// tokens, 32 query heads on 8: 500 to 550 us from card to card (1.00 to 1.10 PFLOP/s, of 1.36 that a
+// large library product reaches), by 4 waves 530 to 600; 2048 tokens over 16k in 4 bits 555 (expanded beforehand), by 4 waves 770.
 // Without reads from LDS the prompt takes 90 % of its time, without loads 86, without the softmax 85,
-// the products alone 60.  Matrix cores are busy 50 to 54 % of it at 1.9 to 2.1 GHz, the clock that
+// the products alone 60.  Matrix cores are busy 48 to 54 % of it at 1.9 to 2.1 GHz, the clock that
 // the power limit leaves (in the library product: 73 % at 1.4 to 1.8).
 // ---------------------------------------------------------------------------
 template <int FMT, int NG, int W, bool HL = false>  // HL: p in two pieces
@@ -1243,11 +1250,11 @@ __global__ __launch_bounds__(64 * W, 2) void chunk_kernel(ChunkArgs a) {
 // its V while its scores are: one wave a SIMD with 400 registers.  64 sequences of 16k to 32k tokens,
 // one new each in a window of 4096, 32 query heads on 8: 174 us, 6.2 TB/s.
 //   Codes: bound by a page's chain (scales, scores, maximum, exponentials, values) of two waves a
-// SIMD: 600 (2 bits, one group) to 800 (4 bits, four groups) vector instructions, 320 to 350 of them to
+// SIMD: 640 (2 bits, one group) to 750 (4 bits, four groups) vector instructions, 320 to 350 of them to
 // expand the codes (a conversion and a multiply-add for two, and masks), 150 the softmax of 32 rows; vector ALUs are busy
 // 50 to 75 % of the time, matrix cores 20.  K and V are loaded a page ahead, V's codes into registers of
-// their own.  32 sequences of 4k to 16k tokens, 5 new each, 32 heads on 8, 4 bits: 114 us and, with
-// rotations and merge, 126; 16 of up to 32k, 4 new, 64 heads, 2 bits: 84 and 94.
+// their own.  32 sequences of 4k to 16k tokens, 5 new each, 32 heads on 8, 4 bits: 107 us and, with
+// rotations and merge, 123; 16 of up to 32k, 4 new, 64 heads, 2 bits: 84 and 97.
 // ---------------------------------------------------------------------------
 template <int FMT, int NG>
 __global__ __launch_bounds__(256, FMT == kBf16 ? 1 : 2) void chunk_few_kernel(ChunkArgs a) {
@@ -1600,14 +1607,14 @@ hipError_t launch_fmt(const ChunkArgs& args, hipStream_t st) {
 // Rows of a tile, by the rows that a sequence and KV head have on average (32 query and 8 KV heads
 // below; us with the smaller tile, with the larger).
 //  32, blocks whose waves take pages of their own: codes are then expanded by every wave for itself,
-//      and no wave idles.  8 sequences of 8k tokens in 4 bits, 36 rows each: 57, 68 with 128; 64 rows:
-//      53, 71; 128 rows: 87, 84; 32 sequences of 2k, 64 rows: 85, 100; 128 rows: 128, 111.  Of bf16
+//      and no wave idles.  8 sequences of 8k tokens in 4 bits, 36 rows each: 58, 69 with 128; 64 rows:
+//      56, 71; 128 rows: 90, 85; 32 sequences of 2k, 64 rows: 68, 77; 128 rows: 119, 84.  Of bf16
 //      pages every wave has a whole page's loads in flight, but a CU holds one block and the next
 //      one's start is seen: 64 sequences of 4k tokens, 4 rows each: 167, 184; of 1k: 48, 43; 128 of
 //      300: 50, 37; 32 of 2k: 46, 49; one of 1k: 14, 26.
 // 128 or 256 (one block of 8 waves to a CU instead of two of 4; codes expanded beforehand, to 2 GiB
-//      at most): 8 sequences of 8k, 4 bits, 512 rows: 236, 242; 768: 347, 325; 1024: 403, 368; 2048:
-//      779, 624.  32 of 2k: 235, 288; 356, 370; 433, 404; 802, 693.  bf16, 32 of 2k: 151, 192; 231, 254;
+//      at most): 8 sequences of 8k, 4 bits, 512 rows: 219, 241; 768: 357, 318; 1024: 381, 350; 2048:
+//      730, 609.  32 of 2k: 220, 237; 306, 316; 398, 402; 757, 679.  bf16, 32 of 2k: 151, 192; 231, 254;
 //      285, 282; 540, 526.
 int chunk_tile_rows(bool quantized, int64_t n_q, int B, int heads_per_kv, int Hkv, int64_t max_pages) {
   const int64_t rows = n_q * heads_per_kv, heads = (int64_t)B * Hkv;
